@@ -512,6 +512,150 @@ int aladdin_predict_workers(double k5, double c5, double rate, int64_t* n_worker
 int aladdin_pick_groups(double rate_a, double rate_max, double e, int64_t n_workers,
                         int64_t* groups);
 
+/* ------------------------------------------------------------------------
+ * A worker's decode step.
+ *
+ * The workers that the scheduler places requests on run decode iterations over
+ * paged KV caches; k2, c2, c3 and the KV capacity describe them (Sec. 3). These
+ * calls are the operators of such an iteration, for one model shape: attention
+ * of new tokens over the cache, the cache's growth by the tokens that are kept,
+ * its reduction to a budget, and the probabilities of tokens.
+ *
+ * Every pointer in them is device memory of the worker's GPU, or managed memory
+ * (ALADDIN_ERR_ARG otherwise, before anything is launched), and every call is
+ * asynchronous on the worker's stream. Results are deterministic. Array
+ * contents are checked on the GPU: a request whose offsets, lengths or
+ * indices make no sense takes no part in the call (its outputs are not
+ * written, its cache does not change), a page index outside the pool hides its
+ * tokens, and aladdin_worker_status returns ALADDIN_ERR_STATE. Calls on one
+ * worker share its workspaces and must not overlap. */
+
+/* Types of keys, values, queries and attention outputs (BF16, F16) and of
+ * logits (all three). */
+#define ALADDIN_BF16 0
+#define ALADDIN_F16 1
+#define ALADDIN_F32 2
+
+#define ALADDIN_TREE_MAX 64              /* new tokens of a request in one call */
+#define ALADDIN_TOP_MAX 64               /* top alternatives of a row */
+#define ALADDIN_WORKER_MAX_REQUESTS 1024 /* requests in one call */
+
+/* A model's attention as one worker runs it: query heads [h G, (h + 1) G) use
+ * key head h, G = q_heads / kv_heads. */
+typedef struct aladdin_worker_shape {
+    int32_t dtype;       /* ALADDIN_BF16 or ALADDIN_F16 */
+    int32_t q_heads;     /* a multiple of kv_heads, at most 1024 */
+    int32_t kv_heads;    /* >= 1 */
+    int32_t head_dim;    /* 64, 96, 128 or 256 */
+    int32_t page_tokens; /* tokens of a cache page: 16, 32, 64, 128 or 256 */
+} aladdin_worker_shape;
+
+/* A paged KV cache; every array is the caller's. Slot i of request r is token
+ * i mod page_tokens of page table[r * table_stride + i / page_tokens]; channel c
+ * of head h of token t of page p is element
+ *     p * page_stride + h * head_stride + t * token_stride + c
+ * of k and v (strides positive multiples of 8, k and v 16-byte aligned).
+ * weight and pos are [pages][kv_heads][page_tokens]: a slot's accumulated
+ * attention weight and its token's position in the request. Pages may be shared
+ * between requests where a call only reads them (aladdin_worker_attend). */
+typedef struct aladdin_kv {
+    void* k;
+    void* v;
+    int64_t page_stride, head_stride, token_stride;
+    int32_t pages;        /* pages of the pool */
+    int32_t table_width;  /* pages that a request may have */
+    int64_t table_stride; /* >= table_width */
+    const int32_t* table;
+    int32_t* len;         /* [requests] cached tokens */
+    float* weight;        /* nullable where a call allows it */
+    int32_t* pos;         /* nullable where a call allows it */
+    int32_t* next;        /* [requests] position of the next token; nullable where a call allows it */
+} aladdin_kv;
+
+/* The new tokens of a step: request r has tokens [off[r], off[r + 1]), at most
+ * ALADDIN_TREE_MAX. parent[t] is the index within its request of the token
+ * that token t follows, lower than t's own, or -1 for one that follows the
+ * cached tokens; NULL: each token follows the one before (a chain). Any other
+ * value counts as -1 and is recorded. Head h of token t of q, k, v starts at
+ * element t * stride + h * head_dim (strides multiples of 8, 16-byte aligned
+ * arrays), so that all three may lie in one projection's output. */
+typedef struct aladdin_tokens {
+    int32_t n_req, n_tok;
+    const int32_t* off;
+    const int32_t* parent;
+    const void* q;
+    const void* k;
+    const void* v;
+    int64_t q_stride, k_stride, v_stride;
+} aladdin_tokens;
+
+typedef struct aladdin_worker aladdin_worker;
+
+/* Create a worker on the current CUDA device, bound to cuda_stream, with its
+ * fixed workspaces. Errors: ALADDIN_ERR_ARG, ALADDIN_ERR_NOMEM,
+ * ALADDIN_ERR_CUDA. On error *out is NULL. */
+int aladdin_worker_create(const aladdin_worker_shape* shape, void* cuda_stream,
+                          aladdin_worker** out);
+int aladdin_worker_destroy(aladdin_worker* wk);
+
+/* Waits for the worker's stream; ALADDIN_ERR_STATE if an input was refused on
+ * the GPU since the last call of this function, which forgets it. */
+int aladdin_worker_status(aladdin_worker* wk);
+
+/* Attention of the new tokens: token t of request r sees the request's len[r]
+ * cached tokens, its ancestors and itself,
+ *     s_j = scale q . k_j,  lse = log sum_j e^s_j,  out = sum_j e^(s_j - lse) v_j.
+ * A row whose scores are all -inf has out = 0 and lse = -inf; what a token
+ * does not see has no influence on it, not finite values either. One new token
+ * a request is plain decoding. out: [n_tok] rows of out_stride elements
+ * (a multiple of 8), q_heads * head_dim of them written; lse [n_tok][q_heads]
+ * (nullable). Reads k, v, table and len of kv. scale finite and > 0. */
+int aladdin_worker_attend(aladdin_worker* wk, const aladdin_kv* kv, const aladdin_tokens* tok,
+                          float scale, void* out, int64_t out_stride, float* lse);
+
+/* Keep new tokens: token acc[i], i in [acc_off[r], acc_off[r + 1]), an index
+ * within request r's tree, takes the next slot of the request. The kept tokens
+ * are a path from the tree's root, in order; acc_off NULL: all new tokens. Their keys
+ * and values are copied to the cache, pos (nullable) receives their positions
+ * (next[r] on; len[r] on where next is NULL), weight (nullable) 0, and len and
+ * next advance. With lse (nullable), as the attention of the same tokens gave it,
+ * and tok->q, the slots' weights then grow by what the kept rows attended to them:
+ *     weight_c += sum over kept tokens i and the group's heads e^(s_c - lse).
+ * n_acc: entries of acc. No slot may belong to two requests. The request's
+ * table has to name the pages of its new slots; a request without room for its
+ * kept tokens keeps none and is recorded. */
+int aladdin_worker_accept(aladdin_worker* wk, const aladdin_kv* kv, const aladdin_tokens* tok,
+                          float scale, const float* lse, const int32_t* acc_off,
+                          const int32_t* acc, int32_t n_acc);
+
+/* Reduce the first n_req requests to at most budget[r] >= 0 cached tokens, per key
+ * head: the slots of the largest weight stay, those of a position of at least
+ * next[r] - recent before all others (a weight of NaN after all others), the
+ * lower slot first among equals. The slots from budget[r] on that stay move, in
+ * order, into the slots before it that do not, with key, value, weight and
+ * position; len[r] becomes budget[r]. Requests within their budget do not
+ * change. The first call on a larger pool than any before allocates a workspace
+ * of 4 bytes per slot of the pool (and waits for the device). */
+int aladdin_worker_evict(aladdin_worker* wk, const aladdin_kv* kv, int32_t n_req,
+                         const int32_t* budget, int32_t recent);
+
+/* Of n rows of vocab logits (row i at element i * stride; logits_dtype any of the
+ * three types) and, nullable, one token a row:
+ *  logprob [n]       log softmax at the token (NaN for a token outside the
+ *                    vocabulary, which is recorded);
+ *  entropy [n]       of the softmax, in nats;
+ *  rank [n]          entries larger than the token's, or equal to it at a lower index
+ *                    (ALADDIN_INVALID for a token outside the vocabulary);
+ *  top_id, top_logprob [n][top]   the largest entries in descending order, the
+ *                    lower index first among equals.
+ * Each output is nullable. 0 <= top <= min(ALADDIN_TOP_MAX, vocab). A row with NaN or
+ * +inf has NaN probabilities and entropy; NaN ranks below everything. In a row of
+ * -inf only, the probabilities are -inf and the entropy 0. */
+int aladdin_worker_logprobs(aladdin_worker* wk, int32_t logits_dtype, int32_t n, int32_t vocab,
+                            const void* logits, int64_t stride, const int32_t* token, int32_t top,
+                            float* logprob, float* entropy, int32_t* rank, int32_t* top_id,
+                            float* top_logprob);
+
 #ifdef __cplusplus
 }
 #endif
