@@ -18,9 +18,8 @@ namespace aladdin {
 namespace wk {
 namespace {
 
-constexpr int S = 3, NT = 128, QR = 64;  // tiles in flight, threads, staged rows
-template <int D>
-constexpr int keys_of() { return D == 256 ? 64 : 128; }  // keys of a tile
+// Keys of a tile, threads, rows that are staged at a time where a unit has more than 16.
+constexpr int KT = 64, NT = 128, QR = 64;
 
 struct Cursor {
     int r, h, tile;
@@ -28,7 +27,6 @@ struct Cursor {
     int t0, c;           // first tile and number of tiles
 };
 
-template <int KT>
 __device__ __forceinline__ void enter(const AcceptArgs& a, Cursor& u, int r)
 {
     u.r = r;
@@ -40,16 +38,14 @@ __device__ __forceinline__ void enter(const AcceptArgs& a, Cursor& u, int r)
     u.c = (u.len + u.A + KT - 1) / KT - u.t0;
 }
 
-template <int KT>
 __device__ __forceinline__ void locate(const AcceptArgs& a, Cursor& u, const int* pre, int x)
 {
-    enter<KT>(a, u, plan_find(pre, a.tok.n_req, x));
+    enter(a, u, plan_find(pre, a.tok.n_req, x));
     const int y = x - pre[u.r];
     u.h = y / u.c;
     u.tile = y - u.h * u.c;
 }
 
-template <int KT>
 __device__ __forceinline__ void advance(const AcceptArgs& a, Cursor& u, const int* pre)
 {
     if (++u.tile < u.c) return;
@@ -58,7 +54,7 @@ __device__ __forceinline__ void advance(const AcceptArgs& a, Cursor& u, const in
     u.h = 0;
     int r = u.r + 1;
     while (r < a.tok.n_req && pre[r + 1] == pre[r]) ++r;
-    if (r < a.tok.n_req) enter<KT>(a, u, r);
+    if (r < a.tok.n_req) enter(a, u, r);
 }
 
 // Index of the i-th kept token of a request among all tokens.
@@ -69,13 +65,16 @@ __device__ __forceinline__ int kept(const AcceptArgs& a, const Cursor& u, int i)
 
 template <int D>
 struct Smem {
-    static constexpr int KT = keys_of<D>(), TILE = tile_bytes<D>(KT);
+    static constexpr int S = D == 256 ? 3 : 4;           // tiles in flight
+    static constexpr int TILE = tile_bytes<D>(KT);
     static constexpr int PG = KT / 16;
+    static constexpr int QT = tile_bytes<D>(16);
     static constexpr int k = 0;                          // S K tiles
-    static constexpr int q = k + S * TILE;               // QR rows of q
+    static constexpr int few = k + S * TILE;             // S x 16 rows, fetched with a unit's first tile
+    static constexpr int q = few + S * QT;               // QR rows
     static constexpr int w = q + tile_bytes<D>(QR);      // S x KT weights
-    static constexpr int lse = w + S * KT * 4;           // QR
-    static constexpr int scratch = lse + QR * 4;         // 32 long longs
+    static constexpr int lse = w + S * KT * 4;           // S x 16, then QR
+    static constexpr int scratch = lse + (S * 16 + QR) * 4;  // 32 long longs
     static constexpr int ring = scratch + 32 * 8;        // (S + 1) x PG pages
     static constexpr int pre = ring + (S + 1) * PG * 4;
     static constexpr int bytes(int n_req) { return pre + (n_req + 1) * 4; }
@@ -85,12 +84,12 @@ template <typename T, int D>
 __global__ void __launch_bounds__(NT, D == 256 ? 1 : 2) k_accept(AcceptArgs a)
 {
     using L = Smem<D>;
-    constexpr int KT = L::KT, CH = D / 8, PG = L::PG, KW = KT / 4, NS = KW / 8;
+    constexpr int S = L::S, CH = D / 8, PG = L::PG, KW = KT / 4, NS = KW / 8;
     extern __shared__ __align__(128) char sm[];
     const uint32_t sm0 = smem_addr(sm);
     int* const pre = reinterpret_cast<int*>(sm + L::pre);
     int* const ring = reinterpret_cast<int*>(sm + L::ring);
-    float* const lse2 = reinterpret_cast<float*>(sm + L::lse);
+    float* const lses = reinterpret_cast<float*>(sm + L::lse);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int G = a.kv.group, H = a.kv.kv_heads;
     const bool weigh = a.lse != nullptr;
@@ -137,41 +136,82 @@ __global__ void __launch_bounds__(NT, D == 256 ? 1 : 2) k_accept(AcceptArgs a)
     if (n > 0) {
         if (tid < (S - 1) * PG && tid / PG < n) {
             Cursor u;
-            locate<KT>(a, u, pre, begin + tid / PG);
+            locate(a, u, pre, begin + tid / PG);
             ring[tid] = page_at(u, tid % PG);
         }
         int page_next = -1;
         if (tid < PG && S - 1 < n) {
             Cursor u;
-            locate<KT>(a, u, pre, begin + S - 1);
+            locate(a, u, pre, begin + S - 1);
             page_next = page_at(u, tid);
         }
         Cursor C, F;
-        locate<KT>(a, C, pre, begin);
+        locate(a, C, pre, begin);
         F = C;
         __syncthreads();
 
+        int fu = -1;  // ordinal of the unit fetched
         auto fetch = [&](int j) {
             if (!weigh) return;  // the cached keys are not needed
             const int b = j % S, key0 = (F.t0 + F.tile) * KT;
             const uint32_t kd = sm0 + L::k + b * L::TILE;
             const int* pg = ring + (j % (S + 1)) * PG;
             const long long head = (long long)F.h * a.kv.head_stride;
+            if (j == 0 || F.tile == 0) {
+                ++fu;
+                const int R = F.A * G;
+                if (R <= 16) {
 #pragma unroll
-            for (int i = 0; i < KT * CH / NT; ++i) {
-                const int x = tid + i * NT, row = x / CH, ch = x - row * CH, key = key0 + row;
-                const char* src = a.kv.k;
-                bool ok = key < F.len + F.A;
-                if (key < F.len) {
-                    const int p = pg[row >> 4];
-                    ok = p >= 0;
-                    if (ok)
-                        src += (p * a.kv.page_stride + head + (key & (a.kv.page - 1)) * a.kv.token_stride +
-                                ch * 8) * 2;
-                } else if (ok) {
-                    src = a.tok.k + (kept(a, F, key - F.len) * a.tok.k_stride + F.h * D + ch * 8) * 2;
+                    for (int i = 0; i < (16 * CH + NT - 1) / NT; ++i) {
+                        const int x = tid + i * NT, row = x / CH, ch = x - row * CH;
+                        if ((16 * CH) % NT && x >= 16 * CH) break;
+                        const bool ok = row < R;
+                        const int t = ok ? row / G : 0, g = ok ? row - t * G : 0;
+                        cp16(sm0 + L::few + (fu % S) * L::QT + tile_at<D>(row, ch),
+                             a.tok.q + (kept(a, F, t) * a.tok.q_stride + (long long)(F.h * G + g) * D + ch * 8) * 2,
+                             ok);
+                    }
+                    if (tid < R) {
+                        const int t = tid / G, g = tid - t * G;
+                        cp4(sm0 + L::lse + ((fu % S) * 16 + tid) * 4,
+                            a.lse + (long long)kept(a, F, t) * (H * G) + F.h * G + g, true);
+                    }
                 }
-                cp16(kd + tile_at<D>(row, ch), src, ok);
+            }
+            if (NT % CH == 0 && key0 + KT <= F.len) {
+                // cached keys only: a thread copies one chunk of every NT / CH-th row
+                constexpr int STEP = NT / CH;
+                const int ch = tid % CH, r0 = tid / CH;
+                long long e[KT / 16];
+#pragma unroll
+                for (int g = 0; g < KT / 16; ++g) {
+                    const int at = (key0 + g * 16) & (a.kv.page - 1);
+                    e[g] = pg[g] * a.kv.page_stride + head + (at + r0 % 16) * a.kv.token_stride + ch * 8;
+                }
+#pragma unroll
+                for (int i = 0; i < KT / STEP; ++i) {
+                    const bool ok = pg[i * STEP / 16] >= 0;
+                    const long long x = ok ? (e[i * STEP / 16] + (i * STEP % 16) * a.kv.token_stride) * 2 : 0;
+                    cp16(kd + tile_at<D>(r0 + i * STEP, ch), a.kv.k + x, ok);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < (KT * CH + NT - 1) / NT; ++i) {
+                    const int x = tid + i * NT, row = x / CH, ch = x - row * CH, key = key0 + row;
+                    if ((KT * CH) % NT && x >= KT * CH) break;
+                    const char* src = a.kv.k;
+                    bool ok = key < F.len + F.A;
+                    if (key < F.len) {
+                        const int p = pg[row >> 4];
+                        ok = p >= 0;
+                        if (ok)
+                            src += (p * a.kv.page_stride + head + (key & (a.kv.page - 1)) * a.kv.token_stride +
+                                    ch * 8) * 2;
+                    } else if (ok) {
+                        src = a.tok.k + (kept(a, F, key - F.len) * a.tok.k_stride + F.h * D + ch * 8) * 2;
+                    }
+                    cp16(kd + tile_at<D>(row, ch), src, ok);
+                }
             }
             if (tid < KT) {
                 const int key = key0 + tid, p = pg[tid >> 4];
@@ -184,11 +224,12 @@ __global__ void __launch_bounds__(NT, D == 256 ? 1 : 2) k_accept(AcceptArgs a)
         for (int j = 0; j < S - 1; ++j) {
             if (j < n) {
                 fetch(j);
-                advance<KT>(a, F, pre);
+                advance(a, F, pre);
             }
             cp_commit();
         }
         bool fresh = true;
+        int cu = -1;  // ordinal of the unit weighed
         for (int j = 0; j < n; ++j) {
             cp_wait<S - 2>();
             if (tid < PG) ring[((j + S - 1) % (S + 1)) * PG + tid] = page_next;
@@ -196,7 +237,7 @@ __global__ void __launch_bounds__(NT, D == 256 ? 1 : 2) k_accept(AcceptArgs a)
             if (j + S - 1 < n) {
                 fetch(j + S - 1);
                 if (j + S < n) {
-                    advance<KT>(a, F, pre);
+                    advance(a, F, pre);
                     if (tid < PG) page_next = page_at(F, tid);
                 }
             }
@@ -232,9 +273,13 @@ __global__ void __launch_bounds__(NT, D == 256 ? 1 : 2) k_accept(AcceptArgs a)
                 float sum[NS][2];
 #pragma unroll
                 for (int x = 0; x < NS; ++x) sum[x][0] = sum[x][1] = 0.0f;
+                if (fresh) ++cu;
+                const bool few = R <= 16;  // the rows came with the unit's first tile
+                const uint32_t qs = sm0 + (few ? L::few + (cu % S) * L::QT : L::q);
+                float* const ls = lses + (few ? (cu % S) * 16 : S * 16);
                 for (int r0 = 0; r0 < R; r0 += QR) {
                     const int rows = R - r0 < QR ? R - r0 : QR;
-                    if (fresh || R > QR) {  // the rows of this unit are not staged yet
+                    if (!few && (fresh || R > QR)) {  // these rows are not staged yet
                         if (r0) __syncthreads();
                         for (int x = tid; x < QR * CH; x += NT) {
                             const int rr = x / CH, ch = x - rr * CH;
@@ -247,12 +292,9 @@ __global__ void __launch_bounds__(NT, D == 256 ? 1 : 2) k_accept(AcceptArgs a)
                             }
                             *reinterpret_cast<uint4*>(sm + L::q + tile_at<D>(rr, ch)) = v;
                         }
-                        if (tid < QR) {
+                        if (tid < rows) {
                             const int i = (r0 + tid) / G, g = r0 + tid - i * G;
-                            // a row without an attention (lse = -inf) has no weights to add
-                            float v = tid < rows ? a.lse[(long long)kept(a, C, i) * (H * G) + C.h * G + g] * LOG2E
-                                                 : INFINITY;
-                            lse2[tid] = v == -INFINITY ? INFINITY : v;
+                            ls[tid] = a.lse[(long long)kept(a, C, i) * (H * G) + C.h * G + g];
                         }
                         __syncthreads();
                     }
@@ -264,7 +306,7 @@ __global__ void __launch_bounds__(NT, D == 256 ? 1 : 2) k_accept(AcceptArgs a)
                         for (int ks = 0; ks < D / 16; ++ks) {
                             uint32_t qf[4];
                             // a fragment's four parts: rows 0-7, rows 8-15, then the same 8 channels on
-                            ldmatrix4(qf, sm0 + L::q + tile_at<D>(m0 + (id & 1) * 8 + lr, ks * 2 + (id >> 1)));
+                            ldmatrix4(qf, qs + tile_at<D>(m0 + (id & 1) * 8 + lr, ks * 2 + (id >> 1)));
 #pragma unroll
                             for (int x = 0; x < NS; x += 2) {
                                 uint32_t f[4];
@@ -276,7 +318,9 @@ __global__ void __launch_bounds__(NT, D == 256 ? 1 : 2) k_accept(AcceptArgs a)
 #pragma unroll
                         for (int y = 0; y < 2; ++y) {
                             const int rr = m0 + gq + y * 8;
-                            const float base = lse2[rr];
+                            // (a row without an attention, lse = -inf, has no weights to add)
+                            const float lse = rr < rows ? ls[rr] : -INFINITY;
+                            const float base = lse == -INFINITY ? INFINITY : lse * LOG2E;
                             const int sees = C.len + (r0 + rr) / G - key0;  // the last key that the row sees
 #pragma unroll
                             for (int x = 0; x < NS; ++x) {
@@ -305,7 +349,7 @@ __global__ void __launch_bounds__(NT, D == 256 ? 1 : 2) k_accept(AcceptArgs a)
                 }
             }
             fresh = C.tile + 1 == C.c;
-            if (j + 1 < n) advance<KT>(a, C, pre);
+            if (j + 1 < n) advance(a, C, pre);
         }
         cp_wait<0>();
     }
@@ -334,7 +378,7 @@ cudaError_t launch(const AcceptArgs& a, int sms, cudaStream_t st)
     static_assert(L::bytes(ALADDIN_WORKER_MAX_REQUESTS) <= 227 * 1024 - 256, "shared memory of a CTA");
     cudaError_t e = allow_smem<k_accept<T, D>>(L::bytes(ALADDIN_WORKER_MAX_REQUESTS));
     if (e != cudaSuccess) return e;
-    const long long tiles = (long long)a.tok.n_req * a.kv.kv_heads * (a.lse ? a.kv.cap / L::KT + 2 : 2);
+    const long long tiles = (long long)a.tok.n_req * a.kv.kv_heads * (a.lse ? a.kv.cap / KT + 2 : 2);
     const long long most = 2ll * sms;
     k_accept<T, D><<<(int)(tiles < most ? tiles : most), NT, L::bytes(a.tok.n_req), st>>>(a);
     return cudaGetLastError();

@@ -32,7 +32,7 @@ struct Shape {
 struct Cursor {
     int r, h, rt, tile;   // request, key head, row tile, key tile
     int lo, T, len;       // its first new token, new tokens, cached tokens
-    int ctile, c, nrt;    // cached key tiles, all key tiles, row tiles
+    int c, nrt;           // key tiles, row tiles
 };
 
 template <int KT, int RM>
@@ -42,8 +42,7 @@ __device__ __forceinline__ void enter(const AttendArgs& a, Cursor& u, int r)
     u.lo = a.tok.off[r];
     u.T = a.tok.off[r + 1] - u.lo;
     u.len = a.kv.len[r];
-    u.ctile = (u.len + KT - 1) / KT;
-    u.c = u.ctile + (u.T + KT - 1) / KT;
+    u.c = (u.len + u.T + KT - 1) / KT;
     u.nrt = (u.T * a.kv.group + RM - 1) / RM;
 }
 
@@ -96,14 +95,16 @@ template <int D, int WR, int WK>
 struct Smem {
     static constexpr int KT = Shape<D>::KT, S = Shape<D>::S, RM = WR * 16;
     static constexpr int TILE = tile_bytes<D>(KT);
-    static constexpr int MERGE = (WK > 1 ? RM * D * 4 : 0);
-    static constexpr int kv = 0;                        // S x (K tile, V tile)
-    static constexpr int merge = kv + S * 2 * TILE;     // RM x D floats
-    static constexpr int ml = merge + MERGE;            // WK x RM (maximum, sum)
-    static constexpr int anc = ml + WK * RM * 8;        // 64 masks
-    static constexpr int scratch = anc + 64 * 8;        // 32 long longs
-    static constexpr int par = scratch + 32 * 8;        // S x 64 parents
-    static constexpr int ring = par + S * 64 * 4;       // (S + 1) x KT / 16 pages
+    static_assert(WK == 1 || WK * RM * D * 4 <= 2 * TILE, "the warps' sums fit a tile's place");
+    static constexpr bool QRING = RM == 16;               // the rows of a unit are fetched with its first tile
+    static constexpr int QT = QRING ? tile_bytes<D>(RM) : 0;
+    static constexpr int kv = 0;                          // S x (K tile, V tile)
+    static constexpr int q = kv + S * 2 * TILE;           // S x RM rows
+    static constexpr int ml = q + S * QT;                 // WK x RM (maximum, sum)
+    static constexpr int anc = ml + WK * RM * 8;          // 64 masks
+    static constexpr int scratch = anc + 64 * 8;          // 32 long longs
+    static constexpr int par = scratch + 32 * 8;          // S x 64 parents
+    static constexpr int ring = par + S * 64 * 4;         // (S + 1) x KT / 16 pages
     static constexpr int pre = ring + (S + 1) * (KT / 16) * 4 + 8;
     static constexpr int bytes(int n_req) { return pre + (n_req + 1) * 4; }
 };
@@ -125,7 +126,6 @@ __global__ void __launch_bounds__(WR* WK * 32, D == 256 ? 1 : 2) k_attend(Attend
     int* const par = reinterpret_cast<int*>(sm + L::par);
     unsigned long long* const anc = reinterpret_cast<unsigned long long*>(sm + L::anc);
     float2* const ml = reinterpret_cast<float2*>(sm + L::ml);
-    float* const merge = reinterpret_cast<float*>(sm + L::merge);
     __shared__ int s_last;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(WR* WK * 32, D == 256 ? 1 : 2) k_attend(Attend
                 return 0;
             }
             const int nt = hi - lo;
-            return (long long)((nt * G + RM - 1) / RM) * H * ((len + KT - 1) / KT + (nt + KT - 1) / KT);
+            return (long long)((nt * G + RM - 1) / RM) * H * ((len + nt + KT - 1) / KT);
         });
     if (total <= 0) {
         if (total < 0 && blockIdx.x == 0 && tid == 0) atomicOr(a.err, WORKER_BAD_INPUT);
@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(WR* WK * 32, D == 256 ? 1 : 2) k_attend(Attend
     // the page of keys [16 g, 16 g + 16) of the tile under a cursor
     auto page_at = [&](const Cursor& u, int g) -> int {
         const int key = u.tile * KT + g * 16;
-        if (u.tile >= u.ctile || key >= u.len) return -1;
+        if (key >= u.len) return -1;
         const int p = a.kv.table[(long long)u.r * a.kv.table_stride + (key >> a.kv.page_shift)];
         if ((unsigned)p >= (unsigned)a.kv.pages) {
             atomicOr(a.err, WORKER_BAD_INPUT);
@@ -183,44 +183,77 @@ __global__ void __launch_bounds__(WR* WK * 32, D == 256 ? 1 : 2) k_attend(Attend
     F = C;
     __syncthreads();
 
-    // ordinal j of the CTA's tiles, under cursor F, into buffer j mod S
+    // ordinal j of the CTA's tiles, under cursor F, into buffer j mod S, and with a
+    // unit's first tile (ordinal fu of the units) its rows
+    int fu = -1;
     auto fetch = [&](int j) {
-        const int b = j % S;
+        const int b = j % S, key0 = F.tile * KT;
         const uint32_t kd = sm0 + L::kv + b * 2 * L::TILE, vd = kd + L::TILE;
         const int* pg = ring + (j % (S + 1)) * PG;
+        const long long head = (long long)F.h * a.kv.head_stride;
         constexpr int PER = (KT * CH + NT - 1) / NT;
-        if (F.tile < F.ctile) {
-            const long long head = (long long)F.h * a.kv.head_stride;
-            const int key0 = F.tile * KT;
+        if (j == 0 || F.tile == 0) {
+            ++fu;
+            if constexpr (L::QRING) {
+                const int rows = F.T * G - F.rt * RM;
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int x = tid + i * NT, row = x / CH, ch = x - row * CH;
-                if ((KT * CH) % NT && x >= KT * CH) break;
-                const int key = key0 + row, p = pg[row >> 4];
-                const bool ok = key < F.len && p >= 0;
+                for (int i = 0; i < (RM * CH + NT - 1) / NT; ++i) {
+                    const int x = tid + i * NT, row = x / CH, ch = x - row * CH;
+                    if ((RM * CH) % NT && x >= RM * CH) break;
+                    const bool ok = row < rows;
+                    const int rho = F.rt * RM + row, t = ok ? rho / G : 0, g = ok ? rho - t * G : 0;
+                    cp16(sm0 + L::q + (fu % S) * L::QT + tile_at<D>(row, ch),
+                         a.tok.q + ((F.lo + t) * a.tok.q_stride + (long long)(F.h * G + g) * D + ch * 8) * 2, ok);
+                }
+            }
+        }
+        if (NT % CH == 0 && key0 + KT <= F.len) {
+            // cached keys only: a thread copies one chunk of every NT / CH-th row
+            constexpr int STEP = NT / CH;
+            const int ch = tid % CH, r0 = tid / CH;
+            long long e[KT / 16];
+#pragma unroll
+            for (int g = 0; g < KT / 16; ++g) {
+                const int at = (key0 + g * 16) & (a.kv.page - 1);
+                e[g] = pg[g] * a.kv.page_stride + head + (at + r0 % 16) * a.kv.token_stride + ch * 8;
+            }
+#pragma unroll
+            for (int i = 0; i < KT / STEP; ++i) {
+                const int row = r0 + i * STEP;
+                const bool ok = pg[i * STEP / 16] >= 0;
+                const long long x = ok ? (e[i * STEP / 16] + (i * STEP % 16) * a.kv.token_stride) * 2 : 0;
+                const uint32_t d = tile_at<D>(row, ch);
+                cp16(kd + d, a.kv.k + x, ok);
+                cp16(vd + d, a.kv.v + x, ok);
+            }
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int x = tid + i * NT, row = x / CH, ch = x - row * CH, key = key0 + row;
+            if ((KT * CH) % NT && x >= KT * CH) break;
+            const char *ks = a.kv.k, *vs = a.kv.v;
+            bool ok = key < F.len + F.T;
+            if (key < F.len) {
+                const int p = pg[row >> 4];
+                ok = p >= 0;
                 const long long e = ok ? p * a.kv.page_stride + head +
                                              (key & (a.kv.page - 1)) * a.kv.token_stride + ch * 8
                                        : 0;
-                const uint32_t d = tile_at<D>(row, ch);
-                cp16(kd + d, a.kv.k + e * 2, ok);
-                cp16(vd + d, a.kv.v + e * 2, ok);
+                ks += e * 2;
+                vs += e * 2;
+            } else if (ok) {
+                const long long t = F.lo + key - F.len;
+                ks = a.tok.k + (t * a.tok.k_stride + F.h * D + ch * 8) * 2;
+                vs = a.tok.v + (t * a.tok.v_stride + F.h * D + ch * 8) * 2;
             }
-        } else {
-            const int key0 = (F.tile - F.ctile) * KT;
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int x = tid + i * NT, row = x / CH, ch = x - row * CH;
-                if ((KT * CH) % NT && x >= KT * CH) break;
-                const bool ok = key0 + row < F.T;
-                const long long t = ok ? F.lo + key0 + row : 0;
-                const uint32_t d = tile_at<D>(row, ch);
-                cp16(kd + d, a.tok.k + (t * a.tok.k_stride + F.h * D + ch * 8) * 2, ok);
-                cp16(vd + d, a.tok.v + (t * a.tok.v_stride + F.h * D + ch * 8) * 2, ok);
-            }
-            if (a.tok.parent && tid < ALADDIN_TREE_MAX)
-                cp4(smem_addr(par + b * ALADDIN_TREE_MAX + tid), a.tok.parent + F.lo + (tid < F.T ? tid : 0),
-                    tid < F.T);
+            const uint32_t d = tile_at<D>(row, ch);
+            cp16(kd + d, ks, ok);
+            cp16(vd + d, vs, ok);
         }
+        if (F.T > 1 && a.tok.parent && key0 + KT > F.len && tid < ALADDIN_TREE_MAX)
+            cp4(smem_addr(par + b * ALADDIN_TREE_MAX + tid), a.tok.parent + F.lo + (tid < F.T ? tid : 0),
+                tid < F.T);
     };
 #pragma unroll
     for (int j = 0; j < S - 1; ++j) {
@@ -236,6 +269,7 @@ __global__ void __launch_bounds__(WR* WK * 32, D == 256 ? 1 : 2) k_attend(Attend
     int row_tok[2];
     const int gq = lane >> 2, tq = lane & 3;
     bool fresh = true;
+    int cu = -1;  // ordinal of the unit computed
 
     for (int j = 0; j < n; ++j) {
         cp_wait<S - 2>();
@@ -257,29 +291,38 @@ __global__ void __launch_bounds__(WR* WK * 32, D == 256 ? 1 : 2) k_attend(Attend
             for (int x = 0; x < NO; ++x) o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.0f;
             m[0] = m[1] = -INFINITY;
             l[0] = l[1] = 0.0f;
+            ++cu;
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
                 const int rr = wr * 16 + gq + y * 8, rho = C.rt * RM + rr;
                 const bool ok = rr < rows;
                 const int t = ok ? rho / G : 0;
                 row_tok[y] = t;
-                const char* p = a.tok.q + ((C.lo + t) * a.tok.q_stride +
-                                           (long long)(C.h * G + (ok ? rho - t * G : 0)) * D) * 2;
+                if constexpr (!L::QRING) {
+                    const char* p = a.tok.q + ((C.lo + t) * a.tok.q_stride +
+                                               (long long)(C.h * G + (ok ? rho - t * G : 0)) * D) * 2;
 #pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks) {
-                    const uint32_t* w = reinterpret_cast<const uint32_t*>(p + ks * 32 + tq * 4);
-                    qf[ks][y] = ok ? __ldg(w) : 0u;
-                    qf[ks][y + 2] = ok ? __ldg(w + 4) : 0u;
+                    for (int ks = 0; ks < D / 16; ++ks) {
+                        const uint32_t* w = reinterpret_cast<const uint32_t*>(p + ks * 32 + tq * 4);
+                        qf[ks][y] = ok ? __ldg(w) : 0u;
+                        qf[ks][y + 2] = ok ? __ldg(w + 4) : 0u;
+                    }
                 }
+            }
+            if constexpr (L::QRING) {
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks)
+                    ldmatrix4(qf[ks], sm0 + L::q + (cu % S) * L::QT +
+                                          tile_at<D>((lane >> 3 & 1) * 8 + (lane & 7), ks * 2 + (lane >> 4)));
             }
         }
 
         const int b = j % S;
         const uint32_t kd = sm0 + L::kv + b * 2 * L::TILE, vd = kd + L::TILE;
-        const bool tree = C.tile >= C.ctile;
-        const int key0 = (tree ? C.tile - C.ctile : C.tile) * KT;
+        const int key0 = C.tile * KT, new0 = C.len - key0;  // the first new key's place in the tile
+        const bool mixed = new0 < KT;                       // the tile holds new keys, or its last ones are none
         bool wild = false;
-        if (tree) {
+        if (mixed && C.T > 1) {
             if (tid < C.T) {
                 unsigned long long see = 0;
                 int u = tid;
@@ -297,14 +340,12 @@ __global__ void __launch_bounds__(WR* WK * 32, D == 256 ? 1 : 2) k_attend(Attend
             // a value that is not finite would reach rows that do not see its token
             // (0 times infinity): such a tile is summed key by key below
             bool w = false;
-            if (C.T > 1) {
-                for (int x = tid; x < KT * CH; x += NT) {
-                    const int row = x / CH;
-                    if (key0 + row >= C.T) break;
-                    const uint4 q = *reinterpret_cast<const uint4*>(
-                        sm + L::kv + (b * 2 + 1) * L::TILE + tile_at<D>(row, x - row * CH));
-                    w |= Num<T>::wild(q.x) || Num<T>::wild(q.y) || Num<T>::wild(q.z) || Num<T>::wild(q.w);
-                }
+            const int k1 = min(KT, new0 + C.T);
+            for (int x = max(new0, 0) * CH + tid; x < k1 * CH; x += NT) {
+                const int row = x / CH;
+                const uint4 q = *reinterpret_cast<const uint4*>(
+                    sm + L::kv + (b * 2 + 1) * L::TILE + tile_at<D>(row, x - row * CH));
+                w |= Num<T>::wild(q.x) || Num<T>::wild(q.y) || Num<T>::wild(q.z) || Num<T>::wild(q.w);
             }
             wild = __syncthreads_or(w);
         }
@@ -325,27 +366,15 @@ __global__ void __launch_bounds__(WR* WK * 32, D == 256 ? 1 : 2) k_attend(Attend
                     Num<T>::mma(s[x + 1], qf[ks], f[2], f[3]);
                 }
             }
-            const int live = (tree ? C.T : C.len) - key0;  // keys of the tile that exist
             float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
             for (int x = 0; x < NS; ++x) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[x][e] *= a.scale_log2;
             }
-            if (tree) {
-                const unsigned long long see[2] = {anc[row_tok[0]] >> key0, anc[row_tok[1]] >> key0};
-#pragma unroll
-                for (int x = 0; x < NS; ++x) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int k = k0 + x * 8 + tq * 2 + (e & 1);
-                        if (k >= 64 || !((see[e >> 1] >> k) & 1)) s[x][e] = -INFINITY;
-                    }
-                }
-            } else {
-                // keys behind the length, and those of a page outside the pool (-1, as are
-                // the pages behind the length)
-                const int* pg = ring + (j % (S + 1)) * PG + k0 / 16;
+            // keys of a page outside the pool (-1, as are the pages behind the cached keys)
+            const int* pg = ring + (j % (S + 1)) * PG + k0 / 16;
+            if (!mixed) {
 #pragma unroll
                 for (int x = 0; x < NS; x += 2) {
                     if (pg[x / 2] < 0) {
@@ -353,12 +382,15 @@ __global__ void __launch_bounds__(WR* WK * 32, D == 256 ? 1 : 2) k_attend(Attend
                         for (int e = 0; e < 4; ++e) s[x][e] = s[x + 1][e] = -INFINITY;
                     }
                 }
-                if (live < KT) {
+            } else {
+                const unsigned long long see[2] = {C.T > 1 ? anc[row_tok[0]] : 1, C.T > 1 ? anc[row_tok[1]] : 1};
 #pragma unroll
-                    for (int x = 0; x < NS; ++x) {
+                for (int x = 0; x < NS; ++x) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (k0 + x * 8 + tq * 2 + (e & 1) >= live) s[x][e] = -INFINITY;
+                    for (int e = 0; e < 4; ++e) {
+                        const int k = k0 + x * 8 + tq * 2 + (e & 1), u = k - new0;
+                        const bool ok = u < 0 ? pg[x / 2] >= 0 : u < 64 && (see[e >> 1] >> u & 1);
+                        if (!ok) s[x][e] = -INFINITY;
                     }
                 }
             }
@@ -476,51 +508,37 @@ __global__ void __launch_bounds__(WR* WK * 32, D == 256 ? 1 : 2) k_attend(Attend
                     ml[wk * RM + wr * 16 + gq] = make_float2(m[0], l[0]);
                     ml[wk * RM + wr * 16 + gq + 8] = make_float2(m[1], l[1]);
                 }
+                // the tile's place takes every warp's sums (8 floats a group, the groups of a
+                // row turned by the row, so that a warp's rows lie in different banks)
                 __syncthreads();
+                float* const sums = reinterpret_cast<float*>(sm + L::kv + b * 2 * L::TILE);
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    float top = -INFINITY;
-#pragma unroll
-                    for (int w = 0; w < WK; ++w) top = fmaxf(top, ml[w * RM + wr * 16 + gq + y * 8].x);
-                    const float f = m[y] == -INFINITY ? 0.0f : ex2(m[y] - top);
-                    m[y] = top;
+                    float* d = sums + (wk * RM + wr * 16 + gq + y * 8) * D + tq * 2;
 #pragma unroll
                     for (int x = 0; x < NO; ++x) {
-                        o[x][y * 2] *= f;
-                        o[x][y * 2 + 1] *= f;
+                        const int at = x + gq < NO ? x + gq : x + gq - NO;
+                        *reinterpret_cast<float2*>(d + at * 8) = make_float2(o[x][y * 2], o[x][y * 2 + 1]);
                     }
                 }
-#pragma unroll
-                for (int w = 0; w < WK; ++w) {
-                    if (wk == w) {
-#pragma unroll
-                        for (int y = 0; y < 2; ++y) {
-                            float* d = merge + (wr * 16 + gq + y * 8) * D + tq * 2;
-#pragma unroll
-                            for (int x = 0; x < NO; ++x) {
-                                float2* e = reinterpret_cast<float2*>(d + x * 8);
-                                float2 v = make_float2(o[x][y * 2], o[x][y * 2 + 1]);
-                                if (w) {
-                                    v.x += e->x;
-                                    v.y += e->y;
-                                }
-                                *e = v;
-                            }
-                        }
-                    }
-                    __syncthreads();
-                }
+                __syncthreads();
                 for (int x = tid; x < live * (D / 2); x += NT) {
                     const int rr = x / (D / 2), col = (x - rr * (D / 2)) * 2;
+                    const int turned = (col >> 3) + (rr & 7), at = (turned < NO ? turned : turned - NO) * 8 + (col & 7);
                     float top = -INFINITY, sum = 0.0f;
+                    float2 v = make_float2(0.0f, 0.0f);
 #pragma unroll
                     for (int w = 0; w < WK; ++w) top = fmaxf(top, ml[w * RM + rr].x);
 #pragma unroll
                     for (int w = 0; w < WK; ++w) {
-                        const float2 v = ml[w * RM + rr];
-                        sum += v.x == -INFINITY ? 0.0f : v.y * ex2(v.x - top);
+                        const float2 q = ml[w * RM + rr];
+                        const float f = q.x == -INFINITY ? 0.0f : ex2(q.x - top);
+                        const float2 u = *reinterpret_cast<const float2*>(sums + (w * RM + rr) * D + at);
+                        sum += q.y * f;
+                        v.x += u.x * f;
+                        v.y += u.y * f;
                     }
-                    put2(rr, col, merge[rr * D + col], merge[rr * D + col + 1], sum);
+                    put2(rr, col, v.x, v.y, sum);
                     if (col == 0) put_ml(rr, top, sum);
                 }
             } else {
@@ -606,7 +624,7 @@ cudaError_t launch(const AttendArgs& a, int sms, cudaStream_t st)
     const long long units = (long long)a.tok.n_req * a.kv.kv_heads *
                             ((long long)(a.tok.n_tok < ALADDIN_TREE_MAX ? a.tok.n_tok : ALADDIN_TREE_MAX) *
                                  a.kv.group / L::RM + 1);
-    const long long tiles = units * (a.kv.cap / L::KT + 3);
+    const long long tiles = units * (a.kv.cap / L::KT + 2);
     const long long most = 2ll * sms;
     k_attend<T, D, WR, WK><<<(int)(tiles < most ? tiles : most), WR * WK * 32, smem, st>>>(a);
     return cudaGetLastError();

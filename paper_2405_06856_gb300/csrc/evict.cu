@@ -9,12 +9,15 @@
 // that the moves are independent of one another. The order of the cached
 // tokens means nothing to the attention; `pos` says what is recent.
 //
-// A cluster of CTAs serves one (request, key head); each keeps the keys of its
-// part of the slots in shared memory. The budget-th largest key is found digit
-// by digit (11 + 11 + 10 bits of the ordered key): each CTA counts its keys
-// that agree with the digits known so far, every CTA adds the cluster's counts
-// and picks the same digit. Two scans then number equal keys, holes and movers
-// in slot order, and the cluster's CTAs share the moves.
+// One CTA, or a cluster where there are few long requests, serves one (request,
+// key head); each CTA keeps the keys of its part of the slots in shared memory.
+// The budget-th largest key is found digit by digit (11 + 11 + 10 bits of the
+// ordered key): each CTA counts its keys that agree with the digits known so far,
+// every CTA adds the cluster's counts and picks the same digit, until all keys of
+// the digit stay. Two scans then number equal keys, holes and movers in slot
+// order, and the warps share the moves, 32 to a warp: a lane looks one of them up
+// and moves its weight and position, then the warp copies their rows, several
+// 16-byte pieces of a lane in flight.
 #include <cooperative_groups.h>
 
 #include "worker_dev.cuh"
@@ -25,7 +28,6 @@ namespace aladdin {
 namespace wk {
 namespace {
 
-constexpr int NT = 512;
 constexpr int BINS = 2048;
 constexpr int MAX_KEYS = 50 * 1024;  // keys that a CTA holds; it forms the others again where it needs them
 
@@ -42,22 +44,49 @@ struct Evict {
     int h, held, recent_from;
 };
 
-__device__ __forceinline__ long long meta_at(const EvictArgs& a, const Evict& e, int slot)
+__device__ __forceinline__ int page_of(const EvictArgs& a, const Evict& e, int slot)
 {
     const int p = e.row[slot >> a.kv.page_shift];
-    if ((unsigned)p >= (unsigned)a.kv.pages) return -1;
-    return ((long long)p * a.kv.kv_heads + e.h) * a.kv.page + (slot & (a.kv.page - 1));
+    return (unsigned)p < (unsigned)a.kv.pages ? p : -1;
+}
+// Index of a slot's weight and position.
+__device__ __forceinline__ long long meta_at(const EvictArgs& a, const Evict& e, int page, int slot)
+{
+    return ((long long)page * a.kv.kv_heads + e.h) * a.kv.page + (slot & (a.kv.page - 1));
+}
+// Element of a slot's key and value.
+__device__ __forceinline__ long long row_at(const EvictArgs& a, const Evict& e, int page, int slot)
+{
+    return page * a.kv.page_stride + e.h * a.kv.head_stride + (slot & (a.kv.page - 1)) * a.kv.token_stride;
 }
 
-__device__ __forceinline__ uint32_t key_of(const EvictArgs& a, const Evict& e, int slot)
+// Keys of N slots first, first + step, ... below end, their loads together; 0 for
+// slots of a page outside the pool, which are recorded.
+template <int N>
+__device__ __forceinline__ void keys_of(const EvictArgs& a, const Evict& e, int first, int step, int end,
+                                        uint32_t (&key)[N])
 {
-    const long long m = meta_at(a, e, slot);
-    if (m < 0) return 0u;
-    if (a.kv.pos[m] >= e.recent_from) return ordered(INFINITY);
-    return ordered(a.kv.weight[m]);
+    int page[N], pos[N];
+    float w[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int slot = first + i * step;
+        page[i] = slot < end ? page_of(a, e, slot) : -1;
+        if (slot < end && page[i] < 0) atomicOr(a.err, WORKER_BAD_INPUT);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const long long m = page[i] < 0 ? 0 : meta_at(a, e, page[i], first + i * step);
+        pos[i] = page[i] < 0 ? 0 : a.kv.pos[m];
+        w[i] = page[i] < 0 ? 0.0f : a.kv.weight[m];
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        key[i] = page[i] < 0 ? 0u : pos[i] >= e.recent_from ? ordered(INFINITY) : ordered(w[i]);
 }
 
 // Exclusive sums of two counts over the block's threads, and their totals.
+template <int NT>
 __device__ __forceinline__ int2 block_scan(int2 v, int2* scratch, int2& total)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -88,163 +117,235 @@ __device__ __forceinline__ int2 block_scan(int2 v, int2* scratch, int2& total)
     return make_int2(before.x + u.x - v.x, before.y + u.y - v.y);
 }
 
-__global__ void __launch_bounds__(NT) k_evict(EvictArgs a, int max_keys)
+// CLUSTER: a cluster serves a (request, head), else one CTA.
+template <int D, int NT, bool CLUSTER>
+__global__ void __launch_bounds__(NT, CLUSTER ? 1 : 4) k_evict(EvictArgs a, int max_keys)
 {
     cg::cluster_group cluster = cg::this_cluster();
     extern __shared__ __align__(16) uint32_t keys[];
-    __shared__ int hist[2][BINS];
+    __shared__ __align__(16) int hist[2][BINS];
     __shared__ int2 scratch[NT / 32];
-    __shared__ int2 counts;    // what the cluster's other CTAs read of this one
-    __shared__ int s_digit, s_above, s_last;
-    const int cs = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-    const int tid = threadIdx.x;
+    __shared__ int2 counts;  // what the cluster's other CTAs read of this one
+    __shared__ int s_digit, s_above, s_here, s_last;
+    const int cs = CLUSTER ? (int)cluster.num_blocks() : 1, rank = CLUSTER ? (int)cluster.block_rank() : 0;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int unit = blockIdx.x / cs, H = a.kv.kv_heads, r = unit / H;
+    auto meet = [&]() {
+        if (CLUSTER) cluster.sync();
+        else __syncthreads();
+    };
 
     Evict e;
     e.h = unit - r * H;
     e.row = a.kv.table + (long long)r * a.kv.table_stride;
     e.held = a.kv.len[r];
     const int budget = a.budget[r];
+    const long long from = (long long)a.kv.next[r] - a.recent;  // recent positions (an int may not hold it)
+    e.recent_from = from < -0x7fffffffll ? -0x7fffffff : (int)from;
     const bool ok = e.held >= 0 && e.held <= a.kv.cap && budget >= 0;
     if (!ok && rank == 0 && e.h == 0 && tid == 0) atomicOr(a.err, WORKER_BAD_INPUT);
     if (ok && e.held > budget) {
-        // positions from next - recent on are recent (an int may not hold the difference)
-        const long long from = (long long)a.kv.next[r] - a.recent;
-        e.recent_from = from < -0x7fffffffll ? -0x7fffffff : (int)from;
         const int span = (e.held + cs - 1) / cs, s0 = min(rank * span, e.held), s1 = min(s0 + span, e.held),
                   n = s1 - s0;
-        for (int i = tid; i < n; i += NT) {
-            if (meta_at(a, e, s0 + i) < 0) atomicOr(a.err, WORKER_BAD_INPUT);
-            if (i < max_keys) keys[i] = key_of(a, e, s0 + i);
-        }
-        // (every thread reads the keys that it wrote, up to the next barrier)
-        auto key = [&](int i) { return i < max_keys ? keys[i] : key_of(a, e, s0 + i); };
-
-        // the budget-th largest key, and how many slots of that very key stay
-        uint32_t known = 0, mask = 0;
-        int want = budget;
-        if (budget > 0) {
+        for (int i = tid; i < BINS; i += NT) hist[0][i] = 0;
+        __syncthreads();
+        // the keys, and the counts of their first digit
+        for (int i = tid; i < n; i += 4 * NT) {
+            uint32_t k[4];
+            keys_of<4>(a, e, s0 + i, NT, s1, k);
 #pragma unroll
-            for (int pass = 0; pass < 3; ++pass) {
-                const int bits = pass < 2 ? 11 : 10, shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-                int* const h = hist[pass & 1];
+            for (int x = 0; x < 4; ++x) {
+                if (i + x * NT < n) {
+                    if (i + x * NT < max_keys) keys[i + x * NT] = k[x];
+                    atomicAdd(&hist[0][k[x] >> 21], 1);
+                }
+            }
+        }
+        auto key = [&](int i) -> uint32_t {
+            if (i < max_keys) return keys[i];
+            uint32_t k[1];
+            keys_of<1>(a, e, s0 + i, 0, s1, k);
+            return k[0];
+        };
+
+        // the digits of the budget-th largest key, and how many slots that agree with them stay
+        uint32_t known = 0, mask = 0;
+        int want = budget, here = 0;
+        bool found = budget == 0;
+#pragma unroll
+        for (int pass = 0; pass < 3; ++pass) {
+            if (found) break;
+            const int bits = pass < 2 ? 11 : 10, shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+            int* const h = hist[pass & 1];
+            if (pass) {
+                // (cleared since all CTAs read it: there was a barrier of the cluster in between)
                 for (int i = tid; i < BINS; i += NT) h[i] = 0;
                 __syncthreads();
                 for (int i = tid; i < n; i += NT) {
                     const uint32_t k = key(i);
                     if ((k & mask) == known) atomicAdd(h + ((k >> shift) & ((1u << bits) - 1)), 1);
                 }
-                cluster.sync();
-                // thread t adds the cluster's counts of four digits, the highest first
-                int c[BINS / NT], sum = 0;
+            }
+            meet();
+            // a thread adds the cluster's counts of a few digits, the highest first
+            constexpr int PER = BINS / NT;
+            int c[PER], sum = 0;
+            const int d0 = BINS - (tid + 1) * PER;  // its lowest digit
 #pragma unroll
-                for (int x = 0; x < BINS / NT; ++x) {
-                    const int d = BINS - 1 - (tid * (BINS / NT) + x);
-                    c[x] = 0;
-                    for (int b = 0; b < cs; ++b) c[x] += cluster.map_shared_rank(h, b)[d];
-                    sum += c[x];
+            for (int x = 0; x < PER; x += 4) {
+                int4 q = *reinterpret_cast<const int4*>(h + d0 + x);
+                if (CLUSTER) {
+                    q = make_int4(0, 0, 0, 0);
+                    for (int b = 0; b < cs; ++b) {
+                        const int4 o = *reinterpret_cast<const int4*>(cluster.map_shared_rank(h, b) + d0 + x);
+                        q.x += o.x, q.y += o.y, q.z += o.z, q.w += o.w;
+                    }
                 }
-                int2 total;
-                int above = block_scan(make_int2(sum, 0), scratch, total).x;
-                if (above < want && above + sum >= want) {
-                    bool found = false;
+                c[x] = q.x, c[x + 1] = q.y, c[x + 2] = q.z, c[x + 3] = q.w;
+                sum += q.x + q.y + q.z + q.w;
+            }
+            int2 total;
+            int above = block_scan<NT>(make_int2(sum, 0), scratch, total).x;
+            if (above < want && above + sum >= want) {
+                bool got = false;
 #pragma unroll
-                    for (int x = 0; x < BINS / NT; ++x) {
-                        if (!found) {
-                            if (above + c[x] >= want) {
-                                s_digit = BINS - 1 - (tid * (BINS / NT) + x);
-                                s_above = above;
-                                found = true;
-                            } else {
-                                above += c[x];
-                            }
+                for (int x = PER - 1; x >= 0; --x) {
+                    if (!got) {
+                        if (above + c[x] >= want) {
+                            s_digit = d0 + x;
+                            s_above = above;
+                            s_here = c[x];
+                            got = true;
+                        } else {
+                            above += c[x];
                         }
                     }
                 }
-                __syncthreads();
-                known |= (uint32_t)s_digit << shift;
-                mask |= ((1u << bits) - 1) << shift;
-                want -= s_above;
-                // hist[pass & 1] is cleared again two passes on, behind a barrier of the cluster
             }
+            __syncthreads();
+            known |= (uint32_t)s_digit << shift;
+            mask |= ((1u << bits) - 1) << shift;
+            want -= s_above;
+            here = s_here;
+            found = want == here;  // all of them stay
         }
-        // budget 0: no key is above the largest one, and none of it stays
-        if (budget == 0) known = 0xffffffffu;
+        if (budget == 0) known = mask = 0xffffffffu;  // nothing is above the largest key, and none of it stays
 
         // a thread looks at a run of slots (odd, so that a warp's reads fall in
         // different banks); counts before it number its equal keys, then its holes and movers
         const int run = ((n + NT - 1) / NT) | 1, i0 = min(tid * run, n), i1 = min(i0 + run, n);
         auto before_me = [&](int2 total) -> int2 {
-            if (tid == 0) counts = total;
-            cluster.sync();
             int2 v = make_int2(0, 0);
-            for (int b = 0; b < rank; ++b) {
-                const int2 c = *cluster.map_shared_rank(&counts, b);
-                v.x += c.x;
-                v.y += c.y;
+            if (CLUSTER) {
+                if (tid == 0) counts = total;
+                cluster.sync();
+                for (int b = 0; b < rank; ++b) {
+                    const int2 c = *cluster.map_shared_rank(&counts, b);
+                    v.x += c.x;
+                    v.y += c.y;
+                }
+                cluster.sync();
             }
-            cluster.sync();
             return v;
         };
         __syncthreads();
-        int2 mine = make_int2(0, 0), total;
-        for (int i = i0; i < i1; ++i) mine.x += key(i) == known;
-        int2 at = block_scan(mine, scratch, total);
-        const int2 eq0 = before_me(total);
-        const int equal0 = at.x + eq0.x;  // equal keys in front of this thread's run
-        mine = make_int2(0, 0);
-        int equal = equal0;
-        for (int i = i0; i < i1; ++i) {
-            const uint32_t k = key(i);
-            const bool stays = k > known || (k == known && equal++ < want);
-            if (s0 + i < budget) mine.x += !stays;
-            else mine.y += stays;
+        int2 mine = make_int2(0, 0), total, at;
+        int equal0 = 0;  // equal keys in front of this thread's run
+        if (want != here && budget > 0) {
+            for (int i = i0; i < i1; ++i) mine.x += (key(i) & mask) == known;
+            at = block_scan<NT>(mine, scratch, total);
+            equal0 = at.x + before_me(total).x;
         }
-        at = block_scan(mine, scratch, total);
+        int equal = equal0;
+        auto stays = [&](uint32_t k) { return (k & mask) > known || ((k & mask) == known && equal++ < want); };
+        mine = make_int2(0, 0);
+        for (int i = i0; i < i1; ++i) {
+            const bool s = stays(key(i));
+            if (s0 + i < budget) mine.x += !s;
+            else mine.y += s;
+        }
+        at = block_scan<NT>(mine, scratch, total);
         const int2 moved0 = before_me(total);
         at.x += moved0.x;
         at.y += moved0.y;
-        auto note = [&](int where, int slot) {
-            const long long m = meta_at(a, e, where);
-            if (m >= 0) a.lists[m] = slot;
+        // the lists of holes and movers: in shared memory (in place of the counts) where one CTA
+        // has few of them, else in the workspace
+        const bool near = !CLUSTER && total.y <= BINS;
+        auto note = [&](int list, int i, int slot) {
+            if (near) {
+                hist[list][i] = slot;
+            } else {
+                const int w = list ? budget + i : i, p = page_of(a, e, w);
+                if (p >= 0) a.lists[meta_at(a, e, p, w)] = slot;
+            }
         };
         equal = equal0;
         for (int i = i0; i < i1; ++i) {
-            const uint32_t k = key(i);
-            const bool stays = k > known || (k == known && equal++ < want);
+            const bool s = stays(key(i));
             if (s0 + i < budget) {
-                if (!stays) note(at.x++, s0 + i);
-            } else if (stays) {
-                note(budget + at.y++, s0 + i);
+                if (!s) note(0, at.x++, s0 + i);
+            } else if (s) {
+                note(1, at.y++, s0 + i);
             }
         }
-        // the number of moves: the movers of all CTAs
         if (tid == 0) counts = total;
-        __threadfence();
-        cluster.sync();
-        int moves = 0;
-        for (int b = 0; b < cs; ++b) moves += cluster.map_shared_rank(&counts, b)->y;
-
-        const int ch = a.dim / 8, per = 2 * ch;  // 16-byte chunks of a key; of a key and a value
-        const long long work = (long long)moves * per;
-        for (long long x = (long long)rank * NT + tid; x < work; x += (long long)cs * NT) {
-            const int i = (int)(x / per), c = (int)(x - (long long)i * per);
-            const long long ls = meta_at(a, e, budget + i), ld = meta_at(a, e, i);
-            if (ls < 0 || ld < 0) continue;
-            const int src = __ldcg(a.lists + ls), dst = __ldcg(a.lists + ld);
-            const long long ms = meta_at(a, e, src), md = meta_at(a, e, dst);
-            if (ms < 0 || md < 0) continue;
-            char* const pool = c < ch ? a.kv.k : a.kv.v;
-            const int cc = c < ch ? c : c - ch;
-            auto at_slot = [&](int slot) {
-                return pool + (e.row[slot >> a.kv.page_shift] * a.kv.page_stride + e.h * a.kv.head_stride +
-                               (slot & (a.kv.page - 1)) * a.kv.token_stride + cc * 8) * 2;
-            };
-            *reinterpret_cast<uint4*>(at_slot(dst)) = *reinterpret_cast<const uint4*>(at_slot(src));
-            if (c == 0) a.kv.weight[md] = a.kv.weight[ms];
-            if (c == ch) a.kv.pos[md] = a.kv.pos[ms];
+        if (!near) __threadfence();
+        meet();
+        int moves = total.y;
+        if (CLUSTER) {
+            moves = 0;
+            for (int b = 0; b < cs; ++b) moves += cluster.map_shared_rank(&counts, b)->y;
         }
-        cluster.sync();  // the others have read this CTA's counts
+
+        constexpr int CH = D / 8, PER = 2 * CH, U = CLUSTER ? 8 : 4;  // 16-byte pieces of a key, of a key and a value
+        for (int m0 = (rank * (NT / 32) + warp) * 32; m0 < moves; m0 += cs * NT) {
+            const int i = m0 + lane;
+            long long src = -1, dst = -1;
+            if (i < moves) {
+                int slot[2];
+#pragma unroll
+                for (int l = 0; l < 2; ++l) {
+                    if (near) {
+                        slot[l] = hist[l][i];
+                    } else {
+                        const int w = l ? budget + i : i, p = page_of(a, e, w);
+                        slot[l] = p < 0 ? -1 : __ldcg(a.lists + meta_at(a, e, p, w));
+                    }
+                }
+                const int pd = slot[0] < 0 ? -1 : page_of(a, e, slot[0]), ps = slot[1] < 0 ? -1 : page_of(a, e, slot[1]);
+                if (pd >= 0 && ps >= 0) {
+                    src = row_at(a, e, ps, slot[1]);
+                    dst = row_at(a, e, pd, slot[0]);
+                    const long long ms = meta_at(a, e, ps, slot[1]), md = meta_at(a, e, pd, slot[0]);
+                    a.kv.weight[md] = a.kv.weight[ms];
+                    a.kv.pos[md] = a.kv.pos[ms];
+                }
+            }
+            const int pieces = min(32, moves - m0) * PER;
+            for (int x0 = 0; x0 < pieces; x0 += 32 * U) {
+                uint4 v[U];
+                long long to[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int x = x0 + u * 32 + lane, m = x / PER, c = x - m * PER;
+                    const long long s = __shfl_sync(0xffffffffu, src, m & 31);
+                    to[u] = __shfl_sync(0xffffffffu, dst, m & 31);
+                    if (x >= pieces || s < 0) to[u] = -1;
+                    else {
+                        const char* const pool = c < CH ? a.kv.k : a.kv.v;
+                        const int cc = (c < CH ? c : c - CH) * 8;
+                        v[u] = *reinterpret_cast<const uint4*>(pool + (s + cc) * 2);
+                        to[u] += cc;
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int x = x0 + u * 32 + lane, c = x % PER;
+                    if (to[u] >= 0) *reinterpret_cast<uint4*>((c < CH ? a.kv.k : a.kv.v) + to[u] * 2) = v[u];
+                }
+            }
+        }
+        if (CLUSTER) cluster.sync();  // the others have read this CTA's counts
     }
 
     // every CTA has read the lengths: the last one to come here cuts them
@@ -263,19 +364,11 @@ __global__ void __launch_bounds__(NT) k_evict(EvictArgs a, int max_keys)
     }
 }
 
-}  // namespace
-}  // namespace wk
-
-cudaError_t launch_evict(const EvictArgs& a, int sms, cudaStream_t st)
+template <int D, int NT, bool CLUSTER>
+cudaError_t launch(const EvictArgs& a, long long units, int cs, cudaStream_t st)
 {
-    using namespace wk;
-    cudaError_t e = allow_smem<k_evict>(MAX_KEYS * 4);
+    cudaError_t e = allow_smem<k_evict<D, NT, CLUSTER>>(MAX_KEYS * 4);
     if (e != cudaSuccess) return e;
-    // CTAs for one (request, head): as many as fill the GPU once, at most the
-    // portable cluster; few slots need no more than one
-    const long long units = (long long)a.n_req * a.kv.kv_heads;
-    int cs = 1;
-    while (cs < 8 && units * cs * 2 <= 2ll * sms && a.kv.cap > 4096ll * cs) cs *= 2;
     const long long span = (a.kv.cap + cs - 1) / cs;
     const int max_keys = (int)(span < MAX_KEYS ? span : MAX_KEYS);
     cudaLaunchConfig_t c = {};
@@ -289,8 +382,33 @@ cudaError_t launch_evict(const EvictArgs& a, int sms, cudaStream_t st)
     at[0].val.clusterDim.y = 1;
     at[0].val.clusterDim.z = 1;
     c.attrs = at;
-    c.numAttrs = 1;
-    return cudaLaunchKernelEx(&c, k_evict, a, max_keys);
+    c.numAttrs = CLUSTER ? 1 : 0;
+    return cudaLaunchKernelEx(&c, k_evict<D, NT, CLUSTER>, a, max_keys);
+}
+
+template <int D>
+cudaError_t launch_dim(const EvictArgs& a, int sms, cudaStream_t st)
+{
+    // CTAs for a (request, head): as many as fill the GPU twice, at most the portable
+    // cluster, but few slots need no more than one
+    const long long units = (long long)a.n_req * a.kv.kv_heads;
+    int cs = 1;
+    while (cs < 8 && units * cs < 2ll * sms && a.kv.cap > 4096ll * cs) cs *= 2;
+    return cs == 1 ? launch<D, 256, false>(a, units, cs, st) : launch<D, 512, true>(a, units, cs, st);
+}
+
+}  // namespace
+}  // namespace wk
+
+cudaError_t launch_evict(const EvictArgs& a, int sms, cudaStream_t st)
+{
+    switch (a.dim) {
+        case 64: return wk::launch_dim<64>(a, sms, st);
+        case 96: return wk::launch_dim<96>(a, sms, st);
+        case 128: return wk::launch_dim<128>(a, sms, st);
+        case 256: return wk::launch_dim<256>(a, sms, st);
+    }
+    return cudaErrorInvalidValue;
 }
 
 }  // namespace aladdin
