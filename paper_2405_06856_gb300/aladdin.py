@@ -489,8 +489,8 @@ class Cluster:
 
 
 # ---------------------------------------------------------------------------
-# A worker's decode step: the C ABI, one function each, then a wrapper over
-# torch tensors.
+# A worker's decode step: the C ABI, one function each (the wrapper over torch
+# tensors, Worker with make_kv and make_tokens, is in worker.py).
 
 def aladdin_worker_create(shape, stream=None):
     h = C.c_void_p()
@@ -530,251 +530,11 @@ def aladdin_worker_logprobs(wk, dtype, n, vocab, logits, stride, token, top, log
                                         _ptr(top_logprob)), "aladdin_worker_logprobs")
 
 
-def _want(name, x, kind, dim=None, device=None):
-    """x is a CUDA tensor of that type (and dimension, on that device)."""
-    import torch
-    if not isinstance(x, torch.Tensor) or not x.is_cuda:
-        raise TypeError("%s must be a CUDA tensor" % name)
-    if x.dtype is not kind:
-        raise TypeError("%s must be %s, got %s" % (name, kind, x.dtype))
-    if dim is not None and x.dim() != dim:
-        raise ValueError("%s must have %d dimensions, got %d" % (name, dim, x.dim()))
-    if device is not None and x.device != device:
-        raise ValueError("%s is on %s, not on %s" % (name, x.device, device))
-    return x
-
-
-def _ints(name, x, shape, device):
-    """x is a contiguous int32 CUDA tensor of that shape."""
-    import torch
-    _want(name, x, torch.int32, len(shape), device)
-    if tuple(x.shape) != tuple(shape) or not x.is_contiguous():
-        raise ValueError("%s must be contiguous of shape %s" % (name, tuple(shape)))
-    return x
-
-
-def make_kv(k, v, table, length, weight=None, pos=None, next_pos=None):
-    """An aladdin_kv over torch tensors (kept alive by the returned object).
-
-    k, v: [pages, kv_heads, page_tokens, head_dim], any strides with contiguous channels
-    (a pool in [page, token, head, channel] order is passed transposed(1, 2));
-    table: int32 [requests, pages a request may have]; length, next_pos: int32
-    [requests]; weight (float32), pos (int32): [pages, kv_heads, page_tokens]."""
-    import torch
-    dev = k.device
-    _want("k", k, k.dtype, 4)
-    _want("v", v, k.dtype, 4, dev)
-    if k.shape != v.shape or k.stride() != v.stride() or k.stride(3) != 1:
-        raise ValueError("k and v must have the same shape and strides, channels contiguous")
-    _want("table", table, torch.int32, 2, dev)
-    if table.shape[1] > 1 and table.stride(1) != 1:
-        raise ValueError("the rows of table must be contiguous")
-    n = table.shape[0]
-    _ints("length", length, (n,), dev)
-    meta = tuple(k.shape[:3])
-    if weight is not None and (_want("weight", weight, torch.float32, 3, dev).shape != meta
-                               or not weight.is_contiguous()):
-        raise ValueError("weight must be contiguous of shape %s" % (meta,))
-    if pos is not None:
-        _ints("pos", pos, meta, dev)
-    if next_pos is not None:
-        _ints("next_pos", next_pos, (n,), dev)
-    s = k.stride()
-    kv = aladdin_kv(k.data_ptr(), v.data_ptr(), s[0], s[1], s[2], k.shape[0], table.shape[1],
-                    max(table.stride(0), table.shape[1]), table.data_ptr(), length.data_ptr(),
-                    None if weight is None else weight.data_ptr(),
-                    None if pos is None else pos.data_ptr(),
-                    None if next_pos is None else next_pos.data_ptr())
-    kv._keep = (k, v, table, length, weight, pos, next_pos)
-    return kv
-
-
-def make_tokens(off, q, k, v, parent=None):
-    """An aladdin_tokens over torch tensors (kept alive by the returned object).
-
-    off: int32 [requests + 1]; q: [tokens, q_heads, head_dim], k, v: [tokens, kv_heads,
-    head_dim], heads and channels contiguous, any token stride (slices of one
-    projection's output); q may be None where no call needs it; parent: int32 [tokens]."""
-    dev = k.device
-    _want("k", k, k.dtype, 3)
-    n, d = k.shape[0], k.shape[2]
-    for name, x in (("q", q), ("k", k), ("v", v)):
-        if x is None and name == "q":
-            continue
-        _want(name, x, k.dtype, 3, dev)
-        if x.shape[0] != n or x.shape[2] != d or (n and (x.stride(2) != 1 or
-                                                         (x.shape[1] > 1 and x.stride(1) != d))):
-            raise ValueError("%s must be [tokens, heads, head_dim], heads and channels contiguous"
-                             % name)
-    if v.shape != k.shape:
-        raise ValueError("k and v must have the same shape")
-    _ints("off", off, (off.shape[0],), dev)
-    if off.shape[0] < 1:
-        raise ValueError("off must have requests + 1 entries")
-    if parent is not None:
-        _ints("parent", parent, (n,), dev)
-    # the stride of one row may be anything in torch: the row itself then
-    stride = lambda x: x.stride(0) if n > 1 else x.shape[1] * d
-    tok = aladdin_tokens(off.shape[0] - 1, n, off.data_ptr(),
-                         None if parent is None else parent.data_ptr(),
-                         None if q is None else q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                         0 if q is None else stride(q), stride(k), stride(v))
-    tok._keep = (off, parent, q, k, v)
-    return tok
-
-
-class Worker:
-    """A worker's decode step over torch tensors (see aladdin_worker_* in the C ABI).
-
-    kind: "bf16" or "f16". The worker is bound to a stream (default: torch's current
-    one at its creation); a call made while another stream is torch's current one
-    waits for what was launched there before, and what is launched there afterwards
-    waits for the call."""
-
-    KINDS = {"bf16": BF16, "f16": F16}
-
-    def __init__(self, kind, q_heads, kv_heads, head_dim, page_tokens, stream=None):
-        import torch
-        if kind not in self.KINDS:
-            raise ValueError("kind must be one of %s" % sorted(self.KINDS))
-        self.handle = None
-        torch.cuda.init()
-        self.device = torch.device("cuda", torch.cuda.current_device())
-        self.stream = torch.cuda.current_stream().cuda_stream if stream is None else stream
-        self.dtype = torch.bfloat16 if kind == "bf16" else torch.float16
-        self.q_heads, self.kv_heads = int(q_heads), int(kv_heads)
-        self.head_dim, self.page_tokens = int(head_dim), int(page_tokens)
-        self._logits = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}
-        shape = aladdin_worker_shape(self.KINDS[kind], self.q_heads, self.kv_heads, self.head_dim,
-                                     self.page_tokens)
-        self.handle = aladdin_worker_create(shape, self.stream)
-
-    def close(self):
-        if getattr(self, "handle", None):
-            aladdin_worker_destroy(self.handle)
-            self.handle = None
-
-    def __del__(self):
-        try:
-            self.close()
-        except Exception:
-            pass
-
-    def __enter__(self):
-        return self
-
-    def __exit__(self, *a):
-        self.close()
-
-    def status(self):
-        return aladdin_worker_status(self.handle)
-
-    def _ordered(self, call, *args):
-        """call(*args) in the order of torch's current stream."""
-        import torch
-        current = torch.cuda.current_stream(self.device)
-        if current.cuda_stream == self.stream:
-            return call(*args)
-        mine = torch.cuda.ExternalStream(self.stream, self.device)
-        mine.wait_stream(current)
-        call(*args)
-        current.wait_stream(mine)
-
-    def _check_kv(self, kv):
-        k = kv._keep[0]
-        if k.dtype is not self.dtype or k.device != self.device or \
-                tuple(k.shape[1:]) != (self.kv_heads, self.page_tokens, self.head_dim):
-            raise ValueError("the cache does not have the worker's type, device or shape")
-
-    def _check_tokens(self, kv, tok):
-        q, k = tok._keep[2], tok._keep[3]
-        if k.dtype is not self.dtype or k.device != self.device or \
-                tuple(k.shape[1:]) != (self.kv_heads, self.head_dim) or \
-                (q is not None and q.shape[1] != self.q_heads):
-            raise ValueError("the tokens do not have the worker's type, device or shape")
-        if kv._keep[2].shape[0] != tok.n_req:
-            raise ValueError("the cache has %d requests, the tokens %d"
-                             % (kv._keep[2].shape[0], tok.n_req))
-
-    def attend(self, kv, tok, scale=None, out=None, lse=None):
-        """(out [tokens, q_heads, head_dim], lse [tokens, q_heads]); scale defaults to
-        head_dim ** -0.5."""
-        import torch
-        self._check_kv(kv)
-        self._check_tokens(kv, tok)
-        if tok._keep[2] is None:
-            raise ValueError("the tokens have no queries")
-        shape = (tok.n_tok, self.q_heads, self.head_dim)
-        if out is None:
-            out = torch.empty(shape, dtype=self.dtype, device=self.device)
-        else:
-            _want("out", out, self.dtype, 3, self.device)
-            if tuple(out.shape) != shape or out.stride(2) != 1 or \
-                    (self.q_heads > 1 and out.stride(1) != self.head_dim):
-                raise ValueError("out must be %s, heads and channels contiguous" % (shape,))
-        if lse is None:
-            lse = torch.empty(shape[:2], dtype=torch.float32, device=self.device)
-        else:
-            self._floats("lse", lse, shape[:2])
-        stride = out.stride(0) if tok.n_tok > 1 else self.q_heads * self.head_dim
-        self._ordered(aladdin_worker_attend, self.handle, kv, tok,
-                      self.head_dim ** -0.5 if scale is None else scale, out.data_ptr(), stride, lse)
-        return out, lse
-
-    def accept(self, kv, tok, scale=None, lse=None, acc_off=None, acc=None):
-        """Keep tokens (all of them without acc_off and acc) in the cache, in place;
-        with the lse of the tokens' attention the cache's weights grow by what the kept
-        rows attended to."""
-        self._check_kv(kv)
-        self._check_tokens(kv, tok)
-        if (acc_off is None) != (acc is None):
-            raise ValueError("acc_off and acc come together")
-        if acc_off is not None:
-            _ints("acc_off", acc_off, (tok.n_req + 1,), self.device)
-            _ints("acc", acc, (acc.shape[0],), self.device)
-        if lse is not None:
-            if kv.weight is None:
-                raise ValueError("the cache has no weights to add to")
-            self._floats("lse", lse, (tok.n_tok, self.q_heads))
-            if tok._keep[2] is None:
-                raise ValueError("the tokens have no queries")
-        self._ordered(aladdin_worker_accept, self.handle, kv, tok,
-                      self.head_dim ** -0.5 if scale is None else scale, lse, acc_off, acc,
-                      0 if acc is None else acc.shape[0])
-
-    def evict(self, kv, budget, recent=0):
-        """Reduce the cache's requests to budget (int32 [requests]) tokens, in place."""
-        self._check_kv(kv)
-        if kv.weight is None or kv.pos is None or kv.next is None:
-            raise ValueError("eviction needs weight, pos and next_pos")
-        n = kv._keep[2].shape[0]
-        _ints("budget", budget, (n,), self.device)
-        self._ordered(aladdin_worker_evict, self.handle, kv, n, budget, recent)
-
-    def logprobs(self, logits, token=None, top=0):
-        """(logprob, entropy, rank, top_id, top_logprob) of logits [rows, vocab] (contiguous
-        vocabulary) at token int32 [rows]; without token logprob and rank are None."""
-        import torch
-        _want("logits", logits, logits.dtype, 2, self.device)
-        if logits.dtype not in self._logits:
-            raise TypeError("logits must be bfloat16, float16 or float32")
-        n, vocab = logits.shape
-        if vocab > 1 and logits.stride(1) != 1:
-            raise ValueError("the rows of logits must be contiguous")
-        f32 = lambda *s: torch.empty(s, dtype=torch.float32, device=self.device)
-        i32 = lambda *s: torch.empty(s, dtype=torch.int32, device=self.device)
-        logprob = rank = None
-        if token is not None:
-            _ints("token", token, (n,), self.device)
-            logprob, rank = f32(n), i32(n)
-        entropy, top_id, top_logprob = f32(n), i32(n, top), f32(n, top)
-        self._ordered(aladdin_worker_logprobs, self.handle, self._logits[logits.dtype], n, vocab,
-                      logits.data_ptr(), max(logits.stride(0), vocab) if n > 1 else vocab, token, top,
-                      logprob, entropy, rank, top_id if top else None, top_logprob if top else None)
-        return logprob, entropy, rank, top_id, top_logprob
-
-    def _floats(self, name, x, shape):
-        import torch
-        _want(name, x, torch.float32, len(shape), self.device)
-        if tuple(x.shape) != tuple(shape) or not x.is_contiguous():
-            raise ValueError("%s must be contiguous of shape %s" % (name, tuple(shape)))
+def __getattr__(name):
+    """The wrapper over torch tensors, imported (and torch with it) when it is first used."""
+    if name in ("Worker", "make_kv", "make_tokens"):
+        from . import worker
+        for x in ("Worker", "make_kv", "make_tokens"):
+            globals()[x] = getattr(worker, x)
+        return globals()[name]
+    raise AttributeError("module %r has no attribute %r" % (__name__, name))

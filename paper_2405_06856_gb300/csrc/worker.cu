@@ -20,7 +20,8 @@ struct aladdin_worker {
     char* fixed = nullptr;
     unsigned* err = nullptr;
     int* done = nullptr;     // CTAs of an accept or evict call that have finished
-    int* arrived = nullptr;  // [2 * sms]
+    int* arrived = nullptr;  // [ATTEND_WORKERS_PER_SM * sms]
+    size_t ints = 0;         // bytes of the word and the counters
     float* part = nullptr;
     int32_t* lists = nullptr;  // evict (grow-only)
     size_t lists_n = 0;
@@ -158,8 +159,9 @@ try {
     wk->st = (cudaStream_t)cuda_stream;
     wk->shape = *shape;
     while ((1 << wk->page_shift) < shape->page_tokens) ++wk->page_shift;
-    const size_t ints = ((size_t)(2 + 2 * d.sms) * 4 + 255) / 256 * 256;
-    const size_t bytes = ints + attend_part_bytes(2 * d.sms, shape->head_dim);
+    const size_t ints = ((size_t)(2 + ATTEND_WORKERS_PER_SM * d.sms) * 4 + 255) / 256 * 256;
+    wk->ints = ints;
+    const size_t bytes = ints + attend_part_bytes(d.sms, shape->head_dim);
     cudaError_t e = cudaMalloc((void**)&wk->fixed, bytes);
     if (e == cudaSuccess) e = cudaMemsetAsync(wk->fixed, 0, ints, wk->st);
     if (e == cudaSuccess) e = cudaStreamSynchronize(wk->st);
@@ -195,8 +197,9 @@ try {
     CK(cudaSetDevice(wk->device));
     unsigned err = 0;
     CK(cudaMemcpyAsync(&err, wk->err, sizeof(err), cudaMemcpyDeviceToHost, wk->st));
-    CK(cudaMemsetAsync(wk->err, 0, sizeof(err), wk->st));
     CK(cudaStreamSynchronize(wk->st));
+    if (err) CK(cudaMemsetAsync(wk->fixed, 0, wk->ints, wk->st));  // counters of a call that gave up, too
+    if (err & WORKER_TIMEOUT) return ALADDIN_ERR_TIMEOUT;
     return err ? ALADDIN_ERR_STATE : ALADDIN_OK;
 } catch (...) {
     return ALADDIN_ERR_NOMEM;

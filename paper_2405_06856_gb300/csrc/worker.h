@@ -57,6 +57,7 @@ struct TokDev {
 
 // Bits of a worker's error word.
 constexpr unsigned WORKER_BAD_INPUT = 1u;
+constexpr unsigned WORKER_TIMEOUT = 4u;  // a wait for a copy ran out
 
 struct AttendArgs {
     KvDev kv;
@@ -65,8 +66,8 @@ struct AttendArgs {
     char* out;
     long long out_stride;
     float* lse;
-    float* part;            // split units' partial results, 2 slots a CTA
-    int* arrived;           // split units' arrivals, one a CTA, zero between calls
+    float* part;            // split units' partial results, 2 slots a worker
+    int* arrived;           // split units' arrivals, one a worker, zero between calls
     unsigned* err;
 };
 
@@ -106,9 +107,16 @@ struct LogprobArgs {
     unsigned* err;
 };
 
-// Bytes of AttendArgs::part on the current device for a head dimension.
-constexpr int ATTEND_MAX_ROWS = 64;
-size_t attend_part_bytes(int ctas, int dim);
+// Workers of an attention launch on one SM, at most (warps, or a CTA's row tiles), and
+// the bytes of AttendArgs::part: two units of each SM's CTA of at most 256 rows (128
+// of 256 channels), or of at most 8 warps of 16 rows.
+constexpr int ATTEND_WORKERS_PER_SM = 8;
+inline size_t attend_part_bytes(int sms, int dim)
+{
+    return (size_t)sms * 2 * (dim < 256 ? 256 : 128) * (dim + 2) * sizeof(float);
+}
+cudaError_t launch_attend_few(const AttendArgs& a, int dtype, int dim, int sms, cudaStream_t st);
+cudaError_t launch_attend_many(const AttendArgs& a, int dtype, int dim, int sms, cudaStream_t st);
 cudaError_t launch_attend(const AttendArgs& a, int dtype, int dim, int sms, cudaStream_t st);
 cudaError_t launch_accept(const AcceptArgs& a, int dtype, int dim, int sms, cudaStream_t st);
 cudaError_t launch_evict(const EvictArgs& a, int sms, cudaStream_t st);

@@ -6,6 +6,8 @@
 #include <cuda_fp16.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "worker.h"
 
 namespace aladdin {
@@ -34,6 +36,54 @@ __device__ __forceinline__ void cp_wait()
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
+// Barriers in shared memory that count arrivals and bytes, by address.
+__device__ __forceinline__ void mbar_init(uint32_t bar, int count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+// Makes this thread's barriers visible to copies.
+__device__ __forceinline__ void mbar_init_fence()
+{
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// Whether the phase of that parity has come.
+__device__ __forceinline__ bool mbar_test(uint32_t bar, unsigned parity)
+{
+    unsigned done;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(done)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return done;
+}
+// Waits for the phase of that parity; false where it did not come within a second.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, unsigned parity)
+{
+    unsigned long long end = 0;
+    for (unsigned it = 0;; ++it) {
+        unsigned done;
+        asm volatile(
+            "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+            : "=r"(done)
+            : "r"(bar), "r"(parity)
+            : "memory");
+        if (done) return true;
+        if ((it & 63) == 63) {
+            unsigned long long now;
+            asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
+            if (!end) end = now + 1000000000ull;
+            else if (now > end) return false;
+        }
+    }
+}
+// Orders this thread's plain accesses to shared memory before later copies by the
+// asynchronous proxy.
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr)
 {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
@@ -47,6 +97,15 @@ __device__ __forceinline__ void ldmatrix4t(uint32_t (&r)[4], uint32_t addr)
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
                  : "r"(addr)
                  : "memory");
+}
+
+// The 8 x 8 matrix of 16-bit values whose row g, columns 2t and 2t + 1 lane
+// 4 g + t holds, transposed.
+__device__ __forceinline__ uint32_t transpose8(uint32_t x)
+{
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
 }
 
 // 2^x; -inf gives 0.
@@ -78,6 +137,12 @@ struct Num<__nv_bfloat16> {
     {
         return (u & 0x7f80u) == 0x7f80u || (u & 0x7f800000u) == 0x7f800000u;
     }
+    // 0 in the place of those
+    static __device__ __forceinline__ uint32_t tame(uint32_t u)
+    {
+        if ((u & 0x7f80u) == 0x7f80u) u &= 0xffff0000u;
+        return (u & 0x7f800000u) == 0x7f800000u ? u & 0xffffu : u;
+    }
     static __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0,
                                                uint32_t b1)
     {
@@ -102,6 +167,11 @@ struct Num<__half> {
     static __device__ __forceinline__ bool wild(uint32_t u)
     {
         return (u & 0x7c00u) == 0x7c00u || (u & 0x7c000000u) == 0x7c000000u;
+    }
+    static __device__ __forceinline__ uint32_t tame(uint32_t u)
+    {
+        if ((u & 0x7c00u) == 0x7c00u) u &= 0xffff0000u;
+        return (u & 0x7c000000u) == 0x7c000000u ? u & 0xffffu : u;
     }
     static __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0,
                                                uint32_t b1)
