@@ -4,7 +4,7 @@
 //
 // A CTA runs through a range of the axis of all key tiles, MT tiles of 128 rows at
 // a time. Its warps have roles:
-//   four warps copy keys and values (and at a unit's start its queries) into a ring
+//   three warps copy keys and values (and at a unit's start its queries) into a ring
 //   of shared memory, in the order K0 V0 K1 V1 ..., in the 128-byte-swizzled layout
 //   of the matrix descriptors: tiles of cached tokens by tensor copies (TMA), a page
 //   or a part of one each, that one thread starts; the queries and the tiles with new
@@ -17,7 +17,9 @@
 // other; with one, the scores of the next tile are formed ahead into a second
 // place. The accumulator stays in tensor memory; it is rescaled only when a row's
 // maximum has grown by more than 2^8 over the one that its weights refer to, which
-// 32-bit sums and 16-bit weights hold without loss.
+// 32-bit sums and 16-bit weights hold without loss. The softmax's loops stay rolled
+// (unrolled over a tile, with the scores read once and the weights held in registers,
+// they took 1.6 times as long).
 //
 // New tokens' values that are not finite would reach rows that do not see them
 // (0 times infinity): they are replaced by 0 in shared memory, and rows that do
@@ -175,7 +177,8 @@ struct Many {
     static constexpr int scratch = last + 8;
     static constexpr int pre = scratch + 32 * 8;
     static constexpr int bytes(int n_req) { return pre + (n_req + 1) * 8; }
-    static constexpr int WARPS = 4 * MT + 1 + 4;         // softmax, products, copies
+    static constexpr int COPIES = 3;                     // warps that copy
+    static constexpr int WARPS = 4 * MT + 1 + COPIES;    // softmax, products, copies
     // columns of tensor memory: the scores' two places, the accumulators
     static constexpr int s0 = 0, o0 = 2 * KT;
     static_assert(o0 + MT * HALVES * 64 <= 512, "tensor memory");
@@ -216,11 +219,11 @@ __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(Atte
     if (warp == 0) tmem_alloc(sm0 + L::tmem, 512);
     if (tid == 0) {
         for (int b = 0; b < NB; ++b) {
-            mbar_init(sm0 + L::full + b * 8, 4);
+            mbar_init(sm0 + L::full + b * 8, L::COPIES);
             mbar_init(sm0 + L::empty + b * 8, 1);
         }
         for (int b = 0; b < NQ; ++b) {
-            mbar_init(sm0 + L::qfull + b * 8, 4);
+            mbar_init(sm0 + L::qfull + b * 8, L::COPIES);
             mbar_init(sm0 + L::qempty + b * 8, 1);
         }
         for (int w = 0; w < 2; ++w) {
@@ -247,17 +250,18 @@ __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(Atte
 
     if (warp >= 4 * MT + 1) {
         // ------------------------------------------------------------ copies
-        const int ct = tid - (4 * MT + 1) * 32;
-        int pg[PG];
-        auto pages = [&]() {
-#pragma unroll
-            for (int g = 0; g < PG; ++g) {
-                const int key = C.tile * KT + g * 16;
-                pg[g] = key < C.len ? a.kv.table[(long long)C.r * a.kv.table_stride + (key >> a.kv.page_shift)] : 0;
-            }
+        constexpr int CT = L::COPIES * 32, STEP = CT / CH;  // rows that the threads copy at a time
+        static_assert(CT % CH == 0, "a thread copies one chunk of every STEP-th row");
+        const int ct = tid - (4 * MT + 1) * 32, cw = ct >> 5, r0 = ct / CH, ch = ct % CH;
+        // the page of keys [16 lane, 16 lane + 16) of the tile under u, as the table has it
+        auto pages = [&](const Cursor& u) -> int {
+            const int key = u.tile * KT + lane * 16;
+            return lane < PG && key < u.len
+                       ? a.kv.table[(long long)u.r * a.kv.table_stride + (key >> a.kv.page_shift)]
+                       : 0;
         };
-        // byte of chunk ch of row `row` in a block of `rows` rows
-        auto at = [](int row, int ch, int rows) {
+        // byte of this thread's chunk of row `row` in a block of `rows` rows
+        auto at = [&](int row, int rows) {
             return (uint32_t)((ch >> 3) * rows * 128 + row * 128 + (((ch & 7) ^ (row & 7)) << 4));
         };
         int units = -1, waiting = 0;   // copies of 16 bytes a time that are not signalled yet: the oldest first,
@@ -289,94 +293,117 @@ __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(Atte
             drain();
             ok = __all_sync(0xffffffffu, wait(bar, phase));
         };
-        pages();
+        int page = pages(C);
         for (int j = 0; j < n && ok; ++j) {
             const bool start = j == 0 || C.tile == 0;
-            unsigned mask = 0;
-#pragma unroll
-            for (int g = 0; g < PG; ++g) {
-                if ((unsigned)pg[g] < (unsigned)a.kv.pages) mask |= 1u << g;
-                else if (ct == 0) atomicOr(a.err, WORKER_BAD_INPUT);
+            const bool have = (unsigned)page < (unsigned)a.kv.pages;
+            if (lane < PG && !have && cw == 0) atomicOr(a.err, WORKER_BAD_INPUT);
+            const unsigned mask = __ballot_sync(0xffffffffu, have) & ((1u << PG) - 1);
+            Cursor N = C;  // the next tile, its pages on their way
+            int page_next = 0;
+            if (j + 1 < n) {
+                advance<KT, RM>(a, N, pre);
+                page_next = pages(N);
             }
             const int key0 = C.tile * KT, own = C.len - key0, all = own + C.T;
-            const long long head = (long long)C.h * a.kv.head_stride, row_at = (long long)C.r * a.kv.table_stride;
+            // boxes of cached keys, in turn to the warps, one a lane
+            const int boxes = maps.rows ? min(max(own, 0), KT) / maps.rows : 0, rest = boxes * maps.rows;
+            const int box = lane * L::COPIES + cw, box_half = box % L::HALVES, box_row = box / L::HALVES * maps.rows;
+            const int box_page = __shfl_sync(0xffffffffu, page, box_row >> 4 & 31);
+            const int my_boxes = (boxes * L::HALVES - cw + L::COPIES - 1) / L::COPIES;
 #pragma unroll 1
             for (int part = 0; part < 2 && ok; ++part) {  // keys, values
                 const int i = 2 * j + part, slot = i % NB;
                 if (i >= NB) room(sm0 + L::empty + slot * 8, i / NB - 1);
                 if (!ok) break;
-                const uint32_t d = sm0 + slot * L::TILE;
+                const uint32_t d = sm0 + slot * L::TILE, bar = sm0 + L::full + slot * 8;
                 if (part == 0 && start) {
                     ++units;
                     if (units >= NQ) room(sm0 + L::qempty + units % NQ * 8, units / NQ - 1);
                     if (!ok) break;
-                    const int rows = C.T * G - C.rt * RM;
-                    const uint32_t qd = sm0 + L::q + units % NQ * (MT * L::QT);
-                    for (int x = ct; x < min(rows, RM) * CH; x += 128) {
-                        const int row = x / CH, ch = x - row * CH, rho = C.rt * RM + row, t = rho / G, g = rho - t * G;
-                        cp16(qd + (row >> 7) * L::QT + at(row & 127, ch, 128),
-                             a.tok.q + ((C.lo + t) * a.tok.q_stride + (long long)(C.h * G + g) * D + ch * 8) * 2, true);
-                    }
-                    copied(128 | units % NQ);
+                }
+                if (boxes) {
+                    if (lane == 0) mbar_expect(bar, my_boxes * maps.rows * 128);
+                    __syncwarp();
+                    // (a page outside the pool: zeros, and the tile's mask hides them)
+                    if (lane < my_boxes)
+                        box_copy(d + box_half * KT * 128 + box_row * 128, part ? &maps.v : &maps.k, box_half * 64,
+                                 (key0 + box_row) & (a.kv.page - 1), C.h, box_page, bar);
+                    __syncwarp();
                 }
                 if (part == 0 && ct == 0) okm[j & 7] = (int)mask;
-                const char* const pool = part ? a.kv.v : a.kv.k;
-                const uint32_t bar = sm0 + L::full + slot * 8;
-                if (own >= KT && maps.rows) {
-                    // cached keys only
-                    if (ct < 32) {
-                        if (lane == 0) mbar_expect(bar, L::TILE);
-                        __syncwarp();
-                        const CUtensorMap* const map = part ? &maps.v : &maps.k;
-                        for (int x = lane; x < KT / maps.rows * L::HALVES; x += 32) {
-                            const int half = x % L::HALVES, row = x / L::HALVES * maps.rows;
-                            // (a page outside the pool: zeros, and the tile's mask hides them)
-                            box_copy(d + half * KT * 128 + row * 128, map, half * 64, (key0 + row) & (a.kv.page - 1),
-                                     C.h, a.kv.table[row_at + ((key0 + row) >> a.kv.page_shift)], bar);
-                        }
-                    }
-                    __syncwarp();
+                if (rest == KT) {
                     if (lane == 0) mbar_arrive(bar);
                 } else {
                     bool w = false;
-                    for (int x = ct; x < KT * CH; x += 128) {
-                        const int row = x / CH, ch = x - row * CH;
-                        const uint32_t to = d + at(row, ch, KT);
-                        if (row >= own && row < all && part) {
-                            // a new token's value: numbers that are not finite become 0
-                            uint4 v = *reinterpret_cast<const uint4*>(
-                                a.tok.v + ((long long)(C.lo + row - own) * a.tok.v_stride + C.h * D + ch * 8) * 2);
-                            if (Num<T>::wild(v.x) || Num<T>::wild(v.y) || Num<T>::wild(v.z) || Num<T>::wild(v.w)) {
-                                w = true;
-                                v.x = Num<T>::tame(v.x), v.y = Num<T>::tame(v.y);
-                                v.z = Num<T>::tame(v.z), v.w = Num<T>::tame(v.w);
-                            }
-                            *reinterpret_cast<uint4*>(sm + (to - sm0)) = v;
-                            continue;
+                    // cached rows behind the boxes
+                    const char* const pool = part ? a.kv.v : a.kv.k;
+                    const long long head = (long long)C.h * a.kv.head_stride + ch * 8;
+                    for (int row0 = rest; row0 < min(own, KT); row0 += STEP) {
+                        const int row = row0 + r0, p = __shfl_sync(0xffffffffu, page, row >> 4 & 31);
+                        if (row < min(own, KT)) {
+                            const bool ok1 = mask >> (row >> 4) & 1;
+                            const long long e = ok1 ? p * a.kv.page_stride + head +
+                                                          ((key0 + row) & (a.kv.page - 1)) * a.kv.token_stride
+                                                    : 0;
+                            cp16(d + at(row, KT), pool + e * 2, ok1);
                         }
-                        const char* src = pool;
-                        bool have = row < all;
-                        if (row < own) {
-                            int p = 0;
-#pragma unroll
-                            for (int g = 0; g < PG; ++g) p = row >> 4 == g ? pg[g] : p;
-                            have = mask >> (row >> 4) & 1;
-                            if (have)
-                                src += (p * a.kv.page_stride + head +
-                                        ((key0 + row) & (a.kv.page - 1)) * a.kv.token_stride + ch * 8) * 2;
-                        } else if (have) {
-                            src = a.tok.k + ((long long)(C.lo + row - own) * a.tok.k_stride + C.h * D + ch * 8) * 2;
-                        }
-                        cp16(to, src, have);
                     }
-                    if (w) wilds[units & 7] = units + 1;
+                    // new tokens
+                    const int lo = max(own, 0), hi = min(all, KT);
+                    if (part == 0) {
+                        const char* src = a.tok.k + ((long long)(C.lo + lo + r0 - own) * a.tok.k_stride + C.h * D + ch * 8) * 2;
+                        for (int row = lo + r0; row < hi; row += STEP, src += STEP * a.tok.k_stride * 2)
+                            cp16(d + at(row, KT), src, true);
+                        // (keys of rows that hold no token are masked, whatever they are)
+                    } else {
+                        // values that are not finite become 0
+                        const char* src = a.tok.v + ((long long)(C.lo + lo + r0 - own) * a.tok.v_stride + C.h * D + ch * 8) * 2;
+                        for (int row = lo + r0; row < hi; row += 4 * STEP) {
+                            uint4 v[4];
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) {
+                                v[x] = make_uint4(0, 0, 0, 0);
+                                if (row + x * STEP < hi) v[x] = *reinterpret_cast<const uint4*>(src);
+                                src += STEP * a.tok.v_stride * 2;
+                            }
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) {
+                                if (Num<T>::wild(v[x].x) || Num<T>::wild(v[x].y) || Num<T>::wild(v[x].z) ||
+                                    Num<T>::wild(v[x].w)) {
+                                    w = true;
+                                    v[x].x = Num<T>::tame(v[x].x), v[x].y = Num<T>::tame(v[x].y);
+                                    v[x].z = Num<T>::tame(v[x].z), v[x].w = Num<T>::tame(v[x].w);
+                                }
+                                if (row + x * STEP < hi)
+                                    *reinterpret_cast<uint4*>(sm + slot * L::TILE + at(row + x * STEP, KT)) = v[x];
+                            }
+                        }
+                        // weights of 0 meet the values of rows that hold no token: zeros
+                        for (int row = hi + r0; row < KT; row += STEP)
+                            *reinterpret_cast<uint4*>(sm + slot * L::TILE + at(row, KT)) = make_uint4(0, 0, 0, 0);
+                        if (w) wilds[units & 7] = units + 1;
+                    }
                     copied(slot + 1);
                 }
+                if (part == 0 && start) {
+                    // the unit's queries, behind its first keys
+                    const int rows = min(C.T * G - C.rt * RM, RM);
+                    const uint32_t qd = sm0 + L::q + units % NQ * (MT * L::QT);
+                    int t = (C.rt * RM + r0) / G, g = C.rt * RM + r0 - t * G;
+                    const char* const base = a.tok.q + ((long long)C.lo * a.tok.q_stride + (long long)C.h * G * D + ch * 8) * 2;
+#pragma unroll 4
+                    for (int row = r0; row < rows; row += STEP) {
+                        cp16(qd + (row >> 7) * L::QT + at(row & 127, 128), base + (t * a.tok.q_stride + g * D) * 2, true);
+                        g += STEP;
+                        while (g >= G) g -= G, ++t;
+                    }
+                    copied(128 | units % NQ);
+                    drain();
+                }
             }
-            if (ok && j + 1 < n) {
-                advance<KT, RM>(a, C, pre);
-                pages();
-            }
+            C = N;
+            page = page_next;
         }
         drain();
     } else if (warp == 4 * MT) {
@@ -434,7 +461,8 @@ __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(Atte
                     leave_tile();
                 }
                 const int v = 2 * j + 1;
-                bool entered = false;
+                // (the next unit's queries may not be there yet: this unit's values come first)
+                const bool turns = C.tile + 1 == C.c;
 #pragma unroll
                 for (int w = 0; w < MT; ++w) {
                     if (active(C, w)) {
@@ -457,10 +485,9 @@ __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(Atte
                         }
                         __syncwarp();
                     }
-                    if (MT == 2 && more) {
-                        if (!entered) {
+                    if (MT == 2 && more && !turns) {
+                        if (w == 0) {
                             enter_tile();
-                            entered = true;
                             if (!ok) break;
                         }
                         if (active(N, w)) scores(w, w);
@@ -469,6 +496,13 @@ __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(Atte
                 if (!ok) break;
                 if (leader) tc_commit(sm0 + L::empty + v % NB * 8);
                 __syncwarp();
+                if (MT == 2 && more && turns) {
+                    enter_tile();
+                    if (!ok) break;
+#pragma unroll
+                    for (int w = 0; w < MT; ++w)
+                        if (active(N, w)) scores(w, w);
+                }
                 if (MT == 2 && more) leave_tile();
                 if (more) advance<KT, RM>(a, C, pre);
             }
@@ -519,16 +553,14 @@ __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(Atte
                 };
                 // 32 scores at a time, the next ones on their way
                 uint32_t va[32], vb[32];
-                float top = -INFINITY;
+                float t0 = -INFINITY, t1 = -INFINITY;
                 auto highest = [&](uint32_t(&v)[32], int c) {
                     if (masked) mask(v, c);
-                    float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int i = 0; i < 32; i += 8)
-#pragma unroll
-                        for (int x = 0; x < 4; ++x)
-                            t[x] = fmaxf(fmaxf(t[x], __uint_as_float(v[i + x * 2])), __uint_as_float(v[i + x * 2 + 1]));
-                    top = fmaxf(top, fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])));
+                    for (int i = 0; i < 32; i += 4) {
+                        t0 = fmaxf(fmaxf(t0, __uint_as_float(v[i])), __uint_as_float(v[i + 1]));
+                        t1 = fmaxf(fmaxf(t1, __uint_as_float(v[i + 2])), __uint_as_float(v[i + 3]));
+                    }
                 };
                 tmem_start(va, st);
 #pragma unroll 1
@@ -540,7 +572,7 @@ __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(Atte
                     tmem_start(va, st + (c + 2 < KT / 32 ? c * 32 + 64 : 0));  // in the end the first ones again
                     highest(vb, c + 1);
                 }
-                top *= a.scale_log2;
+                const float top = fmaxf(t0, t1) * a.scale_log2;
                 // the weights of the tile before are in the accumulator
                 if (done) ok = __all_sync(0xffffffffu, wait(sm0 + L::odone + w * 8, done - 1));
                 if (!ok) break;
@@ -553,13 +585,13 @@ __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(Atte
                         const float f = grown ? ex2(m - top) : 1.0f;
                         if (grown) m = top;
                         l *= f;
+                        tmem_loaded(va);
 #pragma unroll 1
                         for (int c = 0; c < (D + 31) / 32; ++c) {
-                            uint32_t v[32];
-                            tmem_load(v, om + c * 32);
+                            tmem_load(vb, om + c * 32);
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
-                            tmem_store32(om + c * 32, v);
+                            for (int i = 0; i < 32; ++i) vb[i] = __float_as_uint(__uint_as_float(vb[i]) * f);
+                            tmem_store32(om + c * 32, vb);
                         }
                     }
                 }
@@ -678,7 +710,7 @@ __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(Atte
                             const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
                             uint4* const d = reinterpret_cast<uint4*>(
                                 a.out + ((C.lo + t) * a.out_stride + (long long)hd * D) * 2);
-#pragma unroll 1
+#pragma unroll 2
                             for (int c = 0; c < D / 32; ++c) {
                                 float4 acc[8];
 #pragma unroll
