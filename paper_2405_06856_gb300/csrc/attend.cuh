@@ -73,25 +73,13 @@ struct Axis {
     }
 };
 
-// Lays the requests on the axis, the block's threads together; pre and tiles hold
-// n_req + 1 entries each. A request whose offsets or length make no sense has no
-// tiles and is recorded. false: nothing to do.
-template <int KT, int RM, int NT>
-__device__ __forceinline__ bool plan(const AttendArgs& a, Axis& x, int* pre, int* tiles, long long* scratch,
-                                     int most, int ov, int ct)
+// Lays n requests on the axis, the block's threads together; pre and tiles hold n + 1
+// entries each. of(r, c) gives the units of request r and sets c to the tiles of one.
+// false: nothing to do.
+template <int NT, typename F>
+__device__ __forceinline__ bool plan(int n, Axis& x, int* pre, int* tiles, long long* scratch, int most, int ov,
+                                     int ct, unsigned* err, F of)
 {
-    const int n = a.tok.n_req, H = a.kv.kv_heads, G = a.kv.group;
-    // (units, and tiles of one) of a request
-    auto of = [&](int r, int& c) -> int {
-        const int lo = a.tok.off[r], hi = a.tok.off[r + 1], len = a.kv.len[r];
-        if (lo < 0 || hi < lo || hi > a.tok.n_tok || hi - lo > ALADDIN_TREE_MAX || len < 0 || len > a.kv.cap) {
-            if (blockIdx.x == 0) atomicOr(a.err, WORKER_BAD_INPUT);
-            c = 0;
-            return 0;
-        }
-        c = (len + hi - lo + KT - 1) / KT;
-        return ((hi - lo) * G + RM - 1) / RM * H;
-    };
     const int all = plan_prefix<NT>(n, tiles, scratch, [&](int r) -> long long {
         int c;
         const int units = of(r, c);
@@ -105,14 +93,29 @@ __device__ __forceinline__ bool plan(const AttendArgs& a, Axis& x, int* pre, int
     x.total = all <= 0 ? all : plan_prefix<NT>(n, pre, scratch, [&](int r) -> long long {
         int c;
         const int units = of(r, c);
-        return (long long)units * x.places(c);
+        return units ? (long long)units * x.places(c) : 0;
     });
     if (x.total <= 0) {
-        if (x.total < 0 && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.err, WORKER_BAD_INPUT);
+        if (x.total < 0 && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(err, WORKER_BAD_INPUT);
         return false;
     }
     x.workers = min(most, x.total);
     return true;
+}
+
+// The attention's requests: units of a key head's row tiles. A request whose offsets or
+// length make no sense has none and is recorded.
+template <int KT, int RM>
+__device__ __forceinline__ int attend_units(const AttendArgs& a, int r, int& c)
+{
+    const int lo = a.tok.off[r], hi = a.tok.off[r + 1], len = a.kv.len[r];
+    if (lo < 0 || hi < lo || hi > a.tok.n_tok || hi - lo > ALADDIN_TREE_MAX || len < 0 || len > a.kv.cap) {
+        if (blockIdx.x == 0) atomicOr(a.err, WORKER_BAD_INPUT);
+        c = 0;
+        return 0;
+    }
+    c = (len + hi - lo + KT - 1) / KT;
+    return ((hi - lo) * a.kv.group + RM - 1) / RM * a.kv.kv_heads;
 }
 
 // The cursor at place x < total; returns the tiles in front of it.

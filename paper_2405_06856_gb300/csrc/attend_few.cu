@@ -56,8 +56,9 @@ __global__ void __launch_bounds__(Few<D>::WARPS * 32, 1) k_attend_few(AttendArgs
     unsigned* const oks = reinterpret_cast<unsigned*>(sm + L::oks) + warp * S;
 
     Axis ax;
-    if (!plan<TK, RM, NT>(a, ax, pre, pre + a.tok.n_req + 1, reinterpret_cast<long long*>(sm + L::scratch),
-                          (int)gridDim.x * L::WARPS, UNIT_KEYS / TK, PLACE_KEYS / TK))
+    if (!plan<NT>(a.tok.n_req, ax, pre, pre + a.tok.n_req + 1, reinterpret_cast<long long*>(sm + L::scratch),
+                  (int)gridDim.x * L::WARPS, UNIT_KEYS / TK, PLACE_KEYS / TK, a.err,
+                  [&](int r, int& c) { return attend_units<TK, RM>(a, r, c); }))
         return;
     // neighbouring ranges lie on different SMs
     const int me = warp * gridDim.x + blockIdx.x;
@@ -111,7 +112,7 @@ __global__ void __launch_bounds__(Few<D>::WARPS * 32, 1) k_attend_few(AttendArgs
             const int all = own + F.T;  // keys from the tile's start
             const unsigned cached = own >= TK ? ~0u : own > 0 ? (1u << own) - 1 : 0u;
             mask = ((mask & cached) | ~cached) & (all >= TK ? L::FULL : (1u << all) - 1);
-#pragma unroll
+#pragma unroll 2
             for (int i = 0; i < (TK * CH + 31) / 32; ++i) {
                 const int x = lane + i * 32, row = x / CH, ch = x - row * CH;
                 if ((TK * CH) % 32 && x >= TK * CH) break;

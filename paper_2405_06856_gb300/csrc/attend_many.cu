@@ -207,8 +207,9 @@ __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(Atte
         return;
     }
     Axis ax;
-    if (!plan<KT, RM, NT>(a, ax, pre, pre + a.tok.n_req + 1, reinterpret_cast<long long*>(sm + L::scratch),
-                          (int)gridDim.x, UNIT_TILES, 1))
+    if (!plan<NT>(a.tok.n_req, ax, pre, pre + a.tok.n_req + 1, reinterpret_cast<long long*>(sm + L::scratch),
+                  (int)gridDim.x, UNIT_TILES, 1, a.err,
+                  [&](int r, int& c) { return attend_units<KT, RM>(a, r, c); }))
         return;
     const int me = blockIdx.x;
     if (me >= ax.workers) return;
