@@ -10,8 +10,10 @@
 // not know. What counts is bytes in flight, as in the attention of few rows
 // (attend_few.cu), and the kernel is built the same way: every warp works alone on
 // a range of the axis of all key tiles, copies a few tiles ahead and forms keys by
-// rows products with 8 rows an operand; the queries of a unit (request, head) stay
-// in registers, up to 8 NB rows, more are read again for every tile. A slot
+// rows products with 8 rows an operand. The queries of a unit (request, head) stay
+// in registers where they are 8 rows, else in shared memory, in a rolled loop (with
+// 48 rows in registers the unrolled code did not fit the instruction cache: 89 us
+// for 24 requests' trees instead of 72); more rows are read again for every tile. A slot
 // belongs to one tile, so each weight is read and written once, sums run in 32 bits
 // in a fixed order, and the tile that holds a new slot writes its key, value, weight
 // and position. The last CTA to finish advances the lengths.
@@ -21,17 +23,20 @@ namespace aladdin {
 namespace wk {
 namespace {
 
-template <int D, int NB>
+// FEW: a unit has 8 rows.
+template <int D, bool FEW>
 struct Accept {
-    static constexpr int TK = D == 256 || NB == 1 ? 16 : 32;  // keys of a tile
-    static constexpr int KB = TK / 16;                   // blocks of 16 keys
-    static constexpr int WARPS = NB == 1 && D < 256 ? 16 : 8;  // warps of a CTA, one CTA an SM
-    static constexpr int S = D == 64 ? 5 : D == 96 ? 4 : 3;    // tiles of a warp
+    static constexpr int TK = 16;                        // keys of a tile
+    static constexpr int WARPS = FEW && D < 256 ? 16 : 8;  // warps of a CTA, one CTA an SM
+    static constexpr int S = D == 64 ? 5 : D == 96 ? 4 : D == 256 && !FEW ? 2 : 3;  // tiles of a warp
+    static constexpr int ROWS = FEW ? 8 : D == 256 ? 16 : D == 128 ? 48 : 64;  // rows that are held
     static constexpr int PITCH = D * 2 + 16;             // (rows in different banks)
     static constexpr int TILE = TK * PITCH;
-    static constexpr int w = WARPS * S * TILE;           // weights of the tiles' keys
-    static constexpr int pages = w + WARPS * S * TK * 4; // their pages, 16 keys each
-    static constexpr int scratch = (pages + WARPS * S * KB * 4 + 7) / 8 * 8;
+    static constexpr int q = WARPS * S * TILE;           // the warps' rows
+    static constexpr int lse = q + (FEW ? 0 : WARPS * ROWS * PITCH);
+    static constexpr int w = lse + (FEW ? 0 : WARPS * ROWS * 4);  // weights of the tiles' keys
+    static constexpr int pages = w + WARPS * S * TK * 4; // their pages
+    static constexpr int scratch = (pages + WARPS * S * 4 + 7) / 8 * 8;
     static constexpr int pre = scratch + 32 * 8;
     static constexpr int bytes(int n_req) { return pre + (n_req + 1) * 8; }
 };
@@ -86,12 +91,12 @@ __device__ __forceinline__ int kept(const AcceptArgs& a, const Unit& u, int i)
     return u.lo + (a.acc_off ? a.acc[u.a0 + i] : i);
 }
 
-template <typename T, int D, int NB>
-__global__ void __launch_bounds__(Accept<D, NB>::WARPS * 32, 1) k_accept(AcceptArgs a)
+template <typename T, int D, bool FEW>
+__global__ void __launch_bounds__(Accept<D, FEW>::WARPS * 32, 1) k_accept(AcceptArgs a)
 {
-    using L = Accept<D, NB>;
-    constexpr int TK = L::TK, KB = L::KB, S = L::S, NT = L::WARPS * 32, PITCH = L::PITCH, CH = D / 8, MO = D / 16;
-    constexpr int ROWS = NB * 8;  // rows whose queries the registers hold
+    using L = Accept<D, FEW>;
+    constexpr int TK = L::TK, S = L::S, NT = L::WARPS * 32, PITCH = L::PITCH, CH = D / 8, MO = D / 16;
+    constexpr int ROWS = L::ROWS;
     extern __shared__ __align__(128) char sm[];
     int* const pre = reinterpret_cast<int*>(sm + L::pre);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -137,48 +142,36 @@ __global__ void __launch_bounds__(Accept<D, NB>::WARPS * 32, 1) k_accept(AcceptA
         char* const tiles = sm + warp * S * L::TILE;
         const uint32_t tiles0 = smem_addr(tiles);
         float* const ws = reinterpret_cast<float*>(sm + L::w) + warp * S * TK;
-        int* const pgs = reinterpret_cast<int*>(sm + L::pages) + warp * S * KB;
+        int* const pgs = reinterpret_cast<int*>(sm + L::pages) + warp * S;
         const int gq = lane >> 2, tq = lane & 3, id = lane >> 3, lr = lane & 7;
 
-        int page[KB];  // the pages of the tile under F, as the table has them
+        int page = 0;  // the page of the tile under F, as the table has it
         auto pages = [&]() {
-#pragma unroll
-            for (int g = 0; g < KB; ++g) {
-                const int key = (F.t0 + F.tile) * TK + g * 16;
-                page[g] = key < F.len + F.A
-                              ? a.kv.table[(long long)F.r * a.kv.table_stride + (key >> a.kv.page_shift)]
-                              : 0;
-            }
+            const int key = (F.t0 + F.tile) * TK;
+            page = a.kv.table[(long long)F.r * a.kv.table_stride + (key >> a.kv.page_shift)];
         };
         if (n > 0) pages();
         // the tile under F into place b; then F goes on
         auto fetch = [&](int b, bool more) {
             const int key0 = (F.t0 + F.tile) * TK, own = F.len - key0, all = own + F.A;
-            bool valid[KB];
-#pragma unroll
-            for (int g = 0; g < KB; ++g) {
-                valid[g] = (unsigned)page[g] < (unsigned)a.kv.pages;
-                if (!valid[g] && lane == 0) atomicOr(a.err, WORKER_BAD_INPUT);
-                if (lane == 0) pgs[b * KB + g] = valid[g] ? page[g] : -1;
+            const bool valid = (unsigned)page < (unsigned)a.kv.pages;
+            if (lane == 0) {
+                if (!valid) atomicOr(a.err, WORKER_BAD_INPUT);
+                pgs[b] = valid ? page : -1;
             }
             if (weigh) {
                 const uint32_t kd = tiles0 + b * L::TILE;
-                const long long head = (long long)F.h * a.kv.head_stride;
+                const long long from = page * a.kv.page_stride + (long long)F.h * a.kv.head_stride +
+                                       (key0 & (a.kv.page - 1)) * a.kv.token_stride;
                 if (own >= TK && 32 % CH == 0) {
                     constexpr int STEP = 32 / CH;
                     const int r0 = lane / CH, ch = lane % CH;
+                    const char* k = a.kv.k + (valid ? (from + r0 * a.kv.token_stride + ch * 8) * 2 : 0);
+                    const long long step = valid ? STEP * a.kv.token_stride * 2 : 0;
 #pragma unroll
-                    for (int g = 0; g < KB; ++g) {
-                        const char* k = a.kv.k;
-                        if (valid[g])
-                            k += (page[g] * a.kv.page_stride + head +
-                                  (((key0 + g * 16) & (a.kv.page - 1)) + r0) * a.kv.token_stride + ch * 8) * 2;
-                        const long long step = valid[g] ? STEP * a.kv.token_stride * 2 : 0;
-#pragma unroll
-                        for (int i = 0; i < 16 / STEP; ++i) {
-                            cp16(kd + (g * 16 + i * STEP + r0) * PITCH + ch * 16, k, valid[g]);
-                            k += step;
-                        }
+                    for (int i = 0; i < TK / STEP; ++i) {
+                        cp16(kd + (i * STEP + r0) * PITCH + ch * 16, k, valid);
+                        k += step;
                     }
                 } else {
 #pragma unroll 2
@@ -188,33 +181,19 @@ __global__ void __launch_bounds__(Accept<D, NB>::WARPS * 32, 1) k_accept(AcceptA
                         const char* k = a.kv.k;
                         bool ok = row < all;
                         if (row < own) {
-                            int p = page[0];
-                            ok = valid[0];
-#pragma unroll
-                            for (int g = 1; g < KB; ++g)
-                                if (row >> 4 == g) p = page[g], ok = valid[g];
-                            if (ok)
-                                k += (p * a.kv.page_stride + head + ((key0 + row) & (a.kv.page - 1)) * a.kv.token_stride +
-                                      ch * 8) * 2;
+                            ok = valid;
+                            if (ok) k += (from + row * a.kv.token_stride + ch * 8) * 2;
                         } else if (ok) {
                             k = a.tok.k + (kept(a, F, row - own) * a.tok.k_stride + F.h * D + ch * 8) * 2;
                         }
                         cp16(kd + row * PITCH + ch * 16, k, ok);
                     }
                 }
-#pragma unroll
-                for (int i = 0; i < (TK + 31) / 32; ++i) {
-                    const int row = lane + i * 32;
-                    int p = page[0];
-                    bool ok = valid[0];
-#pragma unroll
-                    for (int g = 1; g < KB; ++g)
-                        if (row >> 4 == g) p = page[g], ok = valid[g];
-                    ok = ok && row < own;
-                    if (row < TK)
-                        cp4(smem_addr(ws + b * TK + row),
-                            a.kv.weight + (ok ? ((long long)p * H + F.h) * a.kv.page + ((key0 + row) & (a.kv.page - 1)) : 0),
-                            ok);
+                if (lane < TK) {
+                    const bool ok = valid && lane < own;
+                    cp4(smem_addr(ws + b * TK + lane),
+                        a.kv.weight + (ok ? ((long long)page * H + F.h) * a.kv.page + ((key0 + lane) & (a.kv.page - 1)) : 0),
+                        ok);
                 }
             }
             if (more) {
@@ -228,42 +207,60 @@ __global__ void __launch_bounds__(Accept<D, NB>::WARPS * 32, 1) k_accept(AcceptA
             cp_commit();
         }
 
-        // rows row0 .. of a unit: row gq of every block, channels 2 tq and 2 tq + 1 of every 8,
-        // and the logarithms of the sums of rows 2 tq and 2 tq + 1
-        uint32_t qf[MO][NB][2];
-        float lse2[NB][2];
+        // rows row0 .. of a unit: in registers row gq, channels 2 tq and 2 tq + 1 of every 8, and
+        // the logarithms of the sums of rows 2 tq and 2 tq + 1, or in this warp's shared memory
+        uint32_t qf[FEW ? MO : 1][2];
+        float lse2[2];
+        char* const qs = sm + L::q + warp * ROWS * PITCH;
+        float* const ls = reinterpret_cast<float*>(sm + L::lse) + warp * ROWS;
+        // (rows that are none, and rows without an attention, add nothing)
+        auto log_sum = [](float s) { return s == -INFINITY ? INFINITY : s * LOG2E; };
         auto queries = [&](const Unit& u, int row0) {
             const int R = u.A * G;
-            // (no early end: all loads are on their way together)
-            int tok[NB][3];
-#pragma unroll
-            for (int y = 0; y < NB; ++y)
+            if constexpr (FEW) {
+                int tok[3];
 #pragma unroll
                 for (int e = 0; e < 3; ++e) {
-                    const int row = row0 + y * 8 + (e < 2 ? tq * 2 + e : gq);
-                    tok[y][e] = row < R ? kept(a, u, row / G) : -1;
+                    const int row = row0 + (e < 2 ? tq * 2 + e : gq);
+                    tok[e] = row < R ? kept(a, u, row / G) : -1;
                 }
-#pragma unroll
-            for (int y = 0; y < NB; ++y) {
-                const int row = row0 + y * 8 + gq, t = tok[y][2];
+                const bool ok = tok[2] >= 0;
                 const uint32_t* p = reinterpret_cast<const uint32_t*>(
-                    a.tok.q + ((t < 0 ? 0 : t) * a.tok.q_stride + (long long)(u.h * G + row % G) * D) * 2) + tq;
+                    a.tok.q + ((ok ? tok[2] : 0) * a.tok.q_stride + (long long)(u.h * G + (row0 + gq) % G) * D) * 2) + tq;
 #pragma unroll
                 for (int x = 0; x < MO; ++x) {
-                    qf[x][y][0] = t >= 0 ? __ldg(p + x * 8) : 0u;
-                    qf[x][y][1] = t >= 0 ? __ldg(p + x * 8 + 4) : 0u;
+                    qf[x][0] = ok ? __ldg(p + x * 8) : 0u;
+                    qf[x][1] = ok ? __ldg(p + x * 8 + 4) : 0u;
                 }
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int rr = row0 + y * 8 + tq * 2 + e;
-                    // (rows that are none, and rows without an attention, add nothing)
-                    lse2[y][e] = tok[y][e] >= 0 ? a.lse[(long long)tok[y][e] * (H * G) + u.h * G + rr % G] : -INFINITY;
+                for (int e = 0; e < 2; ++e)
+                    lse2[e] = tok[e] >= 0 ? a.lse[(long long)tok[e] * (H * G) + u.h * G + (row0 + tq * 2 + e) % G] : -INFINITY;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) lse2[e] = log_sum(lse2[e]);
+            } else {
+                __syncwarp();
+                const int rows = min(ROWS, R - row0), held = (rows + 15) / 16 * 16;
+                const uint32_t qd = smem_addr(qs);
+#pragma unroll 4
+                for (int x = lane; x < held * CH; x += 32) {
+                    const int row = x / CH, ch = x - row * CH;
+                    const bool ok = row < rows;
+                    const int i = ok ? (row0 + row) / G : 0, g = ok ? row0 + row - i * G : 0;
+                    cp16(qd + row * PITCH + ch * 16,
+                         a.tok.q + (kept(a, u, i) * a.tok.q_stride + (long long)(u.h * G + g) * D + ch * 8) * 2, ok);
                 }
+                for (int row = lane; row < held; row += 32) {
+                    float s = -INFINITY;
+                    if (row < rows) {
+                        const int i = (row0 + row) / G;
+                        s = a.lse[(long long)kept(a, u, i) * (H * G) + u.h * G + row0 + row - i * G];
+                    }
+                    ls[row] = log_sum(s);
+                }
+                cp_commit();
+                cp_wait<0>();
+                __syncwarp();
             }
-#pragma unroll
-            for (int y = 0; y < NB; ++y)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) lse2[y][e] = lse2[y][e] == -INFINITY ? INFINITY : lse2[y][e] * LOG2E;
         };
         bool fresh = true;
         int b = 0;
@@ -281,7 +278,7 @@ __global__ void __launch_bounds__(Accept<D, NB>::WARPS * 32, 1) k_accept(AcceptA
                 const int s0 = max(new0, 0), s1 = min(new0 + C.A, TK);
                 for (int x = lane; x < (s1 - s0) * CH; x += 32) {
                     const int row = s0 + x / CH, ch = x % CH, slot = key0 + row;
-                    const int p = pgs[b * KB + (row >> 4)], at = slot & (a.kv.page - 1);
+                    const int p = pgs[b], at = slot & (a.kv.page - 1);
                     const long long t = kept(a, C, row - new0);
                     const long long d = (p * a.kv.page_stride + C.h * a.kv.head_stride + at * a.kv.token_stride + ch * 8) * 2;
                     *reinterpret_cast<uint4*>(a.kv.k + d) = *reinterpret_cast<const uint4*>(
@@ -297,56 +294,63 @@ __global__ void __launch_bounds__(Accept<D, NB>::WARPS * 32, 1) k_accept(AcceptA
             }
             if (weigh) {
                 const uint32_t kd = tiles0 + b * L::TILE + ((id & 1) * 8 + lr) * PITCH + (id >> 1) * 16;
-                float sum[KB][2];  // keys gq and gq + 8 of every 16
+                uint32_t f[MO][4];
 #pragma unroll
-                for (int x = 0; x < KB; ++x) sum[x][0] = sum[x][1] = 0.0f;
-                for (int row0 = 0; row0 < R; row0 += ROWS) {
-                    if (R > ROWS) queries(C, row0);
+                for (int ks = 0; ks < MO; ++ks) ldmatrix4(f[ks], kd + ks * 32);
+                float sum[2] = {0.0f, 0.0f};  // keys gq and gq + 8
+                // scores of the keys by rows row, row + 1 (row = the first of a block + 2 tq) join the sums
+                auto add = [&](const float(&s)[4], float ls0, float ls1, int row) {
 #pragma unroll
-                    for (int x = 0; x < KB; ++x) {
-                        uint32_t f[MO][4];
+                    for (int e = 0; e < 4; ++e) {
+                        const float v = ex2(fmaf(s[e], a.scale_log2, e & 1 ? -ls1 : -ls0));
+                        const int rr = row + (e & 1);
+                        bool sees = rr < R;  // (a row that is none may hold anything)
+                        if (new0 < TK) sees = sees && (e >> 1) * 8 + gq - new0 <= rr / G;
+                        sum[e >> 1] += sees ? v : 0.0f;
+                    }
+                };
+                if constexpr (FEW) {
+                    // (a kept token more than the mean may bring more than 8 rows: they are read again)
+                    for (int row0 = 0; row0 < R; row0 += 8) {
+                        if (R > 8) queries(C, row0);
+                        float s[2][4] = {};
 #pragma unroll
-                        for (int ks = 0; ks < MO; ++ks) ldmatrix4(f[ks], kd + x * 16 * PITCH + ks * 32);
-// two blocks at a time: their products do not wait for one another
+                        for (int ks = 0; ks < MO; ++ks) Num<T>::mma(s[ks & 1], f[ks], qf[ks][0], qf[ks][1]);
 #pragma unroll
-                        for (int y0 = 0; y0 < NB; y0 += 2) {
-                            if (row0 + y0 * 8 >= R) break;
-                            constexpr int P = NB > 1 ? 2 : 1;
-                            float s[P][4];
+                        for (int e = 0; e < 4; ++e) s[0][e] += s[1][e];
+                        add(s[0], lse2[0], lse2[1], row0 + tq * 2);
+                    }
+                } else {
+                    for (int row0 = 0; row0 < R; row0 += ROWS) {
+                        if (R > ROWS) queries(C, row0);
+                        const uint32_t qa = smem_addr(qs) + ((id >> 1) * 8 + lr) * PITCH + (id & 1) * 16;
+                        // two blocks of 8 rows at a time: their products do not wait for one another
+#pragma unroll 1
+                        for (int y = 0; y < min(ROWS, R - row0); y += 16) {
+                            float s[2][4] = {};
 #pragma unroll
-                            for (int y = 0; y < P; ++y) s[y][0] = s[y][1] = s[y][2] = s[y][3] = 0.0f;
-#pragma unroll
-                            for (int ks = 0; ks < MO; ++ks)
-#pragma unroll
-                                for (int y = 0; y < P; ++y)
-                                    Num<T>::mma(s[y], f[ks], qf[ks][y0 + y][0], qf[ks][y0 + y][1]);
-#pragma unroll
-                            for (int y = 0; y < P; ++y) {
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) {
-                                    const float v = ex2(fmaf(s[y][e], a.scale_log2, -lse2[y0 + y][e & 1]));
-                                    // row i sees the slots up to its own
-                                    const int rr = row0 + (y0 + y) * 8 + tq * 2 + (e & 1);
-                                    bool sees = rr < R;
-                                    if (new0 < TK) sees = sees && x * 16 + (e >> 1) * 8 + gq - new0 <= rr / G;
-                                    sum[x][e >> 1] += sees ? v : 0.0f;
-                                }
+                            for (int ks = 0; ks < MO; ++ks) {
+                                uint32_t q[4];
+                                ldmatrix4(q, qa + y * PITCH + ks * 32);
+                                Num<T>::mma(s[0], f[ks], q[0], q[1]);
+                                Num<T>::mma(s[1], f[ks], q[2], q[3]);
                             }
+                            const float2 l0 = *reinterpret_cast<const float2*>(ls + y + tq * 2),
+                                         l1 = *reinterpret_cast<const float2*>(ls + y + 8 + tq * 2);
+                            add(s[0], l0.x, l0.y, row0 + y + tq * 2);
+                            add(s[1], l1.x, l1.y, row0 + y + 8 + tq * 2);
                         }
                     }
                 }
 #pragma unroll
-                for (int x = 0; x < KB; ++x) {
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float v = sum[x][e];
-                        v += __shfl_xor_sync(0xffffffffu, v, 1);
-                        v += __shfl_xor_sync(0xffffffffu, v, 2);
-                        const int row = x * 16 + e * 8 + gq, p = pgs[b * KB + x];
-                        if (tq == 0 && row < new0 + C.A && p >= 0)
-                            a.kv.weight[((long long)p * H + C.h) * a.kv.page + ((key0 + row) & (a.kv.page - 1))] =
-                                ws[b * TK + row] + v;
-                    }
+                for (int e = 0; e < 2; ++e) {
+                    float v = sum[e];
+                    v += __shfl_xor_sync(0xffffffffu, v, 1);
+                    v += __shfl_xor_sync(0xffffffffu, v, 2);
+                    const int row = e * 8 + gq, p = pgs[b];
+                    if (tq == 0 && row < new0 + C.A && p >= 0)
+                        a.kv.weight[((long long)p * H + C.h) * a.kv.page + ((key0 + row) & (a.kv.page - 1))] =
+                            ws[b * TK + row] + v;
                 }
             }
             fresh = C.tile + 1 == C.c;
@@ -376,25 +380,24 @@ __global__ void __launch_bounds__(Accept<D, NB>::WARPS * 32, 1) k_accept(AcceptA
     }
 }
 
-template <typename T, int D, int NB>
+template <typename T, int D, bool FEW>
 cudaError_t launch_rows(const AcceptArgs& a, int sms, cudaStream_t st)
 {
-    using L = Accept<D, NB>;
+    using L = Accept<D, FEW>;
     constexpr int most = L::bytes(ALADDIN_WORKER_MAX_REQUESTS);
     static_assert(most <= 227 * 1024, "shared memory of a CTA");
-    cudaError_t e = allow_smem<k_accept<T, D, NB>>(most);
+    cudaError_t e = allow_smem<k_accept<T, D, FEW>>(most);
     if (e != cudaSuccess) return e;
-    k_accept<T, D, NB><<<sms, L::WARPS * 32, L::bytes(a.tok.n_req), st>>>(a);
+    k_accept<T, D, FEW><<<sms, L::WARPS * 32, L::bytes(a.tok.n_req), st>>>(a);
     return cudaGetLastError();
 }
 
-// 8 rows in registers where the mean rows of a request's key head fit them, else as many
-// as the registers hold.
+// 8 rows in registers where the mean rows of a request's key head fit them.
 template <typename T, int D>
 cudaError_t launch(const AcceptArgs& a, int sms, cudaStream_t st)
 {
-    if ((long long)a.n_acc * a.kv.group <= 8ll * a.tok.n_req) return launch_rows<T, D, 1>(a, sms, st);
-    return launch_rows<T, D, D == 256 ? 2 : D == 64 ? 8 : 6>(a, sms, st);
+    if ((long long)a.n_acc * a.kv.group <= 8ll * a.tok.n_req) return launch_rows<T, D, true>(a, sms, st);
+    return launch_rows<T, D, false>(a, sms, st);
 }
 
 template <typename T>
