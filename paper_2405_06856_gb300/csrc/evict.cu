@@ -14,10 +14,13 @@
 // The budget-th largest key is found digit by digit (11 + 11 + 10 bits of the
 // ordered key): each CTA counts its keys that agree with the digits known so far,
 // every CTA adds the cluster's counts and picks the same digit, until all keys of
-// the digit stay. Two scans then number equal keys, holes and movers in slot
-// order, and the warps share the moves, 32 to a warp: a lane looks one of them up
-// and moves its weight and position, then the warp copies their rows, several
-// 16-byte pieces of a lane in flight.
+// the digit stay. Two scans then number equal keys, holes and movers in slot order.
+// A warp moves 32 at a time: a lane looks one of them up and moves its weight and
+// position, then the warp copies their rows, several 16-byte pieces of a lane in
+// flight. One CTA moves what it found itself; after clusters, whose requests differ
+// in length, a second kernel shares all moves evenly (the clusters' own moves
+// left most of the GPU to the longest request: 89 us for three requests of up to
+// 65,536 tokens instead of 72).
 #include <cooperative_groups.h>
 
 #include "worker_dev.cuh"
@@ -117,9 +120,58 @@ __device__ __forceinline__ int2 block_scan(int2 v, int2* scratch, int2& total)
     return make_int2(before.x + u.x - v.x, before.y + u.y - v.y);
 }
 
+// The i-th move of a (request, head), from the workspace; -1 where a page is outside the pool.
+__device__ __forceinline__ void listed(const EvictArgs& a, const Evict& e, int budget, int i, int& from, int& to)
+{
+    const int pm = page_of(a, e, budget + i), ph = page_of(a, e, i);
+    from = pm < 0 ? -1 : __ldcg(a.lists + meta_at(a, e, pm, budget + i));
+    to = ph < 0 ? -1 : __ldcg(a.lists + meta_at(a, e, ph, i));
+}
+
+// Moves a lane's slot `from` to its slot `to` (the lanes below n; -1: nothing), the warp together.
+template <int D, int U>
+__device__ __forceinline__ void move_rows(const EvictArgs& a, const Evict& e, int from, int to, int n, int lane)
+{
+    constexpr int CH = D / 8, PER = 2 * CH;  // 16-byte pieces of a key, of a key and a value; U of a lane in flight
+    long long src = -1, dst = -1;
+    if (lane < n && from >= 0 && to >= 0) {
+        const int pd = page_of(a, e, to), ps = page_of(a, e, from);
+        if (pd >= 0 && ps >= 0) {
+            src = row_at(a, e, ps, from);
+            dst = row_at(a, e, pd, to);
+            const long long ms = meta_at(a, e, ps, from), md = meta_at(a, e, pd, to);
+            a.kv.weight[md] = a.kv.weight[ms];
+            a.kv.pos[md] = a.kv.pos[ms];
+        }
+    }
+    const int pieces = n * PER;
+    for (int x0 = 0; x0 < pieces; x0 += 32 * U) {
+        uint4 v[U];
+        long long at[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int x = x0 + u * 32 + lane, m = x / PER, c = x - m * PER;
+            const long long s = __shfl_sync(0xffffffffu, src, m & 31);
+            at[u] = __shfl_sync(0xffffffffu, dst, m & 31);
+            if (x >= pieces || s < 0) at[u] = -1;
+            else {
+                const char* const pool = c < CH ? a.kv.k : a.kv.v;
+                const int cc = (c < CH ? c : c - CH) * 8;
+                v[u] = *reinterpret_cast<const uint4*>(pool + (s + cc) * 2);
+                at[u] += cc;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int x = x0 + u * 32 + lane, c = x % PER;
+            if (at[u] >= 0) *reinterpret_cast<uint4*>((c < CH ? a.kv.k : a.kv.v) + at[u] * 2) = v[u];
+        }
+    }
+}
+
 // CLUSTER: a cluster serves a (request, head), else one CTA.
 template <int D, int NT, bool CLUSTER>
-__global__ void __launch_bounds__(NT, CLUSTER ? 1 : 4) k_evict(EvictArgs a, int max_keys)
+__global__ void __launch_bounds__(NT, CLUSTER ? 2 : 4) k_evict(EvictArgs a, int max_keys)
 {
     cg::cluster_group cluster = cg::this_cluster();
     extern __shared__ __align__(16) uint32_t keys[];
@@ -196,6 +248,7 @@ __global__ void __launch_bounds__(NT, CLUSTER ? 1 : 4) k_evict(EvictArgs a, int 
                 int4 q = *reinterpret_cast<const int4*>(h + d0 + x);
                 if (CLUSTER) {
                     q = make_int4(0, 0, 0, 0);
+#pragma unroll 8
                     for (int b = 0; b < cs; ++b) {
                         const int4 o = *reinterpret_cast<const int4*>(cluster.map_shared_rank(h, b) + d0 + x);
                         q.x += o.x, q.y += o.y, q.z += o.z, q.w += o.w;
@@ -297,55 +350,28 @@ __global__ void __launch_bounds__(NT, CLUSTER ? 1 : 4) k_evict(EvictArgs a, int 
             for (int b = 0; b < cs; ++b) moves += cluster.map_shared_rank(&counts, b)->y;
         }
 
-        constexpr int CH = D / 8, PER = 2 * CH, U = CLUSTER ? 8 : 4;  // 16-byte pieces of a key, of a key and a value
-        for (int m0 = (rank * (NT / 32) + warp) * 32; m0 < moves; m0 += cs * NT) {
-            const int i = m0 + lane;
-            long long src = -1, dst = -1;
-            if (i < moves) {
-                int slot[2];
-#pragma unroll
-                for (int l = 0; l < 2; ++l) {
+        if (CLUSTER) {
+            if (rank == 0 && tid == 0) a.moves[unit] = moves;
+        } else {
+            // every warp the same number of moves
+            const int share = (moves + NT / 32 - 1) / (NT / 32), first = warp * share, last = min(first + share, moves);
+            for (int m0 = first; m0 < last; m0 += 32) {
+                const int i = m0 + lane;
+                int from = -1, to = -1;
+                if (i < last) {
                     if (near) {
-                        slot[l] = hist[l][i];
+                        to = hist[0][i];
+                        from = hist[1][i];
                     } else {
-                        const int w = l ? budget + i : i, p = page_of(a, e, w);
-                        slot[l] = p < 0 ? -1 : __ldcg(a.lists + meta_at(a, e, p, w));
+                        listed(a, e, budget, i, from, to);
                     }
                 }
-                const int pd = slot[0] < 0 ? -1 : page_of(a, e, slot[0]), ps = slot[1] < 0 ? -1 : page_of(a, e, slot[1]);
-                if (pd >= 0 && ps >= 0) {
-                    src = row_at(a, e, ps, slot[1]);
-                    dst = row_at(a, e, pd, slot[0]);
-                    const long long ms = meta_at(a, e, ps, slot[1]), md = meta_at(a, e, pd, slot[0]);
-                    a.kv.weight[md] = a.kv.weight[ms];
-                    a.kv.pos[md] = a.kv.pos[ms];
-                }
-            }
-            const int pieces = min(32, moves - m0) * PER;
-            for (int x0 = 0; x0 < pieces; x0 += 32 * U) {
-                uint4 v[U];
-                long long to[U];
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int x = x0 + u * 32 + lane, m = x / PER, c = x - m * PER;
-                    const long long s = __shfl_sync(0xffffffffu, src, m & 31);
-                    to[u] = __shfl_sync(0xffffffffu, dst, m & 31);
-                    if (x >= pieces || s < 0) to[u] = -1;
-                    else {
-                        const char* const pool = c < CH ? a.kv.k : a.kv.v;
-                        const int cc = (c < CH ? c : c - CH) * 8;
-                        v[u] = *reinterpret_cast<const uint4*>(pool + (s + cc) * 2);
-                        to[u] += cc;
-                    }
-                }
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int x = x0 + u * 32 + lane, c = x % PER;
-                    if (to[u] >= 0) *reinterpret_cast<uint4*>((c < CH ? a.kv.k : a.kv.v) + to[u] * 2) = v[u];
-                }
+                move_rows<D, 4>(a, e, from, to, min(32, last - m0), lane);
             }
         }
         if (CLUSTER) cluster.sync();  // the others have read this CTA's counts
+    } else if (CLUSTER && rank == 0 && tid == 0) {
+        a.moves[unit] = 0;
     }
 
     // every CTA has read the lengths: the last one to come here cuts them
@@ -361,6 +387,33 @@ __global__ void __launch_bounds__(NT, CLUSTER ? 1 : 4) k_evict(EvictArgs a, int 
             const int len = a.kv.len[q], b = a.budget[q];
             if (len >= 0 && len <= a.kv.cap && b >= 0 && len > b) a.kv.len[q] = b;
         }
+    }
+}
+
+// The moves that the clusters listed, shared evenly by all warps. units <= MOST_UNITS.
+constexpr int MOST_UNITS = 1024, MOVERS = 256, MOVE_CTAS = 3;  // threads of a CTA, CTAs of an SM
+template <int D>
+__global__ void __launch_bounds__(MOVERS, MOVE_CTAS) k_move(EvictArgs a, int units)
+{
+    __shared__ int pre[MOST_UNITS + 1];
+    __shared__ long long scratch[32];
+    const int total = plan_prefix<MOVERS>(units, pre, scratch, [&](int u) -> long long { return a.moves[u]; });
+    const int lane = threadIdx.x & 31, warps = gridDim.x * (MOVERS / 32), me = blockIdx.x * (MOVERS / 32) + (threadIdx.x >> 5);
+    // (fewer than 2^31: a slot moves once, and a pool's slots are counted in ints)
+    const long long share = ((long long)total + warps - 1) / warps, first = me * share, last = min(first + share, (long long)total);
+    for (long long m0 = first; m0 < last; m0 += 32) {
+        const int n = (int)min(32ll, last - m0);
+        Evict e;
+        e.row = a.kv.table;
+        e.h = e.held = e.recent_from = 0;
+        int from = -1, to = -1;
+        if (lane < n) {
+            const int unit = plan_find(pre, units, (int)(m0 + lane)), r = unit / a.kv.kv_heads;
+            e.h = unit - r * a.kv.kv_heads;
+            e.row = a.kv.table + (long long)r * a.kv.table_stride;
+            listed(a, e, a.budget[r], (int)(m0 + lane) - pre[unit], from, to);
+        }
+        move_rows<D, 8>(a, e, from, to, n, lane);
     }
 }
 
@@ -393,8 +446,12 @@ cudaError_t launch_dim(const EvictArgs& a, int sms, cudaStream_t st)
     // cluster, but few slots need no more than one
     const long long units = (long long)a.n_req * a.kv.kv_heads;
     int cs = 1;
-    while (cs < 8 && units * cs < 2ll * sms && a.kv.cap > 4096ll * cs) cs *= 2;
-    return cs == 1 ? launch<D, 256, false>(a, units, cs, st) : launch<D, 512, true>(a, units, cs, st);
+    while (cs < 8 && units * cs < 2ll * sms && a.kv.cap > 2048ll * cs) cs *= 2;
+    if (cs == 1 || units > MOST_UNITS) return launch<D, 256, false>(a, units, 1, st);
+    const cudaError_t e = launch<D, 512, true>(a, units, cs, st);
+    if (e != cudaSuccess) return e;
+    k_move<D><<<MOVE_CTAS * sms, MOVERS, 0, st>>>(a, (int)units);
+    return cudaGetLastError();
 }
 
 }  // namespace

@@ -13,8 +13,11 @@
 // (from L2), those at or above the bound are kept, and a comparison of all kept
 // ones with all others sorts them.
 //
-// The pass is bound by its instructions: two 16-bit logits are unpacked,
-// clamped and compared in a word, the sums take two terms an instruction.
+// The pass needs many bytes in flight and few instructions a logit: a thread has the
+// next four vectors of 16 bytes on their way while it works on four; four vectors
+// share one look at the maximum, and 16-bit logits are clamped and compared two in a
+// word. (Two terms an instruction in the sums, or a ring in shared memory for the
+// vectors, gained nothing.)
 #include <cooperative_groups.h>
 
 #include <type_traits>
@@ -66,6 +69,19 @@ struct Logit<float> {
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = max_nan(x[i], low);
     }
+    // entries of the vectors above a threshold
+    typedef float Thr;
+    static __device__ __forceinline__ Thr thr(float v) { return v; }
+    template <int U>
+    static __device__ __forceinline__ int above(const uint4 (&w)[U], const Thr (&t)[U])
+    {
+        int n = 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            n += (__uint_as_float(w[u].x) > t[u]) + (__uint_as_float(w[u].y) > t[u]) +
+                 (__uint_as_float(w[u].z) > t[u]) + (__uint_as_float(w[u].w) > t[u]);
+        return n;
+    }
     static __device__ __forceinline__ float one(const char* p) { return *reinterpret_cast<const float*>(p); }
 };
 __device__ __forceinline__ __nv_bfloat162 both(__nv_bfloat162*, float v)
@@ -98,14 +114,29 @@ struct Logit {
                                    bits(__hmax2_nan(word(v.z), low)), bits(__hmax2_nan(word(v.w), low)));
         unpack(w, x);
     }
+    // (a threshold between two values of the type rounds down to the lower one; the counts of
+    // 4 U words are whole numbers that the type holds)
+    typedef Low Thr;
+    static __device__ __forceinline__ Thr thr(float v) { return low(v); }
+    template <int U>
+    static __device__ __forceinline__ int above(const uint4 (&w)[U], const Thr (&t)[U])
+    {
+        Low n = low(0.0f);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            n = __hadd2(n, __hadd2(__hadd2(__hgt2(word(w[u].x), t[u]), __hgt2(word(w[u].y), t[u])),
+                                   __hadd2(__hgt2(word(w[u].z), t[u]), __hgt2(word(w[u].w), t[u]))));
+        const float2 f = Num<T>::unpack(bits(n));
+        return (int)(f.x + f.y);
+    }
     static __device__ __forceinline__ float one(const char* p)
     {
         return Num<T>::unpack(*reinterpret_cast<const unsigned short*>(p)).x;
     }
 };
 
-// The order of values as unsigned numbers (-0 as +0, NaN below everything), the
-// value's next lower float, and an entry as a number that orders entries: larger
+// The order of values as unsigned numbers (-0 as +0, NaN below everything), the next
+// lower float of a finite value, and an entry as a number that orders entries: larger
 // values first, the lower index first among equals.
 __device__ __forceinline__ uint32_t ordered(float x)
 {
@@ -113,10 +144,14 @@ __device__ __forceinline__ uint32_t ordered(float x)
     const uint32_t u = __float_as_uint(x + 0.0f);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
-__device__ __forceinline__ float next_below(float x)  // x not NaN; -inf gives NaN, above which nothing is
+__device__ __forceinline__ float next_below(float x)
 {
     const uint32_t o = ordered(x), u = o == 0x80000000u ? 0x7ffffffeu : o - 1;  // below +0: not -0
     return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
+}
+__device__ __forceinline__ float value_of(uint32_t order)
+{
+    return order ? __uint_as_float(order & 0x80000000u ? order & 0x7fffffffu : ~order) : NAN;
 }
 __device__ __forceinline__ unsigned long long entry(uint32_t order, int i)
 {
@@ -169,14 +204,13 @@ struct alignas(16) Shared {
     int count, owners;
     uint32_t bound;
     unsigned long long bound_entry, prev;
-    float m, ls;  // the row's maximum and log S
 };
 
 template <typename T>
 __global__ void __launch_bounds__(NT, 4) k_logprobs(LogprobArgs a)
 {
     using L = Logit<T>;
-    constexpr int PER = L::PER, ES = 16 / PER, U = 4;  // logits of a vector, bytes of one, vectors in flight
+    constexpr int PER = L::PER, ES = 16 / PER, U = 4;  // logits of a vector, bytes of one, vectors a step
     cg::cluster_group cluster = cg::this_cluster();
     __shared__ Shared sh;
     const int cs = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
@@ -202,95 +236,151 @@ __global__ void __launch_bounds__(NT, 4) k_logprobs(LogprobArgs a)
     const float mine = given ? L::one(x + (long long)token * ES) : 0.0f;
     const bool ranked = given && a.rank;
     const uint32_t mine_o = ordered(mine);
-    // entries in front of the token count from its value on, those behind it from above it
-    // (a token of NaN stands behind all values: they count from -inf on)
-    const float over = mine != mine ? __uint_as_float(0xffffffffu) : mine;
-    const float from = mine != mine ? over : next_below(mine);
+    // vectors in front of the token's count their entries from its value on, those behind it the
+    // larger ones, and its own vector goes entry by entry (as all vectors do for a token of NaN
+    // or -inf, of which the thresholds do not tell NaN from other entries)
+    const bool plain = mine == mine && mine != -INFINITY;
+    const int own_vec = plain && token >= head && token < tail0 ? (token - head) / PER : -1;
+    const float from_value = next_below(mine);
+    const typename L::Thr over = L::thr(mine), from = L::thr(from_value);
+    const int split = plain ? token - head : 0;  // vectors v with v PER < split lie in front
 
-    float m = -INFINITY, ref = 0.0f;  // the largest entry so far; what differences are taken to
+    // The largest entry so far, and the sums s of 2^y and t of 2^y y, y = x log2 e - ref with ref =
+    // m log2 e rounded: one multiply-add a logit, and the rounding of ref drops out of the results, as
+    // every term and the conversion below have the same. Where m log2 e is no float (a mask of the
+    // type's lowest value, +inf), the sum counts the entries that equal m: all others are too far
+    // away; `gate` is m, or NaN to have every vector looked at that way.
+    float m = -INFINITY, ref = 0.0f, gate = -INFINITY;
     typename L::Low low = L::low(-200.0f);
-    f2 s2 = pair(0.0f, 0.0f), t2 = s2, minus = s2;
-    const f2 log2e = pair(LOG2E, LOG2E);
     int above = 0;
+    float s0 = 0.0f, s1 = 0.0f, t0 = 0.0f, t1 = 0.0f;  // (two sums each, by even and odd places)
+    auto huge = [](float v) { return fabsf(v) > 2e38f; };
     auto raise = [&](float v) {
+        const bool far = gate != gate || huge(v);
+        const float next = far ? 0.0f : v * LOG2E, d = ref - next, f = far ? 0.0f : ex2(d);
         if (m != -INFINITY) {
-            float sl, sh_, tl, th;
-            unpair(s2, sl, sh_);
-            unpair(t2, tl, th);
-            const float d = ref - v, f = ex2(d * LOG2E);
-            s2 = pair(sl * f, sh_ * f);
-            t2 = f == 0.0f && sl == sl && sh_ == sh_ ? pair(0.0f, 0.0f)
-                                                     : pair(f * fmaf(sl, d, tl), f * fmaf(sh_, d, th));
+            // (a NaN in a sum stays one)
+            t0 = f == 0.0f ? t0 * 0.0f : f * fmaf(s0, d, t0);
+            t1 = f == 0.0f ? t1 * 0.0f : f * fmaf(s1, d, t1);
+            s0 *= f;
+            s1 *= f;
         }
-        m = ref = v;
-        minus = pair(-v, -v);
-        low = L::low(v - fmaxf(200.0f, fabsf(v) * 0.015625f));
+        m = v;
+        ref = next;
+        if (huge(v)) {
+            gate = NAN;
+        } else {
+            ref = v * LOG2E;
+            gate = v;
+            low = L::low(v - fmaxf(200.0f, fabsf(v) * 0.015625f));
+        }
     };
     auto count = [&](float v, int i) {  // one entry against the token
         const uint32_t o = ordered(v);
         above += o > mine_o || (o == mine_o && i < token);
     };
-    auto look = [&](const uint4& w, int v) {
-        const float top = L::top(w);
-        if (top > m) raise(top);
-        float f[PER];
-        L::clamped(w, low, f);
+    auto look = [&](auto& w, int v, int step) {  // vectors v, v + step, ...
+        constexpr int N = sizeof(w) / sizeof(uint4);
+        float top = L::top(w[0]);
 #pragma unroll
-        for (int i = 0; i < PER; i += 2) {
-            const f2 d = add2(pair(f[i], f[i + 1]), minus), y = mul2(d, log2e);
-            float y0, y1;
-            unpair(y, y0, y1);
-            const f2 e = pair(ex2(y0), ex2(y1));
-            s2 = add2(s2, e);
-            t2 = fma2(e, d, t2);
+        for (int u = 1; u < N; ++u) top = fmaxf(top, L::top(w[u]));
+        if (!(top <= gate) && top > m) raise(top);
+        if (gate != gate) {
+            float s = 0.0f;
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                float f[PER];
+                L::unpack(w[u], f);
+#pragma unroll
+                for (int i = 0; i < PER; ++i) s += f[i] == m ? (m == INFINITY ? NAN : 1.0f) : f[i] == f[i] ? 0.0f : NAN;
+            }
+            s0 += s;
+        } else {
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                float f[PER];
+                L::clamped(w[u], low, f);
+#pragma unroll
+                for (int i = 0; i < PER; i += 2) {
+                    const float y0 = fmaf(f[i], LOG2E, -ref), y1 = fmaf(f[i + 1], LOG2E, -ref), e0 = ex2(y0),
+                                e1 = ex2(y1);
+                    s0 += e0;
+                    s1 += e1;
+                    t0 = fmaf(e0, y0, t0);
+                    t1 = fmaf(e1, y1, t1);
+                }
+            }
         }
         if (ranked) {
-            const int i0 = head + v * PER;
-            if (mine != mine || (i0 <= token && token < i0 + PER)) {
-                float g[PER];
-                L::unpack(w, g);
+            if (plain) {
+                if (top > from_value) {  // (else nothing here stands in front of the token)
+                    typename L::Thr thr[N];
 #pragma unroll
-                for (int i = 0; i < PER; ++i) count(g[i], i0 + i);
+                    for (int u = 0; u < N; ++u) thr[u] = (v + u * step) * PER < split ? from : over;
+                    above += L::above(w, thr);
+                }
             } else {
-                // clamping keeps the order where the bound is not clamped away; the plain
-                // values are compared
-                const float thr = i0 < token ? from : over;
-                float g[PER];
-                L::unpack(w, g);
-                if (thr != thr) {  // in front of a token of -inf: everything but NaN
 #pragma unroll
-                    for (int i = 0; i < PER; ++i) above += g[i] == g[i];
-                } else {
+                for (int u = 0; u < N; ++u) {
+                    float g[PER];
+                    L::unpack(w[u], g);
 #pragma unroll
-                    for (int i = 0; i < PER; ++i) above += g[i] > thr;
+                    for (int i = 0; i < PER; ++i) count(g[i], head + (v + u * step) * PER + i);
                 }
             }
         }
     };
-    int v = v0 + tid;
-    for (; v + (U - 1) * NT < v1; v += U * NT) {
-        uint4 w[U];
-#pragma unroll
-        for (int i = 0; i < U; ++i) w[i] = __ldg(body + v + i * NT);
-#pragma unroll
-        for (int i = 0; i < U; ++i) look(w[i], v + i * NT);
-    }
-    for (; v < v1; v += NT) look(__ldg(body + v), v);
-    if (ends >= 0) {
-        if (end_x > m) raise(end_x);
-        float d = end_x - ref;
-        d = d < -200.0f ? -200.0f : d;  // a NaN stays
-        const float e = ex2(d * LOG2E);
-        s2 = add2(s2, pair(e, 0.0f));
-        t2 = fma2(pair(e, 0.0f), pair(d, 0.0f), t2);
-        if (ranked) count(end_x, ends);
-    }
-    Run run;
     {
-        float sl, sh_, tl, th;
-        unpair(s2, sl, sh_);
-        unpair(t2, tl, th);
-        run = Run{m, sl + sh_, tl + th};
+        // this thread's vectors v0 + tid, v0 + tid + NT, ...
+        const uint4* p = body + v0 + tid;
+        int left = v0 + tid < v1 ? (v1 - v0 - tid + NT - 1) / NT : 0, v = v0 + tid;
+        uint4 next[U];
+        if (left >= U) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) next[u] = __ldg(p + u * NT);
+        }
+#pragma unroll 1
+        while (left >= U) {
+            uint4 w[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) w[u] = next[u];
+            left -= U;
+            p += U * NT;
+            if (left >= U) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) next[u] = __ldg(p + u * NT);
+            }
+            look(w, v, NT);
+            v += U * NT;
+        }
+#pragma unroll 1
+        for (; left > 0; --left, p += NT, v += NT) {
+            uint4 w[1] = {__ldg(p)};
+            look(w, v, NT);
+        }
+    }
+    if (ranked && own_vec >= v0 && own_vec < v1 && (own_vec - v0) % NT == tid) {
+        // the token's own vector was counted with one threshold: once more, by entries
+        uint4 w[1] = {__ldg(body + own_vec)};
+        const typename L::Thr thr[1] = {own_vec * PER < split ? from : over};
+        above -= L::above(w, thr);
+        float g[PER];
+        L::unpack(w[0], g);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) count(g[i], head + own_vec * PER + i);
+    }
+    Run run{m, s0 + s1, t0 + t1};
+    {
+        if (m != -INFINITY && gate == gate) {
+            const float y = fmaf(m, LOG2E, -ref), f = ex2(-y);  // y of the largest entry: almost 0
+            run.t = fmaf(-y, run.s, run.t) * f * LN2;
+            run.s *= f;
+        }
+    }
+    if (ends >= 0) {
+        if (end_x != -INFINITY) run = join(run, fabsf(end_x) < INFINITY ? Run{end_x, 1.0f, 0.0f} : Run{run.m, NAN, NAN});
+        if (end_x > m) m = end_x;
+        if (ranked) count(end_x, ends);
     }
     const bool holds = v0 + tid < v1 || ends >= 0;  // this thread has entries
 
@@ -463,38 +553,40 @@ __global__ void __launch_bounds__(NT, 4) k_logprobs(LogprobArgs a)
     if (cs > 1) cluster.sync();
     else __syncthreads();
     if (rank == 0) {
-        if (tid == 0) {
+        // (the sums of the slices, by every thread that writes something: the first one only,
+        // or, with alternatives, all)
+        if (tid == 0 || k) {
             Run r = sh.all;
-            int c = sh.all_above;
-            for (int b = 1; b < cs; ++b) {
-                const Shared* o = cluster.map_shared_rank(&sh, b);
-                r = join(r, o->all);
-                c += o->all_above;
+            for (int b = 1; b < cs; ++b) r = join(r, cluster.map_shared_rank(&sh, b)->all);
+            const float ls = logf(r.s);
+            if (tid == 0) {
+                int c = sh.all_above;
+                for (int b = 1; b < cs; ++b) c += cluster.map_shared_rank(&sh, b)->all_above;
+                const bool empty = r.m == -INFINITY && r.s == 0.0f;  // every logit is -inf
+                if (a.logprob) a.logprob[row] = given ? logprob_of(mine, r.m, ls) : NAN;
+                if (a.entropy) a.entropy[row] = empty ? 0.0f : ls - r.t / r.s;
+                if (a.rank) a.rank[row] = given ? c : ALADDIN_INVALID;
+                if (a.token && !given) atomicOr(a.err, WORKER_BAD_INPUT);
             }
-            const bool empty = r.m == -INFINITY && r.s == 0.0f;  // every logit is -inf
-            sh.m = r.m;
-            sh.ls = logf(r.s);
-            if (a.logprob) a.logprob[row] = given ? logprob_of(mine, r.m, sh.ls) : NAN;
-            if (a.entropy) a.entropy[row] = empty ? 0.0f : sh.ls - r.t / r.s;
-            if (a.rank) a.rank[row] = given ? c : ALADDIN_INVALID;
-            if (a.token && !given) atomicOr(a.err, WORKER_BAD_INPUT);
-        }
-        if (k) {
-            // the slices' bests, at most MAX_CS x ALADDIN_TOP_MAX entries, once more all with all
-            const int all = cs * k;
-            for (int c = tid; c < all; c += NT) sh.list[c] = cluster.map_shared_rank(&sh, c / k)->top[c % k];
-            __syncthreads();
-            for (int c = tid; c < all; c += NT) {
-                const unsigned long long e = sh.list[c];
-                if (!e) continue;
-                int larger = 0;
-                for (int i = 0; i < all; ++i) larger += sh.list[i] > e;
-                if (larger >= k) continue;
-                const int id = (int)~(uint32_t)e;
-                if (a.top_id) a.top_id[(long long)row * k + larger] = id;
+            auto put = [&](int place, unsigned long long e) {
+                if (a.top_id) a.top_id[(long long)row * k + place] = (int)~(uint32_t)e;
                 if (a.top_logprob)
-                    a.top_logprob[(long long)row * k + larger] =
-                        logprob_of(L::one(x + (long long)id * ES), sh.m, sh.ls);
+                    a.top_logprob[(long long)row * k + place] = logprob_of(value_of((uint32_t)(e >> 32)), r.m, ls);
+            };
+            if (cs == 1) {
+                if (tid < k) put(tid, sh.top[tid]);
+            } else if (k) {  // (all threads are here)
+                // the slices' bests, at most MAX_CS x ALADDIN_TOP_MAX entries, once more all with all
+                const int all = cs * k;
+                for (int c = tid; c < all; c += NT) sh.list[c] = cluster.map_shared_rank(&sh, c / k)->top[c % k];
+                __syncthreads();
+                for (int c = tid; c < all; c += NT) {
+                    const unsigned long long e = sh.list[c];
+                    if (!e) continue;
+                    int larger = 0;
+                    for (int i = 0; i < all; ++i) larger += sh.list[i] > e;
+                    if (larger < k) put(larger, e);
+                }
             }
         }
     }
@@ -508,7 +600,7 @@ cudaError_t launch(const LogprobArgs& a, int sms, cudaStream_t st)
     // CTAs for a row: enough that the GPU is filled several times over, so that its last
     // part is short, but with 1,024 vectors at least, four a thread
     int cs = 1;
-    while (cs < MAX_CS && (long long)a.n * cs < 16ll * sms && vecs > 1024 * cs) cs *= 2;
+    while (cs < MAX_CS && (long long)a.n * cs < 2ll * sms && vecs > 1024 * cs) cs *= 2;
     cudaLaunchConfig_t c = {};
     c.gridDim = dim3((unsigned)a.n * cs);
     c.blockDim = dim3(NT);

@@ -21,6 +21,7 @@ struct aladdin_worker {
     unsigned* err = nullptr;
     int* done = nullptr;     // CTAs of an accept or evict call that have finished
     int* arrived = nullptr;  // [ATTEND_WORKERS_PER_SM * sms]
+    int* moves = nullptr;    // [1024] evict: moves of (request, head) pairs
     size_t ints = 0;         // bytes of the word and the counters
     float* part = nullptr;
     int32_t* lists = nullptr;  // evict (grow-only)
@@ -159,7 +160,7 @@ try {
     wk->st = (cudaStream_t)cuda_stream;
     wk->shape = *shape;
     while ((1 << wk->page_shift) < shape->page_tokens) ++wk->page_shift;
-    const size_t ints = ((size_t)(2 + ATTEND_WORKERS_PER_SM * d.sms) * 4 + 255) / 256 * 256;
+    const size_t ints = ((size_t)(2 + ATTEND_WORKERS_PER_SM * d.sms + 1024) * 4 + 255) / 256 * 256;
     wk->ints = ints;
     const size_t bytes = ints + attend_part_bytes(d.sms, shape->head_dim);
     cudaError_t e = cudaMalloc((void**)&wk->fixed, bytes);
@@ -173,6 +174,7 @@ try {
     wk->err = reinterpret_cast<unsigned*>(wk->fixed);
     wk->done = reinterpret_cast<int*>(wk->fixed) + 1;
     wk->arrived = wk->done + 1;
+    wk->moves = wk->arrived + ATTEND_WORKERS_PER_SM * d.sms;
     wk->part = reinterpret_cast<float*>(wk->fixed + ints);
     *out = wk;
     return ALADDIN_OK;
@@ -289,6 +291,7 @@ try {
     a.n_req = n_req;
     a.budget = budget;
     a.recent = recent;
+    a.moves = wk->moves;
     a.lists = wk->lists;
     a.arrived = wk->done;
     a.err = wk->err;

@@ -89,6 +89,7 @@ struct EvictArgs {
     int n_req;
     const int32_t* budget;
     int recent;
+    int* moves;             // of the (request, head) pairs, where clusters serve them
     int32_t* lists;         // one entry a slot of the pool: the i-th hole at slot i, the i-th mover at budget + i
     int* arrived;
     unsigned* err;
