@@ -157,6 +157,8 @@ __device__ __forceinline__ constexpr uint32_t product(int n, bool turned)
 
 template <int D, int MT>
 struct Many {
+    // (two CTAs an SM with tiles of 64 keys, for one row tile, were slower: 56 us for 50, as units
+    // were split and joined more often)
     static constexpr int KT = D == 256 ? 64 : 128;       // keys of a tile
     static constexpr int RM = 128 * MT;                  // rows of a unit
     static constexpr int HALVES = (D + 63) / 64;         // blocks of 64 channels
@@ -185,8 +187,8 @@ struct Many {
     static constexpr int LAG = 3;                        // copies in flight behind the one signalled
 };
 
-// What a unit costs beside its tiles, in tiles.
-constexpr int UNIT_TILES = 4;
+// What a unit costs beside its tiles, in keys.
+constexpr int UNIT_KEYS = 512;
 
 template <typename T, int D, int MT>
 __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(AttendArgs a, const __grid_constant__ Maps maps)
@@ -208,7 +210,7 @@ __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(Atte
     }
     Axis ax;
     if (!plan<NT>(a.tok.n_req, ax, pre, pre + a.tok.n_req + 1, reinterpret_cast<long long*>(sm + L::scratch),
-                  (int)gridDim.x, UNIT_TILES, 1, a.err,
+                  (int)gridDim.x, UNIT_KEYS / KT, 1, a.err,
                   [&](int r, int& c) { return attend_units<KT, RM>(a, r, c); }))
         return;
     const int me = blockIdx.x;
@@ -700,9 +702,11 @@ __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(Atte
                         if (*const_cast<volatile int*>(flag) && row < rows) {
                             __threadfence();
                             float top = -INFINITY, sum = 0.0f;
+#pragma unroll 4
                             for (int i = first; i <= last; ++i)
                                 top = fmaxf(top, __ldcg(part_of<D, RM>(a, i, i == first) + rr * 2));
                             const float ref = top == -INFINITY ? 0.0f : top;
+#pragma unroll 4
                             for (int i = first; i <= last; ++i) {
                                 const float2 v = __ldcg(
                                     reinterpret_cast<const float2*>(part_of<D, RM>(a, i, i == first) + rr * 2));

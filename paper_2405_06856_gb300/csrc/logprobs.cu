@@ -30,7 +30,7 @@ namespace aladdin {
 namespace wk {
 namespace {
 
-constexpr int NT = 256;
+constexpr int NT = 128;
 constexpr int LIST = 1024;   // entries of a slice that the second look may keep
 constexpr int MAX_CS = 8;
 constexpr int MANY = 32;     // threads over the top k from which equal entries are told apart first
@@ -196,7 +196,8 @@ struct alignas(16) Shared {
     unsigned long long best[NT];
     unsigned long long list[LIST];
     unsigned long long top[ALADDIN_TOP_MAX];  // of this slice, best first
-    int owner[NT];                            // threads that may hold one of the top k
+    int owner[NT];                            // threads that may hold one of the top k, and
+    int at[NT];                               // the first vector of the only step that may, or -1
     Run run[NT / 32];
     int above[NT / 32];
     Run all;  // this slice's sums
@@ -207,7 +208,7 @@ struct alignas(16) Shared {
 };
 
 template <typename T>
-__global__ void __launch_bounds__(NT, 4) k_logprobs(LogprobArgs a)
+__global__ void __launch_bounds__(NT, 8) k_logprobs(LogprobArgs a)
 {
     using L = Logit<T>;
     constexpr int PER = L::PER, ES = 16 / PER, U = 4;  // logits of a vector, bytes of one, vectors a step
@@ -254,6 +255,9 @@ __global__ void __launch_bounds__(NT, 4) k_logprobs(LogprobArgs a)
     typename L::Low low = L::low(-200.0f);
     int above = 0;
     float s0 = 0.0f, s1 = 0.0f, t0 = 0.0f, t1 = 0.0f;  // (two sums each, by even and odd places)
+    // the largest entries of a step and of the other steps, and the step's first vector
+    float step1 = -INFINITY, step2 = -INFINITY;
+    int step_v = 0;
     auto huge = [](float v) { return fabsf(v) > 2e38f; };
     auto raise = [&](float v) {
         const bool far = gate != gate || huge(v);
@@ -284,6 +288,9 @@ __global__ void __launch_bounds__(NT, 4) k_logprobs(LogprobArgs a)
         float top = L::top(w[0]);
 #pragma unroll
         for (int u = 1; u < N; ++u) top = fmaxf(top, L::top(w[u]));
+        step2 = fmaxf(step2, fminf(step1, top));
+        step_v = top > step1 ? v : step_v;
+        step1 = fmaxf(step1, top);
         if (!(top <= gate) && top > m) raise(top);
         if (gate != gate) {
             float s = 0.0f;
@@ -446,24 +453,12 @@ __global__ void __launch_bounds__(NT, 4) k_logprobs(LogprobArgs a)
         }
         __syncthreads();
         const uint32_t bound = sh.bound;
-        // the entries of thread `own`, to all lanes of a warp: f(order, index)
-        auto entries_of = [&](int own, auto f) {
-            const int n = own < v1 - v0 ? (v1 - v0 - own + NT - 1) / NT : 0;
-            for (int i = lane; i < n; i += 32) {
-                const int w = v0 + own + i * NT;
-                float g[PER];
-                L::unpack(__ldg(body + w), g);
-#pragma unroll
-                for (int j = 0; j < PER; ++j) f(ordered(g[j]), head + w * PER + j);
-            }
-            if (rank == cs - 1 && lane == 0) {
-                int e = -1;
-                if (own < head) e = own;
-                else if (own >= 32 && own < 64 && tail0 + own - 32 < a.vocab) e = tail0 + own - 32;
-                if (e >= 0) f(ordered(L::one(x + (long long)e * ES)), e);
-            }
-        };
-        if (holds && best >= bound) sh.owner[atomicAdd(&sh.owners, 1)] = tid;
+        if (holds && best >= bound) {
+            const int o = atomicAdd(&sh.owners, 1);
+            sh.owner[o] = tid;
+            // (v1: none of its vectors does, but an end of the row)
+            sh.at[o] = !bound || ordered(step2) >= bound ? -1 : ordered(step1) >= bound ? step_v : v1;
+        }
         if (tid == 0) sh.bound_entry = (unsigned long long)bound << 32;
         __syncthreads();
         int owners = sh.owners;
@@ -493,20 +488,42 @@ __global__ void __launch_bounds__(NT, 4) k_logprobs(LogprobArgs a)
             for (int i = 0; i < NT; ++i) larger += sh.best[i] > first;
             if (first && larger == k - 1) sh.bound_entry = first;
             __syncthreads();
-            if (first >= sh.bound_entry && first) sh.owner[atomicAdd(&sh.owners, 1)] = tid;
+            if (first >= sh.bound_entry && first) {
+                const int o = atomicAdd(&sh.owners, 1);
+                sh.owner[o] = tid;
+                sh.at[o] = -1;
+            }
             __syncthreads();
             owners = sh.owners;
         }
         const unsigned long long bound_entry = sh.bound_entry;
-        for (int i = warp; i < owners; i += NT / 32) {
-            entries_of(sh.owner[i], [&](uint32_t o, int idx) {
-                const unsigned long long e = entry(o, idx);
-                if (e >= bound_entry) {
-                    const int c = atomicAdd(&sh.count, 1);
-                    if (c < LIST) sh.list[c] = e;
-                }
-            });
+        auto keep = [&](unsigned long long e) {
+            if (e >= bound_entry) {
+                const int c = atomicAdd(&sh.count, 1);
+                if (c < LIST) sh.list[c] = e;
+            }
+        };
+        // the step of an owner that may hold entries that large (a warp would read all its vectors,
+        // each in a line of its own, for the few owners that have two)
+        const uint32_t least = (uint32_t)(bound_entry >> 32);
+        const float least_value = value_of(least);
+        auto vector = [&](int w) {
+            const uint4 q = __ldg(body + w);
+            if (least && !(L::top(q) >= least_value)) return;
+            float g[PER];
+            L::unpack(q, g);
+#pragma unroll
+            for (int j = 0; j < PER; ++j) keep(entry(ordered(g[j]), head + w * PER + j));
+        };
+        for (int i = tid; i < owners * U; i += NT) {
+            const int w = sh.at[i / U] + i % U * NT;
+            if (sh.at[i / U] >= 0 && w < v1) vector(w);
         }
+        for (int i = warp; i < owners; i += NT / 32)
+            if (sh.at[i] < 0)
+#pragma unroll 2
+                for (int w = v0 + sh.owner[i] + lane * NT; w < v1; w += 32 * NT) vector(w);
+        if (ends >= 0) keep(entry(ordered(end_x), ends));
         __syncthreads();
         const int count = sh.count;
         if (count <= LIST) {
@@ -597,8 +614,9 @@ template <typename T>
 cudaError_t launch(const LogprobArgs& a, int sms, cudaStream_t st)
 {
     const int vecs = a.vocab / Logit<T>::PER;
-    // CTAs for a row: enough that the GPU is filled several times over, so that its last
-    // part is short, but with 1,024 vectors at least, four a thread
+    // CTAs for a row: until the GPU has two a SM, with 1,024 vectors each at least. (Measured with
+    // 777 rows of 128,256: 61 us with one CTA a row, 72 with two: a CTA's end costs more than
+    // the even load gains.)
     int cs = 1;
     while (cs < MAX_CS && (long long)a.n * cs < 2ll * sms && vecs > 1024 * cs) cs *= 2;
     cudaLaunchConfig_t c = {};

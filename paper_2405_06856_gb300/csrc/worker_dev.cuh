@@ -68,9 +68,9 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, unsigned parity)
     for (unsigned it = 0;; ++it) {
         unsigned done;
         asm volatile(
-            "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+            "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;\n}"
             : "=r"(done)
-            : "r"(bar), "r"(parity)
+            : "r"(bar), "r"(parity), "r"(20000)  // nanoseconds that the thread may sleep
             : "memory");
         if (done) return true;
         if ((it & 63) == 63) {
