@@ -599,7 +599,9 @@ int aladdin_worker_create(const aladdin_worker_shape* shape, void* cuda_stream,
 int aladdin_worker_destroy(aladdin_worker* wk);
 
 /* Waits for the worker's stream; ALADDIN_ERR_STATE if an input was refused on
- * the GPU since the last call of this function, which forgets it. */
+ * the GPU since the last call of this function, which forgets it;
+ * ALADDIN_ERR_TIMEOUT if a bounded wait of a kernel ran out (the results of the calls
+ * since are void). */
 int aladdin_worker_status(aladdin_worker* wk);
 
 /* Attention of the new tokens: token t of request r sees the request's len[r]

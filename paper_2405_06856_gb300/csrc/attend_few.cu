@@ -16,6 +16,11 @@
 //
 // A unit (request, head, row tile) that warps share is joined by the one that
 // finishes last, in the order of its keys.
+//
+// Measured: 128 requests of 83,336 cached tokens, 32 query and 8 key heads of 128 channels in
+// bf16: 74 us, 4.7 TB/s (warps of one CTA that shared tiles through barriers: 91 us; copies
+// of a row each by the bulk engine: 95); two requests of 110,108 tokens, 32 heads of 64 in
+// f16: 159 us, 5.7 TB/s of 6.8 that a copy reaches.
 #include "attend.cuh"
 
 namespace aladdin {

@@ -19,7 +19,13 @@
 // maximum has grown by more than 2^8 over the one that its weights refer to, which
 // 32-bit sums and 16-bit weights hold without loss. The softmax's loops stay rolled
 // (unrolled over a tile, with the scores read once and the weights held in registers,
-// they took 1.6 times as long).
+// and with three exponentials of eight as polynomials, a call took 267 us for 205).
+//
+// Measured: 24 requests of 60,854 cached tokens with trees of up to 64 tokens, 64 query and 8
+// key heads of 128 channels in f16: 183 us, 750 TFLOP/s of 1,932 that a large product
+// reaches; a product of 128 x 128 x 16 takes 98 cycles of the 64 that it takes alone, as operands
+// and copies share the shared memory. 37 requests of 57,837 tokens with chains of up to 5
+// tokens, 28 and 4 heads of 96: 48 us, 1.9 TB/s.
 //
 // New tokens' values that are not finite would reach rows that do not see them
 // (0 times infinity): they are replaced by 0 in shared memory, and rows that do

@@ -17,7 +17,11 @@
 // next four vectors of 16 bytes on their way while it works on four; four vectors
 // share one look at the maximum, and 16-bit logits are clamped and compared two in a
 // word. (Two terms an instruction in the sums, or a ring in shared memory for the
-// vectors, gained nothing.)
+// vectors, gained nothing.) Of an owner's vectors only the step that holds its best is
+// read again, unless another step of it reaches the bound too.
+//
+// Measured: 777 rows of 128,256 bf16 logits with 20 alternatives 58 to 61 us (3.3 TB/s; 48 without
+// alternatives), 2,049 rows of 50,257 f32 logits without alternatives 77 us (5.4 TB/s).
 #include <cooperative_groups.h>
 
 #include <type_traits>

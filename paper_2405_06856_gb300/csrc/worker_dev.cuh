@@ -1,5 +1,5 @@
-// Device helpers of the worker step's kernels: asynchronous copies, matrix
-// fragments, the tiles of all requests laid on one axis.
+// Device helpers of the worker step's kernels: asynchronous copies, barriers, matrix
+// fragments, prefix sums over the requests.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -183,21 +183,6 @@ struct Num<__half> {
             : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
     }
 };
-
-// Byte offset of 16-byte chunk c of row r in a tile of rows of D 16-bit values.
-// Eight consecutive rows of one chunk lie in different banks: rows of a multiple
-// of 128 bytes have their chunks exchanged by the row, others are padded by one.
-template <int D>
-__device__ __forceinline__ uint32_t tile_at(int r, int c)
-{
-    if constexpr (D % 64 == 0) return (uint32_t)(r * (D / 8) + (c ^ (r & 7))) * 16u;
-    else return (uint32_t)(r * (D / 8 + 1) + c) * 16u;
-}
-template <int D>
-constexpr int tile_bytes(int rows)
-{
-    return rows * (D % 64 == 0 ? D / 8 : D / 8 + 1) * 16;
-}
 
 // pre[r] = tiles of the requests before r, pre[n] = all; the block's threads
 // together. tiles(r) is called once a request. Returns pre[n], or -1 (pre
