@@ -22,7 +22,7 @@
 // and with three exponentials of eight as polynomials, a call took 267 us for 205).
 //
 // Measured: 24 requests of 60,854 cached tokens with trees of up to 64 tokens, 64 query and 8
-// key heads of 128 channels in f16: 183 us, 750 TFLOP/s of 1,932 that a large product
+// key heads of 128 channels in f16: 183 us, 556 TFLOP/s of 1,932 that a large product
 // reaches; a product of 128 x 128 x 16 takes 98 cycles of the 64 that it takes alone, as operands
 // and copies share the shared memory. 37 requests of 57,837 tokens with chains of up to 5
 // tokens, 28 and 4 heads of 96: 48 us, 1.9 TB/s.

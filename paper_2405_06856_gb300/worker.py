@@ -62,7 +62,9 @@ def make_kv(k, v, table, length, weight=None, pos=None, next_pos=None):
               "[requests], weight and pos contiguous [pages, kv_heads, page_tokens]",
               ("k", k, getattr(k, "dtype", None)), ("v", v, getattr(k, "dtype", None)), ("table", table, _I32),
               ("length", length, _I32), ("weight", weight, _F32), ("pos", pos, _I32), ("next_pos", next_pos, _I32))
-    kv = A.aladdin_kv(k.data_ptr(), v.data_ptr(), st[0], st[1], st[2], pages, width,
+    # the stride of a dimension of one entry may be anything in torch
+    kv = A.aladdin_kv(k.data_ptr(), v.data_ptr(), st[0] if pages > 1 else heads * tokens * dim,
+                      st[1] if heads > 1 else tokens * dim, st[2], pages, width,
                       row[0] if row[0] > width else width, table.data_ptr(), length.data_ptr(),
                       None if weight is None else weight.data_ptr(),
                       None if pos is None else pos.data_ptr(),
