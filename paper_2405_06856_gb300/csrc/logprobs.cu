@@ -207,6 +207,7 @@ struct alignas(16) Shared {
     Run all;  // this slice's sums
     int all_above;
     int count, owners;
+    int apart;  // owners that are left when equal maxima are told apart
     uint32_t bound;
     unsigned long long bound_entry, prev;
 };
@@ -422,7 +423,7 @@ __global__ void __launch_bounds__(NT, 8) k_logprobs(LogprobArgs a)
         if (tid % width == 0) sh.group[tid / width] = g;
         if (tid == 0) {
             sh.bound = 0;
-            sh.count = sh.owners = 0;
+            sh.count = sh.owners = sh.apart = 0;
         }
     }
     __syncthreads();
@@ -465,6 +466,7 @@ __global__ void __launch_bounds__(NT, 8) k_logprobs(LogprobArgs a)
         }
         if (tid == 0) sh.bound_entry = (unsigned long long)bound << 32;
         __syncthreads();
+        // (nothing writes sh.owners behind this barrier: all threads take the same side here)
         int owners = sh.owners;
         if (owners > k + MANY) {
             // many equal maxima (a row of masked or equal logits): the first entry of
@@ -486,19 +488,18 @@ __global__ void __launch_bounds__(NT, 8) k_logprobs(LogprobArgs a)
                 }
             }
             sh.best[tid] = first;
-            if (tid == 0) sh.owners = 0;
             __syncthreads();
             int larger = 0;
             for (int i = 0; i < NT; ++i) larger += sh.best[i] > first;
             if (first && larger == k - 1) sh.bound_entry = first;
             __syncthreads();
             if (first >= sh.bound_entry && first) {
-                const int o = atomicAdd(&sh.owners, 1);
+                const int o = atomicAdd(&sh.apart, 1);
                 sh.owner[o] = tid;
                 sh.at[o] = -1;
             }
             __syncthreads();
-            owners = sh.owners;
+            owners = sh.apart;
         }
         const unsigned long long bound_entry = sh.bound_entry;
         auto keep = [&](unsigned long long e) {
