@@ -249,8 +249,8 @@ class Worker:
             raise TypeError("logits must be a CUDA tensor of bfloat16, float16 or float32")
         n, vocab = logits.shape
         st = logits.stride()
-        if vocab > 1 and st[1] != 1:
-            raise ValueError("the rows of logits must be contiguous")
+        if (vocab > 1 and st[1] != 1) or (n > 1 and st[0] < vocab):
+            raise ValueError("the rows of logits must be contiguous and share no memory")
         dev, empty = self.device, torch.empty
         logprob = rank = ids = tops = None
         lp = rk = ip = tp = tk = None
@@ -264,5 +264,5 @@ class Worker:
             ids, tops = empty((n, top), dtype=_I32, device=dev), empty((n, top), dtype=_F32, device=dev)
             ip, tp = ids.data_ptr(), tops.data_ptr()
         self._call("aladdin_worker_logprobs", kind, n, vocab, logits.data_ptr(),
-                   st[0] if n > 1 and st[0] > vocab else vocab, tk, top, lp, entropy.data_ptr(), rk, ip, tp)
+                   st[0] if n > 1 else vocab, tk, top, lp, entropy.data_ptr(), rk, ip, tp)
         return logprob, entropy, rank, ids, tops

@@ -1,0 +1,46 @@
+"""What the worker's torch layer hands to the library, on the host: tensors that say that they are on a GPU, and a
+call that is recorded in place of the library's."""
+import pytest
+import torch
+
+
+class OnGpu(torch.Tensor):
+    is_cuda = property(lambda self: True)
+
+
+def put(x):
+    return x.as_subclass(OnGpu)
+
+
+@pytest.fixture(scope="module")
+def W():
+    from paper_2405_06856_gb300 import build
+    build.build()
+    from paper_2405_06856_gb300 import worker
+    return worker
+
+
+@pytest.fixture
+def worker(W):
+    w = W.Worker.__new__(W.Worker)
+    w.handle = None
+    w.device = torch.device("cpu")
+    w.calls = []
+    w._call = lambda name, *args: w.calls.append(args)
+    w._kv_shape = (torch.bfloat16, 2, 16, 64)
+    return w
+
+
+def test_rows_of_logits_keep_their_stride(worker):
+    x = put(torch.zeros(4, 40))
+    for logits, stride in ((x, 40), (x[:, :33], 40), (x[::2], 80), (x[:1], 40), (x[:1].expand(1, -1), 40),
+                           (put(torch.zeros(40)).as_strided((1, 40), (3, 1)), 40)):
+        worker.logprobs(logits)
+        n, vocab, at, got = worker.calls[-1][1:5]
+        assert (n, vocab, at) == (*logits.shape, logits.data_ptr()) and got == (stride if n > 1 else vocab)
+    seen = len(worker.calls)
+    # rows that share memory have a stride below their width: read with another one they would lie outside
+    for logits in (x[:1].expand(8, -1), x.as_strided((3, 40), (39, 1)), put(torch.zeros(1, 1)).expand(2, 1)):
+        with pytest.raises(ValueError, match="rows"):
+            worker.logprobs(logits)
+    assert len(worker.calls) == seen
