@@ -38,7 +38,8 @@ def make_kv(k, v, table, length, weight=None, pos=None, next_pos=None):
 
     k, v: [pages, kv_heads, page_tokens, head_dim], any strides with contiguous channels
     (a pool in [page, token, head, channel] order is passed transposed(1, 2));
-    table: int32 [requests, pages a request may have]; length, next_pos: int32
+    table: int32 [requests, pages a request may have], a row in memory for each request
+    (not an expanded one: their pages may be the same, their entries not); length, next_pos: int32
     [requests]; weight (float32), pos (int32): [pages, kv_heads, page_tokens]."""
     try:
         kind, shape, st = k.dtype, k.shape, k.stride()
@@ -47,7 +48,7 @@ def make_kv(k, v, table, length, weight=None, pos=None, next_pos=None):
         row = table.stride()
         meta = shape[:3]
         ok = (k.is_cuda and v.dtype is kind and v.shape == shape and v.stride() == st and st[3] == 1
-              and table.dtype is _I32 and (row[1] == 1 or width == 1)
+              and table.dtype is _I32 and (row[1] == 1 or width == 1) and (n < 2 or row[0] >= width)
               and length.dtype is _I32 and length.shape == (n,) and length.is_contiguous()
               and (weight is None or (weight.dtype is _F32 and weight.shape == meta
                                       and weight.is_contiguous()))
@@ -58,14 +59,14 @@ def make_kv(k, v, table, length, weight=None, pos=None, next_pos=None):
         ok = False
     if not ok:
         _fail("k and v must be [pages, kv_heads, page_tokens, head_dim] with equal strides and contiguous "
-              "channels, table [requests, pages] with contiguous rows, length and next_pos contiguous "
+              "channels, table [requests, pages] with contiguous rows that share no memory, length and next_pos contiguous "
               "[requests], weight and pos contiguous [pages, kv_heads, page_tokens]",
               ("k", k, getattr(k, "dtype", None)), ("v", v, getattr(k, "dtype", None)), ("table", table, _I32),
               ("length", length, _I32), ("weight", weight, _F32), ("pos", pos, _I32), ("next_pos", next_pos, _I32))
     # the stride of a dimension of one entry may be anything in torch
     kv = A.aladdin_kv(k.data_ptr(), v.data_ptr(), st[0] if pages > 1 else heads * tokens * dim,
                       st[1] if heads > 1 else tokens * dim, st[2], pages, width,
-                      row[0] if row[0] > width else width, table.data_ptr(), length.data_ptr(),
+                      row[0] if n > 1 else width, table.data_ptr(), length.data_ptr(),
                       None if weight is None else weight.data_ptr(),
                       None if pos is None else pos.data_ptr(),
                       None if next_pos is None else next_pos.data_ptr())

@@ -44,3 +44,23 @@ def test_rows_of_logits_keep_their_stride(worker):
         with pytest.raises(ValueError, match="rows"):
             worker.logprobs(logits)
     assert len(worker.calls) == seen
+
+
+def cache(n, width, pages=6):
+    k = put(torch.zeros(pages, 2, 16, 64, dtype=torch.bfloat16))
+    table = put(torch.zeros(n, width, dtype=torch.int32))
+    length = put(torch.zeros(n, dtype=torch.int32))
+    return k, table, length
+
+
+def test_rows_of_the_page_table_keep_their_stride(W):
+    k, table, length = cache(4, 8)
+    for t, stride in ((table, 8), (table[:, :5], 8), (table[:, 3:], 8), (table[:, :1], 8)):
+        kv = W.make_kv(k, k.clone(), t, length)
+        assert (kv.table, kv.table_width, kv.table_stride) == (t.data_ptr(), t.shape[1], stride)
+    kv = W.make_kv(k, k.clone(), table[:1].expand(1, -1), length[:1])
+    assert kv.table_stride == 8
+    # requests that share their pages by one row of the table: read with the row's width they would lie outside
+    for t in (table[:1].expand(4, -1), table[:1, :1].expand(4, 1), table.as_strided((4, 8), (7, 1))):
+        with pytest.raises(ValueError, match="table"):
+            W.make_kv(k, k.clone(), t, length)
