@@ -49,12 +49,15 @@ __device__ __forceinline__ float max_nan(float a, float b)
 // How a vector of 16 bytes of logits is taken apart. low() is what top - 200 or
 // less looks like in the type (at least a step below top): entries below it
 // count as it, since both exponentials are 0, so that products with differences
-// stay finite; a NaN stays one.
+// stay finite; a NaN stays one. A top of more than FAR in size has no such value (in f16, -65504
+// less 1,024 is -inf; else m log2 e may be no float): its row counts the entries equal to it,
+// which leaves out e^-32 at most for each other one, as values of the type lie 32 or more apart there.
 template <typename T>
 struct Logit;
 template <>
 struct Logit<float> {
     static constexpr int PER = 4;
+    static constexpr float FAR = 2e38f;
     typedef float Low;
     static __device__ __forceinline__ Low low(float v) { return v; }
     static __device__ __forceinline__ float top(const uint4& v)
@@ -96,6 +99,7 @@ __device__ __forceinline__ __half2 both(__half2*, float v) { return __half2half2
 template <typename T>
 struct Logit {
     static constexpr int PER = 8;
+    static constexpr float FAR = std::is_same<T, __half>::value ? 32768.0f : 2e38f;
     typedef typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type Low;
     static __device__ __forceinline__ Low low(float v) { return both((Low*)nullptr, v); }
     static __device__ __forceinline__ Low word(uint32_t w) { return *reinterpret_cast<Low*>(&w); }
@@ -253,7 +257,7 @@ __global__ void __launch_bounds__(NT, 8) k_logprobs(LogprobArgs a)
 
     // The largest entry so far, and the sums s of 2^y and t of 2^y y, y = x log2 e - ref with ref =
     // m log2 e rounded: one multiply-add a logit, and the rounding of ref drops out of the results, as
-    // every term and the conversion below have the same. Where m log2 e is no float (a mask of the
+    // every term and the conversion below have the same. Where |m| is more than FAR (a mask of the
     // type's lowest value, +inf), the sum counts the entries that equal m: all others are too far
     // away; `gate` is m, or NaN to have every vector looked at that way.
     float m = -INFINITY, ref = 0.0f, gate = -INFINITY;
@@ -263,7 +267,7 @@ __global__ void __launch_bounds__(NT, 8) k_logprobs(LogprobArgs a)
     // the largest entries of a step and of the other steps, and the step's first vector
     float step1 = -INFINITY, step2 = -INFINITY;
     int step_v = 0;
-    auto huge = [](float v) { return fabsf(v) > 2e38f; };
+    auto huge = [](float v) { return fabsf(v) > L::FAR; };
     auto raise = [&](float v) {
         const bool far = gate != gate || huge(v);
         const float next = far ? 0.0f : v * LOG2E, d = ref - next, f = far ? 0.0f : ex2(d);

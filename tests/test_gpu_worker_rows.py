@@ -44,3 +44,50 @@ def test_logprobs_many_equal_maxima(A, kind, vocab, holders):
         # every row's alternatives: the first of the equal ones
         order = np.argsort(-t.double().numpy(), axis=1, kind="stable")[:, :top]
         assert np.array_equal(got[3].cpu().numpy(), order)
+
+
+def check_rows(A, x, token, top):
+    """Every row by itself: x and the maximum are exact, so that errors are those of the difference, 2^-21 of the
+    result, and of the sums."""
+    import torch
+    import worker_ref as ref
+    with A.Worker("bf16", 1, 1, 64, 16) as w:
+        got = w.logprobs(x.cuda(), torch.from_numpy(np.asarray(token, np.int32)).cuda(), top)
+        assert w.status() == A.OK
+    got = [g.double().cpu().numpy() for g in got]
+    rows = x.double().numpy()
+    lp, ent, rank, ids, tlp = ref.logprobs(rows, token, top)
+    for r, row in enumerate(rows):  # with the maximum taken off first: next to 1e30 a logarithm vanishes in 64 bits, too
+        if np.isfinite(row.max()):
+            d = row - row.max()
+            d -= np.log(np.exp(d).sum())
+            lp[r], tlp[r] = d[token[r]], d[ids[r]]
+    assert np.array_equal(got[2], rank) and np.array_equal(got[3], ids)
+    for name, g, w, tol in (("logprob", got[0], lp, None), ("top_logprob", got[4], tlp, None),
+                            ("entropy", got[1], ent, 1e-5 * (1 + np.abs(ent)))):
+        fin = np.isfinite(w)
+        assert np.array_equal(np.isnan(g), np.isnan(w)), (name, g, w)
+        assert np.array_equal(g[~fin & ~np.isnan(w)], w[~fin & ~np.isnan(w)]), (name, g, w)
+        if tol is None:
+            tol = 1e-5 + 2.0 ** -21 * np.abs(w)
+        off = np.abs(np.where(fin, g, 0.0) - np.where(fin, w, 0.0))
+        assert np.all(off <= np.where(fin, tol, 0.0)), (name, off.max(), g, w)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("vocab", [40, 3000, 20000])
+def test_logprobs_masks_of_the_lowest_value(A, kind, vocab):
+    """Rows masked by the type's lowest value, by -inf, and by both, alone and beside ordinary logits."""
+    import torch
+    rng = np.random.default_rng(7)
+    low = float(torch.finfo(tensor(np.zeros(1), kind).dtype).min)
+    place = np.arange(vocab)
+    both = np.where(place % 2 == 0, low, -np.inf)
+    some = 3.0 * rng.normal(size=vocab)
+    x = np.stack([np.full(vocab, low), both, np.where(place == vocab // 2, low, -np.inf),
+                  np.where(place < vocab // 2, both, some), np.where(place < vocab - 3, both, some),
+                  np.where(place >= vocab // 4, both, some), np.where(place % 97 == 5, some, both),
+                  np.where(place % 97 == 5, some, low), np.where(place % 97 == 5, some, -np.inf)])
+    token = rng.integers(0, vocab, len(x))
+    for top in (1, 20):
+        check_rows(A, tensor(x, kind), token, top)
