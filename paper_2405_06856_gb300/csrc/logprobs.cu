@@ -50,14 +50,15 @@ __device__ __forceinline__ float max_nan(float a, float b)
 // less looks like in the type (at least a step below top): entries below it
 // count as it, since both exponentials are 0, so that products with differences
 // stay finite; a NaN stays one. A top of more than FAR in size has no such value (in f16, -65504
-// less 1,024 is -inf; else m log2 e may be no float): its row counts the entries equal to it,
-// which leaves out e^-32 at most for each other one, as values of the type lie 32 or more apart there.
+// less 1,024 is -inf), or the rounding of top log2 e leaves 2^(its rounding) out of range (in 32 bits it is 16
+// at most up to 2^28): its row counts the entries equal to it, which leaves out e^-32 at most for each
+// other one, as values of the type lie 32 or more apart there.
 template <typename T>
 struct Logit;
 template <>
 struct Logit<float> {
     static constexpr int PER = 4;
-    static constexpr float FAR = 2e38f;
+    static constexpr float FAR = 268435456.0f;
     typedef float Low;
     static __device__ __forceinline__ Low low(float v) { return v; }
     static __device__ __forceinline__ float top(const uint4& v)
@@ -99,7 +100,7 @@ __device__ __forceinline__ __half2 both(__half2*, float v) { return __half2half2
 template <typename T>
 struct Logit {
     static constexpr int PER = 8;
-    static constexpr float FAR = std::is_same<T, __half>::value ? 32768.0f : 2e38f;
+    static constexpr float FAR = std::is_same<T, __half>::value ? 32768.0f : 268435456.0f;
     typedef typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type Low;
     static __device__ __forceinline__ Low low(float v) { return both((Low*)nullptr, v); }
     static __device__ __forceinline__ Low word(uint32_t w) { return *reinterpret_cast<Low*>(&w); }

@@ -91,3 +91,55 @@ def test_logprobs_masks_of_the_lowest_value(A, kind, vocab):
     token = rng.integers(0, vocab, len(x))
     for top in (1, 20):
         check_rows(A, tensor(x, kind), token, top)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("vocab", [40, 3000, 20000])
+def test_logprobs_large_logits(A, kind, vocab):
+    """Rows of large logits of either sign: equal ones, neighbours in the type, with -inf, and as a mask in front of
+    ordinary ones (a row masked by -1e9 or -1e30 is one of them)."""
+    import torch
+    rng = np.random.default_rng(8)
+    sizes = [1e3, 5e3, 2e4, 3.3e4, 5e4, 6.5e4] if kind == "f16" else [1e5, 1e7, 1e8, 4e8, 1e9, 1e10, 1e20, 1e30, 1e37, 3e38]
+    t = tensor(np.zeros(1), kind).dtype
+    place = np.arange(vocab)
+    some = 3.0 * rng.normal(size=vocab)
+    rows = []
+    for size in sizes:
+        for v in (size, -size):
+            a = torch.tensor(v).to(t)
+            b = torch.nextafter(a.float(), torch.tensor(0.0)) if kind == "f32" else (a.view(torch.int16) - 1).view(t)
+            a, b = float(a), float(b)  # b: the neighbour nearer to 0
+            rows += [np.full(vocab, a), np.where(place % 3 == 1, a, b), np.where(place % 2 == 0, a, -np.inf)]
+            if v < 0:
+                rows += [np.where(place < vocab // 2, a, some), np.where(place % 97 == 5, some, a)]
+    x = np.stack(rows)
+    token = rng.integers(0, vocab, len(x))
+    check_rows(A, tensor(x, kind), token, 5)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("vocab", [40, 3000, 20000])
+def test_logprobs_odd_rows_of_16_bits(A, kind, vocab):
+    """Equal and rounded values, infinities, NaN, -0 and denormal ones in rows of 16 bits; every row's token among
+    several places."""
+    rng = np.random.default_rng(3)
+    tiny = 1e-39 if kind == "bf16" else 1e-7  # denormal in the type
+    x = (2.0 * rng.normal(size=(14, vocab))).astype(np.float32)
+    x[0] = 1.5
+    x[1] = -np.inf
+    x[2, ::2] = -np.inf
+    x[3, vocab // 2] = np.nan
+    x[4, vocab // 3] = np.inf
+    x[5] = np.nan
+    x[6] = np.where(np.arange(vocab) % 3 == 0, 0.0, -0.0)
+    x[7] = np.round(x[7])
+    x[8] = tiny * rng.integers(-4, 5, vocab)
+    x[9, ::1024], x[9, 1::1024], x[9, 2::1024] = 30.0, 31.0, 32.0
+    x[10, ::3] = np.nan
+    x[10, 1::3] = -np.inf
+    x[11] = np.where(np.arange(vocab) // 8 % 128 == 3, 40.0 + x[11], x[11])
+    x[12] = -100.0 + x[12]
+    x[13, 5:] = -np.inf
+    for at in (0, vocab // 3, vocab // 2, vocab - 1):
+        check_rows(A, tensor(x, kind), np.full(14, at), 20)
