@@ -636,7 +636,9 @@ int aladdin_worker_accept(aladdin_worker* wk, const aladdin_kv* kv, const aladdi
  * lower slot first among equals. The slots from budget[r] on that stay move, in
  * order, into the slots before it that do not, with key, value, weight and
  * position; len[r] becomes budget[r]. Requests within their budget do not
- * change. The first call on a larger pool than any before allocates a workspace
+ * change. Slots on a page outside the pool do not move either: those before the
+ * budget stay, and of the other slots as many as it has room for then. No slot may belong
+ * to two requests. The first call on a larger pool than any before allocates a workspace
  * of 4 bytes per slot of the pool (and waits for the device). */
 int aladdin_worker_evict(aladdin_worker* wk, const aladdin_kv* kv, int32_t n_req,
                          const int32_t* budget, int32_t recent);

@@ -7,7 +7,9 @@
 // that stay (movers) go, in order, to the dropped slots before it (holes): as
 // many as the call needs to move, and no slot is both read and written, so
 // that the moves are independent of one another. The order of the cached
-// tokens means nothing to the attention; `pos` says what is recent.
+// tokens means nothing to the attention; `pos` says what is recent. Slots of a page
+// outside the pool are neither: before the budget they stay, whatever the others hold, behind
+// it only where all others do. So every hole and mover can be read and written.
 //
 // One CTA, or a cluster where there are few long requests, serves one (request,
 // key head); each CTA keeps the keys of its part of the slots in shared memory.
@@ -34,17 +36,18 @@ namespace {
 constexpr int BINS = 2048;
 constexpr int MAX_KEYS = 50 * 1024;  // keys that a CTA holds; it forms the others again where it needs them
 
-// Order of the floats as unsigned numbers: -0 as +0, NaN below everything.
+// Order of the floats as unsigned numbers: -0 as +0, NaN below everything. 0 and the largest
+// number stand for slots of pages outside the pool, behind the budget and before it.
 __device__ __forceinline__ uint32_t ordered(float w)
 {
-    if (w != w) return 0u;
+    if (w != w) return 1u;
     const uint32_t u = __float_as_uint(w + 0.0f);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
 struct Evict {
     const int32_t* row;  // the request's pages
-    int h, held, recent_from;
+    int h, held, budget, recent_from;
 };
 
 __device__ __forceinline__ int page_of(const EvictArgs& a, const Evict& e, int slot)
@@ -63,8 +66,8 @@ __device__ __forceinline__ long long row_at(const EvictArgs& a, const Evict& e, 
     return page * a.kv.page_stride + e.h * a.kv.head_stride + (slot & (a.kv.page - 1)) * a.kv.token_stride;
 }
 
-// Keys of N slots first, first + step, ... below end, their loads together; 0 for
-// slots of a page outside the pool, which are recorded.
+// Keys of N slots first, first + step, ... below end, their loads together; pages outside
+// the pool are recorded.
 template <int N>
 __device__ __forceinline__ void keys_of(const EvictArgs& a, const Evict& e, int first, int step, int end,
                                         uint32_t (&key)[N])
@@ -85,7 +88,8 @@ __device__ __forceinline__ void keys_of(const EvictArgs& a, const Evict& e, int 
     }
 #pragma unroll
     for (int i = 0; i < N; ++i)
-        key[i] = page[i] < 0 ? 0u : pos[i] >= e.recent_from ? ordered(INFINITY) : ordered(w[i]);
+        key[i] = page[i] < 0 ? (first + i * step < e.budget ? 0xffffffffu : 0u)
+                             : pos[i] >= e.recent_from ? ordered(INFINITY) : ordered(w[i]);
 }
 
 // Exclusive sums of two counts over the block's threads, and their totals.
@@ -120,12 +124,12 @@ __device__ __forceinline__ int2 block_scan(int2 v, int2* scratch, int2& total)
     return make_int2(before.x + u.x - v.x, before.y + u.y - v.y);
 }
 
-// The i-th move of a (request, head), from the workspace; -1 where a page is outside the pool.
-__device__ __forceinline__ void listed(const EvictArgs& a, const Evict& e, int budget, int i, int& from, int& to)
+// The i-th of a (request, head)'s moves, whose holes and then movers lie in the workspace from
+// `base` on.
+__device__ __forceinline__ void listed(const EvictArgs& a, long long base, int moves, int i, int& from, int& to)
 {
-    const int pm = page_of(a, e, budget + i), ph = page_of(a, e, i);
-    from = pm < 0 ? -1 : __ldcg(a.lists + meta_at(a, e, pm, budget + i));
-    to = ph < 0 ? -1 : __ldcg(a.lists + meta_at(a, e, ph, i));
+    to = __ldcg(a.lists + base + i);
+    from = __ldcg(a.lists + base + moves + i);
 }
 
 // Moves a lane's slot `from` to its slot `to` (the lanes below n; -1: nothing), the warp together.
@@ -134,7 +138,8 @@ __device__ __forceinline__ void move_rows(const EvictArgs& a, const Evict& e, in
 {
     constexpr int CH = D / 8, PER = 2 * CH;  // 16-byte pieces of a key, of a key and a value; U of a lane in flight
     long long src = -1, dst = -1;
-    if (lane < n && from >= 0 && to >= 0) {
+    // (lists of a request whose arrays changed under the call may not be full)
+    if (lane < n && from >= 0 && to >= 0 && from < a.kv.cap && to < a.kv.cap) {
         const int pd = page_of(a, e, to), ps = page_of(a, e, from);
         if (pd >= 0 && ps >= 0) {
             src = row_at(a, e, ps, from);
@@ -179,6 +184,7 @@ __global__ void __launch_bounds__(NT, CLUSTER ? 2 : 4) k_evict(EvictArgs a, int 
     __shared__ int2 scratch[NT / 32];
     __shared__ int2 counts;  // what the cluster's other CTAs read of this one
     __shared__ int s_digit, s_above, s_here, s_last;
+    __shared__ long long s_base;  // where this (request, head)'s lists start; -1: there is no room
     const int cs = CLUSTER ? (int)cluster.num_blocks() : 1, rank = CLUSTER ? (int)cluster.block_rank() : 0;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int unit = blockIdx.x / cs, H = a.kv.kv_heads, r = unit / H;
@@ -191,7 +197,7 @@ __global__ void __launch_bounds__(NT, CLUSTER ? 2 : 4) k_evict(EvictArgs a, int 
     e.h = unit - r * H;
     e.row = a.kv.table + (long long)r * a.kv.table_stride;
     e.held = a.kv.len[r];
-    const int budget = a.budget[r];
+    const int budget = e.budget = a.budget[r];
     const long long from = (long long)a.kv.next[r] - a.recent;  // recent positions (an int may not hold it)
     e.recent_from = from < -0x7fffffffll ? -0x7fffffff : (int)from;
     const bool ok = e.held >= 0 && e.held <= a.kv.cap && budget >= 0;
@@ -282,32 +288,45 @@ __global__ void __launch_bounds__(NT, CLUSTER ? 2 : 4) k_evict(EvictArgs a, int 
             here = s_here;
             found = want == here;  // all of them stay
         }
-        if (budget == 0) known = mask = 0xffffffffu;  // nothing is above the largest key, and none of it stays
+        if (budget == 0) known = mask = 0xffffffffu;  // nothing is above the largest number, and none of it stays
 
         // a thread looks at a run of slots (odd, so that a warp's reads fall in
         // different banks); counts before it number its equal keys, then its holes and movers
         const int run = ((n + NT - 1) / NT) | 1, i0 = min(tid * run, n), i1 = min(i0 + run, n);
-        auto before_me = [&](int2 total) -> int2 {
+        // counts of the cluster's CTAs before this one; `all` becomes those of all. `take`: room for the
+        // lists of as many moves
+        auto before_me = [&](int2 total, int2& all, bool take) -> int2 {
             int2 v = make_int2(0, 0);
+            all = total;
             if (CLUSTER) {
                 if (tid == 0) counts = total;
                 cluster.sync();
-                for (int b = 0; b < rank; ++b) {
+                all = v;
+                for (int b = 0; b < cs; ++b) {
                     const int2 c = *cluster.map_shared_rank(&counts, b);
-                    v.x += c.x;
-                    v.y += c.y;
+                    if (b < rank) v.x += c.x, v.y += c.y;
+                    all.x += c.x;
+                    all.y += c.y;
                 }
-                cluster.sync();
             }
+            if (take && rank == 0 && tid == 0) {
+                // (slots that move or are moved into are a slot of the pool each: there is room, unless
+                // requests share them)
+                const unsigned long long n = 2ull * all.y, at = atomicAdd(a.cursor, n);
+                s_base = at + n <= a.lists_n ? (long long)at : -1;
+                if (s_base < 0) atomicOr(a.err, WORKER_BAD_INPUT);
+            }
+            if (CLUSTER) cluster.sync();
+            else if (take) __syncthreads();
             return v;
         };
         __syncthreads();
-        int2 mine = make_int2(0, 0), total, at;
+        int2 mine = make_int2(0, 0), total, all, at;
         int equal0 = 0;  // equal keys in front of this thread's run
         if (want != here && budget > 0) {
             for (int i = i0; i < i1; ++i) mine.x += (key(i) & mask) == known;
             at = block_scan<NT>(mine, scratch, total);
-            equal0 = at.x + before_me(total).x;
+            equal0 = at.x + before_me(total, all, false).x;
         }
         int equal = equal0;
         auto stays = [&](uint32_t k) { return (k & mask) > known || ((k & mask) == known && equal++ < want); };
@@ -318,19 +337,19 @@ __global__ void __launch_bounds__(NT, CLUSTER ? 2 : 4) k_evict(EvictArgs a, int 
             else mine.y += s;
         }
         at = block_scan<NT>(mine, scratch, total);
-        const int2 moved0 = before_me(total);
-        at.x += moved0.x;
-        at.y += moved0.y;
         // the lists of holes and movers: in shared memory (in place of the counts) where one CTA
         // has few of them, else in the workspace
         const bool near = !CLUSTER && total.y <= BINS;
+        const int2 moved0 = before_me(total, all, !near);
+        at.x += moved0.x;
+        at.y += moved0.y;
+        int moves = all.y;
+        const long long base = near ? 0 : CLUSTER ? *cluster.map_shared_rank(&s_base, 0) : s_base;
+        if (base < 0) moves = 0;
         auto note = [&](int list, int i, int slot) {
-            if (near) {
-                hist[list][i] = slot;
-            } else {
-                const int w = list ? budget + i : i, p = page_of(a, e, w);
-                if (p >= 0) a.lists[meta_at(a, e, p, w)] = slot;
-            }
+            if (i >= moves) return;
+            if (near) hist[list][i] = slot;
+            else a.lists[base + (list ? moves : 0) + i] = slot;
         };
         equal = equal0;
         for (int i = i0; i < i1; ++i) {
@@ -341,18 +360,15 @@ __global__ void __launch_bounds__(NT, CLUSTER ? 2 : 4) k_evict(EvictArgs a, int 
                 note(1, at.y++, s0 + i);
             }
         }
-        if (tid == 0) counts = total;
-        if (!near) __threadfence();
-        meet();
-        int moves = total.y;
         if (CLUSTER) {
-            moves = 0;
-            for (int b = 0; b < cs; ++b) moves += cluster.map_shared_rank(&counts, b)->y;
-        }
-
-        if (CLUSTER) {
-            if (rank == 0 && tid == 0) a.moves[unit] = moves;
+            if (rank == 0 && tid == 0) {
+                a.moves[unit] = moves;
+                a.bases[unit] = base;
+            }
+            cluster.sync();  // the others have read this CTA's counts
         } else {
+            if (!near) __threadfence();
+            __syncthreads();
             // every warp the same number of moves
             const int share = (moves + NT / 32 - 1) / (NT / 32), first = warp * share, last = min(first + share, moves);
             for (int m0 = first; m0 < last; m0 += 32) {
@@ -363,13 +379,12 @@ __global__ void __launch_bounds__(NT, CLUSTER ? 2 : 4) k_evict(EvictArgs a, int 
                         to = hist[0][i];
                         from = hist[1][i];
                     } else {
-                        listed(a, e, budget, i, from, to);
+                        listed(a, base, moves, i, from, to);
                     }
                 }
                 move_rows<D, 4>(a, e, from, to, min(32, last - m0), lane);
             }
         }
-        if (CLUSTER) cluster.sync();  // the others have read this CTA's counts
     } else if (CLUSTER && rank == 0 && tid == 0) {
         a.moves[unit] = 0;
     }
@@ -382,7 +397,10 @@ __global__ void __launch_bounds__(NT, CLUSTER ? 2 : 4) k_evict(EvictArgs a, int 
     }
     __syncthreads();
     if (s_last) {
-        if (tid == 0) *a.arrived = 0;
+        if (tid == 0) {
+            *a.arrived = 0;
+            *a.cursor = 0;
+        }
         for (int q = tid; q < a.n_req; q += NT) {
             const int len = a.kv.len[q], b = a.budget[q];
             if (len >= 0 && len <= a.kv.cap && b >= 0 && len > b) a.kv.len[q] = b;
@@ -405,13 +423,13 @@ __global__ void __launch_bounds__(MOVERS, MOVE_CTAS) k_move(EvictArgs a, int uni
         const int n = (int)min(32ll, last - m0);
         Evict e;
         e.row = a.kv.table;
-        e.h = e.held = e.recent_from = 0;
+        e.h = e.held = e.budget = e.recent_from = 0;
         int from = -1, to = -1;
         if (lane < n) {
             const int unit = plan_find(pre, units, (int)(m0 + lane)), r = unit / a.kv.kv_heads;
             e.h = unit - r * a.kv.kv_heads;
             e.row = a.kv.table + (long long)r * a.kv.table_stride;
-            listed(a, e, a.budget[r], (int)(m0 + lane) - pre[unit], from, to);
+            listed(a, a.bases[unit], pre[unit + 1] - pre[unit], (int)(m0 + lane) - pre[unit], from, to);
         }
         move_rows<D, 8>(a, e, from, to, n, lane);
     }

@@ -21,7 +21,9 @@ struct aladdin_worker {
     unsigned* err = nullptr;
     int* done = nullptr;     // CTAs of an accept or evict call that have finished
     int* arrived = nullptr;  // [ATTEND_WORKERS_PER_SM * sms]
-    int* moves = nullptr;    // [1024] evict: moves of (request, head) pairs
+    int* moves = nullptr;    // [1024] evict: moves of (request, head) pairs,
+    long long* bases = nullptr;            // [1024] where their lists start,
+    unsigned long long* cursor = nullptr;  // and what is taken of the lists
     size_t ints = 0;         // bytes of the word and the counters
     float* part = nullptr;
     int32_t* lists = nullptr;  // evict (grow-only)
@@ -160,7 +162,8 @@ try {
     wk->st = (cudaStream_t)cuda_stream;
     wk->shape = *shape;
     while ((1 << wk->page_shift) < shape->page_tokens) ++wk->page_shift;
-    const size_t ints = ((size_t)(2 + ATTEND_WORKERS_PER_SM * d.sms + 1024) * 4 + 255) / 256 * 256;
+    const size_t words = (size_t)(2 + ATTEND_WORKERS_PER_SM * d.sms + 1024);  // an even number
+    const size_t ints = (words * 4 + (1024 + 1) * 8 + 255) / 256 * 256;
     wk->ints = ints;
     const size_t bytes = ints + attend_part_bytes(d.sms, shape->head_dim);
     cudaError_t e = cudaMalloc((void**)&wk->fixed, bytes);
@@ -175,6 +178,8 @@ try {
     wk->done = reinterpret_cast<int*>(wk->fixed) + 1;
     wk->arrived = wk->done + 1;
     wk->moves = wk->arrived + ATTEND_WORKERS_PER_SM * d.sms;
+    wk->cursor = reinterpret_cast<unsigned long long*>(wk->fixed + words * 4);
+    wk->bases = reinterpret_cast<long long*>(wk->cursor + 1);
     wk->part = reinterpret_cast<float*>(wk->fixed + ints);
     *out = wk;
     return ALADDIN_OK;
@@ -292,7 +297,10 @@ try {
     a.budget = budget;
     a.recent = recent;
     a.moves = wk->moves;
+    a.bases = wk->bases;
     a.lists = wk->lists;
+    a.lists_n = wk->lists_n;
+    a.cursor = wk->cursor;
     a.arrived = wk->done;
     a.err = wk->err;
     CK(launch_evict(a, wk->sms, wk->st));

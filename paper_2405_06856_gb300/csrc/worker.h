@@ -89,8 +89,11 @@ struct EvictArgs {
     int n_req;
     const int32_t* budget;
     int recent;
-    int* moves;             // of the (request, head) pairs, where clusters serve them
-    int32_t* lists;         // one entry a slot of the pool: the i-th hole at slot i, the i-th mover at budget + i
+    int* moves;             // of the (request, head) pairs, where clusters serve them,
+    long long* bases;       // and where their lists start
+    int32_t* lists;         // holes, then movers of each pair in a place of its own
+    unsigned long long lists_n;  // entries: as many as the pool has slots
+    unsigned long long* cursor;  // entries that are taken, zero between calls
     int* arrived;
     unsigned* err;
 };
