@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(Atte
             // boxes of cached keys, in turn to the warps, one a lane
             const int boxes = maps.rows ? min(max(own, 0), KT) / maps.rows : 0, rest = boxes * maps.rows;
             const int box = lane * L::COPIES + cw, box_half = box % L::HALVES, box_row = box / L::HALVES * maps.rows;
-            const int box_page = __shfl_sync(0xffffffffu, page, box_row >> 4 & 31);
+            const int box_page = __shfl_sync(0xffffffffu, have ? page : a.kv.pages, box_row >> 4 & 31);
             const int my_boxes = (boxes * L::HALVES - cw + L::COPIES - 1) / L::COPIES;
 #pragma unroll 1
             for (int part = 0; part < 2 && ok; ++part) {  // keys, values
@@ -334,7 +334,8 @@ __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(Atte
                 if (boxes) {
                     if (lane == 0) mbar_expect(bar, my_boxes * maps.rows * 128);
                     __syncwarp();
-                    // (a page outside the pool: zeros, and the tile's mask hides them)
+                    // (a page outside the pool, whatever its index: the one behind the pool, which
+                    // gives zeros, and the tile's mask hides them)
                     if (lane < my_boxes)
                         box_copy(d + box_half * KT * 128 + box_row * 128, part ? &maps.v : &maps.k, box_half * 64,
                                  (key0 + box_row) & (a.kv.page - 1), C.h, box_page, bar);
