@@ -181,8 +181,7 @@ struct Many {
                          tmem = ofree + 16;
     static constexpr int okm = tmem + 16;                // 8 masks of valid pages, a tile each
     static constexpr int wild = okm + 8 * 4;             // 8 flags of units
-    static constexpr int last = wild + 8 * 4;            // 2 flags of the joins
-    static constexpr int scratch = last + 8;
+    static constexpr int scratch = wild + 8 * 4;
     static constexpr int pre = scratch + 32 * 8;
     static constexpr int bytes(int n_req) { return pre + (n_req + 1) * 8; }
     static constexpr int COPIES = 3;                     // warps that copy
@@ -250,7 +249,8 @@ __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(Atte
     const uint32_t tm = *reinterpret_cast<volatile uint32_t*>(sm + L::tmem);
 
     // A wait that runs out is recorded and ends its warp's part; the others' waits run
-    // out after it, and all meet at the end, where tensor memory is freed.
+    // out after it (no warps meet at a barrier without a limit before the end), and all meet at
+    // the end, where tensor memory is freed.
     auto wait = [&](uint32_t bar, int phase) -> bool {
         if (mbar_wait(bar, phase & 1)) return true;
         atomicOr(a.err, WORKER_TIMEOUT);
@@ -698,15 +698,16 @@ __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(Atte
                     if (!whole) {
                         int first, last;
                         ax.sharers(C, first, last);
-                        int* const flag = reinterpret_cast<int*>(sm + L::last) + w;
+                        // (a row's parts come from warps of one number in their CTAs: no other warp is
+                        // waited for)
+                        int* const arrived = a.arrived + first * ATTEND_WORKERS_PER_SM + warp;
                         __threadfence();
-                        asm volatile("bar.sync %0, 128;" ::"r"(1 + w) : "memory");
-                        if (row == 0) {
-                            *flag = atomicAdd(a.arrived + first * 2 + w, 1) == last - first;
-                            if (*flag) a.arrived[first * 2 + w] = 0;
-                        }
-                        asm volatile("bar.sync %0, 128;" ::"r"(1 + w) : "memory");
-                        if (*const_cast<volatile int*>(flag) && row < rows) {
+                        __syncwarp();
+                        int count = 0;
+                        if (lane == 0) count = atomicAdd(arrived, 1);
+                        count = __shfl_sync(0xffffffffu, count, 0);
+                        if (count == last - first && lane == 0) *arrived = 0;
+                        if (count == last - first && row < rows) {
                             __threadfence();
                             float top = -INFINITY, sum = 0.0f;
 #pragma unroll 4
