@@ -175,13 +175,14 @@ struct Many {
     static constexpr int NB = ROOM / TILE < 8 ? ROOM / TILE : 8;  // tiles of the ring
     static_assert(NB >= 4, "keys and values of two tiles");
     static constexpr int q = NB * TILE;
-    static constexpr int bars = q + NQ * MT * QT;        // full NB, empty NB, the queries' 2 NQ, then 2 x 4
+    static constexpr int bars = q + NQ * MT * QT;        // full NB, empty NB, the queries' 2 NQ, then 2 x 4, 1
     static constexpr int full = bars, empty = full + NB * 8, qfull = empty + NB * 8, qempty = qfull + NQ * 8,
                          sready = qempty + NQ * 8, pready = sready + 16, odone = pready + 16, ofree = odone + 16,
-                         tmem = ofree + 16;
+                         over = ofree + 16, tmem = over + 16;
     static constexpr int okm = tmem + 16;                // 8 masks of valid pages, a tile each
     static constexpr int wild = okm + 8 * 4;             // 8 flags of units
-    static constexpr int scratch = wild + 8 * 4;
+    static constexpr int late = wild + 8 * 4;            // whether a wait ran out
+    static constexpr int scratch = late + 8;
     static constexpr int pre = scratch + 32 * 8;
     static constexpr int bytes(int n_req) { return pre + (n_req + 1) * 8; }
     static constexpr int COPIES = 3;                     // warps that copy
@@ -206,6 +207,7 @@ __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(Atte
     volatile int* const okm = reinterpret_cast<volatile int*>(sm + L::okm);
     // (a tile's mask, a unit's flag: the copies run fewer than 8 tiles ahead of the softmax)
     volatile int* const wilds = reinterpret_cast<volatile int*>(sm + L::wild);
+    volatile int* const late = reinterpret_cast<volatile int*>(sm + L::late);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int G = a.kv.group, H = a.kv.kv_heads;
 
@@ -240,7 +242,9 @@ __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(Atte
             mbar_init(sm0 + L::odone + w * 8, 1);
             mbar_init(sm0 + L::ofree + w * 8, 4);
         }
+        mbar_init(sm0 + L::over, 1);
         for (int u = 0; u < 8; ++u) wilds[u] = 0;
+        *late = 0;
         mbar_init_fence();
     }
     tc_before();
@@ -250,12 +254,14 @@ __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(Atte
 
     // A wait that runs out is recorded and ends its warp's part; the others' waits run
     // out after it (no warps meet at a barrier without a limit before the end), and all meet at
-    // the end, where tensor memory is freed.
+    // the end, where what is in flight is waited for and tensor memory is freed.
     auto wait = [&](uint32_t bar, int phase) -> bool {
         if (mbar_wait(bar, phase & 1)) return true;
         atomicOr(a.err, WORKER_TIMEOUT);
         return false;
     };
+    int filled = 0;  // places of the ring that a copying warp has filled
+    bool ok = true;  // no wait of this warp ran out
 
     if (warp >= 4 * MT + 1) {
         // ------------------------------------------------------------ copies
@@ -275,7 +281,6 @@ __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(Atte
         };
         int units = -1, waiting = 0;   // copies of 16 bytes a time that are not signalled yet: the oldest first,
         uint32_t slots = 0;            // 8 bits each, the slot + 1 or (queries) 128 + their set
-        bool ok = true;
         auto landed = [&]() {
             fence_async();
             __syncwarp();
@@ -411,6 +416,7 @@ __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(Atte
                     copied(128 | units % NQ);
                     drain();
                 }
+                ++filled;
             }
             C = N;
             page = page_next;
@@ -423,7 +429,6 @@ __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(Atte
             const bool leader = elected();
             Cursor N = C;  // the tile whose scores are formed next
             int scored = 0, units = -1, run0 = 0, run1 = 0, start0 = 0, start1 = 0;
-            bool ok = true;
             // scores of tile `scored` for row tile w, into place s
             auto scores = [&](int w, int s) {
                 const uint32_t k0 = operand_lo(sm0 + 2 * scored % NB * L::TILE, 0),
@@ -525,7 +530,6 @@ __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(Atte
         float m = -INFINITY, l = 0.0f;
         unsigned long long see = 0;
         int token = 0, units = -1, tile0 = 0, used[2] = {0, 0}, done = 0;
-        bool ok = true;
         for (int j = 0; j < n && ok; ++j) {
             const bool start = j == 0 || C.tile == 0, unit_ends = C.tile + 1 == C.c;
             const int rows = C.T * G - C.rt * RM - w * 128;
@@ -757,9 +761,24 @@ __global__ void __launch_bounds__(Many<D, MT>::WARPS * 32, 1) k_attend_many(Atte
             if (j + 1 < n) advance<KT, RM>(a, C, pre);
         }
     }
+    if (!ok) *late = 1;
     tc_before();
     __syncthreads();
     tc_after();
+    if (*late) {
+        // products, boxes, loads and stores of tensor memory may be in flight
+        if (warp == 4 * MT) {
+            if (elected()) tc_commit(sm0 + L::over);
+            __syncwarp();
+            wait(sm0 + L::over, 0);
+        } else if (warp > 4 * MT) {
+            for (int i = max(0, filled - NB); i < filled; ++i) wait(sm0 + L::full + i % NB * 8, i / NB);
+        } else {
+            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+            tmem_stored();
+        }
+        __syncthreads();
+    }
     if (warp == 0) tmem_free(tm, 512);
 }
 

@@ -77,7 +77,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, unsigned parity)
             unsigned long long now;
             asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
             if (!end) end = now + 1000000000ull;
-            else if (now > end) return false;
+            else if (now > end) return mbar_test(bar, parity);  // (the thread may have been off for longer)
         }
     }
 }
