@@ -237,6 +237,8 @@ class Worker:
             raise ValueError("eviction needs weight, pos and next_pos")
         if budget.dtype is not _I32 or budget.shape != (kv._n,) or not budget.is_contiguous():
             _fail("budget must be contiguous [requests]", ("budget", budget, _I32))
+        if not 0 <= recent < 1 << 31:
+            raise ValueError("recent must be at least 0 and fit in 32 bits")
         self._call("aladdin_worker_evict", C.byref(kv), kv._n, budget.data_ptr(), recent)
 
     def logprobs(self, logits, token=None, top=0):
@@ -252,6 +254,8 @@ class Worker:
         st = logits.stride()
         if (vocab > 1 and st[1] != 1) or (n > 1 and st[0] < vocab):
             raise ValueError("the rows of logits must be contiguous and share no memory")
+        if not 0 <= top < 1 << 31:
+            raise ValueError("top must be at least 0 and fit in 32 bits")
         dev, empty = self.device, torch.empty
         logprob = rank = ids = tops = None
         lp = rk = ip = tp = tk = None

@@ -64,3 +64,22 @@ def test_rows_of_the_page_table_keep_their_stride(W):
     for t in (table[:1].expand(4, -1), table[:1, :1].expand(4, 1), table.as_strided((4, 8), (7, 1))):
         with pytest.raises(ValueError, match="table"):
             W.make_kv(k, k.clone(), t, length)
+
+
+def test_numbers_that_32_bits_do_not_hold(W, worker):
+    """The library's arguments are 32-bit: others are refused, not cut down to what they hold."""
+    k, table, length = cache(4, 8)
+    zeros = lambda t: put(torch.zeros(6, 2, 16, dtype=t))
+    kv = W.make_kv(k, k.clone(), table, length, zeros(torch.float32), zeros(torch.int32), put(length.clone()))
+    worker.evict(kv, length, 2 ** 31 - 1)
+    assert worker.calls[-1][-1] == 2 ** 31 - 1
+    x = put(torch.zeros(2, 40))
+    worker.logprobs(x, None, 3)
+    assert len(worker.calls) == 2
+    for recent in (2 ** 31, 2 ** 32, 2 ** 40 + 7, -1):
+        with pytest.raises(ValueError, match="recent"):
+            worker.evict(kv, length, recent)
+    for top in (2 ** 32 + 3, 2 ** 31, -1):
+        with pytest.raises(ValueError, match="top"):
+            worker.logprobs(x[:0], None, top)
+    assert len(worker.calls) == 2
