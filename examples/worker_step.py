@@ -91,12 +91,13 @@ class ServingWorker:
         ints = lambda v: torch.tensor(v, dtype=torch.int32, device=dev)
         self.worker.accept(self.kv, tok, None, lse, ints(at), ints(path))
         if self.budget is not None:
-            self.worker.evict(self.kv, self.budget, recent=64)
+            self.worker.evict(self.kv, self.budget, self.recent)
         self.root = torch.tensor([g[0][-1] for g in gained], device=dev)
         return gained
 
-    def limit(self, budget):
-        self.budget = torch.full_like(self.length, budget)
+    def limit(self, budget, recent=64):
+        """From the next step on every request keeps ``budget`` tokens a head, the last ``recent`` ones among them."""
+        self.budget, self.recent = torch.full_like(self.length, budget), recent
 
 
 def iteration_ms(requests, context, repeat=5, **shape):
