@@ -557,7 +557,8 @@ typedef struct aladdin_worker_shape {
  * of k and v (strides positive multiples of 8, k and v 16-byte aligned).
  * weight and pos are [pages][kv_heads][page_tokens]: a slot's accumulated
  * attention weight and its token's position in the request. Pages may be shared
- * between requests where a call only reads them (aladdin_worker_attend). */
+ * between requests where a call only reads them (aladdin_worker_attend); the calls that write
+ * (aladdin_worker_accept, aladdin_worker_evict) do not look for it, and a slot of two requests is void after them. */
 typedef struct aladdin_kv {
     void* k;
     void* v;
@@ -608,7 +609,8 @@ int aladdin_worker_status(aladdin_worker* wk);
  * cached tokens, its ancestors and itself,
  *     s_j = scale q . k_j,  lse = log sum_j e^s_j,  out = sum_j e^(s_j - lse) v_j.
  * A row whose scores are all -inf has out = 0 and lse = -inf; what a token
- * does not see has no influence on it, not finite values either. One new token
+ * does not see has no influence on it, not finite values either. Scores and sums are 32-bit; the
+ * weights e^(s_j - m), m a maximum so far, are rounded to the cache's type before they meet the values. One new token
  * a request is plain decoding. out: [n_tok] rows of out_stride elements
  * (a multiple of 8), q_heads * head_dim of them written; lse [n_tok][q_heads]
  * (nullable). Reads k, v, table and len of kv. scale finite and > 0. */
@@ -632,7 +634,7 @@ int aladdin_worker_accept(aladdin_worker* wk, const aladdin_kv* kv, const aladdi
 
 /* Reduce the first n_req requests to at most budget[r] >= 0 cached tokens, per key
  * head: the slots of the largest weight stay, those of a position of at least
- * next[r] - recent before all others (a weight of NaN after all others), the
+ * next[r] - recent as of infinite weight (a weight of NaN after all others), the
  * lower slot first among equals. The slots from budget[r] on that stay move, in
  * order, into the slots before it that do not, with key, value, weight and
  * position; len[r] becomes budget[r]. Requests within their budget do not

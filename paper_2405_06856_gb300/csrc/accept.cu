@@ -395,7 +395,8 @@ cudaError_t launch_rows(const AcceptArgs& a, int sms, cudaStream_t st)
     return cudaGetLastError();
 }
 
-// 8 rows in registers where the mean rows of a request's key head fit them.
+// 8 rows in registers where the mean rows of a request's key head fit them (64 requests of about 1,500
+// tokens, 8 key heads of 128: 8 rows 59 us in registers and 66 in shared memory, 12 rows 92 and 68).
 template <typename T, int D>
 cudaError_t launch(const AcceptArgs& a, int sms, cudaStream_t st)
 {

@@ -45,8 +45,9 @@ __device__ __forceinline__ void enter(const AttendArgs& a, Cursor& u, int r)
 // The axis. A unit of c tiles takes `ov` + ceil(c / ct) places: `ov` stand for what a
 // unit costs beside its tiles (a worker whose range ends within them has no tile
 // of it), then ct tiles a place. Large calls count an overhead and single tiles;
-// calls that give every worker few tiles, places of several and no overhead: each
-// worker has one place then, and a request's results do not depend on the others.
+// calls that give every worker ct tiles on average or fewer, places of ct and no overhead. Where
+// those have no more places than workers, each worker has one at most, and the split of a
+// unit does not depend on the others; with more units of few tiles than workers it does.
 struct Axis {
     const int* pre;    // places of the requests before each, and of all
     const int* tiles;  // their tiles

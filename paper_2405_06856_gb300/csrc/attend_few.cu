@@ -445,7 +445,8 @@ cudaError_t launch_rows(const AttendArgs& a, int sms, cudaStream_t st)
 template <typename T, int D>
 cudaError_t launch(const AttendArgs& a, int sms, cudaStream_t st)
 {
-    // 8 rows where the mean rows of a request's key head fit them
+    // 8 rows where the mean rows of a request's key head fit them (64 requests of about 1,500 tokens, 8 key
+    // heads of 128: 8 rows 104 us with tiles of 8 and 111 of 16, 12 rows 145 and 121)
     if ((long long)a.tok.n_tok * a.kv.group <= 8ll * a.tok.n_req) return launch_rows<T, D, 1>(a, sms, st);
     return launch_rows<T, D, 2>(a, sms, st);
 }

@@ -22,7 +22,8 @@
 // flight. One CTA moves what it found itself; after clusters, whose requests differ
 // in length, a second kernel shares all moves evenly (the clusters' own moves
 // left most of the GPU to the longest request: 89 us for three requests of up to
-// 65,536 tokens instead of 72). One token over 1,024 on 64 requests of 8 heads takes 11 us.
+// 65,536 tokens; with the second kernel 69, 33 for the lists and 39 for the moves when each
+// runs alone). One token over 1,024 on 64 requests of 8 heads takes 13 us, 15 with the launch.
 #include <cooperative_groups.h>
 
 #include "worker_dev.cuh"
@@ -461,7 +462,9 @@ template <int D>
 cudaError_t launch_dim(const EvictArgs& a, int sms, cudaStream_t st)
 {
     // CTAs for a (request, head): as many as fill the GPU twice, at most the portable
-    // cluster, but few slots need no more than one
+    // cluster, but few slots need no more than one. (Shared memory and clusters follow the slots that
+    // the table has room for, as the host does not know the lengths: a wide table over short requests
+    // leaves fewer CTAs on an SM.)
     const long long units = (long long)a.n_req * a.kv.kv_heads;
     int cs = 1;
     while (cs < 8 && units * cs < 2ll * sms && a.kv.cap > 2048ll * cs) cs *= 2;
