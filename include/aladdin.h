@@ -662,6 +662,87 @@ int aladdin_worker_logprobs(aladdin_worker* wk, int32_t logits_dtype, int32_t n,
                             float* logprob, float* entropy, int32_t* rank, int32_t* top_id,
                             float* top_logprob);
 
+/* Rotary positions: the first dim channels of a head form pairs, HALF (c, c + dim / 2) or INTERLEAVED
+ * (2 c, 2 c + 1), c < dim / 2, and pair c of a token at position p becomes
+ *     scale (x cos t - y sin t, x sin t + y cos t),  t = p freq[c].
+ * turn[c] (device memory) is freq[c] in units of 2^-64 turns (aladdin_rope_turns): p turn[c] mod 2^64 is the
+ * angle of any position without loss. Channels from dim on stay as they are. */
+#define ALADDIN_ROPE_HALF 0
+#define ALADDIN_ROPE_INTERLEAVED 1
+typedef struct aladdin_rope {
+    int32_t dim;          /* even, 2 .. head_dim */
+    int32_t layout;
+    float scale;          /* finite, > 0 */
+    const uint64_t* turn; /* [dim / 2], 8-byte aligned */
+} aladdin_rope;
+
+/* Frequencies, in radians a position, for contexts longer than a model was made for. NONE: freq_c =
+ * base^(-2 c / dim). LINEAR: positions interpolated, freq_c / factor. BASE: a larger base, base factor^(dim / (dim - 2))
+ * (dim > 2). PARTS: pairs that turn fewer than slow times within original positions are interpolated, those of more
+ * than fast times are left, in between in proportion, and *scale = 0.1 ln(factor) + 1 (1 otherwise). Host function;
+ * base > 1, factor >= 1, original > 0, 0 < slow < fast, all finite. */
+#define ALADDIN_ROPE_NONE 0
+#define ALADDIN_ROPE_LINEAR 1
+#define ALADDIN_ROPE_BASE 2
+#define ALADDIN_ROPE_PARTS 3
+int aladdin_rope_frequencies(int32_t dim, double base, int32_t scaling, double factor, double original,
+                             double slow, double fast, double* freq, float* scale);
+
+/* turn[c] of n finite frequencies, on the host. */
+int aladdin_rope_turns(int32_t n, const double* freq, uint64_t* turn);
+
+/* Rotate the new tokens' queries and keys to their positions: pos[t] for token t where pos is given, else next[r]
+ * (0 where next is NULL) plus the token's depth in its request's tree (its index, for chains, which may have any
+ * number of tokens). q_out, k_out [n_tok]: rows of q_out_stride and k_out_stride elements (multiples of 8), heads and
+ * channels as in tok; each is NULL (not rotated), or tok's own array with its stride (in place), or memory apart from it.
+ * 32-bit products, rounded once; sines and cosines are good to 2^-23. tok->v is not read, nor are off
+ * and parent with pos. */
+int aladdin_worker_rotate(aladdin_worker* wk, const aladdin_rope* rope, const aladdin_tokens* tok,
+                          const int32_t* next, const int32_t* pos, void* q_out, int64_t q_out_stride,
+                          void* k_out, int64_t k_out_stride);
+
+/* Append tokens to the cache: those that acc_off and acc choose, as in aladdin_worker_accept (at most
+ * ALADDIN_TREE_MAX a request), or all new tokens (acc_off NULL), any number of them. The i-th takes slot len[r] + i
+ * and position next[r] + i (len[r] + i where next is NULL); its key is rotated to that position (rope NULL: copied),
+ * rounded once, its value copied, pos (nullable) receives the position, weight (nullable) 0, and len and next advance.
+ * tok->q and tok->parent are not read. Slots on a page outside the pool are not written (and recorded); a request
+ * without room for its tokens, or whose choice makes no sense, keeps none and is recorded. No slot may belong to
+ * two requests. */
+int aladdin_worker_append(aladdin_worker* wk, const aladdin_kv* kv, const aladdin_tokens* tok,
+                          const aladdin_rope* rope, const int32_t* acc_off, const int32_t* acc, int32_t n_acc);
+
+/* A paged KV cache of 8 bits: e4m3 codes (4 exponent and 3 fraction bits, no infinities), laid out as in aladdin_kv
+ * with strides in bytes (positive multiples of 16, k and v 16-byte aligned). The tokens [i block, (i + 1) block) of a
+ * page share a scale: value = code * k_scale[(page * kv_heads + head) * (page_tokens / block) + i], v_scale likewise. */
+typedef struct aladdin_kv8 {
+    void* k;
+    void* v;
+    int64_t page_stride, head_stride, token_stride;
+    int32_t pages;
+    int32_t table_width;
+    int64_t table_stride;
+    const int32_t* table;
+    int32_t* len;
+    int32_t* next;   /* nullable */
+    float* k_scale;
+    float* v_scale;
+    int32_t block;   /* tokens: 16, 32, 64, 128 or 256, at most page_tokens */
+} aladdin_kv8;
+
+/* aladdin_worker_append into a cache of 8 bits. A block's scale is the least power of two, 2^-126 at least, of which
+ * its largest finite value is 448 times at most; a block that holds tokens keeps its scale where that is
+ * larger, and where the new one is, its codes are rounded again (which changes only values below 2^-6 scales, with scales
+ * that are powers of two). Values are rounded once, from 32 bits; those that are not finite become NaN. */
+int aladdin_worker_append8(aladdin_worker* wk, const aladdin_kv8* kv, const aladdin_tokens* tok,
+                           const aladdin_rope* rope, const int32_t* acc_off, const int32_t* acc, int32_t n_acc);
+
+/* aladdin_worker_attend over a cache of 8 bits; the new tokens, of 16 bits, are not in it. Scores are 32-bit sums
+ * of exact products with the codes, times their scales; the weights meet the values' codes in 16 bits, half precision.
+ * Scales are >= 0; one that is not finite makes the rows of its request not finite. Reads k, v, table, len and
+ * the scales of kv. */
+int aladdin_worker_attend8(aladdin_worker* wk, const aladdin_kv8* kv, const aladdin_tokens* tok,
+                           float scale, void* out, int64_t out_stride, float* lse);
+
 #ifdef __cplusplus
 }
 #endif

@@ -28,6 +28,8 @@ NOALLOC_MAX_CAND = 32768
 BF16, F16, F32 = 0, 1, 2
 TREE_MAX, TOP_MAX = 64, 64
 WORKER_MAX_REQUESTS = 1024
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_NONE, ROPE_LINEAR, ROPE_BASE, ROPE_PARTS = 0, 1, 2, 3
 FLAG_KV, FLAG_TTFT, FLAG_ONGOING, FLAG_NEW, FEASIBLE, FLAG_INVALID = 1, 2, 4, 8, 15, 128
 NONE, INVALID = -1, -2
 
@@ -91,6 +93,17 @@ class aladdin_tokens(C.Structure):
                 ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64)]
 
 
+class aladdin_rope(C.Structure):
+    _fields_ = [("dim", C.c_int32), ("layout", C.c_int32), ("scale", C.c_float), ("turn", C.c_void_p)]
+
+
+class aladdin_kv8(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("token_stride", C.c_int64), ("pages", C.c_int32), ("table_width", C.c_int32),
+                ("table_stride", C.c_int64), ("table", C.c_void_p), ("len", C.c_void_p), ("next", C.c_void_p),
+                ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("block", C.c_int32)]
+
+
 _P = C.c_void_p
 _sig = {
     "aladdin_cluster_create": [_P, C.c_int32, _P, _P, _P, _P, _P, _P, _P, _P],
@@ -125,6 +138,13 @@ _sig = {
     "aladdin_worker_attend": [_P, _P, _P, C.c_float, _P, C.c_int64, _P],
     "aladdin_worker_accept": [_P, _P, _P, C.c_float, _P, _P, _P, C.c_int32],
     "aladdin_worker_evict": [_P, _P, C.c_int32, _P, C.c_int32],
+    "aladdin_rope_frequencies": [C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_double, C.c_double, C.c_double,
+                                 _P, _P],
+    "aladdin_rope_turns": [C.c_int32, _P, _P],
+    "aladdin_worker_rotate": [_P, _P, _P, _P, _P, _P, C.c_int64, _P, C.c_int64],
+    "aladdin_worker_append": [_P, _P, _P, _P, _P, _P, C.c_int32],
+    "aladdin_worker_append8": [_P, _P, _P, _P, _P, _P, C.c_int32],
+    "aladdin_worker_attend8": [_P, _P, _P, C.c_float, _P, C.c_int64, _P],
     "aladdin_worker_logprobs": [_P, C.c_int32, C.c_int32, C.c_int32, _P, C.c_int64, _P, C.c_int32,
                                 _P, _P, _P, _P, _P],
 }
@@ -490,7 +510,7 @@ class Cluster:
 
 # ---------------------------------------------------------------------------
 # A worker's decode step: the C ABI, one function each (the wrapper over torch
-# tensors, Worker with make_kv and make_tokens, is in worker.py).
+# tensors, Worker with make_kv, make_kv8, make_tokens and make_rope, is in worker.py).
 
 def aladdin_worker_create(shape, stream=None):
     h = C.c_void_p()
@@ -517,6 +537,46 @@ def aladdin_worker_accept(wk, kv, tok, scale, lse, acc_off, acc, n_acc):
                                       _ptr(acc_off), _ptr(acc), n_acc), "aladdin_worker_accept")
 
 
+def aladdin_rope_frequencies(dim, base=10000.0, scaling=ROPE_NONE, factor=1.0, original=0.0, slow=1.0, fast=32.0):
+    """(frequencies in radians a position, float64 [dim / 2]; factor of the rotated channels)."""
+    freq, scale = np.empty(max(0, int(dim) // 2)), C.c_float()
+    _check(_lib.aladdin_rope_frequencies(int(dim), base, int(scaling), factor, original, slow, fast,
+                                         _ptr(freq), C.byref(scale)), "aladdin_rope_frequencies")
+    return freq, scale.value
+
+
+def aladdin_rope_turns(freq):
+    """Frequencies in units of 2^-64 turns, uint64."""
+    freq = np.ascontiguousarray(freq, np.float64)
+    turn = np.empty(freq.shape, np.uint64)
+    _check(_lib.aladdin_rope_turns(freq.size, _ptr(freq), _ptr(turn)), "aladdin_rope_turns")
+    return turn
+
+
+def aladdin_worker_rotate(wk, rope, tok, next_pos, pos, q_out, q_out_stride, k_out, k_out_stride):
+    """q_out, k_out: device addresses (their rows q_out_stride and k_out_stride elements apart) or None."""
+    _check(_lib.aladdin_worker_rotate(wk, C.byref(rope), C.byref(tok), _ptr(next_pos), _ptr(pos), q_out,
+                                      q_out_stride, k_out, k_out_stride), "aladdin_worker_rotate")
+
+
+def aladdin_worker_append(wk, kv, tok, rope, acc_off, acc, n_acc):
+    """rope: an aladdin_rope or None."""
+    _check(_lib.aladdin_worker_append(wk, C.byref(kv), C.byref(tok), None if rope is None else C.byref(rope),
+                                      _ptr(acc_off), _ptr(acc), n_acc), "aladdin_worker_append")
+
+
+def aladdin_worker_append8(wk, kv, tok, rope, acc_off, acc, n_acc):
+    """kv: an aladdin_kv8; rope: an aladdin_rope or None."""
+    _check(_lib.aladdin_worker_append8(wk, C.byref(kv), C.byref(tok), None if rope is None else C.byref(rope),
+                                       _ptr(acc_off), _ptr(acc), n_acc), "aladdin_worker_append8")
+
+
+def aladdin_worker_attend8(wk, kv, tok, scale, out, out_stride, lse):
+    """kv: an aladdin_kv8; out: a device address (its rows out_stride elements apart)."""
+    _check(_lib.aladdin_worker_attend8(wk, C.byref(kv), C.byref(tok), scale, out, out_stride,
+                                       _ptr(lse)), "aladdin_worker_attend8")
+
+
 def aladdin_worker_evict(wk, kv, n_req, budget, recent):
     _check(_lib.aladdin_worker_evict(wk, C.byref(kv), n_req, _ptr(budget), int(recent)),
            "aladdin_worker_evict")
@@ -532,9 +592,10 @@ def aladdin_worker_logprobs(wk, dtype, n, vocab, logits, stride, token, top, log
 
 def __getattr__(name):
     """The wrapper over torch tensors, imported (and torch with it) when it is first used."""
-    if name in ("Worker", "make_kv", "make_tokens"):
+    names = ("Worker", "make_kv", "make_kv8", "make_rope", "make_tokens")
+    if name in names:
         from . import worker
-        for x in ("Worker", "make_kv", "make_tokens"):
+        for x in names:
             globals()[x] = getattr(worker, x)
         return globals()[name]
     raise AttributeError("module %r has no attribute %r" % (__name__, name))

@@ -31,14 +31,21 @@ struct Cursor {
     int c, nrt;           // key tiles, row tiles
 };
 
-template <int KT, int RM>
+// Key tiles of a row tile: KT keys each, cached then new; TN: new tokens begin a tile of their own, TN to a tile.
+template <int KT, int TN>
+__device__ __forceinline__ int key_tiles(int len, int T)
+{
+    return TN ? (len + KT - 1) / KT + (T + (TN ? TN : 1) - 1) / (TN ? TN : 1) : (len + T + KT - 1) / KT;
+}
+
+template <int KT, int RM, int TN = 0>
 __device__ __forceinline__ void enter(const AttendArgs& a, Cursor& u, int r)
 {
     u.r = r;
     u.lo = a.tok.off[r];
     u.T = a.tok.off[r + 1] - u.lo;
     u.len = a.kv.len[r];
-    u.c = (u.len + u.T + KT - 1) / KT;
+    u.c = key_tiles<KT, TN>(u.len, u.T);
     u.nrt = (u.T * a.kv.group + RM - 1) / RM;
 }
 
@@ -106,7 +113,7 @@ __device__ __forceinline__ bool plan(int n, Axis& x, int* pre, int* tiles, long 
 
 // The attention's requests: units of a key head's row tiles. A request whose offsets or
 // length make no sense has none and is recorded.
-template <int KT, int RM>
+template <int KT, int RM, int TN = 0>
 __device__ __forceinline__ int attend_units(const AttendArgs& a, int r, int& c)
 {
     const int lo = a.tok.off[r], hi = a.tok.off[r + 1], len = a.kv.len[r];
@@ -115,16 +122,16 @@ __device__ __forceinline__ int attend_units(const AttendArgs& a, int r, int& c)
         c = 0;
         return 0;
     }
-    c = (len + hi - lo + KT - 1) / KT;
+    c = key_tiles<KT, TN>(len, hi - lo);
     return ((hi - lo) * a.kv.group + RM - 1) / RM * a.kv.kv_heads;
 }
 
 // The cursor at place x < total; returns the tiles in front of it.
-template <int KT, int RM>
+template <int KT, int RM, int TN = 0>
 __device__ __forceinline__ int locate(const AttendArgs& a, const Axis& ax, Cursor& u, int x)
 {
     const int r = plan_find(ax.pre, a.tok.n_req, x);
-    enter<KT, RM>(a, u, r);
+    enter<KT, RM, TN>(a, u, r);
     const int n = ax.places(u.c), y = x - ax.pre[r], unit = y / n;
     u.tile = ax.tile_at(y - unit * n);
     u.h = unit / u.nrt;
@@ -133,16 +140,16 @@ __device__ __forceinline__ int locate(const AttendArgs& a, const Axis& ax, Curso
 }
 
 // Worker i's first tile under u; returns the number of its tiles.
-template <int KT, int RM>
+template <int KT, int RM, int TN = 0>
 __device__ __forceinline__ int range(const AttendArgs& a, const Axis& ax, Cursor& u, int i)
 {
     const int end = ax.begin(i + 1);
-    const int t1 = end < ax.total ? locate<KT, RM>(a, ax, u, end) : ax.tiles[a.tok.n_req];
-    return t1 - locate<KT, RM>(a, ax, u, ax.begin(i));
+    const int t1 = end < ax.total ? locate<KT, RM, TN>(a, ax, u, end) : ax.tiles[a.tok.n_req];
+    return t1 - locate<KT, RM, TN>(a, ax, u, ax.begin(i));
 }
 
 // To the next tile; pre[r] == pre[r + 1] for requests without tiles.
-template <int KT, int RM>
+template <int KT, int RM, int TN = 0>
 __device__ __forceinline__ void advance(const AttendArgs& a, Cursor& u, const int* pre)
 {
     if (++u.tile < u.c) return;
@@ -153,7 +160,7 @@ __device__ __forceinline__ void advance(const AttendArgs& a, Cursor& u, const in
     u.h = 0;
     int r = u.r + 1;
     while (r < a.tok.n_req && pre[r + 1] == pre[r]) ++r;
-    if (r < a.tok.n_req) enter<KT, RM>(a, u, r);
+    if (r < a.tok.n_req) enter<KT, RM, TN>(a, u, r);
 }
 
 // The tokens that token t of the request under u sees, itself among them. A parent

@@ -1,0 +1,541 @@
+// aladdin_worker_attend8 where the rows of a (request, key head) are few. See attend8.cuh for the operator.
+//
+// Every cached byte is read once and next to nothing is computed with it: what counts is bytes in flight
+// and few instructions a byte. As in the attention over 16 bits, every warp works alone on a range of the axis of
+// all key tiles, with a few tiles of shared memory that it fills by asynchronous copies ahead, and the products
+// are formed transposed: keys by rows, then channels by rows, 8 rows an operand. The codes become half-precision operands
+// in registers, one conversion for two values. No lane needs another one's codes:
+//   scores    the index that is summed over, the channels, may be taken in any order, the same for both operands:
+//             a lane takes runs of 4 channels, so that the two halves of a word are the pairs that it needs;
+//   results   a lane takes the same channels of the tile's keys 2t, 2t + 1, 2t + 8, 2t + 9 and interleaves the bytes
+//             of two keys; which of its channels stands for which row of the operand is its own choice again, so that
+//             a lane ends with runs of channels of two rows and writes them as they are.
+// Chunks of 16 bytes are exchanged within a tile so that the loads of both meet different banks.
+//
+// New tokens have tiles of their own, 16 bits wide. Their scores are matrix products in the worker's type; their values,
+// few a row, are added in 32 bits one by one, which leaves out what a row does not see even where it is
+// not finite.
+#include "attend8.cuh"
+
+namespace aladdin {
+namespace wk {
+namespace {
+
+template <int D, int NB>
+struct Few8 {
+    static constexpr int TK = D == 64 ? 32 : 16;                      // cached keys of a tile
+    static constexpr int TN = TK / 2;                                 // new keys of a tile
+    static constexpr int WARPS = D == 256 ? 8 : NB == 2 && D == 128 ? 12 : 16;  // of a CTA, one CTA an SM
+    static constexpr int S = 3;                                       // tiles of a warp
+    static constexpr int TILE = 2 * TK * D;                           // keys, then values
+    static constexpr int SLOT = TILE + 16;                            // and the scales of 16 keys each, then of 16 values
+    static constexpr unsigned FULL = TK == 32 ? 0xffffffffu : 0xffffu;
+    static constexpr int oks = WARPS * S * SLOT;                      // masks of tiles
+    static constexpr int scratch = (oks + WARPS * S * 4 + 7) / 8 * 8;
+    static constexpr int pre = scratch + 32 * 8;
+    static constexpr int bytes(int n_req) { return pre + (n_req + 1) * 8; }
+
+    // byte of chunk c (16 bytes) of a tile's row, keys and values
+    static __device__ __forceinline__ int key_at(int row, int c)
+    {
+        return row * D + (D % 128 == 0 ? c ^ (row & 1) << 2 : c) * 16;
+    }
+    static __device__ __forceinline__ int value_at(int row, int c)
+    {
+        if (D == 64) return (row >> 1) * 128 + (((row & 1) * 4 + c) ^ (row >> 1 & 3) << 1) * 16;
+        return row * D + (D % 128 == 0 ? c ^ (row >> 1 & 3) << 1 : c) * 16;
+    }
+    // first of the 4 channels that lane t of 4 has in the x-th product of 16 channels
+    static __device__ __forceinline__ int key_channel(int x, int t)
+    {
+        return D == 96 ? 32 * (x / 2) + 8 * t + 4 * (x % 2) : 64 * (x / 4) + 16 * t + 4 * (x % 4);
+    }
+    // first of the 4 channels of the w-th word that lane g of 8 has of a value
+    static __device__ __forceinline__ int value_channel(int w, int g)
+    {
+        if (D == 96) return 32 * w + 4 * g;
+        if (D == 64) return 8 * g + 4 * w;
+        return 128 * (w / 4) + 16 * g + 4 * (w % 4);
+    }
+};
+
+// Keys of a place in calls that give every warp few tiles, and what a unit costs beside
+// its tiles, in keys.
+constexpr int PLACE_KEYS = 64, UNIT_KEYS = 32;
+
+// The results from now on in units of 2^to.
+template <int MO, int NB>
+__device__ __forceinline__ void rebase(float (&o)[MO][NB][4], float& ref, float to)
+{
+    const float f = ex2(ref - to);
+#pragma unroll
+    for (int x = 0; x < MO; ++x)
+#pragma unroll
+        for (int y = 0; y < NB; ++y)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[x][y][e] *= f;
+    ref = to;
+}
+
+// NB: blocks of 8 rows.
+template <typename T, int D, int NB>
+__global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Attend8Args a)
+{
+    constexpr int RM = NB * 8;
+    using L = Few8<D, NB>;
+    constexpr int TK = L::TK, TN = L::TN, S = L::S, NT = L::WARPS * 32;
+    constexpr int KB = TK / 16, MO = D / 16, NW = D / 32;  // blocks of 16 keys, of 16 channels; words of a value a lane
+    extern __shared__ __align__(128) char sm[];
+    int* const pre = reinterpret_cast<int*>(sm + L::pre);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int G = a.kv.group, H = a.kv.kv_heads;
+    char* const tiles = sm + warp * S * L::SLOT;
+    const uint32_t tiles0 = smem_addr(tiles);
+    unsigned* const oks = reinterpret_cast<unsigned*>(sm + L::oks) + warp * S;
+
+    Axis ax;
+    if (!plan<NT>(a.tok.n_req, ax, pre, pre + a.tok.n_req + 1, reinterpret_cast<long long*>(sm + L::scratch),
+                  (int)gridDim.x * L::WARPS, UNIT_KEYS / TK, PLACE_KEYS / TK, a.err,
+                  [&](int r, int& c) { return attend_units<TK, RM, TN>(a, r, c); }))
+        return;
+    // neighbouring ranges lie on different SMs
+    const int me = warp * gridDim.x + blockIdx.x;
+    if (me >= ax.workers) return;
+    Cursor C, F;  // the tile computed, the tile fetched
+    const int n = range<TK, RM, TN>(a, ax, C, me);
+    F = C;
+    // the pages of the tile under F, 16 keys each, as the table has them
+    int page[KB];
+    auto pages = [&]() {
+#pragma unroll
+        for (int g = 0; g < KB; ++g) {
+            const int key = F.tile * TK + g * 16;
+            page[g] = key < F.len ? a.kv.table[(long long)F.r * a.kv.table_stride + (key >> a.kv.page_shift)] : 0;
+        }
+    };
+    pages();
+    // the tile under F into place b; then F goes on
+    auto fetch = [&](int b, bool more) {
+        const int key0 = F.tile * TK, own = F.len - key0;  // cached keys from the tile's start
+        const uint32_t d = tiles0 + b * L::SLOT;
+        if (own > 0) {
+            unsigned mask = 0;
+#pragma unroll
+            for (int g = 0; g < KB; ++g) {
+                if ((unsigned)page[g] < (unsigned)a.kv.pages) mask |= 0xffffu << (g * 16);
+                else if (lane == 0) atomicOr(a.err, WORKER_BAD_INPUT);
+            }
+            if (own < TK) mask &= (1u << own) - 1;
+            const long long head = (long long)F.h * a.kv.head_stride;
+            constexpr int CH = D / 16;
+#pragma unroll
+            for (int i = 0; i < TK * CH / 32; ++i) {
+                const int x = lane + i * 32, row = x / CH, ch = x - row * CH;
+                const bool ok = mask >> row & 1;
+                const int p = KB == 1 || row < 16 ? page[0] : page[KB - 1];
+                const long long e = ok ? p * a.kv.page_stride + head +
+                                             ((key0 + row) & (a.kv.page - 1)) * a.kv.token_stride + ch * 16
+                                       : 0;
+                // (weights of 0 meet the codes of rows that hold no key: zeros)
+                cp16(d + L::key_at(row, ch), a.kv.k + e, ok);
+                cp16(d + TK * D + L::value_at(row, ch), a.kv.v + e, ok);
+            }
+            if (lane < 2 * KB) {
+                const int g = lane % KB, p = KB == 1 || g == 0 ? page[0] : page[KB - 1];
+                const bool ok = mask >> (g * 16) & 1;
+                const long long e = ok ? ((long long)p * H + F.h) * a.scales.per_page +
+                                             (((key0 + g * 16) & (a.kv.page - 1)) >> a.scales.block_shift)
+                                       : 0;
+                cp4(d + L::TILE + lane * 4, (lane < KB ? a.scales.k : a.scales.v) + e, ok);
+            }
+            if (lane == 0) oks[b] = mask;
+        } else {
+            const int first = (F.tile - (F.len + TK - 1) / TK) * TN;
+            constexpr int CH = D / 8;
+#pragma unroll 2
+            for (int i = 0; i < TN * CH / 32; ++i) {
+                const int x = lane + i * 32, row = x / CH, ch = x - row * CH;
+                const bool ok = first + row < F.T;
+                const long long t = F.lo + (ok ? first + row : 0);
+                cp16(d + row * (D * 2) + ch * 16, a.tok.k + (t * a.tok.k_stride + F.h * D + ch * 8) * 2, ok);
+                cp16(d + TK * D + row * (D * 2) + ch * 16, a.tok.v + (t * a.tok.v_stride + F.h * D + ch * 8) * 2, ok);
+            }
+        }
+        if (more) {
+            advance<TK, RM, TN>(a, F, pre);
+            pages();
+        }
+    };
+#pragma unroll
+    for (int j = 0; j < S - 1; ++j) {
+        if (j < n) fetch(j, j + 1 < n);
+        cp_commit();
+    }
+
+    const int gq = lane >> 2, tq = lane & 3;
+    uint32_t qf[MO][NB][2];   // row gq of every block, in half precision
+    float factor[NB][2];      // of the scores of rows 2 tq, 2 tq + 1, to base 2
+    // this lane's channels of row gq of block y in the worker's type
+    auto query = [&](const Cursor& u, int y, int x) -> uint2 {
+        const int rho = u.rt * RM + y * 8 + gq;
+        if (rho >= u.T * G) return make_uint2(0u, 0u);
+        const int t = rho / G;
+        return __ldg(reinterpret_cast<const uint2*>(
+            a.tok.q + ((u.lo + t) * a.tok.q_stride + (long long)(u.h * G + rho - t * G) * D + L::key_channel(x, tq)) * 2));
+    };
+
+    float o[MO][NB][4], m[NB][2], l[NB][2];  // channels of rows 2 tq, 2 tq + 1
+    float ref = -INFINITY;                   // the results count in units of 2^ref
+    unsigned long long see[NB][2];
+    bool fresh = true;
+    int b = 0, tile0 = 0;  // a tile's place; the first tile of the unit that this warp has
+
+    for (int j = 0; j < n; ++j) {
+        __syncwarp();
+        if (j + S - 1 < n) fetch(b == 0 ? S - 1 : b - 1, j + S < n);
+        cp_commit();
+        const int rows = C.T * G - C.rt * RM;
+        if (fresh) {
+            fresh = false;
+            tile0 = C.tile;
+            ref = -INFINITY;
+#pragma unroll
+            for (int y = 0; y < NB; ++y) {
+#pragma unroll
+                for (int x = 0; x < MO; ++x) o[x][y][0] = o[x][y][1] = o[x][y][2] = o[x][y][3] = 0.0f;
+                m[y][0] = m[y][1] = -INFINITY;
+                l[y][0] = l[y][1] = 0.0f;
+                see[y][0] = see[y][1] = 1;
+                uint2 q[MO];
+#pragma unroll
+                for (int x = 0; x < MO; ++x) q[x] = query(C, y, x);
+                float back = half_row<T, MO>(q);
+#pragma unroll
+                for (int x = 0; x < MO; ++x) {
+                    qf[x][y][0] = q[x].x;
+                    qf[x][y][1] = q[x].y;
+                }
+                back *= a.scale_log2;
+                factor[y][0] = __shfl_sync(0xffffffffu, back, tq * 8);
+                factor[y][1] = __shfl_sync(0xffffffffu, back, tq * 8 + 4);
+            }
+            if (C.T > 1) {
+#pragma unroll
+                for (int y = 0; y < NB; ++y)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int rr = y * 8 + tq * 2 + e;
+                        see[y][e] = ancestors(a, C, rr < rows ? (C.rt * RM + rr) / G : 0);
+                    }
+            }
+        }
+        cp_wait<S - 1>();
+        __syncwarp();
+        const char* const slot = tiles + b * L::SLOT;
+        const bool cached = C.tile * TK < C.len;
+        const int first = cached ? 0 : (C.tile - (C.len + TK - 1) / TK) * TN;  // the first new token
+
+        float s[KB][NB][4];  // keys gq, gq + 8 of a block by rows 2 tq, 2 tq + 1
+        float lv[KB];        // logarithms of the blocks' scales of values, relative to ref
+#pragma unroll
+        for (int x = 0; x < KB; ++x)
+#pragma unroll
+            for (int y = 0; y < NB; ++y) s[x][y][0] = s[x][y][1] = s[x][y][2] = s[x][y][3] = 0.0f;
+        if (cached) {
+            const unsigned okm = oks[b];
+            const float* const scales = reinterpret_cast<const float*>(slot + L::TILE);
+#pragma unroll
+            for (int x = 0; x < KB; ++x) {
+                constexpr int CW = D == 96 ? 2 : 4;  // words of a load
+#pragma unroll
+                for (int i = 0; i < MO / CW; ++i) {
+                    uint32_t w[2][CW];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int row = x * 16 + e * 8 + gq;
+                        if constexpr (D == 96) {
+                            const uint2 v = *reinterpret_cast<const uint2*>(slot + row * D + i * 32 + tq * 8);
+                            w[e][0] = v.x, w[e][1] = v.y;
+                        } else {
+                            const uint4 v = *reinterpret_cast<const uint4*>(slot + L::key_at(row, i * 4 + tq));
+                            w[e][0] = v.x, w[e][1] = v.y, w[e][2] = v.z, w[e][3] = v.w;
+                        }
+                    }
+#pragma unroll
+                    for (int c = 0; c < CW; ++c) {
+                        const uint32_t f[4] = {half2_lo(w[0][c]), half2_lo(w[1][c]), half2_hi(w[0][c]), half2_hi(w[1][c])};
+#pragma unroll
+                        for (int y = 0; y < NB; ++y)
+                            Num<__half>::mma(s[x][y], f, qf[i * CW + c][y][0], qf[i * CW + c][y][1]);
+                    }
+                }
+                const float ks = scales[x];
+#pragma unroll
+                for (int y = 0; y < NB; ++y) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        s[x][y][e] *= ks * factor[y][e & 1];
+                        if (okm != L::FULL && !(okm >> (x * 16 + (e >> 1) * 8 + gq) & 1)) s[x][y][e] = -INFINITY;
+                    }
+                }
+            }
+            // the reference follows scales that are more than 2^4 times it
+            float grown = ref;
+#pragma unroll
+            for (int x = 0; x < KB; ++x) {
+                lv[x] = log_scale(okm >> (x * 16) & 1 ? scales[KB + x] : 0.0f);
+                if (lv[x] > grown + 4.0f) grown = lv[x];
+            }
+            if (grown > ref) rebase<MO, NB>(o, ref, grown);
+#pragma unroll
+            for (int x = 0; x < KB; ++x) lv[x] = relative(lv[x], ref);
+        } else {
+            // 8 new keys in the place of 16
+#pragma unroll
+            for (int x = 0; x < KB; ++x) {
+                lv[x] = 0.0f;
+#pragma unroll 4
+                for (int i = 0; i < MO; ++i) {
+                    const uint2 v = *reinterpret_cast<const uint2*>(slot + (x * 8 + gq) * (D * 2) + L::key_channel(i, tq) * 2);
+                    const uint32_t f[4] = {v.x, 0u, v.y, 0u};
+#pragma unroll
+                    for (int y = 0; y < NB; ++y) {
+                        const uint2 q = query(C, y, i);
+                        Num<T>::mma(s[x][y], f, q.x, q.y);
+                    }
+                }
+                const int key = first + x * 8 + gq;
+#pragma unroll
+                for (int y = 0; y < NB; ++y) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        s[x][y][e] = key < C.T && (see[y][e] >> key & 1) ? s[x][y][e] * a.scale_log2 : -INFINITY;
+                        s[x][y][e + 2] = -INFINITY;
+                    }
+                }
+            }
+            if (0.0f > ref + 4.0f) rebase<MO, NB>(o, ref, 0.0f);
+        }
+
+        float top[NB][2];
+        bool higher = false;
+#pragma unroll
+        for (int y = 0; y < NB; ++y) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                top[y][e] = m[y][e];
+#pragma unroll
+                for (int x = 0; x < KB; ++x) top[y][e] = fmaxf(top[y][e], fmaxf(s[x][y][e], s[x][y][e + 2]));
+                higher = higher || top[y][e] > m[y][e];
+            }
+        }
+        if (__any_sync(0xffffffffu, higher)) {
+#pragma unroll
+            for (int y = 0; y < NB; ++y) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                    for (int x = 4; x < 32; x <<= 1)
+                        top[y][e] = fmaxf(top[y][e], __shfl_xor_sync(0xffffffffu, top[y][e], x));
+                    const float f = top[y][e] > m[y][e] ? ex2(m[y][e] - top[y][e]) : 1.0f;
+                    m[y][e] = top[y][e];
+                    l[y][e] *= f;
+#pragma unroll
+                    for (int x = 0; x < MO; ++x) {
+                        o[x][y][e] *= f;
+                        o[x][y][e + 2] *= f;
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < KB; ++x) {
+            const float back = ex2(-lv[x]);
+#pragma unroll
+            for (int y = 0; y < NB; ++y) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float base = (m[y][e] == -INFINITY ? 0.0f : m[y][e]) - lv[x];
+                    s[x][y][e] = ex2(s[x][y][e] - base);
+                    s[x][y][e + 2] = ex2(s[x][y][e + 2] - base);
+                    l[y][e] += (s[x][y][e] + s[x][y][e + 2]) * back;
+                }
+            }
+        }
+        if (cached) {
+#pragma unroll
+            for (int x = 0; x < KB; ++x) {
+                uint32_t p[NB][2];
+#pragma unroll
+                for (int y = 0; y < NB; ++y) {
+                    p[y][0] = transpose8(Num<__half>::pack(s[x][y][0], s[x][y][1]));
+                    p[y][1] = transpose8(Num<__half>::pack(s[x][y][2], s[x][y][3]));
+                }
+                constexpr int VW = D == 96 ? 1 : D == 64 ? 2 : 4;  // words of a load
+#pragma unroll
+                for (int i = 0; i < NW / VW; ++i) {
+                    uint32_t w[4][VW];  // keys 2 tq, 2 tq + 1, 2 tq + 8, 2 tq + 9
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int row = x * 16 + (e >> 1) * 8 + tq * 2 + (e & 1);
+                        const char* const v = slot + TK * D;
+                        if constexpr (D == 96) {
+                            w[e][0] = *reinterpret_cast<const uint32_t*>(v + row * D + i * 32 + gq * 4);
+                        } else if constexpr (D == 64) {
+                            const uint2 z = *reinterpret_cast<const uint2*>(v + L::value_at(row, gq >> 1) + (gq & 1) * 8);
+                            w[e][0] = z.x, w[e][1] = z.y;
+                        } else {
+                            const uint4 z = *reinterpret_cast<const uint4*>(v + L::value_at(row, i * 8 + gq));
+                            w[e][0] = z.x, w[e][1] = z.y, w[e][2] = z.z, w[e][3] = z.w;
+                        }
+                    }
+#pragma unroll
+                    for (int c = 0; c < VW; ++c) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            // channels 2 h, 2 h + 1 of the word, two keys side by side
+                            const uint32_t u = __byte_perm(w[0][c], w[1][c], h ? 0x7362 : 0x5140),
+                                           v = __byte_perm(w[2][c], w[3][c], h ? 0x7362 : 0x5140);
+                            const uint32_t f[4] = {half2_lo(u), half2_hi(u), half2_lo(v), half2_hi(v)};
+#pragma unroll
+                            for (int y = 0; y < NB; ++y)
+                                Num<__half>::mma(o[(i * VW + c) * 2 + h][y], f, p[y][0], p[y][1]);
+                        }
+                    }
+                }
+            }
+        } else {
+            const float unit = ex2(-ref);
+#pragma unroll
+            for (int x = 0; x < KB; ++x) {
+#pragma unroll 1
+                for (int k = 0; k < min(8, C.T - first - x * 8); ++k) {
+                    const char* const v = slot + TK * D + (x * 8 + k) * (D * 2);
+                    float p[NB][2];
+#pragma unroll
+                    for (int y = 0; y < NB; ++y)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) p[y][e] = __shfl_sync(0xffffffffu, s[x][y][e], k * 4 + tq) * unit;
+#pragma unroll
+                    for (int w = 0; w < NW; ++w) {
+                        const uint2 z = *reinterpret_cast<const uint2*>(v + L::value_channel(w, gq) * 2);
+                        const float2 z0 = Num<T>::unpack(z.x), z1 = Num<T>::unpack(z.y);
+#pragma unroll
+                        for (int y = 0; y < NB; ++y) {
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                if (p[y][e] != 0.0f) {
+                                    o[2 * w][y][e] += p[y][e] * z0.x;
+                                    o[2 * w][y][e + 2] += p[y][e] * z0.y;
+                                    o[2 * w + 1][y][e] += p[y][e] * z1.x;
+                                    o[2 * w + 1][y][e + 2] += p[y][e] * z1.y;
+                                }
+                            }
+                        }
+                    }
+                }
+            }
+        }
+
+        if (C.tile + 1 == C.c || j + 1 == n) {
+            const bool whole = tile0 == 0 && C.tile + 1 == C.c;
+            const int live = min(rows, RM);
+            float* const part = part_of<D, RM>(a, me, tile0 == 0 ? 1 : 0);
+            const float unit = ex2(ref);
+#pragma unroll
+            for (int y = 0; y < NB; ++y) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                    for (int x = 4; x < 32; x <<= 1) l[y][e] += __shfl_xor_sync(0xffffffffu, l[y][e], x);
+                    const float sum = l[y][e];
+                    const int rr = y * 8 + tq * 2 + e;
+                    if (rr < live) {
+                        if (!whole) {
+                            float* const d = part + RM * 2 + rr * D;
+#pragma unroll
+                            for (int w = 0; w < NW; ++w)
+                                *reinterpret_cast<float4*>(d + L::value_channel(w, gq)) =
+                                    make_float4(o[2 * w][y][e] * unit, o[2 * w][y][e + 2] * unit,
+                                                o[2 * w + 1][y][e] * unit, o[2 * w + 1][y][e + 2] * unit);
+                            if (gq == 0) *reinterpret_cast<float2*>(part + rr * 2) = make_float2(m[y][e], sum);
+                        } else {
+                            const int rho = C.rt * RM + rr, t = rho / G, head = C.h * G + rho - t * G;
+                            const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+                            char* const d = a.out + ((C.lo + t) * a.out_stride + (long long)head * D) * 2;
+#pragma unroll
+                            for (int w = 0; w < NW; ++w)
+                                *reinterpret_cast<uint2*>(d + L::value_channel(w, gq) * 2) =
+                                    make_uint2(Num<T>::pack(o[2 * w][y][e] * unit * inv, o[2 * w][y][e + 2] * unit * inv),
+                                               Num<T>::pack(o[2 * w + 1][y][e] * unit * inv, o[2 * w + 1][y][e + 2] * unit * inv));
+                            if (gq == 0 && a.lse) a.lse[(long long)(C.lo + t) * (H * G) + head] = (m[y][e] + log2f(sum)) * LN2;
+                        }
+                    }
+                }
+            }
+            if (!whole) {
+                int first_w, last_w;
+                ax.sharers(C, first_w, last_w);
+                __threadfence();
+                __syncwarp();
+                int arrived = 0;
+                if (lane == 0) arrived = atomicAdd(a.arrived + first_w, 1);
+                arrived = __shfl_sync(0xffffffffu, arrived, 0);
+                if (arrived == last_w - first_w) {
+                    if (lane == 0) a.arrived[first_w] = 0;
+                    __threadfence();
+                    join_rows<T, D, RM>(a, C, first_w, last_w, 0, live, 4, lane);
+                }
+            }
+            fresh = true;
+        }
+        if (j + 1 < n) advance<TK, RM, TN>(a, C, pre);
+        if (++b == S) b = 0;
+    }
+    cp_wait<0>();
+}
+
+template <typename T, int D, int NB>
+cudaError_t launch_rows(const Attend8Args& a, int sms, cudaStream_t st)
+{
+    using L = Few8<D, NB>;
+    constexpr int most = L::bytes(ALADDIN_WORKER_MAX_REQUESTS);
+    static_assert(most <= 227 * 1024 && L::WARPS <= ATTEND_WORKERS_PER_SM, "what a CTA has");
+    static_assert(L::WARPS * NB * 8 <= (D < 256 ? 256 : 128), "the partial results' room");
+    cudaError_t e = allow_smem<k_attend8_few<T, D, NB>>(most);
+    if (e != cudaSuccess) return e;
+    k_attend8_few<T, D, NB><<<sms, L::WARPS * 32, L::bytes(a.tok.n_req), st>>>(a);
+    return cudaGetLastError();
+}
+
+template <typename T, int D>
+cudaError_t launch(const Attend8Args& a, int sms, cudaStream_t st)
+{
+    if constexpr (D < 256) {
+        if ((long long)a.tok.n_tok * a.kv.group > 8ll * a.tok.n_req) return launch_rows<T, D, 2>(a, sms, st);
+    }
+    return launch_rows<T, D, 1>(a, sms, st);
+}
+
+template <typename T>
+cudaError_t launch_dim(const Attend8Args& a, int dim, int sms, cudaStream_t st)
+{
+    switch (dim) {
+        case 64: return launch<T, 64>(a, sms, st);
+        case 96: return launch<T, 96>(a, sms, st);
+        case 128: return launch<T, 128>(a, sms, st);
+        case 256: return launch<T, 256>(a, sms, st);
+    }
+    return cudaErrorInvalidValue;
+}
+
+}  // namespace
+}  // namespace wk
+
+cudaError_t launch_attend8(const Attend8Args& a, int dtype, int dim, int sms, cudaStream_t st)
+{
+    return dtype == ALADDIN_BF16 ? wk::launch_dim<__nv_bfloat16>(a, dim, sms, st)
+                                 : wk::launch_dim<__half>(a, dim, sms, st);
+}
+
+}  // namespace aladdin

@@ -1,0 +1,120 @@
+// Rotary positions on 8 channels at a time: shared by rotate.cu and append.cu.
+//
+// Pair c of a token at position p is turned by the angle p freq_c. The frequency comes in
+// turns, as a 64-bit fraction of one, so that p times it wraps around exactly and its upper
+// 32 bits are the angle to 2^-32 turns, however far the position is, without 64-bit floating point,
+// of which this GPU has little. The angle's distance x to the nearest quarter turn, at most pi / 4, goes
+// through the Taylor series of sine and cosine: what they leave out is x^11 / 11! < 2^-29 and x^10 / 10! < 2^-25.
+#pragma once
+
+#include "worker_dev.cuh"
+
+namespace aladdin {
+namespace wk {
+
+// What turns channels [8 ch, 8 ch + 8) of a head: the frequencies of their pairs.
+template <bool INTERLEAVED>
+struct Turns {
+    static constexpr int N = INTERLEAVED ? 4 : 8;
+    uint32_t hi[N], lo[N];
+
+    __device__ __forceinline__ void load(const RopeDev& rope, int ch)
+    {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int c = ch * 8 + j, p = INTERLEAVED ? ch * 4 + j : c < rope.half ? c : c - rope.half;
+            const unsigned long long t = p < rope.half ? __ldg(rope.turn + p) : 0;
+            hi[j] = (uint32_t)(t >> 32);
+            lo[j] = (uint32_t)t;
+        }
+    }
+    // cosine and sine of pair j at position p, times the factor
+    __device__ __forceinline__ void at(const RopeDev& rope, int p, int j, float& c, float& s) const
+    {
+        // the upper word of p (hi, lo), p signed
+        const uint32_t turn = (uint32_t)p * hi[j] + __umulhi((uint32_t)p, lo[j]) - (p < 0 ? lo[j] : 0u);
+        const uint32_t quarter = (turn + 0x20000000u) & 0xc0000000u;
+        const float x = (float)(int)(turn - quarter) * 1.46291807927e-9f;  // 2 pi / 2^32
+        const float x2 = x * x;
+        const float a = fmaf(x * x2, fmaf(x2, fmaf(x2, fmaf(x2, 1.0f / 362880, -1.0f / 5040), 1.0f / 120), -1.0f / 6), x);
+        const float b = fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, 1.0f / 40320, -1.0f / 720), 1.0f / 24), -0.5f), 1.0f);
+        // of 0, 1, 2, 3 quarters more: (b, a), (-a, b), (-b, -a), (a, -b)
+        const bool odd = quarter & 0x40000000u;
+        const float u = odd ? a : b, v = odd ? b : a;
+        c = __uint_as_float(__float_as_uint(u) ^ ((quarter + 0x40000000u) & 0x80000000u)) * rope.scale;
+        s = __uint_as_float(__float_as_uint(v) ^ (quarter & 0x80000000u)) * rope.scale;
+    }
+};
+
+// 8 values of 16 bits in 32
+template <typename T>
+__device__ __forceinline__ void widen(const uint4& v, float (&x)[8])
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = Num<T>::unpack(w[i]);
+        x[2 * i] = f.x;
+        x[2 * i + 1] = f.y;
+    }
+}
+template <typename T>
+__device__ __forceinline__ uint4 narrow(const float (&x)[8])
+{
+    return make_uint4(Num<T>::pack(x[0], x[1]), Num<T>::pack(x[2], x[3]), Num<T>::pack(x[4], x[5]),
+                      Num<T>::pack(x[6], x[7]));
+}
+
+// The partners of channels [8 ch, 8 ch + 8) in the half layout, from the head's row in global memory (16 bytes at a
+// time where the halves begin at multiples of 8 channels); anything for channels that are not turned.
+template <typename T>
+__device__ __forceinline__ uint4 partners(const RopeDev& rope, const char* row, int ch)
+{
+    const int h = rope.half, c0 = ch * 8;
+    if (c0 >= 2 * h) return make_uint4(0, 0, 0, 0);
+    if ((h & 7) == 0) return *reinterpret_cast<const uint4*>(row + (c0 < h ? c0 + h : c0 - h) * 2);
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t u[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int c = c0 + 2 * i + e, p = c < h ? c + h : c < 2 * h ? c - h : c;
+            u[e] = *reinterpret_cast<const unsigned short*>(row + p * 2);
+        }
+        w[i] = u[0] | u[1] << 16;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// x, channels [8 ch, 8 ch + 8) of a head, turned to position p; y: their partners (half layout).
+template <bool INTERLEAVED>
+__device__ __forceinline__ void turn(const RopeDev& rope, const Turns<INTERLEAVED>& t, int p, int ch, float (&x)[8],
+                                     const float (&y)[8])
+{
+    if constexpr (INTERLEAVED) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (ch * 4 + j < rope.half) {
+                float c, s;
+                t.at(rope, p, j, c, s);
+                const float a = x[2 * j], b = x[2 * j + 1];
+                x[2 * j] = a * c - b * s;
+                x[2 * j + 1] = a * s + b * c;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int at = ch * 8 + j;
+            if (at < 2 * rope.half) {
+                float c, s;
+                t.at(rope, p, j, c, s);
+                x[j] = x[j] * c + (at < rope.half ? -y[j] : y[j]) * s;
+            }
+        }
+    }
+}
+
+}  // namespace wk
+}  // namespace aladdin

@@ -1,6 +1,6 @@
 // C ABI of a worker's decode step (include/aladdin.h): the worker object, the
-// checks of its arguments and its workspaces. The kernels are in attend.cu,
-// accept.cu, evict.cu and logprobs.cu.
+// checks of its arguments and its workspaces. The kernels are in rotate.cu, attend*.cu,
+// append.cu, accept.cu, evict.cu and logprobs.cu.
 #include <cmath>
 #include <new>
 
@@ -114,6 +114,41 @@ int check_kv(const aladdin_worker* wk, const aladdin_kv* kv, KvDev* d)
     return ALADDIN_OK;
 }
 
+// A cache of 8 bits, whose strides count bytes.
+int check_kv8(const aladdin_worker* wk, const aladdin_kv8* kv, KvDev* d, ScaleDev* sc)
+{
+    if (!kv || !kv->k || !kv->v || !kv->table || !kv->len || !kv->k_scale || !kv->v_scale) return ALADDIN_ERR_ARG;
+    const aladdin_worker_shape& s = wk->shape;
+    const int b = kv->block;
+    if (!(b == 16 || b == 32 || b == 64 || b == 128 || b == 256) || b > s.page_tokens) return ALADDIN_ERR_ARG;
+    for (const int64_t st : {kv->page_stride, kv->head_stride, kv->token_stride})
+        if (st < 16 || st % 16) return ALADDIN_ERR_ARG;
+    // (checked as a cache of 16 bits but for the least stride of a token, whose unit differs)
+    const aladdin_kv k16 = {kv->k, kv->v, kv->page_stride, kv->head_stride, kv->token_stride, kv->pages, kv->table_width,
+                            kv->table_stride, kv->table, kv->len, nullptr, nullptr, kv->next};
+    if (!all_on_device(wk, {kv->k_scale, kv->v_scale}, 4)) return ALADDIN_ERR_ARG;
+    const int rc = check_kv(wk, &k16, d);
+    if (rc) return rc;
+    sc->k = kv->k_scale;
+    sc->v = kv->v_scale;
+    sc->block_shift = 0;
+    while ((1 << sc->block_shift) < b) ++sc->block_shift;
+    sc->per_page = s.page_tokens / b;
+    return ALADDIN_OK;
+}
+
+int check_rope(const aladdin_worker* wk, const aladdin_rope* r, RopeDev* d)
+{
+    if (!r || !r->turn || r->dim < 2 || r->dim % 2 || r->dim > wk->shape.head_dim) return ALADDIN_ERR_ARG;
+    if (r->layout != ALADDIN_ROPE_HALF && r->layout != ALADDIN_ROPE_INTERLEAVED) return ALADDIN_ERR_ARG;
+    if (!std::isfinite(r->scale) || r->scale <= 0.0f || !on_device(wk, r->turn, 8)) return ALADDIN_ERR_ARG;
+    d->turn = reinterpret_cast<const unsigned long long*>(r->turn);
+    d->half = r->dim / 2;
+    d->interleaved = r->layout == ALADDIN_ROPE_INTERLEAVED;
+    d->scale = r->scale;
+    return ALADDIN_OK;
+}
+
 int check_tokens(const aladdin_worker* wk, const aladdin_tokens* t, bool need_q, TokDev* d)
 {
     if (!t || t->n_req < 0 || t->n_req > ALADDIN_WORKER_MAX_REQUESTS || t->n_tok < 0) return ALADDIN_ERR_ARG;
@@ -136,6 +171,22 @@ int check_tokens(const aladdin_worker* wk, const aladdin_tokens* t, bool need_q,
     d->q_stride = t->q_stride;
     d->k_stride = t->k_stride;
     d->v_stride = t->v_stride;
+    return ALADDIN_OK;
+}
+
+// What both kinds of append share.
+int check_append(const aladdin_worker* wk, const aladdin_tokens* tok, const aladdin_rope* rope, const int32_t* acc_off,
+                 const int32_t* acc, int32_t n_acc, AppendArgs* a)
+{
+    int rc = check_tokens(wk, tok, false, &a->tok);
+    if (rc) return rc;
+    if (rope && (rc = check_rope(wk, rope, &a->rope))) return rc;
+    if (!acc_off != !acc || (acc_off && n_acc < 0) || !all_on_device(wk, {acc_off, acc}, 4)) return ALADDIN_ERR_ARG;
+    a->acc_off = acc_off;
+    a->acc = acc;
+    a->n_acc = acc_off ? n_acc : a->tok.n_tok;
+    a->arrived = wk->done;
+    a->err = wk->err;
     return ALADDIN_OK;
 }
 
@@ -266,6 +317,144 @@ try {
     return ALADDIN_OK;
 } catch (...) {
     return ALADDIN_ERR_NOMEM;
+}
+
+int aladdin_worker_attend8(aladdin_worker* wk, const aladdin_kv8* kv, const aladdin_tokens* tok, float scale,
+                           void* out, int64_t out_stride, float* lse)
+try {
+    if (!wk || !scale_ok(scale)) return ALADDIN_ERR_ARG;
+    Attend8Args a = {};
+    int rc = check_tokens(wk, tok, true, &a.tok);
+    if (rc) return rc;
+    if (a.tok.n_req == 0 || a.tok.n_tok == 0) return ALADDIN_OK;
+    if ((rc = check_kv8(wk, kv, &a.kv, &a.scales))) return rc;
+    if (!out || !stride_ok(out_stride, (int64_t)wk->shape.q_heads * wk->shape.head_dim) ||
+        !all_on_device(wk, {out}, 16) || !all_on_device(wk, {lse}, 4))
+        return ALADDIN_ERR_ARG;
+    CK(cudaSetDevice(wk->device));
+    a.scale_log2 = (float)(scale * LOG2E_D);
+    a.out = static_cast<char*>(out);
+    a.out_stride = out_stride;
+    a.lse = lse;
+    a.part = wk->part;
+    a.arrived = wk->arrived;
+    a.err = wk->err;
+    CK(launch_attend8(a, wk->shape.dtype, wk->shape.head_dim, wk->sms, wk->st));
+    return ALADDIN_OK;
+} catch (...) {
+    return ALADDIN_ERR_NOMEM;
+}
+
+int aladdin_worker_rotate(aladdin_worker* wk, const aladdin_rope* rope, const aladdin_tokens* tok, const int32_t* next,
+                          const int32_t* pos, void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride)
+try {
+    if (!wk || !tok) return ALADDIN_ERR_ARG;
+    RotateArgs a = {};
+    const aladdin_worker_shape& s = wk->shape;
+    aladdin_tokens t = *tok;  // (values are not read: the keys stand for them)
+    t.v = t.k;
+    t.v_stride = t.k_stride;
+    int rc = check_tokens(wk, &t, q_out != nullptr, &a.tok);
+    if (rc) return rc;
+    if ((rc = check_rope(wk, rope, &a.rope))) return rc;
+    if (a.tok.n_req == 0 || a.tok.n_tok == 0) return ALADDIN_OK;
+    const auto out_ok = [&](const void* out, int64_t stride, const void* in, int64_t in_stride, int heads) {
+        return !out || (stride_ok(stride, (int64_t)heads * s.head_dim) && on_device(wk, out, 16) &&
+                        (out != in || stride == in_stride));
+    };
+    if (!out_ok(q_out, q_out_stride, tok->q, tok->q_stride, s.q_heads) ||
+        !out_ok(k_out, k_out_stride, tok->k, tok->k_stride, s.kv_heads) || !all_on_device(wk, {next, pos}, 4))
+        return ALADDIN_ERR_ARG;
+    if (!q_out && !k_out) return ALADDIN_OK;
+    CK(cudaSetDevice(wk->device));
+    a.q_heads = s.q_heads;
+    a.kv_heads = s.kv_heads;
+    a.next = next;
+    a.pos = pos;
+    a.q_out = static_cast<char*>(q_out);
+    a.k_out = static_cast<char*>(k_out);
+    a.q_out_stride = q_out_stride;
+    a.k_out_stride = k_out_stride;
+    a.err = wk->err;
+    CK(launch_rotate(a, s.dtype, s.head_dim, wk->sms, wk->st));
+    return ALADDIN_OK;
+} catch (...) {
+    return ALADDIN_ERR_NOMEM;
+}
+
+int aladdin_worker_append(aladdin_worker* wk, const aladdin_kv* kv, const aladdin_tokens* tok, const aladdin_rope* rope,
+                          const int32_t* acc_off, const int32_t* acc, int32_t n_acc)
+try {
+    if (!wk || !kv) return ALADDIN_ERR_ARG;
+    AppendArgs a = {};
+    int rc = check_append(wk, tok, rope, acc_off, acc, n_acc, &a);
+    if (rc) return rc;
+    if (a.tok.n_req == 0 || a.tok.n_tok == 0) return ALADDIN_OK;
+    if ((rc = check_kv(wk, kv, &a.kv))) return rc;
+    if (a.n_acc == 0) return ALADDIN_OK;
+    CK(cudaSetDevice(wk->device));
+    CK(launch_append(a, wk->shape.dtype, wk->shape.head_dim, wk->sms, wk->st));
+    return ALADDIN_OK;
+} catch (...) {
+    return ALADDIN_ERR_NOMEM;
+}
+
+int aladdin_worker_append8(aladdin_worker* wk, const aladdin_kv8* kv, const aladdin_tokens* tok,
+                           const aladdin_rope* rope, const int32_t* acc_off, const int32_t* acc, int32_t n_acc)
+try {
+    if (!wk || !kv) return ALADDIN_ERR_ARG;
+    AppendArgs a = {};
+    int rc = check_append(wk, tok, rope, acc_off, acc, n_acc, &a);
+    if (rc) return rc;
+    if (a.tok.n_req == 0 || a.tok.n_tok == 0) return ALADDIN_OK;
+    if ((rc = check_kv8(wk, kv, &a.kv, &a.scales))) return rc;
+    if (a.n_acc == 0) return ALADDIN_OK;
+    CK(cudaSetDevice(wk->device));
+    CK(launch_append(a, wk->shape.dtype, wk->shape.head_dim, wk->sms, wk->st));
+    return ALADDIN_OK;
+} catch (...) {
+    return ALADDIN_ERR_NOMEM;
+}
+
+int aladdin_rope_frequencies(int32_t dim, double base, int32_t scaling, double factor, double original, double slow,
+                             double fast, double* freq, float* scale)
+{
+    if (!freq || !scale || dim < 2 || dim % 2 || !std::isfinite(base) || base <= 1.0) return ALADDIN_ERR_ARG;
+    if (scaling < ALADDIN_ROPE_NONE || scaling > ALADDIN_ROPE_PARTS) return ALADDIN_ERR_ARG;
+    if (scaling != ALADDIN_ROPE_NONE && (!std::isfinite(factor) || factor < 1.0)) return ALADDIN_ERR_ARG;
+    if (scaling == ALADDIN_ROPE_BASE && dim == 2) return ALADDIN_ERR_ARG;
+    if (scaling == ALADDIN_ROPE_PARTS && (!std::isfinite(original) || original <= 0.0 || !std::isfinite(slow) ||
+                                          !std::isfinite(fast) || slow <= 0.0 || fast <= slow))
+        return ALADDIN_ERR_ARG;
+    if (scaling == ALADDIN_ROPE_BASE) {
+        base *= std::pow(factor, (double)dim / (dim - 2));
+        if (!std::isfinite(base)) return ALADDIN_ERR_ARG;
+    }
+    *scale = 1.0f;
+    for (int c = 0; c < dim / 2; ++c) {
+        double f = std::pow(base, -2.0 * c / dim);
+        if (scaling == ALADDIN_ROPE_LINEAR) f /= factor;
+        if (scaling == ALADDIN_ROPE_PARTS) {
+            double whole = (original * f / (2.0 * M_PI) - slow) / (fast - slow);
+            whole = whole < 0.0 ? 0.0 : whole > 1.0 ? 1.0 : whole;
+            f = f * whole + f / factor * (1.0 - whole);
+        }
+        freq[c] = f;
+    }
+    if (scaling == ALADDIN_ROPE_PARTS) *scale = (float)(0.1 * std::log(factor) + 1.0);
+    return ALADDIN_OK;
+}
+
+int aladdin_rope_turns(int32_t n, const double* freq, uint64_t* turn)
+{
+    if (n < 0 || (n > 0 && (!freq || !turn))) return ALADDIN_ERR_ARG;
+    for (int i = 0; i < n; ++i)
+        if (!std::isfinite(freq[i])) return ALADDIN_ERR_ARG;
+    for (int i = 0; i < n; ++i) {
+        const double t = freq[i] / (2.0 * M_PI), part = t - std::floor(t);  // (1 where t is barely below 0)
+        turn[i] = part < 1.0 ? (uint64_t)std::ldexp(part, 64) : 0;
+    }
+    return ALADDIN_OK;
 }
 
 int aladdin_worker_evict(aladdin_worker* wk, const aladdin_kv* kv, int32_t n_req, const int32_t* budget,

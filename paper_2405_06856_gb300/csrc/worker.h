@@ -55,6 +55,22 @@ struct TokDev {
     long long q_stride, k_stride, v_stride;  // elements from token to token
 };
 
+// Rotary positions as the kernels see them; half 0: none.
+struct RopeDev {
+    const unsigned long long* turn;
+    int half;               // pairs
+    bool interleaved;
+    float scale;
+};
+
+// Scales of a cache of 8 bits, whose strides (KvDev) count bytes.
+struct ScaleDev {
+    float* k;
+    float* v;
+    int block_shift;        // tokens of a block
+    int per_page;           // blocks of a page
+};
+
 // Bits of a worker's error word.
 constexpr unsigned WORKER_BAD_INPUT = 1u;
 constexpr unsigned WORKER_TIMEOUT = 4u;  // a wait for a copy ran out
@@ -98,6 +114,34 @@ struct EvictArgs {
     unsigned* err;
 };
 
+struct Attend8Args : AttendArgs {
+    ScaleDev scales;
+};
+
+struct RotateArgs {
+    TokDev tok;
+    RopeDev rope;
+    int q_heads, kv_heads;
+    const int32_t* next;
+    const int32_t* pos;
+    char* q_out;
+    char* k_out;
+    long long q_out_stride, k_out_stride;  // elements from token to token
+    unsigned* err;
+};
+
+struct AppendArgs {
+    KvDev kv;
+    TokDev tok;
+    RopeDev rope;
+    const int32_t* acc_off;
+    const int32_t* acc;
+    int n_acc;
+    int* arrived;           // finished CTAs, zero between calls
+    unsigned* err;
+    ScaleDev scales;        // k null: a cache of 16 bits
+};
+
 struct LogprobArgs {
     int n, vocab, top;
     const char* x;
@@ -113,8 +157,8 @@ struct LogprobArgs {
 
 // Workers of an attention launch on one SM, at most (warps, or a CTA's row tiles), and
 // the bytes of AttendArgs::part: two units of each SM's CTA of at most 256 rows (128
-// of 256 channels), or of at most 8 warps of 16 rows.
-constexpr int ATTEND_WORKERS_PER_SM = 8;
+// of 256 channels), or of its warps of at most as many rows in all.
+constexpr int ATTEND_WORKERS_PER_SM = 16;
 inline size_t attend_part_bytes(int sms, int dim)
 {
     return (size_t)sms * 2 * (dim < 256 ? 256 : 128) * (dim + 2) * sizeof(float);
@@ -123,6 +167,9 @@ cudaError_t launch_attend_few(const AttendArgs& a, int dtype, int dim, int sms, 
 cudaError_t launch_attend_many(const AttendArgs& a, int dtype, int dim, int sms, cudaStream_t st);
 cudaError_t launch_attend(const AttendArgs& a, int dtype, int dim, int sms, cudaStream_t st);
 cudaError_t launch_accept(const AcceptArgs& a, int dtype, int dim, int sms, cudaStream_t st);
+cudaError_t launch_attend8(const Attend8Args& a, int dtype, int dim, int sms, cudaStream_t st);
+cudaError_t launch_rotate(const RotateArgs& a, int dtype, int dim, int sms, cudaStream_t st);
+cudaError_t launch_append(const AppendArgs& a, int dtype, int dim, int sms, cudaStream_t st);
 cudaError_t launch_evict(const EvictArgs& a, int sms, cudaStream_t st);
 cudaError_t launch_logprobs(const LogprobArgs& a, int dtype, int sms, cudaStream_t st);
 

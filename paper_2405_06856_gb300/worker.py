@@ -1,6 +1,6 @@
 """A worker's decode step over torch tensors: a thin layer on the C ABI's
 ``aladdin_worker_*`` calls (``include/aladdin.h``), reached as ``aladdin.Worker``,
-``aladdin.make_kv`` and ``aladdin.make_tokens``.
+``aladdin.make_kv``, ``aladdin.make_kv8``, ``aladdin.make_tokens`` and ``aladdin.make_rope``.
 
 A step of a few microseconds should not wait for Python, so each function looks at
 what it needs once, in one condition, and looks for what is wrong only when that
@@ -15,8 +15,10 @@ import torch
 from . import aladdin as A
 
 _lib = A._lib
-_I32, _F32 = torch.int32, torch.float32
+_I32, _F32, _F8 = torch.int32, torch.float32, torch.float8_e4m3fn
 _LOGITS = {torch.bfloat16: A.BF16, torch.float16: A.F16, torch.float32: A.F32}
+_LAYOUTS = {"half": A.ROPE_HALF, "interleaved": A.ROPE_INTERLEAVED}
+_SCALINGS = {None: A.ROPE_NONE, "linear": A.ROPE_LINEAR, "base": A.ROPE_BASE, "parts": A.ROPE_PARTS}
 _KINDS = {"bf16": (A.BF16, torch.bfloat16), "f16": (A.F16, torch.float16)}
 
 
@@ -74,6 +76,75 @@ def make_kv(k, v, table, length, weight=None, pos=None, next_pos=None):
     kv._n = n
     kv._keep = (k, v, table, length, weight, pos, next_pos)
     return kv
+
+
+def make_kv8(k, v, k_scale, v_scale, table, length, next_pos=None):
+    """An aladdin_kv8 over torch tensors (kept alive by the returned object).
+
+    k, v: float8_e4m3fn [pages, kv_heads, page_tokens, head_dim], strides as for make_kv; k_scale, v_scale: contiguous
+    float32 [pages, kv_heads, page_tokens / block], of the tokens [i block, (i + 1) block) of a page; table, length,
+    next_pos as for make_kv."""
+    try:
+        shape, st = k.shape, k.stride()
+        pages, heads, tokens, dim = shape
+        n, width = table.shape
+        row = table.stride()
+        meta = k_scale.shape
+        ok = (k.is_cuda and k.dtype is _F8 and v.dtype is _F8 and v.shape == shape and v.stride() == st and st[3] == 1
+              and k_scale.dtype is _F32 and v_scale.dtype is _F32 and v_scale.shape == meta
+              and k_scale.is_contiguous() and v_scale.is_contiguous()
+              and meta[:2] == shape[:2] and len(meta) == 3 and meta[2] > 0 and tokens % meta[2] == 0
+              and table.dtype is _I32 and (row[1] == 1 or width == 1) and (n < 2 or row[0] >= width)
+              and length.dtype is _I32 and length.shape == (n,) and length.is_contiguous()
+              and (next_pos is None or (next_pos.dtype is _I32 and next_pos.shape == (n,)
+                                        and next_pos.is_contiguous())))
+    except (AttributeError, TypeError, ValueError):
+        ok = False
+    if not ok:
+        _fail("k and v must be [pages, kv_heads, page_tokens, head_dim] with equal strides and contiguous "
+              "channels, k_scale and v_scale contiguous [pages, kv_heads, page_tokens / block], table [requests, pages] with "
+              "contiguous rows that share no memory, length and next_pos contiguous [requests]",
+              ("k", k, _F8), ("v", v, _F8), ("k_scale", k_scale, _F32), ("v_scale", v_scale, _F32),
+              ("table", table, _I32), ("length", length, _I32), ("next_pos", next_pos, _I32))
+    kv = A.aladdin_kv8(k.data_ptr(), v.data_ptr(), st[0] if pages > 1 else heads * tokens * dim,
+                       st[1] if heads > 1 else tokens * dim, st[2], pages, width, row[0] if n > 1 else width,
+                       table.data_ptr(), length.data_ptr(), None if next_pos is None else next_pos.data_ptr(),
+                       k_scale.data_ptr(), v_scale.data_ptr(), tokens // meta[2])
+    kv._shape = ("e4m3", heads, tokens, dim)
+    kv._n = n
+    kv._keep = (k, v, k_scale, v_scale, table, length, next_pos)
+    return kv
+
+
+def make_rope(dim, base=10000.0, layout="half", scaling=None, factor=1.0, original=None, slow=1.0, fast=32.0,
+              freq=None, scale=None, device=None):
+    """Rotary positions of the first ``dim`` channels of a head (an aladdin_rope, its frequencies on the GPU).
+
+    layout: "half" (channels c, c + dim / 2 form a pair) or "interleaved" (2 c, 2 c + 1). Frequencies are base^(-2 c / dim),
+    scaled for long contexts by ``factor``: "linear", "base", or "parts" (of a model made for ``original`` positions: pairs
+    that turn fewer than ``slow`` times in them are slowed down, those of more than ``fast`` times are left);
+    or ``freq``, dim / 2 numbers in radians a position. ``scale`` multiplies rotated channels (default: 1, for "parts"
+    0.1 ln(factor) + 1)."""
+    if layout not in _LAYOUTS:
+        raise ValueError("layout must be one of %s" % sorted(_LAYOUTS))
+    if scaling not in _SCALINGS:
+        raise ValueError("scaling must be None or one of %s" % sorted(s for s in _SCALINGS if s))
+    if dim < 2 or dim % 2:
+        raise ValueError("dim must be even and at least 2")
+    if freq is None:
+        if scaling == "parts" and original is None:
+            raise ValueError("scaling by parts needs the positions that the model was made for (original)")
+        freq, own = A.aladdin_rope_frequencies(dim, base, _SCALINGS[scaling], factor, original or 0.0, slow, fast)
+    else:
+        if scaling is not None:
+            raise ValueError("freq and scaling exclude each other")
+        freq, own = torch.as_tensor(freq, dtype=torch.float64).cpu().numpy(), 1.0
+        if freq.shape != (dim // 2,):
+            raise ValueError("freq must have dim / 2 numbers")
+    turn = torch.from_numpy(A.aladdin_rope_turns(freq).view("int64")).to("cuda" if device is None else device)
+    rope = A.aladdin_rope(dim, _LAYOUTS[layout], own if scale is None else scale, turn.data_ptr())
+    rope._keep = turn
+    return rope
 
 
 def make_tokens(off, q, k, v, parent=None):
@@ -136,6 +207,7 @@ class Worker:
         self._kv_shape = (self.dtype, self.kv_heads, self.page_tokens, self.head_dim)
         self._tok_shape = (self.dtype, self.q_heads, self.kv_heads, self.head_dim)
         self._tok_bare = (self.dtype, 0, self.kv_heads, self.head_dim)  # without queries
+        self._kv8_shape = ("e4m3", self.kv_heads, self.page_tokens, self.head_dim)
         self.handle = A.aladdin_worker_create(
             A.aladdin_worker_shape(number, self.q_heads, self.kv_heads, self.head_dim, self.page_tokens),
             self.stream)
@@ -173,8 +245,8 @@ class Worker:
         if rc:
             raise A.AladdinError(rc, name)
 
-    def _check(self, kv, tok, bare):
-        if kv._shape != self._kv_shape:
+    def _check(self, kv, tok, bare, eight=False):
+        if kv._shape != self._kv_shape and not (eight and kv._shape == self._kv8_shape):
             raise ValueError("the cache does not have the worker's type or shape: %s, not %s"
                              % (kv._shape, self._kv_shape))
         if tok._shape != self._tok_shape and not (bare and tok._shape == self._tok_bare):
@@ -185,8 +257,8 @@ class Worker:
 
     def attend(self, kv, tok, scale=None, out=None, lse=None):
         """(out [tokens, q_heads, head_dim], lse [tokens, q_heads]); scale defaults to
-        head_dim ** -0.5."""
-        self._check(kv, tok, False)
+        head_dim ** -0.5. kv: a cache of 16 or (make_kv8) of 8 bits."""
+        self._check(kv, tok, False, True)
         n = tok.n_tok
         stride = self.q_heads * self.head_dim
         if out is None:
@@ -202,23 +274,68 @@ class Worker:
             lse = torch.empty((n, self.q_heads), dtype=_F32, device=self.device)
         elif lse.dtype is not _F32 or lse.shape != (n, self.q_heads) or not lse.is_contiguous():
             _fail("lse must be contiguous [tokens, q_heads]", ("lse", lse, _F32))
-        self._call("aladdin_worker_attend", C.byref(kv), C.byref(tok),
+        self._call("aladdin_worker_attend8" if kv._shape[0] == "e4m3" else "aladdin_worker_attend", C.byref(kv), C.byref(tok),
                    self.head_dim ** -0.5 if scale is None else scale, out.data_ptr(), stride, lse.data_ptr())
         return out, lse
+
+    def rotate(self, rope, tok, next_pos=None, pos=None, q_out=None, k_out=None):
+        """(q, k) of the tokens rotated to their positions: ``pos`` (int32 [tokens]), or ``next_pos`` (int32 [requests];
+        None: 0) plus a token's depth in its tree. q_out, k_out: None for a new tensor, the tokens' own tensor (in place),
+        another one, or False to leave them out."""
+        if tok._shape != self._tok_shape and not (q_out is False and tok._shape == self._tok_bare):
+            raise ValueError("the tokens do not have the worker's type or heads: %s, not %s"
+                             % (tok._shape, self._tok_shape))
+        n = tok.n_tok
+        if (next_pos is not None and (next_pos.dtype is not _I32 or next_pos.shape != (tok.n_req,)
+                                      or not next_pos.is_contiguous())) or \
+                (pos is not None and (pos.dtype is not _I32 or pos.shape != (n,) or not pos.is_contiguous())):
+            _fail("next_pos must be contiguous [requests], pos contiguous [tokens]",
+                  ("next_pos", next_pos, _I32), ("pos", pos, _I32))
+        args = []
+        outs = []
+        for out, heads in ((q_out, self.q_heads), (k_out, self.kv_heads)):
+            stride = heads * self.head_dim
+            if out is None:
+                out = torch.empty((n, heads, self.head_dim), dtype=self.dtype, device=self.device)
+            elif out is not False:
+                if out.dtype is not self.dtype or out.shape != (n, heads, self.head_dim) or \
+                        out.stride(2) != 1 or (heads > 1 and out.stride(1) != self.head_dim):
+                    _fail("q_out and k_out must be [tokens, heads, head_dim], heads and channels contiguous",
+                          ("out", out, self.dtype))
+                if n > 1:
+                    stride = out.stride(0)
+            outs.append(None if out is False else out)
+            args += [None if out is False else out.data_ptr(), stride]
+        self._call("aladdin_worker_rotate", C.byref(rope), C.byref(tok),
+                   None if next_pos is None else next_pos.data_ptr(), None if pos is None else pos.data_ptr(), *args)
+        return tuple(outs)
+
+    def append(self, kv, tok, rope=None, acc_off=None, acc=None):
+        """Append tokens (all of them, any number, without acc_off and acc) to a cache of 16 or (make_kv8) of 8 bits, in
+        place; with ``rope`` keys are rotated to their positions on the way."""
+        self._check(kv, tok, True, True)
+        n, acc_off, acc = self._choice(tok, acc_off, acc)
+        self._call("aladdin_worker_append8" if kv._shape[0] == "e4m3" else "aladdin_worker_append", C.byref(kv),
+                   C.byref(tok), None if rope is None else C.byref(rope), acc_off, acc, n)
+
+    @staticmethod
+    def _choice(tok, acc_off, acc):
+        """Number and addresses of the chosen tokens."""
+        if acc_off is None and acc is None:
+            return 0, None, None
+        if acc_off is None or acc is None or acc_off.dtype is not _I32 or acc.dtype is not _I32 or \
+                acc_off.shape != (tok.n_req + 1,) or acc.dim() != 1 or not acc_off.is_contiguous() or \
+                not acc.is_contiguous():
+            _fail("acc_off and acc come together, contiguous [requests + 1] and [kept tokens]",
+                  ("acc_off", acc_off, _I32), ("acc", acc, _I32))
+        return acc.shape[0], acc_off.data_ptr(), acc.data_ptr()
 
     def accept(self, kv, tok, scale=None, lse=None, acc_off=None, acc=None):
         """Keep tokens (all of them without acc_off and acc) in the cache, in place;
         with the lse of the tokens' attention the cache's weights grow by what the kept
         rows attended to."""
         self._check(kv, tok, lse is None)
-        n = 0
-        if acc_off is not None or acc is not None:
-            if acc_off is None or acc is None or acc_off.dtype is not _I32 or acc.dtype is not _I32 or \
-                    acc_off.shape != (tok.n_req + 1,) or acc.dim() != 1 or not acc_off.is_contiguous() or \
-                    not acc.is_contiguous():
-                _fail("acc_off and acc come together, contiguous [requests + 1] and [kept tokens]",
-                      ("acc_off", acc_off, _I32), ("acc", acc, _I32))
-            n, acc_off, acc = acc.shape[0], acc_off.data_ptr(), acc.data_ptr()
+        n, acc_off, acc = self._choice(tok, acc_off, acc)
         if lse is not None:
             if kv.weight is None:
                 raise ValueError("the cache has no weights to add to")
