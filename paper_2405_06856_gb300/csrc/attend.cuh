@@ -275,5 +275,53 @@ __device__ __forceinline__ void join_rows(const AttendArgs& a, const Cursor& u, 
     }
 }
 
+// Row rr (of token t, query head hd) of the unit under u, whose partial results the workers first .. last left with four
+// columns of all rows together; one thread.
+template <typename T, int D, int RM>
+__device__ __forceinline__ void join_row(const AttendArgs& a, const Cursor& u, int first, int last, int rr, int t, int hd)
+{
+    float top = -INFINITY, sum = 0.0f;
+#pragma unroll 4
+    for (int i = first; i <= last; ++i)
+        top = fmaxf(top, __ldcg(part_of<D, RM>(a, i, i == first) + rr * 2));
+    const float ref = top == -INFINITY ? 0.0f : top;
+#pragma unroll 4
+    for (int i = first; i <= last; ++i) {
+        const float2 v = __ldcg(
+            reinterpret_cast<const float2*>(part_of<D, RM>(a, i, i == first) + rr * 2));
+        sum += v.y * ex2(v.x - ref);
+    }
+    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+    uint4* const d = reinterpret_cast<uint4*>(
+        a.out + ((u.lo + t) * a.out_stride + (long long)hd * D) * 2);
+#pragma unroll 2
+    for (int c = 0; c < D / 32; ++c) {
+        float4 acc[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) acc[x] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 2
+        for (int i = first; i <= last; ++i) {
+            const float* const p = part_of<D, RM>(a, i, i == first);
+            const float f = ex2(__ldcg(p + rr * 2) - ref);
+            const float4* const q = reinterpret_cast<const float4*>(p + RM * 2) + c * 8 * RM + rr;
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                const float4 v = __ldcg(q + x * RM);
+                acc[x].x += f * v.x;
+                acc[x].y += f * v.y;
+                acc[x].z += f * v.z;
+                acc[x].w += f * v.w;
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const float4 y = acc[x * 2], z = acc[x * 2 + 1];
+            d[c * 4 + x] = make_uint4(Num<T>::pack(y.x * inv, y.y * inv), Num<T>::pack(y.z * inv, y.w * inv),
+                                      Num<T>::pack(z.x * inv, z.y * inv), Num<T>::pack(z.z * inv, z.w * inv));
+        }
+    }
+    if (a.lse) a.lse[(long long)(u.lo + t) * (a.kv.kv_heads * a.kv.group) + hd] = (ref + log2f(sum)) * LN2;
+}
+
 }  // namespace wk
 }  // namespace aladdin

@@ -532,7 +532,7 @@ cudaError_t launch_dim(const Attend8Args& a, int dim, int sms, cudaStream_t st)
 }  // namespace
 }  // namespace wk
 
-cudaError_t launch_attend8(const Attend8Args& a, int dtype, int dim, int sms, cudaStream_t st)
+cudaError_t launch_attend8_few(const Attend8Args& a, int dtype, int dim, int sms, cudaStream_t st)
 {
     return dtype == ALADDIN_BF16 ? wk::launch_dim<__nv_bfloat16>(a, dim, sms, st)
                                  : wk::launch_dim<__half>(a, dim, sms, st);

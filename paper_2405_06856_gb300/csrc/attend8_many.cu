@@ -1,0 +1,745 @@
+// aladdin_worker_attend8 where the rows of a (request, key head) are many (trees of drafted tokens, large groups): the
+// products run on the fifth-generation tensor cores (tcgen05). See attend8.cuh for the operator.
+//
+// A CTA runs through a range of the axis of all key tiles, up to MT tiles of 128 rows at a time. Its warps have roles:
+//   four warps for each row tile do the softmax, one thread a row. A thread brings its row of queries into tensor memory,
+//   in half precision and scaled for it, reads a tile's scores once, and leaves the weights in the place of the scores;
+//   one thread issues the products: scores S = Q K' and out += P V, both with the first operand, Q or P, from tensor
+//   memory, so that shared memory, which the copies and conversions use too, is read for K and V only;
+//   four warps convert: codes come by asynchronous copies a few tiles ahead, each thread's own, and go as half
+//   precision into a ring of shared memory, K0 V0 K1 V1 ..., in the 128-byte-swizzled layout of the matrix
+//   descriptors. New tokens have a tile of their own; those of bfloat16 are scaled by a power of two for each.
+// With two row tiles the tensor cores work on one while the softmax works on the other; with one, the scores of the next
+// tile are formed ahead into the second place. The accumulator stays in tensor memory; it is rescaled only when a row's
+// maximum has grown by more than 2^8 over the one that its weights refer to, or a scale by more than 2^4.
+//
+// New tokens' values that are not finite would reach rows that do not see them (0 times infinity): they are replaced by
+// 0 in shared memory, and rows that do see them get them added at the end.
+#include "attend8.cuh"
+#include "tensor_dev.cuh"
+
+namespace aladdin {
+namespace wk {
+namespace {
+
+template <int D, int MT>
+struct Many8 {
+    static constexpr int KT = 64;                        // keys of a tile
+    static constexpr int RM = 128 * MT;                  // rows of a unit
+    static constexpr int HALVES = (D + 63) / 64;         // blocks of 64 channels
+    static constexpr int TILE = HALVES * KT * 128;       // keys or values of a tile, half precision
+    static constexpr int NB = D == 256 ? 4 : 8;          // of them in the ring
+    static constexpr int CPT = HALVES * KT / 32;         // 16 codes each: what a converting thread has of them
+    static constexpr int NR = D == 256 ? 4 : 8;          // codes in flight: keys or values of a tile
+    static constexpr int RAW = CPT * 128 * 16;
+    static constexpr int raw = NB * TILE;
+    static constexpr int bars = raw + NR * RAW;
+    static constexpr int full = bars, empty = full + NB * 8, qready = empty + NB * 8, sready = qready + 16,
+                         pready = sready + 24, odone = pready + 16, ofree = odone + 16, over = ofree + 16,
+                         tmem = over + 8;
+    static constexpr int wild = tmem + 8;                // 8 flags of units
+    static constexpr int late = wild + 8 * 4;            // whether a wait ran out
+    static constexpr int rscale = late + 8;              // 8 tiles' scales: of 4 blocks' keys, then values
+    static constexpr int rvalid = rscale + 8 * 32;       // and which blocks of 16 keys are on pages of the pool
+    static constexpr int info = rvalid + 8 * 4;          // 8 tiles' Info
+    static constexpr int scratch = info + 8 * (64 * 8 + 32);
+    static constexpr int pre = scratch + 32 * 8;
+    static constexpr int bytes(int n_req) { return pre + (n_req + 1) * 8; }
+    static constexpr int WARPS = 4 * MT + 1 + 4;         // softmax, products, conversions
+    // columns of tensor memory: the scores' two places, the accumulators, the queries
+    static constexpr int s0 = 0, o0 = 2 * KT, q0 = o0 + MT * HALVES * 64;
+    static_assert(q0 + MT * (D / 2) <= 512, "tensor memory");
+    static_assert(scratch % 8 == 0 && TILE % 1024 == 0, "alignment");
+};
+
+// A tile's scales for the softmax: of blocks of 16 keys, or of each key where they are new.
+struct Info {
+    float k[64];    // factors of scores
+    float lv[64];   // logarithms of the values' scales
+    float top[4];   // the largest are among these
+    int valid;      // blocks of 16 keys on pages of the pool
+    int pad[3];
+};
+
+// What a unit costs beside its tiles, in keys.
+constexpr int UNIT_KEYS = 512;
+
+__device__ __forceinline__ uint64_t pair2(uint32_t lo, uint32_t hi) { return (uint64_t)hi << 32 | lo; }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ float low2(uint64_t a) { return __uint_as_float((uint32_t)a); }
+__device__ __forceinline__ float high2(uint64_t a) { return __uint_as_float((uint32_t)(a >> 32)); }
+
+template <typename T, int D, int MT>
+__global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(Attend8Args a)
+{
+    using L = Many8<D, MT>;
+    constexpr int KT = L::KT, RM = L::RM, NB = L::NB, NR = L::NR, NT = L::WARPS * 32;
+    constexpr bool BF16 = !std::is_same<T, __half>::value;
+    extern __shared__ __align__(1024) char sm[];
+    const uint32_t sm0 = smem_addr(sm);
+    int* const pre = reinterpret_cast<int*>(sm + L::pre);
+    // (tiles' scales, units' flags: the conversions run fewer than 8 tiles ahead of the softmax)
+    Info* const infos = reinterpret_cast<Info*>(sm + L::info);
+    volatile int* const wilds = reinterpret_cast<volatile int*>(sm + L::wild);
+    volatile int* const late = reinterpret_cast<volatile int*>(sm + L::late);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int G = a.kv.group, H = a.kv.kv_heads;
+
+    if (sm0 & 1023) {  // the operands' layout wants it
+        if (tid == 0) atomicOr(a.err, WORKER_TIMEOUT);
+        return;
+    }
+    Axis ax;
+    if (!plan<NT>(a.tok.n_req, ax, pre, pre + a.tok.n_req + 1, reinterpret_cast<long long*>(sm + L::scratch),
+                  (int)gridDim.x, UNIT_KEYS / KT, 1, a.err,
+                  [&](int r, int& c) { return attend_units<KT, RM, KT>(a, r, c); }))
+        return;
+    const int me = blockIdx.x;
+    if (me >= ax.workers) return;
+    Cursor C;
+    const int n = range<KT, RM, KT>(a, ax, C, me);
+    if (n == 0) return;
+
+    if (warp == 0) tmem_alloc(sm0 + L::tmem, 512);
+    if (tid == 0) {
+        for (int b = 0; b < NB; ++b) {
+            mbar_init(sm0 + L::full + b * 8, 4);
+            mbar_init(sm0 + L::empty + b * 8, 1);
+        }
+        for (int w = 0; w < 2; ++w) {
+            mbar_init(sm0 + L::qready + w * 8, 4);
+            mbar_init(sm0 + L::pready + w * 8, 4);
+            mbar_init(sm0 + L::odone + w * 8, 1);
+            mbar_init(sm0 + L::ofree + w * 8, 4);
+        }
+        for (int w = 0; w < 3; ++w) mbar_init(sm0 + L::sready + w * 8, 1);
+        mbar_init(sm0 + L::over, 1);
+        for (int u = 0; u < 8; ++u) wilds[u] = 0;
+        *late = 0;
+        mbar_init_fence();
+    }
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tm = *reinterpret_cast<volatile uint32_t*>(sm + L::tmem);
+
+    // A wait that runs out is recorded and ends its warp's part; the others' waits run
+    // out after it (no warps meet at a barrier without a limit before the end), and all meet at
+    // the end, where what is in flight is waited for and tensor memory is freed.
+    auto wait = [&](uint32_t bar, int phase) -> bool {
+        if (mbar_wait(bar, phase & 1)) return true;
+        atomicOr(a.err, WORKER_TIMEOUT);
+        return false;
+    };
+    // row tiles of the unit under u, of MT at most
+    auto active = [&](const Cursor& u) { return MT == 2 && u.T * G - u.rt * RM > 128 ? 2 : 1; };
+    // the barrier of the scores of row tile w, in place s: whoever waits for one waits for all of its phases
+    auto scored_bar = [&](bool both, int w, int s) { return both && w ? 2 : s; };
+    bool ok = true;  // no wait of this warp ran out
+
+    if (warp >= 4 * MT + 1) {
+        // ------------------------------------------------------------ conversions
+        const int ct = tid - (4 * MT + 1) * 32, cw = ct >> 5, r0 = ct >> 2, ch = ct & 3;  // row of 32, chunk of a half
+        float* const rscale = reinterpret_cast<float*>(sm + L::rscale);
+        volatile int* const rvalid = reinterpret_cast<volatile int*>(sm + L::rvalid);
+        const uint32_t raw0 = sm0 + L::raw + ct * 16;
+        Cursor F = C;  // the tile whose codes are fetched
+        // pages of this thread's rows of the tile under F and, lanes 0 .. 7 of the first warp, of the block whose
+        // scale they fetch, as the table has them
+        int page[KT / 32], spage = 0;
+        auto pages = [&]() {
+            const int32_t* const row = a.kv.table + (long long)F.r * a.kv.table_stride;
+#pragma unroll
+            for (int p = 0; p < KT / 32; ++p) {
+                const int key = F.tile * KT + p * 32 + r0;
+                page[p] = key < F.len ? row[key >> a.kv.page_shift] : 0;
+            }
+            const int key = F.tile * KT + (lane & 3) * 16;
+            spage = cw == 0 && lane < 8 && key < F.len ? row[key >> a.kv.page_shift] : 0;
+        };
+        pages();
+        // codes of half i, keys or values of tile i / 2, under F
+        auto fetch = [&](int i) {
+            if (i < 2 * n) {
+                const int key0 = F.tile * KT, own = F.len - key0;
+                if (own > 0) {
+                    const char* const pool = i & 1 ? a.kv.v : a.kv.k;
+                    const uint32_t d = raw0 + i % NR * L::RAW;
+#pragma unroll
+                    for (int p = 0; p < KT / 32; ++p) {
+                        const int row = p * 32 + r0;
+                        const bool in = row < own && (unsigned)page[p] < (unsigned)a.kv.pages;
+                        const long long e = in ? page[p] * a.kv.page_stride + F.h * a.kv.head_stride +
+                                                     ((key0 + row) & (a.kv.page - 1)) * a.kv.token_stride + ch * 16
+                                               : 0;
+                        // (weights of 0 meet the codes of rows that hold no key: zeros)
+#pragma unroll
+                        for (int h = 0; h < L::HALVES; ++h)
+                            if (D % 64 == 0 || h * 64 + ch * 16 < D)
+                                cp16(d + (p * L::HALVES + h) * 2048, pool + e + (in ? h * 64 : 0), in);
+                    }
+                    if ((i & 1) == 0 && cw == 0) {
+                        const int x = lane & 3, key = key0 + x * 16;
+                        const bool in = lane < 8 && x * 16 < own && (unsigned)spage < (unsigned)a.kv.pages;
+                        if (lane < 4 && x * 16 < own && !in) atomicOr(a.err, WORKER_BAD_INPUT);
+                        const long long e = in ? ((long long)spage * H + F.h) * a.scales.per_page +
+                                                     ((key & (a.kv.page - 1)) >> a.scales.block_shift)
+                                               : 0;
+                        if (lane < 8) cp4(sm0 + L::rscale + (i / 2 % 8) * 32 + lane * 4, (lane < 4 ? a.scales.k : a.scales.v) + e, in);
+                        const unsigned valid = __ballot_sync(0xffffffffu, in) & 15;
+                        if (lane == 0) rvalid[i / 2 % 8] = (int)valid;
+                    }
+                }
+                if (i & 1 && i + 1 < 2 * n) {
+                    advance<KT, RM, KT>(a, F, pre);
+                    pages();
+                }
+            }
+            cp_commit();
+        };
+#pragma unroll 1
+        for (int i = 0; i < NR - 1; ++i) fetch(i);
+        int units = -1, vtop = 0;
+        for (int j = 0; j < n && ok; ++j) {
+            if (j == 0 || C.tile == 0) ++units;
+            const bool cached = C.tile * KT < C.len;
+            Info& info = infos[j & 7];
+#pragma unroll 1
+            for (int part = 0; part < 2; ++part) {
+                const int i = 2 * j + part, slot = i % NB;
+                fetch(i + NR - 1);
+                if (i >= NB) ok = __all_sync(0xffffffffu, wait(sm0 + L::empty + slot * 8, i / NB - 1));
+                if (!ok) break;
+                cp_wait<NR - 1>();
+                char* const d = sm + slot * L::TILE;
+                // the place of 8 channels, chunk c of a row
+                auto at = [&](int row, int c) { return (c >> 3) * (KT * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4); };
+                if (cached) {
+                    if (part == 0 && cw == 0) {
+                        __syncwarp();
+                        const float s = lane < 8 ? rscale[(j & 7) * 8 + lane] : 0.0f;
+                        const int valid = rvalid[j & 7];
+                        // (a factor that is not 0: scores of 0 stay 0, and those that do not count -inf)
+                        if (lane < 4) info.k[lane] = s < 1e-30f ? 1e-30f : s;
+                        float lv = -INFINITY;
+                        if (lane >= 4 && lane < 8) {
+                            lv = valid >> (lane - 4) & 1 ? log_scale(s) : -INFINITY;
+                            info.lv[lane - 4] = lv;
+                        }
+#pragma unroll
+                        for (int x = 4; x; x >>= 1) lv = fmaxf(lv, __shfl_xor_sync(0xffffffffu, lv, x));
+                        if (lane < 4) info.top[lane] = lv;
+                        if (lane == 0) info.valid = valid;
+                    }
+                    const char* const src = sm + L::raw + i % NR * L::RAW + ct * 16;
+#pragma unroll
+                    for (int p = 0; p < KT / 32; ++p) {
+#pragma unroll
+                        for (int h = 0; h < L::HALVES; ++h) {
+                            if (D % 64 == 0 || h * 64 + ch * 16 < D) {
+                                const uint4 c = *reinterpret_cast<const uint4*>(src + (p * L::HALVES + h) * 2048);
+                                const int row = p * 32 + r0;
+                                *reinterpret_cast<uint4*>(d + at(row, h * 8 + ch * 2)) =
+                                    make_uint4(half2_lo(c.x), half2_hi(c.x), half2_lo(c.y), half2_hi(c.y));
+                                *reinterpret_cast<uint4*>(d + at(row, h * 8 + ch * 2 + 1)) =
+                                    make_uint4(half2_lo(c.z), half2_hi(c.z), half2_lo(c.w), half2_hi(c.w));
+                            }
+                        }
+                    }
+                } else {
+                    // 16 new tokens a warp
+                    constexpr int CH = D / 8;
+                    const char* const base = part ? a.tok.v : a.tok.k;
+                    const long long stride = (part ? a.tok.v_stride : a.tok.k_stride) * 2;
+                    const char* const src = base + C.lo * stride + C.h * D * 2;
+                    if (BF16 && part == 0) {
+                        // the largest exponents of two halves of a row a lane, of keys and values, not of infinities and NaN
+                        const int row = cw * 16 + (lane >> 1);
+                        int top[2] = {0, 0};
+                        if (row < C.T) {
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const char* const q = (e ? a.tok.v + (C.lo + row) * a.tok.v_stride * 2 : a.tok.k + (C.lo + row) * a.tok.k_stride * 2) +
+                                                      (C.h * D + (lane & 1) * (D / 2)) * 2;
+#pragma unroll 4
+                                for (int c = 0; c < D / 16; ++c) {
+                                    const uint4 v = *reinterpret_cast<const uint4*>(q + c * 16);
+                                    top[e] = exponent(Num<T>::tame(v.x), exponent(Num<T>::tame(v.y), exponent(Num<T>::tame(v.z), exponent(Num<T>::tame(v.w), top[e]))));
+                                }
+                            }
+                        }
+                        top[0] = max(top[0], __shfl_xor_sync(0xffffffffu, top[0], 1));
+                        top[1] = max(top[1], __shfl_xor_sync(0xffffffffu, top[1], 1));
+                        vtop = top[1];
+                        const int clamped = min(max(top[1], 15), 254) - 141;
+                        float lv = row < C.T ? (float)clamped : -INFINITY;
+                        if ((lane & 1) == 0) {
+                            info.k[row] = half_back(top[0]);
+                            info.lv[row] = lv;
+                        }
+#pragma unroll
+                        for (int x = 16; x; x >>= 1) lv = fmaxf(lv, __shfl_xor_sync(0xffffffffu, lv, x));
+                        if (lane == 0) info.top[cw] = lv;
+                        // (the keys' factor is needed now, the values' in the next part)
+                        top[1] = top[0];
+                        vtop |= top[0] << 16;
+                    } else if (part == 0) {
+                        if (lane < 16) info.k[cw * 16 + lane] = 1.0f, info.lv[cw * 16 + lane] = 0.0f;
+                        if (lane == 0) info.top[cw] = 0.0f;
+                    }
+                    if (part == 0 && cw == 0 && lane == 0) info.valid = 15;
+                    bool w = false;
+#pragma unroll 1
+                    for (int x = lane; x < 16 * CH; x += 32) {
+                        const int row = x / CH, c = x - row * CH, t = cw * 16 + row;
+                        uint4 v = make_uint4(0, 0, 0, 0);
+                        if (t < C.T) v = *reinterpret_cast<const uint4*>(src + t * stride + c * 16);
+                        if (part && (Num<T>::wild(v.x) || Num<T>::wild(v.y) || Num<T>::wild(v.z) || Num<T>::wild(v.w))) {
+                            w = true;
+                            v.x = Num<T>::tame(v.x), v.y = Num<T>::tame(v.y), v.z = Num<T>::tame(v.z), v.w = Num<T>::tame(v.w);
+                        }
+                        if constexpr (BF16) {
+                            static_assert(16 * CH % 32 == 0, "all lanes take part");
+                            const int both = __shfl_sync(0xffffffffu, vtop, row * 2);
+                            const float f = half_factor(part ? both & 0xffff : both >> 16);
+                            v = make_uint4(to_half(v.x, f), to_half(v.y, f), to_half(v.z, f), to_half(v.w, f));
+                        }
+                        *reinterpret_cast<uint4*>(d + at(t, c)) = v;
+                    }
+                    if (w) wilds[units & 7] = units + 1;
+                }
+                fence_async();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(sm0 + L::full + slot * 8);
+            }
+            if (j + 1 < n) advance<KT, RM, KT>(a, C, pre);
+        }
+        cp_wait<0>();
+    } else if (warp == 4 * MT) {
+        // ------------------------------------------------------------ products
+        constexpr uint32_t qk = product<__half>(KT, false), pv = product<__half>(D, true);
+        const bool leader = elected();
+        Cursor N = C;  // the tile whose scores are formed next
+        int scored = 0, local = 0, run[2] = {0, 0}, starts[2] = {0, 0}, asked[2] = {0, 0};
+        // waits for the keys (and queries) of the tile under N
+        auto enter_tile = [&]() {
+            if (scored == 0 || N.tile == 0) {
+                local = 0;
+#pragma unroll
+                for (int w = 0; w < MT; ++w)
+                    if (w < active(N)) ok = ok && wait(sm0 + L::qready + w * 8, asked[w]++);
+            }
+            ok = __all_sync(0xffffffffu, ok && wait(sm0 + L::full + 2 * scored % NB * 8, 2 * scored / NB));
+            tc_after();
+        };
+        // its scores for row tile w
+        auto scores = [&](int w) {
+            const uint32_t k0 = operand_lo(sm0 + 2 * scored % NB * L::TILE, 0);
+            const int s = active(N) == 2 ? w : local & 1;
+            if (leader) {
+#pragma unroll
+                for (int x = 0; x < D / 16; ++x)
+                    tc_mma_ts(tm + L::s0 + s * KT, tm + L::q0 + w * (D / 2) + x * 8,
+                              whole(k0 + ((x >> 2) * KT * 128 + (x & 3) * 32) / 16, OPERAND_HI), qk, x > 0);
+                tc_commit(sm0 + L::sready + scored_bar(active(N) == 2, w, s) * 8);
+            }
+            __syncwarp();
+        };
+        // the tile under N has its scores on the way
+        auto leave_tile = [&]() {
+            if (leader) tc_commit(sm0 + L::empty + 2 * scored % NB * 8);
+            __syncwarp();
+            ++local;
+            if (++scored < n) advance<KT, RM, KT>(a, N, pre);
+        };
+        auto tile_scores = [&]() {
+            enter_tile();
+            if (!ok) return;
+#pragma unroll
+            for (int w = 0; w < MT; ++w)
+                if (w < active(N)) scores(w);
+            leave_tile();
+        };
+        tile_scores();
+        int place = 0;  // of the weights, with one row tile
+        for (int j = 0; j < n && ok; ++j) {
+            const bool more = j + 1 < n, turns = C.tile + 1 == C.c;
+            const bool start = j == 0 || C.tile == 0;
+            const int both = active(C) == 2;
+            if (start) place = 0;
+            if (!both && more && !turns) {
+                tile_scores();
+                if (!ok) break;
+            }
+            const int v = 2 * j + 1;
+#pragma unroll
+            for (int w = 0; w < MT; ++w) {
+                if (w == 0 || both) {
+                    ok = ok && wait(sm0 + L::pready + w * 8, run[w]++);
+                    ok = ok && wait(sm0 + L::full + v % NB * 8, v / NB);
+                    if (start && starts[w]++ > 0) ok = ok && wait(sm0 + L::ofree + w * 8, starts[w] - 2);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    tc_after();
+                    const uint32_t v0 = operand_lo(sm0 + v % NB * L::TILE, KT * 128),
+                                   p = tm + L::s0 + (both ? w : place) * KT;
+                    if (leader) {
+#pragma unroll
+                        for (int x = 0; x < KT / 16; ++x)
+                            tc_mma_ts(tm + L::o0 + w * (L::HALVES * 64), p + x * 8,
+                                      whole(v0 + x * 2048 / 16, OPERAND_HI), pv, !start || x > 0);
+                        tc_commit(sm0 + L::odone + w * 8);
+                    }
+                    __syncwarp();
+                    if (both && more && !turns) {
+                        if (w == 0) {
+                            enter_tile();
+                            if (!ok) break;
+                        }
+                        scores(w);
+                    }
+                }
+            }
+            if (!ok) break;
+            if (leader) tc_commit(sm0 + L::empty + v % NB * 8);
+            __syncwarp();
+            if (both && more && !turns) leave_tile();
+            if (more && turns) tile_scores();
+            place ^= 1;
+            if (more) advance<KT, RM, KT>(a, C, pre);
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------------------ softmax
+        const int w = warp >> 2, row = tid & 127;
+        const uint32_t lanes = (uint32_t)(warp & 3) * 32u << 16, om = tm + lanes + L::o0 + w * (L::HALVES * 64);
+        float m = -INFINITY, l = 0.0f, ref = -1000.0f, factor = 0.0f;
+        unsigned long long see = 0;
+        int units = -1, tile0 = 0, scored[3] = {0, 0, 0}, done = 0, local = 0;
+        // this row's queries of the unit under u, 32 channels a time, into tensor memory
+        auto queries = [&](const Cursor& u) {
+            const int rho = u.rt * RM + w * 128 + row, t = rho / G;
+            if (u.T * G - u.rt * RM <= w * 128) return;
+            const bool live = rho < u.T * G;
+            const uint4* const src = reinterpret_cast<const uint4*>(
+                a.tok.q + ((u.lo + (live ? t : 0)) * a.tok.q_stride + (long long)(u.h * G + (live ? rho - t * G : 0)) * D) * 2);
+            const uint4 none = make_uint4(0, 0, 0, 0);
+            int top = 0;
+            if constexpr (BF16) {
+#pragma unroll 8
+                for (int c = 0; c < D / 8; ++c) {
+                    const uint4 v = live ? __ldg(src + c) : none;
+                    top = exponent(v.x, exponent(v.y, exponent(v.z, exponent(v.w, top))));
+                }
+            }
+            const float f = half_factor(top);
+            factor = (BF16 ? half_back(top) : 1.0f) * a.scale_log2;
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+                uint32_t x[16];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint4 v = live ? __ldg(src + c * 4 + i) : none;
+                    x[i * 4] = v.x, x[i * 4 + 1] = v.y, x[i * 4 + 2] = v.z, x[i * 4 + 3] = v.w;
+                }
+                if constexpr (BF16) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] = to_half(x[i], f);
+                }
+                tmem_store16(tm + lanes + L::q0 + w * (D / 2) + c * 16, x);
+            }
+            tmem_stored();
+            tc_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(sm0 + L::qready + w * 8);
+        };
+        queries(C);
+        for (int j = 0; j < n && ok; ++j) {
+            const bool start = j == 0 || C.tile == 0, unit_ends = C.tile + 1 == C.c;
+            const int rows = C.T * G - C.rt * RM - w * 128;
+            const bool both = active(C) == 2;
+            if (start) {
+                ++units;
+                tile0 = C.tile;
+                local = 0;
+            }
+            const int s = both ? w : local & 1, bar = scored_bar(both, w, s);
+            ++local;
+            if (rows > 0) {
+                if (start) {
+                    const int rho = C.rt * RM + w * 128 + row;
+                    see = ancestors(a, C, row < rows ? rho / G : 0);
+                }
+                ok = __all_sync(0xffffffffu, wait(sm0 + L::sready + bar * 8, bar == 2 ? scored[2]++ : bar ? scored[1]++ : scored[0]++));
+                if (!ok) break;
+                tc_after();
+                const uint32_t st = tm + lanes + L::s0 + s * KT;
+                uint32_t v[2][32];
+                tmem_start(v[0], st);
+                tmem_start(v[1], st + 32);
+                const Info& info = infos[j & 7];
+                const int own = C.len - C.tile * KT;  // cached keys from the tile's start
+                float f[4], lv[4];
+                {
+                    const float4 x = *reinterpret_cast<const float4*>(info.k), y = *reinterpret_cast<const float4*>(info.lv);
+                    f[0] = x.x * factor, f[1] = x.y * factor, f[2] = x.z * factor, f[3] = x.w * factor;
+                    lv[0] = y.x, lv[1] = y.y, lv[2] = y.z, lv[3] = y.w;
+                }
+                const float4 tops = *reinterpret_cast<const float4*>(info.top);
+                const float scale_top = fmaxf(fmaxf(tops.x, tops.y), fmaxf(tops.z, tops.w));
+                const int valid = info.valid;
+                tmem_loaded(v[0]);
+                tmem_loaded(v[1]);
+                if (own < KT || valid != 15) {
+                    // what this row sees
+                    uint32_t vis[2];
+                    if (own > 0) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const int left = own - h * 32;
+                            vis[h] = ((valid >> (h * 2) & 1 ? 0xffffu : 0u) | (valid >> (h * 2) & 2 ? 0xffff0000u : 0u)) &
+                                     (left >= 32 ? 0xffffffffu : left > 0 ? (1u << left) - 1 : 0u);
+                        }
+                    } else {
+                        vis[0] = (uint32_t)see;
+                        vis[1] = (uint32_t)(see >> 32);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 64; ++i) {
+                        const float g = own > 0 ? f[i / 16] : info.k[i] * factor;
+                        v[i / 32][i % 32] = vis[i / 32] >> (i % 32) & 1 ? __float_as_uint(__uint_as_float(v[i / 32][i % 32]) * g) : 0xff800000u;
+                    }
+                    f[0] = f[1] = f[2] = f[3] = 1.0f;
+                }
+                float top = -INFINITY;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    float t0 = -INFINITY, t1 = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        const uint32_t* const y = &v[x / 2][x % 2 * 16 + i];
+                        t0 = fmaxf(fmaxf(t0, __uint_as_float(y[0])), __uint_as_float(y[1]));
+                        t1 = fmaxf(fmaxf(t1, __uint_as_float(y[2])), __uint_as_float(y[3]));
+                    }
+                    top = fmaxf(top, fmaxf(t0, t1) * f[x]);
+                }
+                if (start) {
+                    m = top;
+                    l = 0.0f;
+                    ref = fmaxf(scale_top, -1000.0f);
+                } else {
+                    const bool grown = top > m + 8.0f;  // (always where m is -inf and top is not)
+                    const bool larger = scale_top > ref + 4.0f;
+                    if (larger || __any_sync(0xffffffffu, grown)) {
+                        // the weights of the tiles before are in the accumulator
+                        if (done) ok = __all_sync(0xffffffffu, wait(sm0 + L::odone + w * 8, done - 1));
+                        if (!ok) break;
+                        tc_after();
+                        float g = grown ? ex2(m - top) : 1.0f;
+                        if (grown) m = top;
+                        l *= g;
+                        if (larger) {
+                            g *= ex2(ref - scale_top);
+                            ref = scale_top;
+                        }
+#pragma unroll 1
+                        for (int c = 0; c < (D + 15) / 16; ++c) {
+                            uint32_t o[16];
+                            tmem_load16(o, om + c * 16);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * g);
+                            tmem_store16(om + c * 16, o);
+                        }
+                    }
+                }
+                const float base = m == -INFINITY ? 0.0f : m;
+                if (own > 0) {
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const float at = relative(lv[x], ref), shift = at - base;
+                        const uint64_t ff = pair2(__float_as_uint(f[x]), __float_as_uint(f[x])),
+                                       bb = pair2(__float_as_uint(shift), __float_as_uint(shift));
+                        uint64_t sum = 0;
+#pragma unroll
+                        for (int i = 0; i < 16; i += 2) {
+                            uint32_t* const y = &v[x / 2][x % 2 * 16 + i];
+                            const uint64_t z = fma2(pair2(y[0], y[1]), ff, bb);
+                            const float e0 = ex2(low2(z)), e1 = ex2(high2(z));
+                            sum = add2(sum, pair2(__float_as_uint(e0), __float_as_uint(e1)));
+                            v[x / 2][x % 2 * 8 + i / 2] = Num<__half>::pack(e0, e1);
+                        }
+                        l += (low2(sum) + high2(sum)) * ex2(-at);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 64; i += 2) {
+                        float e[2];
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const float at = relative(info.lv[i + k], ref);
+                            e[k] = ex2(__uint_as_float(v[i / 32][i % 32 + k]) - base + at);
+                            l += e[k] * ex2(-at);
+                        }
+                        v[i / 32][i % 32 / 2] = Num<__half>::pack(e[0], e[1]);
+                    }
+                }
+                // (the scores of all 64 keys have been read)
+                tmem_store16(st, *reinterpret_cast<const uint32_t(*)[16]>(&v[0][0]));
+                tmem_store16(st + 16, *reinterpret_cast<const uint32_t(*)[16]>(&v[1][0]));
+                tmem_stored();
+                tc_before();
+                // (the products of the tile before are done, so that the arrivals before these have been seen)
+                if (done) ok = __all_sync(0xffffffffu, wait(sm0 + L::odone + w * 8, done - 1));
+                if (!ok) break;
+                if (lane == 0) mbar_arrive(sm0 + L::pready + w * 8);
+                ++done;
+            }
+            Cursor next = C;
+            if (unit_ends && j + 1 < n) {
+                // the next unit's queries, while the last products run: this unit's scores are done
+                advance<KT, RM, KT>(a, next, pre);
+                queries(next);
+            }
+            if (rows > 0 && (unit_ends || j + 1 == n)) {
+                ok = __all_sync(0xffffffffu, wait(sm0 + L::odone + w * 8, done - 1));
+                if (!ok) break;
+                tc_after();
+                const bool whole = tile0 == 0 && unit_ends;
+                const int rr = w * 128 + row, rho = C.rt * RM + rr, t = rho / G, hd = C.h * G + rho - t * G;
+                float* const part = part_of<D, RM>(a, me, tile0 == 0 ? 1 : 0);
+                const float unit = ex2(ref), scale = whole ? (l > 0.0f || l != l ? 1.0f / l : 0.0f) : 1.0f;
+                const bool wild = wilds[units & 7] == units + 1;
+#pragma unroll 1
+                for (int c = 0; c < D / 32; ++c) {
+                    uint32_t o[32];
+                    tmem_load(o, om + c * 32);
+                    if (row < rows) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * unit * scale);
+                        if (wild) {
+                            // values that are not finite, of the tokens that this row sees
+                            for (int x = 0; x < C.T; ++x) {
+                                if (!(see >> x & 1)) continue;
+                                const unsigned short* p = reinterpret_cast<const unsigned short*>(
+                                    a.tok.v + ((long long)(C.lo + x) * a.tok.v_stride + C.h * D + c * 32) * 2);
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) {
+                                    const float y = Num<T>::unpack(p[i]).x;
+                                    if (y - y != 0.0f) o[i] = __float_as_uint(__uint_as_float(o[i]) + y);
+                                }
+                            }
+                        }
+                        if (whole) {
+                            uint4* const d = reinterpret_cast<uint4*>(
+                                a.out + ((C.lo + t) * a.out_stride + (long long)hd * D + c * 32) * 2);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                uint32_t q[4];
+#pragma unroll
+                                for (int k = 0; k < 4; ++k)
+                                    q[k] = Num<T>::pack(__uint_as_float(o[i * 8 + k * 2]), __uint_as_float(o[i * 8 + k * 2 + 1]));
+                                d[i] = make_uint4(q[0], q[1], q[2], q[3]);
+                            }
+                        } else {
+                            // four columns of all rows together: neighbouring threads' stores meet
+                            uint4* const d = reinterpret_cast<uint4*>(part + RM * 2) + c * 8 * RM + rr;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                d[i * RM] = make_uint4(o[i * 4], o[i * 4 + 1], o[i * 4 + 2], o[i * 4 + 3]);
+                        }
+                    }
+                }
+                tc_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(sm0 + L::ofree + w * 8);
+                if (row < rows) {
+                    if (!whole) *reinterpret_cast<float2*>(part + rr * 2) = make_float2(m, l);
+                    else if (a.lse) a.lse[(long long)(C.lo + t) * (H * G) + hd] = (m + log2f(l)) * LN2;
+                }
+                if (!whole) {
+                    int first, last;
+                    ax.sharers(C, first, last);
+                    // (a row's parts come from warps of one number in their CTAs: no other warp is
+                    // waited for)
+                    int* const arrived = a.arrived + first * ATTEND_WORKERS_PER_SM + warp;
+                    __threadfence();
+                    __syncwarp();
+                    int count = 0;
+                    if (lane == 0) count = atomicAdd(arrived, 1);
+                    count = __shfl_sync(0xffffffffu, count, 0);
+                    if (count == last - first && lane == 0) *arrived = 0;
+                    if (count == last - first && row < rows) {
+                        __threadfence();
+                        join_row<T, D, RM>(a, C, first, last, rr, t, hd);
+                    }
+                }
+            }
+            C = next;
+            if (j + 1 < n && !unit_ends) advance<KT, RM, KT>(a, C, pre);
+        }
+    }
+    if (!ok) *late = 1;
+    tc_before();
+    __syncthreads();
+    tc_after();
+    if (*late) {
+        // products, loads and stores of tensor memory may be in flight
+        if (warp == 4 * MT) {
+            if (elected()) tc_commit(sm0 + L::over);
+            __syncwarp();
+            wait(sm0 + L::over, 0);
+        } else if (warp < 4 * MT) {
+            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+            tmem_stored();
+        }
+        __syncthreads();
+    }
+    if (warp == 0) tmem_free(tm, 512);
+}
+
+template <typename T, int D>
+cudaError_t launch(const Attend8Args& a, int sms, cudaStream_t st)
+{
+    constexpr int MT = D < 256 ? 2 : 1;
+    using L = Many8<D, MT>;
+    constexpr int most = L::bytes(ALADDIN_WORKER_MAX_REQUESTS);
+    static_assert(most <= 227 * 1024, "shared memory of a CTA");
+    cudaError_t e = allow_smem<k_attend8_many<T, D, MT>>(most);
+    if (e != cudaSuccess) return e;
+    k_attend8_many<T, D, MT><<<sms, L::WARPS * 32, L::bytes(a.tok.n_req), st>>>(a);
+    return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t launch_dim(const Attend8Args& a, int dim, int sms, cudaStream_t st)
+{
+    switch (dim) {
+        case 64: return launch<T, 64>(a, sms, st);
+        case 96: return launch<T, 96>(a, sms, st);
+        case 128: return launch<T, 128>(a, sms, st);
+        case 256: return launch<T, 256>(a, sms, st);
+    }
+    return cudaErrorInvalidValue;
+}
+
+}  // namespace
+}  // namespace wk
+
+cudaError_t launch_attend8_many(const Attend8Args& a, int dtype, int dim, int sms, cudaStream_t st)
+{
+    return dtype == ALADDIN_BF16 ? wk::launch_dim<__nv_bfloat16>(a, dim, sms, st)
+                                 : wk::launch_dim<__half>(a, dim, sms, st);
+}
+
+}  // namespace aladdin

@@ -167,6 +167,8 @@ cudaError_t launch_attend_few(const AttendArgs& a, int dtype, int dim, int sms, 
 cudaError_t launch_attend_many(const AttendArgs& a, int dtype, int dim, int sms, cudaStream_t st);
 cudaError_t launch_attend(const AttendArgs& a, int dtype, int dim, int sms, cudaStream_t st);
 cudaError_t launch_accept(const AcceptArgs& a, int dtype, int dim, int sms, cudaStream_t st);
+cudaError_t launch_attend8_few(const Attend8Args& a, int dtype, int dim, int sms, cudaStream_t st);
+cudaError_t launch_attend8_many(const Attend8Args& a, int dtype, int dim, int sms, cudaStream_t st);
 cudaError_t launch_attend8(const Attend8Args& a, int dtype, int dim, int sms, cudaStream_t st);
 cudaError_t launch_rotate(const RotateArgs& a, int dtype, int dim, int sms, cudaStream_t st);
 cudaError_t launch_append(const AppendArgs& a, int dtype, int dim, int sms, cudaStream_t st);

@@ -167,6 +167,20 @@ def test_attend8_long(A, kind, q_heads, kv_heads, dim, new):  # noqa: F811
     check_attend8(case, out, lse)
 
 
+@pytest.mark.parametrize("kind,q_heads,kv_heads,dim,new", [("bf16", 64, 8, 128, 40), ("f16", 16, 8, 64, 40), ("bf16", 24, 8, 96, 60),
+                                                           ("f16", 8, 8, 256, 30), ("bf16", 40, 8, 128, 30), ("f16", 16, 8, 128, 3),
+                                                           ("bf16", 8, 8, 64, 2), ("f16", 8, 8, 256, 1)])
+def test_attend8_many_units(A, kind, q_heads, kv_heads, dim, new):  # noqa: F811
+    """Warps and CTAs with several units each, of one and of two row tiles in turn, and more tiles than their rings hold."""
+    rng = np.random.default_rng(new)
+    n = 70
+    case = make8(kind, q_heads, kv_heads, dim, 32, rng.integers(0, 900, n).tolist(), rng.integers(0, new + 1, n).tolist(), 32)
+    d = Dev8(A, case)
+    out, lse = d.worker.attend(d.kv, d.tok)
+    assert d.worker.status() == 0
+    check_attend8(case, out, lse)
+
+
 def test_attend8_chains(A):  # noqa: F811
     case = make8("bf16", 8, 2, 128, 16, [33, 0, 200], [5, 1, 64], trees=False)
     d = Dev8(A, case)
