@@ -30,10 +30,10 @@ struct Many8 {
     static constexpr int TILE = HALVES * KT * 128;       // keys or values of a tile, half precision
     static constexpr int NB = D == 256 ? 4 : 8;          // of them in the ring
     static constexpr int CPT = HALVES * KT / 32;         // 16 codes each: what a converting thread has of them
-    static constexpr int NR = D == 256 ? 4 : 8;          // codes in flight: keys or values of a tile
-    static constexpr int RAW = CPT * 128 * 16;
+    static constexpr int NR = D == 256 ? 2 : 4;          // tiles of codes in flight
+    static constexpr int RAW = CPT * 128 * 16;           // keys or values of one
     static constexpr int raw = NB * TILE;
-    static constexpr int bars = raw + NR * RAW;
+    static constexpr int bars = raw + NR * 2 * RAW;
     static constexpr int full = bars, empty = full + NB * 8, qready = empty + NB * 8, sready = qready + 16,
                          pready = sready + 24, odone = pready + 16, ofree = odone + 16, over = ofree + 16,
                          tmem = over + 8;
@@ -93,7 +93,8 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
     Info* const infos = reinterpret_cast<Info*>(sm + L::info);
     volatile int* const wilds = reinterpret_cast<volatile int*>(sm + L::wild);
     volatile int* const late = reinterpret_cast<volatile int*>(sm + L::late);
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    // (the warp's number by one lane: what follows from it is the same for all lanes, and the compiler sees it)
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     const int G = a.kv.group, H = a.kv.kv_heads;
 
     if (sm0 & 1023) {  // the operands' layout wants it
@@ -136,7 +137,8 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
 
     // A wait that runs out is recorded and ends its warp's part; the others' waits run
     // out after it (no warps meet at a barrier without a limit before the end), and all meet at
-    // the end, where what is in flight is waited for and tensor memory is freed.
+    // the end, where what is in flight is waited for and tensor memory is freed. Whoever waits for a
+    // barrier waits for all of its phases.
     auto wait = [&](uint32_t bar, int phase) -> bool {
         if (mbar_wait(bar, phase & 1)) return true;
         atomicOr(a.err, WORKER_TIMEOUT);
@@ -144,17 +146,25 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
     };
     // row tiles of the unit under u, of MT at most
     auto active = [&](const Cursor& u) { return MT == 2 && u.T * G - u.rt * RM > 128 ? 2 : 1; };
-    // the barrier of the scores of row tile w, in place s: whoever waits for one waits for all of its phases
-    auto scored_bar = [&](bool both, int w, int s) { return both && w ? 2 : s; };
+    // to the next unit
+    auto next_unit = [&](Cursor& u) {
+        u.tile = u.c - 1;
+        advance<KT, RM, KT>(a, u, pre);
+    };
     bool ok = true;  // no wait of this warp ran out
 
+    // Every role goes over the units of the range, and in each over its tiles; tile `done` + t of the range has place
+    // (done + t) % NR of the codes, 2 (done + t) % NB and the one behind it of the ring.
     if (warp >= 4 * MT + 1) {
         // ------------------------------------------------------------ conversions
         const int ct = tid - (4 * MT + 1) * 32, cw = ct >> 5, r0 = ct >> 2, ch = ct & 3;  // row of 32, chunk of a half
         float* const rscale = reinterpret_cast<float*>(sm + L::rscale);
         volatile int* const rvalid = reinterpret_cast<volatile int*>(sm + L::rvalid);
         const uint32_t raw0 = sm0 + L::raw + ct * 16;
+        // the place of this thread's first 8 channels of row r0 in a tile, and of the next 8
+        const int to0 = r0 * 128 + (((ch * 2) ^ (r0 & 7)) << 4), to1 = r0 * 128 + (((ch * 2 + 1) ^ (r0 & 7)) << 4);
         Cursor F = C;  // the tile whose codes are fetched
+        int fetched = 0;
         // pages of this thread's rows of the tile under F and, lanes 0 .. 7 of the first warp, of the block whose
         // scale they fetch, as the table has them
         int page[KT / 32], spage = 0;
@@ -163,73 +173,73 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
 #pragma unroll
             for (int p = 0; p < KT / 32; ++p) {
                 const int key = F.tile * KT + p * 32 + r0;
-                page[p] = key < F.len ? row[key >> a.kv.page_shift] : 0;
+                page[p] = key < F.len ? row[key >> a.kv.page_shift] : -1;
             }
             const int key = F.tile * KT + (lane & 3) * 16;
-            spage = cw == 0 && lane < 8 && key < F.len ? row[key >> a.kv.page_shift] : 0;
+            spage = cw == 0 && lane < 8 && key < F.len ? row[key >> a.kv.page_shift] : -1;
         };
         pages();
-        // codes of half i, keys or values of tile i / 2, under F
-        auto fetch = [&](int i) {
-            if (i < 2 * n) {
+        // the codes of the tile under F; then F goes on
+        auto fetch = [&]() {
+            if (fetched < n) {
                 const int key0 = F.tile * KT, own = F.len - key0;
                 if (own > 0) {
-                    const char* const pool = i & 1 ? a.kv.v : a.kv.k;
-                    const uint32_t d = raw0 + i % NR * L::RAW;
+                    const uint32_t d = raw0 + fetched % NR * (2 * L::RAW);
 #pragma unroll
                     for (int p = 0; p < KT / 32; ++p) {
-                        const int row = p * 32 + r0;
-                        const bool in = row < own && (unsigned)page[p] < (unsigned)a.kv.pages;
+                        const bool in = (unsigned)page[p] < (unsigned)a.kv.pages;
                         const long long e = in ? page[p] * a.kv.page_stride + F.h * a.kv.head_stride +
-                                                     ((key0 + row) & (a.kv.page - 1)) * a.kv.token_stride + ch * 16
+                                                     ((key0 + p * 32 + r0) & (a.kv.page - 1)) * a.kv.token_stride + ch * 16
                                                : 0;
                         // (weights of 0 meet the codes of rows that hold no key: zeros)
 #pragma unroll
-                        for (int h = 0; h < L::HALVES; ++h)
-                            if (D % 64 == 0 || h * 64 + ch * 16 < D)
-                                cp16(d + (p * L::HALVES + h) * 2048, pool + e + (in ? h * 64 : 0), in);
+                        for (int h = 0; h < L::HALVES; ++h) {
+                            if (D % 64 == 0 || h * 64 + ch * 16 < D) {
+                                cp16(d + (p * L::HALVES + h) * 2048, a.kv.k + e + (in ? h * 64 : 0), in);
+                                cp16(d + L::RAW + (p * L::HALVES + h) * 2048, a.kv.v + e + (in ? h * 64 : 0), in);
+                            }
+                        }
                     }
-                    if ((i & 1) == 0 && cw == 0) {
+                    if (cw == 0) {
                         const int x = lane & 3, key = key0 + x * 16;
-                        const bool in = lane < 8 && x * 16 < own && (unsigned)spage < (unsigned)a.kv.pages;
+                        const bool in = (unsigned)spage < (unsigned)a.kv.pages;
                         if (lane < 4 && x * 16 < own && !in) atomicOr(a.err, WORKER_BAD_INPUT);
                         const long long e = in ? ((long long)spage * H + F.h) * a.scales.per_page +
                                                      ((key & (a.kv.page - 1)) >> a.scales.block_shift)
                                                : 0;
-                        if (lane < 8) cp4(sm0 + L::rscale + (i / 2 % 8) * 32 + lane * 4, (lane < 4 ? a.scales.k : a.scales.v) + e, in);
+                        if (lane < 8) cp4(sm0 + L::rscale + (fetched & 7) * 32 + lane * 4, (lane < 4 ? a.scales.k : a.scales.v) + e, in);
                         const unsigned valid = __ballot_sync(0xffffffffu, in) & 15;
-                        if (lane == 0) rvalid[i / 2 % 8] = (int)valid;
+                        if (lane == 0) rvalid[fetched & 7] = (int)valid;
                     }
                 }
-                if (i & 1 && i + 1 < 2 * n) {
+                if (++fetched < n) {
                     advance<KT, RM, KT>(a, F, pre);
                     pages();
                 }
             }
             cp_commit();
         };
+        int units = 0, i = -(NR - 1);  // the tile that is converted
+        Cursor u = C;
 #pragma unroll 1
-        for (int i = 0; i < NR - 1; ++i) fetch(i);
-        int units = -1, vtop = 0;
-        for (int j = 0; j < n && ok; ++j) {
-            if (j == 0 || C.tile == 0) ++units;
-            const bool cached = C.tile * KT < C.len;
-            Info& info = infos[j & 7];
+        for (; i < n; ++i) {
+            fetch();
+            if (i < 0) continue;
+            const bool cached = u.tile * KT < u.len;
+            Info& info = infos[i & 7];
+            cp_wait<NR - 1>();
+            int vtop = 0;
 #pragma unroll 1
             for (int part = 0; part < 2; ++part) {
-                const int i = 2 * j + part, slot = i % NB;
-                fetch(i + NR - 1);
-                if (i >= NB) ok = __all_sync(0xffffffffu, wait(sm0 + L::empty + slot * 8, i / NB - 1));
+                const int half = 2 * i + part, slot = half % NB;
+                if (half >= NB) ok = __all_sync(0xffffffffu, wait(sm0 + L::empty + slot * 8, half / NB - 1));
                 if (!ok) break;
-                cp_wait<NR - 1>();
                 char* const d = sm + slot * L::TILE;
-                // the place of 8 channels, chunk c of a row
-                auto at = [&](int row, int c) { return (c >> 3) * (KT * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4); };
                 if (cached) {
                     if (part == 0 && cw == 0) {
                         __syncwarp();
-                        const float s = lane < 8 ? rscale[(j & 7) * 8 + lane] : 0.0f;
-                        const int valid = rvalid[j & 7];
+                        const float s = lane < 8 ? rscale[(i & 7) * 8 + lane] : 0.0f;
+                        const int valid = rvalid[i & 7];
                         // (a factor that is not 0: scores of 0 stay 0, and those that do not count -inf)
                         if (lane < 4) info.k[lane] = s < 1e-30f ? 1e-30f : s;
                         float lv = -INFINITY;
@@ -242,17 +252,16 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                         if (lane < 4) info.top[lane] = lv;
                         if (lane == 0) info.valid = valid;
                     }
-                    const char* const src = sm + L::raw + i % NR * L::RAW + ct * 16;
+                    const char* const src = sm + L::raw + (i % NR * 2 + part) * L::RAW + ct * 16;
 #pragma unroll
                     for (int p = 0; p < KT / 32; ++p) {
 #pragma unroll
                         for (int h = 0; h < L::HALVES; ++h) {
                             if (D % 64 == 0 || h * 64 + ch * 16 < D) {
                                 const uint4 c = *reinterpret_cast<const uint4*>(src + (p * L::HALVES + h) * 2048);
-                                const int row = p * 32 + r0;
-                                *reinterpret_cast<uint4*>(d + at(row, h * 8 + ch * 2)) =
+                                *reinterpret_cast<uint4*>(d + to0 + h * (KT * 128) + p * (32 * 128)) =
                                     make_uint4(half2_lo(c.x), half2_hi(c.x), half2_lo(c.y), half2_hi(c.y));
-                                *reinterpret_cast<uint4*>(d + at(row, h * 8 + ch * 2 + 1)) =
+                                *reinterpret_cast<uint4*>(d + to1 + h * (KT * 128) + p * (32 * 128)) =
                                     make_uint4(half2_lo(c.z), half2_hi(c.z), half2_lo(c.w), half2_hi(c.w));
                             }
                         }
@@ -262,28 +271,29 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                     constexpr int CH = D / 8;
                     const char* const base = part ? a.tok.v : a.tok.k;
                     const long long stride = (part ? a.tok.v_stride : a.tok.k_stride) * 2;
-                    const char* const src = base + C.lo * stride + C.h * D * 2;
+                    const char* const src = base + u.lo * stride + u.h * D * 2;
                     if (BF16 && part == 0) {
                         // the largest exponents of two halves of a row a lane, of keys and values, not of infinities and NaN
                         const int row = cw * 16 + (lane >> 1);
                         int top[2] = {0, 0};
-                        if (row < C.T) {
-#pragma unroll
+                        if (row < u.T) {
+#pragma unroll 1
                             for (int e = 0; e < 2; ++e) {
-                                const char* const q = (e ? a.tok.v + (C.lo + row) * a.tok.v_stride * 2 : a.tok.k + (C.lo + row) * a.tok.k_stride * 2) +
-                                                      (C.h * D + (lane & 1) * (D / 2)) * 2;
+                                const char* const q = (e ? a.tok.v + (u.lo + row) * a.tok.v_stride * 2 : a.tok.k + (u.lo + row) * a.tok.k_stride * 2) +
+                                                      (u.h * D + (lane & 1) * (D / 2)) * 2;
+                                int most = 0;
 #pragma unroll 4
                                 for (int c = 0; c < D / 16; ++c) {
                                     const uint4 v = *reinterpret_cast<const uint4*>(q + c * 16);
-                                    top[e] = exponent(Num<T>::tame(v.x), exponent(Num<T>::tame(v.y), exponent(Num<T>::tame(v.z), exponent(Num<T>::tame(v.w), top[e]))));
+                                    most = exponent(Num<T>::tame(v.x), exponent(Num<T>::tame(v.y), exponent(Num<T>::tame(v.z), exponent(Num<T>::tame(v.w), most))));
                                 }
+                                if (e) top[1] = most;
+                                else top[0] = most;
                             }
                         }
                         top[0] = max(top[0], __shfl_xor_sync(0xffffffffu, top[0], 1));
                         top[1] = max(top[1], __shfl_xor_sync(0xffffffffu, top[1], 1));
-                        vtop = top[1];
-                        const int clamped = min(max(top[1], 15), 254) - 141;
-                        float lv = row < C.T ? (float)clamped : -INFINITY;
+                        float lv = row < u.T ? (float)(min(max(top[1], 15), 254) - 141) : -INFINITY;
                         if ((lane & 1) == 0) {
                             info.k[row] = half_back(top[0]);
                             info.lv[row] = lv;
@@ -291,20 +301,18 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
 #pragma unroll
                         for (int x = 16; x; x >>= 1) lv = fmaxf(lv, __shfl_xor_sync(0xffffffffu, lv, x));
                         if (lane == 0) info.top[cw] = lv;
-                        // (the keys' factor is needed now, the values' in the next part)
-                        top[1] = top[0];
-                        vtop |= top[0] << 16;
+                        vtop = top[1] | top[0] << 16;  // (the keys' is needed now, the values' in the next part)
                     } else if (part == 0) {
                         if (lane < 16) info.k[cw * 16 + lane] = 1.0f, info.lv[cw * 16 + lane] = 0.0f;
                         if (lane == 0) info.top[cw] = 0.0f;
                     }
-                    if (part == 0 && cw == 0 && lane == 0) info.valid = 15;
+                    if (part == 0 && cw == 0 && lane == 0) info.valid = 0;
                     bool w = false;
 #pragma unroll 1
                     for (int x = lane; x < 16 * CH; x += 32) {
                         const int row = x / CH, c = x - row * CH, t = cw * 16 + row;
                         uint4 v = make_uint4(0, 0, 0, 0);
-                        if (t < C.T) v = *reinterpret_cast<const uint4*>(src + t * stride + c * 16);
+                        if (t < u.T) v = *reinterpret_cast<const uint4*>(src + t * stride + c * 16);
                         if (part && (Num<T>::wild(v.x) || Num<T>::wild(v.y) || Num<T>::wild(v.z) || Num<T>::wild(v.w))) {
                             w = true;
                             v.x = Num<T>::tame(v.x), v.y = Num<T>::tame(v.y), v.z = Num<T>::tame(v.z), v.w = Num<T>::tame(v.w);
@@ -315,7 +323,7 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                             const float f = half_factor(part ? both & 0xffff : both >> 16);
                             v = make_uint4(to_half(v.x, f), to_half(v.y, f), to_half(v.z, f), to_half(v.w, f));
                         }
-                        *reinterpret_cast<uint4*>(d + at(t, c)) = v;
+                        *reinterpret_cast<uint4*>(d + (c >> 3) * (KT * 128) + t * 128 + (((c & 7) ^ (t & 7)) << 4)) = v;
                     }
                     if (w) wilds[units & 7] = units + 1;
                 }
@@ -323,114 +331,81 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                 __syncwarp();
                 if (lane == 0) mbar_arrive(sm0 + L::full + slot * 8);
             }
-            if (j + 1 < n) advance<KT, RM, KT>(a, C, pre);
+            if (!ok) break;
+            if (u.tile + 1 == u.c) ++units;
+            if (i + 1 < n) advance<KT, RM, KT>(a, u, pre);
         }
         cp_wait<0>();
     } else if (warp == 4 * MT) {
         // ------------------------------------------------------------ products
+        // Steps of a tile and a row tile each. The scores of a step go to place step % 2; they are formed when the
+        // products with values of the step two before have been started.
         constexpr uint32_t qk = product<__half>(KT, false), pv = product<__half>(D, true);
         const bool leader = elected();
-        Cursor N = C;  // the tile whose scores are formed next
-        int scored = 0, local = 0, run[2] = {0, 0}, starts[2] = {0, 0}, asked[2] = {0, 0};
-        // waits for the keys (and queries) of the tile under N
-        auto enter_tile = [&]() {
-            if (scored == 0 || N.tile == 0) {
-                local = 0;
-#pragma unroll
-                for (int w = 0; w < MT; ++w)
-                    if (w < active(N)) ok = ok && wait(sm0 + L::qready + w * 8, asked[w]++);
-            }
-            ok = __all_sync(0xffffffffu, ok && wait(sm0 + L::full + 2 * scored % NB * 8, 2 * scored / NB));
-            tc_after();
-        };
-        // its scores for row tile w
-        auto scores = [&](int w) {
-            const uint32_t k0 = operand_lo(sm0 + 2 * scored % NB * L::TILE, 0);
-            const int s = active(N) == 2 ? w : local & 1;
-            if (leader) {
-#pragma unroll
-                for (int x = 0; x < D / 16; ++x)
-                    tc_mma_ts(tm + L::s0 + s * KT, tm + L::q0 + w * (D / 2) + x * 8,
-                              whole(k0 + ((x >> 2) * KT * 128 + (x & 3) * 32) / 16, OPERAND_HI), qk, x > 0);
-                tc_commit(sm0 + L::sready + scored_bar(active(N) == 2, w, s) * 8);
-            }
-            __syncwarp();
-        };
-        // the tile under N has its scores on the way
-        auto leave_tile = [&]() {
-            if (leader) tc_commit(sm0 + L::empty + 2 * scored % NB * 8);
-            __syncwarp();
-            ++local;
-            if (++scored < n) advance<KT, RM, KT>(a, N, pre);
-        };
-        auto tile_scores = [&]() {
-            enter_tile();
-            if (!ok) return;
-#pragma unroll
-            for (int w = 0; w < MT; ++w)
-                if (w < active(N)) scores(w);
-            leave_tile();
-        };
-        tile_scores();
-        int place = 0;  // of the weights, with one row tile
-        for (int j = 0; j < n && ok; ++j) {
-            const bool more = j + 1 < n, turns = C.tile + 1 == C.c;
-            const bool start = j == 0 || C.tile == 0;
-            const int both = active(C) == 2;
-            if (start) place = 0;
-            if (!both && more && !turns) {
-                tile_scores();
-                if (!ok) break;
-            }
-            const int v = 2 * j + 1;
-#pragma unroll
-            for (int w = 0; w < MT; ++w) {
-                if (w == 0 || both) {
-                    ok = ok && wait(sm0 + L::pready + w * 8, run[w]++);
-                    ok = ok && wait(sm0 + L::full + v % NB * 8, v / NB);
-                    if (start && starts[w]++ > 0) ok = ok && wait(sm0 + L::ofree + w * 8, starts[w] - 2);
+        Cursor u = C;
+        int asked[2] = {0, 0}, run[2] = {0, 0}, started[2] = {0, 0};
+#pragma unroll 1
+        for (int done = 0; done < n && ok;) {
+            const int count = min(u.c - u.tile, n - done), act = active(u), steps = count * act;
+            if (MT == 2 && act == 2) ok = wait(sm0 + L::qready + 8, asked[1]++);
+            ok = ok && wait(sm0 + L::qready, asked[0]++);
+#pragma unroll 1
+            for (int k = -2; k < steps; ++k) {
+                if (k >= 0) {
+                    // out += P V of step k
+                    const int w = MT == 2 && act == 2 ? k & 1 : 0, t = MT == 2 && act == 2 ? k >> 1 : k, v = 2 * (done + t) + 1;
+                    ok = ok && wait(sm0 + L::pready + w * 8, w ? run[1]++ : run[0]++);
+                    if (w == 0) ok = ok && wait(sm0 + L::full + v % NB * 8, v / NB);
+                    if (t == 0) {
+                        const int before = w ? started[1]++ : started[0]++;
+                        if (before > 0) ok = ok && wait(sm0 + L::ofree + w * 8, before - 1);
+                    }
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
                     tc_after();
-                    const uint32_t v0 = operand_lo(sm0 + v % NB * L::TILE, KT * 128),
-                                   p = tm + L::s0 + (both ? w : place) * KT;
+                    const uint32_t v0 = operand_lo(sm0 + v % NB * L::TILE, KT * 128), at = tm + L::s0 + (k & 1) * KT,
+                                   o = tm + L::o0 + w * (L::HALVES * 64);
                     if (leader) {
 #pragma unroll
                         for (int x = 0; x < KT / 16; ++x)
-                            tc_mma_ts(tm + L::o0 + w * (L::HALVES * 64), p + x * 8,
-                                      whole(v0 + x * 2048 / 16, OPERAND_HI), pv, !start || x > 0);
+                            tc_mma_ts(o, at + x * 8, whole(v0 + x * 2048 / 16, OPERAND_HI), pv, t > 0 || x > 0);
                         tc_commit(sm0 + L::odone + w * 8);
+                        if (w == act - 1) tc_commit(sm0 + L::empty + v % NB * 8);
                     }
                     __syncwarp();
-                    if (both && more && !turns) {
-                        if (w == 0) {
-                            enter_tile();
-                            if (!ok) break;
-                        }
-                        scores(w);
+                }
+                if (k + 2 < steps) {
+                    // S = Q K' of step k + 2
+                    const int y = k + 2, w = MT == 2 && act == 2 ? y & 1 : 0, t = MT == 2 && act == 2 ? y >> 1 : y, i = 2 * (done + t);
+                    if (w == 0) ok = __all_sync(0xffffffffu, ok && wait(sm0 + L::full + i % NB * 8, i / NB));
+                    if (!ok) break;
+                    tc_after();
+                    const uint32_t k0 = operand_lo(sm0 + i % NB * L::TILE, 0), at = tm + L::s0 + (y & 1) * KT,
+                                   q = tm + L::q0 + w * (D / 2);
+                    if (leader) {
+#pragma unroll
+                        for (int x = 0; x < D / 16; ++x)
+                            tc_mma_ts(at, q + x * 8, whole(k0 + ((x >> 2) * KT * 128 + (x & 3) * 32) / 16, OPERAND_HI), qk, x > 0);
+                        tc_commit(sm0 + L::sready + ((y & 1) + w) * 8);
+                        if (w == act - 1) tc_commit(sm0 + L::empty + i % NB * 8);
                     }
+                    __syncwarp();
                 }
             }
-            if (!ok) break;
-            if (leader) tc_commit(sm0 + L::empty + v % NB * 8);
-            __syncwarp();
-            if (both && more && !turns) leave_tile();
-            if (more && turns) tile_scores();
-            place ^= 1;
-            if (more) advance<KT, RM, KT>(a, C, pre);
+            done += count;
+            if (done < n) next_unit(u);
         }
         __syncwarp();
     } else {
         // ------------------------------------------------------------ softmax
         const int w = warp >> 2, row = tid & 127;
         const uint32_t lanes = (uint32_t)(warp & 3) * 32u << 16, om = tm + lanes + L::o0 + w * (L::HALVES * 64);
-        float m = -INFINITY, l = 0.0f, ref = -1000.0f, factor = 0.0f;
-        unsigned long long see = 0;
-        int units = -1, tile0 = 0, scored[3] = {0, 0, 0}, done = 0, local = 0;
+        float factor = 0.0f;  // of this row's scores
+        int scored[3] = {0, 0, 0}, weighed = 0;
         // this row's queries of the unit under u, 32 channels a time, into tensor memory
         auto queries = [&](const Cursor& u) {
-            const int rho = u.rt * RM + w * 128 + row, t = rho / G;
             if (u.T * G - u.rt * RM <= w * 128) return;
+            const int rho = u.rt * RM + w * 128 + row, t = rho / G;
             const bool live = rho < u.T * G;
             const uint4* const src = reinterpret_cast<const uint4*>(
                 a.tok.q + ((u.lo + (live ? t : 0)) * a.tok.q_stride + (long long)(u.h * G + (live ? rho - t * G : 0)) * D) * 2);
@@ -464,161 +439,161 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
             __syncwarp();
             if (lane == 0) mbar_arrive(sm0 + L::qready + w * 8);
         };
-        queries(C);
-        for (int j = 0; j < n && ok; ++j) {
-            const bool start = j == 0 || C.tile == 0, unit_ends = C.tile + 1 == C.c;
-            const int rows = C.T * G - C.rt * RM - w * 128;
-            const bool both = active(C) == 2;
-            if (start) {
-                ++units;
-                tile0 = C.tile;
-                local = 0;
-            }
-            const int s = both ? w : local & 1, bar = scored_bar(both, w, s);
-            ++local;
-            if (rows > 0) {
-                if (start) {
-                    const int rho = C.rt * RM + w * 128 + row;
-                    see = ancestors(a, C, row < rows ? rho / G : 0);
-                }
-                ok = __all_sync(0xffffffffu, wait(sm0 + L::sready + bar * 8, bar == 2 ? scored[2]++ : bar ? scored[1]++ : scored[0]++));
-                if (!ok) break;
-                tc_after();
-                const uint32_t st = tm + lanes + L::s0 + s * KT;
-                uint32_t v[2][32];
-                tmem_start(v[0], st);
-                tmem_start(v[1], st + 32);
-                const Info& info = infos[j & 7];
-                const int own = C.len - C.tile * KT;  // cached keys from the tile's start
-                float f[4], lv[4];
-                {
-                    const float4 x = *reinterpret_cast<const float4*>(info.k), y = *reinterpret_cast<const float4*>(info.lv);
-                    f[0] = x.x * factor, f[1] = x.y * factor, f[2] = x.z * factor, f[3] = x.w * factor;
-                    lv[0] = y.x, lv[1] = y.y, lv[2] = y.z, lv[3] = y.w;
-                }
-                const float4 tops = *reinterpret_cast<const float4*>(info.top);
-                const float scale_top = fmaxf(fmaxf(tops.x, tops.y), fmaxf(tops.z, tops.w));
-                const int valid = info.valid;
-                tmem_loaded(v[0]);
-                tmem_loaded(v[1]);
-                if (own < KT || valid != 15) {
-                    // what this row sees
-                    uint32_t vis[2];
-                    if (own > 0) {
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const int left = own - h * 32;
-                            vis[h] = ((valid >> (h * 2) & 1 ? 0xffffu : 0u) | (valid >> (h * 2) & 2 ? 0xffff0000u : 0u)) &
-                                     (left >= 32 ? 0xffffffffu : left > 0 ? (1u << left) - 1 : 0u);
-                        }
-                    } else {
-                        vis[0] = (uint32_t)see;
-                        vis[1] = (uint32_t)(see >> 32);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 64; ++i) {
-                        const float g = own > 0 ? f[i / 16] : info.k[i] * factor;
-                        v[i / 32][i % 32] = vis[i / 32] >> (i % 32) & 1 ? __float_as_uint(__uint_as_float(v[i / 32][i % 32]) * g) : 0xff800000u;
-                    }
-                    f[0] = f[1] = f[2] = f[3] = 1.0f;
-                }
-                float top = -INFINITY;
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    float t0 = -INFINITY, t1 = -INFINITY;
-#pragma unroll
-                    for (int i = 0; i < 16; i += 4) {
-                        const uint32_t* const y = &v[x / 2][x % 2 * 16 + i];
-                        t0 = fmaxf(fmaxf(t0, __uint_as_float(y[0])), __uint_as_float(y[1]));
-                        t1 = fmaxf(fmaxf(t1, __uint_as_float(y[2])), __uint_as_float(y[3]));
-                    }
-                    top = fmaxf(top, fmaxf(t0, t1) * f[x]);
-                }
-                if (start) {
-                    m = top;
-                    l = 0.0f;
-                    ref = fmaxf(scale_top, -1000.0f);
-                } else {
-                    const bool grown = top > m + 8.0f;  // (always where m is -inf and top is not)
-                    const bool larger = scale_top > ref + 4.0f;
-                    if (larger || __any_sync(0xffffffffu, grown)) {
-                        // the weights of the tiles before are in the accumulator
-                        if (done) ok = __all_sync(0xffffffffu, wait(sm0 + L::odone + w * 8, done - 1));
-                        if (!ok) break;
-                        tc_after();
-                        float g = grown ? ex2(m - top) : 1.0f;
-                        if (grown) m = top;
-                        l *= g;
-                        if (larger) {
-                            g *= ex2(ref - scale_top);
-                            ref = scale_top;
-                        }
+        Cursor u = C;
+        queries(u);
+        int units = 0;
 #pragma unroll 1
-                        for (int c = 0; c < (D + 15) / 16; ++c) {
-                            uint32_t o[16];
-                            tmem_load16(o, om + c * 16);
+        for (int done = 0; done < n && ok;) {
+            const int count = min(u.c - u.tile, n - done), rows = u.T * G - u.rt * RM - w * 128, act = active(u);
+            Cursor next = u;
+            if (done + count < n) next_unit(next);
+            if (rows <= 0) {
+                if (done + count < n) queries(next);
+            } else {
+                const unsigned long long see = ancestors(a, u, row < rows ? (u.rt * RM + w * 128 + row) / G : 0);
+                float m = -INFINITY, l = 0.0f, ref = -1000.0f;
+                const int bar1 = MT == 2 && act == 2 ? 0 : 1;  // with one row tile the places alternate
+#pragma unroll 1
+                for (int t = 0; t < count; ++t) {
+                    const int s = bar1 ? t & 1 : w, bar = s + w;
+                    ok = __all_sync(0xffffffffu, wait(sm0 + L::sready + bar * 8, bar == 2 ? scored[2]++ : bar ? scored[1]++ : scored[0]++));
+                    if (!ok) break;
+                    tc_after();
+                    const uint32_t st = tm + lanes + L::s0 + s * KT;
+                    const Info& info = infos[(done + t) & 7];
+                    const int own = u.len - (u.tile + t) * KT;  // cached keys from the tile's start
+                    const int valid = info.valid;
+                    const bool special = own < KT || valid != 15;
+                    if (special) {
+                        // keys that are not seen or have scales of their own: scores are scaled in their place
+                        const float* ks = info.k;
+                        const int step = own > 0 ? 0 : 1;
+#pragma unroll 1
+                        for (int c = 0; c < 4; ++c) {
+                            uint32_t y[16];
+                            tmem_load16(y, st + c * 16);
+                            const int left = own - c * 16;
+                            const uint32_t vis = own <= 0 ? (uint32_t)(see >> (c * 16))
+                                                 : !(valid >> c & 1) ? 0u : left >= 16 ? 0xffffu : left > 0 ? (1u << left) - 1 : 0u;
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * g);
-                            tmem_store16(om + c * 16, o);
+                            for (int i = 0; i < 16; ++i)
+                                y[i] = vis >> i & 1 ? __float_as_uint(__uint_as_float(y[i]) * (ks[i * step] * factor)) : 0xff800000u;
+                            tmem_store16(st + c * 16, y);
+                            ks += step ? 16 : 1;
                         }
+                        tmem_stored();
                     }
-                }
-                const float base = m == -INFINITY ? 0.0f : m;
-                if (own > 0) {
+                    uint32_t v[2][32];
+                    tmem_start(v[0], st);
+                    tmem_start(v[1], st + 32);
+                    const float4 kf = *reinterpret_cast<const float4*>(info.k), lf = *reinterpret_cast<const float4*>(info.lv),
+                                 tops = *reinterpret_cast<const float4*>(info.top);
+                    const float scale_top = fmaxf(fmaxf(tops.x, tops.y), fmaxf(tops.z, tops.w));
+                    float f[4] = {kf.x * factor, kf.y * factor, kf.z * factor, kf.w * factor};
+                    if (special) f[0] = f[1] = f[2] = f[3] = 1.0f;
+                    tmem_loaded(v[0]);
+                    tmem_loaded(v[1]);
+                    float top = -INFINITY;
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
-                        const float at = relative(lv[x], ref), shift = at - base;
-                        const uint64_t ff = pair2(__float_as_uint(f[x]), __float_as_uint(f[x])),
-                                       bb = pair2(__float_as_uint(shift), __float_as_uint(shift));
-                        uint64_t sum = 0;
+                        float t0 = -INFINITY, t1 = -INFINITY;
 #pragma unroll
-                        for (int i = 0; i < 16; i += 2) {
-                            uint32_t* const y = &v[x / 2][x % 2 * 16 + i];
-                            const uint64_t z = fma2(pair2(y[0], y[1]), ff, bb);
-                            const float e0 = ex2(low2(z)), e1 = ex2(high2(z));
-                            sum = add2(sum, pair2(__float_as_uint(e0), __float_as_uint(e1)));
-                            v[x / 2][x % 2 * 8 + i / 2] = Num<__half>::pack(e0, e1);
+                        for (int i = 0; i < 16; i += 4) {
+                            const uint32_t* const y = &v[x / 2][x % 2 * 16 + i];
+                            t0 = fmaxf(fmaxf(t0, __uint_as_float(y[0])), __uint_as_float(y[1]));
+                            t1 = fmaxf(fmaxf(t1, __uint_as_float(y[2])), __uint_as_float(y[3]));
                         }
-                        l += (low2(sum) + high2(sum)) * ex2(-at);
+                        top = fmaxf(top, fmaxf(t0, t1) * f[x]);
                     }
-                } else {
+                    if (t == 0) {
+                        m = top;
+                        ref = fmaxf(scale_top, -1000.0f);
+                    } else {
+                        const bool grown = top > m + 8.0f;  // (always where m is -inf and top is not)
+                        const bool larger = scale_top > ref + 4.0f;
+                        if (larger || __any_sync(0xffffffffu, grown)) {
+                            // the weights of the tiles before are in the accumulator
+                            ok = __all_sync(0xffffffffu, wait(sm0 + L::odone + w * 8, weighed - 1));
+                            if (!ok) break;
+                            tc_after();
+                            float g = grown ? ex2(m - top) : 1.0f;
+                            if (grown) m = top;
+                            l *= g;
+                            if (larger) {
+                                g *= ex2(ref - scale_top);
+                                ref = scale_top;
+                            }
+#pragma unroll 1
+                            for (int c = 0; c < D / 16; ++c) {
+                                uint32_t o[16];
+                                tmem_load16(o, om + c * 16);
 #pragma unroll
-                    for (int i = 0; i < 64; i += 2) {
-                        float e[2];
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const float at = relative(info.lv[i + k], ref);
-                            e[k] = ex2(__uint_as_float(v[i / 32][i % 32 + k]) - base + at);
-                            l += e[k] * ex2(-at);
+                                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * g);
+                                tmem_store16(om + c * 16, o);
+                            }
                         }
-                        v[i / 32][i % 32 / 2] = Num<__half>::pack(e[0], e[1]);
                     }
+                    const float base = m == -INFINITY ? 0.0f : m;
+                    if (own > 0) {
+                        const float lv[4] = {lf.x, lf.y, lf.z, lf.w};
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            const float at = relative(lv[x], ref), shift = at - base;
+                            const uint64_t ff = pair2(__float_as_uint(f[x]), __float_as_uint(f[x])),
+                                           bb = pair2(__float_as_uint(shift), __float_as_uint(shift));
+                            uint64_t sum = 0;
+#pragma unroll
+                            for (int i = 0; i < 16; i += 2) {
+                                const uint32_t* const y = &v[x / 2][x % 2 * 16 + i];
+                                const uint64_t z = fma2(pair2(y[0], y[1]), ff, bb);
+                                const float e0 = ex2(low2(z)), e1 = ex2(high2(z));
+                                sum = add2(sum, pair2(__float_as_uint(e0), __float_as_uint(e1)));
+                                v[x / 2][x % 2 * 8 + i / 2] = Num<__half>::pack(e0, e1);
+                            }
+                            l += (low2(sum) + high2(sum)) * ex2(-at);
+                        }
+                        // (the scores of all 64 keys have been read)
+                        tmem_store16(st, *reinterpret_cast<const uint32_t(*)[16]>(&v[0][0]));
+                        tmem_store16(st + 16, *reinterpret_cast<const uint32_t(*)[16]>(&v[1][0]));
+                    } else {
+                        // new tokens: a scale each; weights lie where scores were that have been read
+#pragma unroll 1
+                        for (int c = 0; c < 4; ++c) {
+                            uint32_t y[16], p[8];
+                            tmem_load16(y, st + c * 16);
+#pragma unroll
+                            for (int i = 0; i < 16; i += 2) {
+                                float e[2];
+#pragma unroll
+                                for (int k = 0; k < 2; ++k) {
+                                    const float at = relative(info.lv[c * 16 + i + k], ref);
+                                    e[k] = ex2(__uint_as_float(y[i + k]) - base + at);
+                                    l += e[k] * ex2(-at);
+                                }
+                                p[i / 2] = Num<__half>::pack(e[0], e[1]);
+                            }
+                            tmem_store8(st + c * 8, p);
+                        }
+                    }
+                    tmem_stored();
+                    tc_before();
+                    // (the products of the tile before are done, so that the arrivals before these have been seen)
+                    if (weighed) ok = __all_sync(0xffffffffu, wait(sm0 + L::odone + w * 8, weighed - 1));
+                    if (!ok) break;
+                    if (lane == 0) mbar_arrive(sm0 + L::pready + w * 8);
+                    ++weighed;
                 }
-                // (the scores of all 64 keys have been read)
-                tmem_store16(st, *reinterpret_cast<const uint32_t(*)[16]>(&v[0][0]));
-                tmem_store16(st + 16, *reinterpret_cast<const uint32_t(*)[16]>(&v[1][0]));
-                tmem_stored();
-                tc_before();
-                // (the products of the tile before are done, so that the arrivals before these have been seen)
-                if (done) ok = __all_sync(0xffffffffu, wait(sm0 + L::odone + w * 8, done - 1));
                 if (!ok) break;
-                if (lane == 0) mbar_arrive(sm0 + L::pready + w * 8);
-                ++done;
-            }
-            Cursor next = C;
-            if (unit_ends && j + 1 < n) {
                 // the next unit's queries, while the last products run: this unit's scores are done
-                advance<KT, RM, KT>(a, next, pre);
-                queries(next);
-            }
-            if (rows > 0 && (unit_ends || j + 1 == n)) {
-                ok = __all_sync(0xffffffffu, wait(sm0 + L::odone + w * 8, done - 1));
+                const float unit = ex2(ref);
+                if (done + count < n) queries(next);
+                ok = __all_sync(0xffffffffu, wait(sm0 + L::odone + w * 8, weighed - 1));
                 if (!ok) break;
                 tc_after();
-                const bool whole = tile0 == 0 && unit_ends;
-                const int rr = w * 128 + row, rho = C.rt * RM + rr, t = rho / G, hd = C.h * G + rho - t * G;
-                float* const part = part_of<D, RM>(a, me, tile0 == 0 ? 1 : 0);
-                const float unit = ex2(ref), scale = whole ? (l > 0.0f || l != l ? 1.0f / l : 0.0f) : 1.0f;
+                const bool whole = u.tile == 0 && count == u.c;
+                const int rr = w * 128 + row, rho = u.rt * RM + rr, t = rho / G, hd = u.h * G + rho - t * G;
+                float* const part = part_of<D, RM>(a, me, u.tile == 0 ? 1 : 0);
+                const float scale = whole ? (l > 0.0f || l != l ? 1.0f / l : 0.0f) : 1.0f;
                 const bool wild = wilds[units & 7] == units + 1;
 #pragma unroll 1
                 for (int c = 0; c < D / 32; ++c) {
@@ -629,10 +604,10 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                         for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * unit * scale);
                         if (wild) {
                             // values that are not finite, of the tokens that this row sees
-                            for (int x = 0; x < C.T; ++x) {
+                            for (int x = 0; x < u.T; ++x) {
                                 if (!(see >> x & 1)) continue;
                                 const unsigned short* p = reinterpret_cast<const unsigned short*>(
-                                    a.tok.v + ((long long)(C.lo + x) * a.tok.v_stride + C.h * D + c * 32) * 2);
+                                    a.tok.v + ((long long)(u.lo + x) * a.tok.v_stride + u.h * D + c * 32) * 2);
 #pragma unroll
                                 for (int i = 0; i < 32; ++i) {
                                     const float y = Num<T>::unpack(p[i]).x;
@@ -642,7 +617,7 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                         }
                         if (whole) {
                             uint4* const d = reinterpret_cast<uint4*>(
-                                a.out + ((C.lo + t) * a.out_stride + (long long)hd * D + c * 32) * 2);
+                                a.out + ((u.lo + t) * a.out_stride + (long long)hd * D + c * 32) * 2);
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
                                 uint32_t q[4];
@@ -665,28 +640,29 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                 if (lane == 0) mbar_arrive(sm0 + L::ofree + w * 8);
                 if (row < rows) {
                     if (!whole) *reinterpret_cast<float2*>(part + rr * 2) = make_float2(m, l);
-                    else if (a.lse) a.lse[(long long)(C.lo + t) * (H * G) + hd] = (m + log2f(l)) * LN2;
+                    else if (a.lse) a.lse[(long long)(u.lo + t) * (H * G) + hd] = (m + log2f(l)) * LN2;
                 }
                 if (!whole) {
                     int first, last;
-                    ax.sharers(C, first, last);
+                    ax.sharers(u, first, last);
                     // (a row's parts come from warps of one number in their CTAs: no other warp is
                     // waited for)
                     int* const arrived = a.arrived + first * ATTEND_WORKERS_PER_SM + warp;
                     __threadfence();
                     __syncwarp();
-                    int count = 0;
-                    if (lane == 0) count = atomicAdd(arrived, 1);
-                    count = __shfl_sync(0xffffffffu, count, 0);
-                    if (count == last - first && lane == 0) *arrived = 0;
-                    if (count == last - first && row < rows) {
+                    int seen = 0;
+                    if (lane == 0) seen = atomicAdd(arrived, 1);
+                    seen = __shfl_sync(0xffffffffu, seen, 0);
+                    if (seen == last - first && lane == 0) *arrived = 0;
+                    if (seen == last - first && row < rows) {
                         __threadfence();
-                        join_row<T, D, RM>(a, C, first, last, rr, t, hd);
+                        join_row<T, D, RM>(a, u, first, last, rr, t, hd);
                     }
                 }
             }
-            C = next;
-            if (j + 1 < n && !unit_ends) advance<KT, RM, KT>(a, C, pre);
+            done += count;
+            ++units;
+            u = next;
         }
     }
     if (!ok) *late = 1;

@@ -93,6 +93,12 @@ __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&v)[16
                  ALADDIN_I8(v, 0), ALADDIN_I8(v, 8)
                  : "memory");
 }
+__device__ __forceinline__ void tmem_store8(uint32_t at, const uint32_t (&v)[8])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(at),
+                 ALADDIN_I8(v, 0)
+                 : "memory");
+}
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Descriptor of an operand in shared memory: rows of 128 bytes (64 values), the
