@@ -6,9 +6,9 @@
 //   in half precision and scaled for it, reads a tile's scores once, and leaves the weights in the place of the scores;
 //   one thread issues the products: scores S = Q K' and out += P V, both with the first operand, Q or P, from tensor
 //   memory, so that shared memory, which the copies and conversions use too, is read for K and V only;
-//   four warps convert: codes come by asynchronous copies a few tiles ahead, each thread's own, and go as half
-//   precision into a ring of shared memory, K0 V0 K1 V1 ..., in the 128-byte-swizzled layout of the matrix
-//   descriptors. New tokens have a tile of their own; those of bfloat16 are scaled by a power of two for each.
+//   seven warps convert, 16 keys or values at a time in turn: codes come by asynchronous copies a few of those ahead, each
+//   lane's own, and go as half precision into a ring of shared memory, K0 V0 K1 V1 ..., in the 128-byte-swizzled layout of
+//   the matrix descriptors. New tokens have a tile of their own; those of bfloat16 are scaled by a power of two for each.
 // With two row tiles the tensor cores work on one while the softmax works on the other; with one, the scores of the next
 // tile are formed ahead into the second place. The accumulator stays in tensor memory; it is rescaled only when a row's
 // maximum has grown by more than 2^8 over the one that its weights refer to, or a scale by more than 2^4.
@@ -29,27 +29,26 @@ struct Many8 {
     static constexpr int HALVES = (D + 63) / 64;         // blocks of 64 channels
     static constexpr int TILE = HALVES * KT * 128;       // keys or values of a tile, half precision
     static constexpr int NB = D == 256 ? 4 : 8;          // of them in the ring
-    static constexpr int CPT = HALVES * KT / 32;         // 16 codes each: what a converting thread has of them
-    static constexpr int NR = D == 256 ? 2 : 4;          // tiles of codes in flight
-    static constexpr int RAW = CPT * 128 * 16;           // keys or values of one
+    static constexpr int CONV = 7;                       // warps that convert, 16 keys or values at a time
+    static constexpr int CPL = D / 32;                   // 16 codes each: what a lane has of those
+    static constexpr int NF = D == 256 ? 2 : 4;          // of them in flight, a warp
+    static constexpr int RAW = CPL * 512 + 16;           // their codes, scales, whether their page is one of the pool
     static constexpr int raw = NB * TILE;
-    static constexpr int bars = raw + NR * 2 * RAW;
+    static constexpr int bars = (raw + CONV * NF * RAW + 15) / 16 * 16;
     static constexpr int full = bars, empty = full + NB * 8, qready = empty + NB * 8, sready = qready + 16,
                          pready = sready + 24, odone = pready + 16, ofree = odone + 16, over = ofree + 16,
                          tmem = over + 8;
     static constexpr int wild = tmem + 8;                // 8 flags of units
     static constexpr int late = wild + 8 * 4;            // whether a wait ran out
-    static constexpr int rscale = late + 8;              // 8 tiles' scales: of 4 blocks' keys, then values
-    static constexpr int rvalid = rscale + 8 * 32;       // and which blocks of 16 keys are on pages of the pool
-    static constexpr int info = rvalid + 8 * 4;          // 8 tiles' Info
+    static constexpr int info = late + 8;                // 8 tiles' Info
     static constexpr int scratch = info + 8 * (64 * 8 + 32);
     static constexpr int pre = scratch + 32 * 8;
     static constexpr int bytes(int n_req) { return pre + (n_req + 1) * 8; }
-    static constexpr int WARPS = 4 * MT + 1 + 4;         // softmax, products, conversions
+    static constexpr int WARPS = 4 * MT + 1 + CONV;      // softmax, products, conversions
     // columns of tensor memory: the scores' two places, the accumulators, the queries
     static constexpr int s0 = 0, o0 = 2 * KT, q0 = o0 + MT * HALVES * 64;
     static_assert(q0 + MT * (D / 2) <= 512, "tensor memory");
-    static_assert(scratch % 8 == 0 && TILE % 1024 == 0, "alignment");
+    static_assert(info % 16 == 0 && scratch % 8 == 0 && TILE % 1024 == 0, "alignment");
 };
 
 // A tile's scales for the softmax: of blocks of 16 keys, or of each key where they are new.
@@ -57,8 +56,7 @@ struct Info {
     float k[64];    // factors of scores
     float lv[64];   // logarithms of the values' scales
     float top[4];   // the largest are among these
-    int valid;      // blocks of 16 keys on pages of the pool
-    int pad[3];
+    int valid[4];   // blocks of 16 keys on pages of the pool
 };
 
 // What a unit costs beside its tiles, in keys.
@@ -84,7 +82,7 @@ template <typename T, int D, int MT>
 __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(Attend8Args a)
 {
     using L = Many8<D, MT>;
-    constexpr int KT = L::KT, RM = L::RM, NB = L::NB, NR = L::NR, NT = L::WARPS * 32;
+    constexpr int KT = L::KT, RM = L::RM, NB = L::NB, NT = L::WARPS * 32;
     constexpr bool BF16 = !std::is_same<T, __half>::value;
     extern __shared__ __align__(1024) char sm[];
     const uint32_t sm0 = smem_addr(sm);
@@ -138,7 +136,7 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
     // A wait that runs out is recorded and ends its warp's part; the others' waits run
     // out after it (no warps meet at a barrier without a limit before the end), and all meet at
     // the end, where what is in flight is waited for and tensor memory is freed. Whoever waits for a
-    // barrier waits for all of its phases.
+    // barrier waits for all of its phases (the conversions: see there).
     auto wait = [&](uint32_t bar, int phase) -> bool {
         if (mbar_wait(bar, phase & 1)) return true;
         atomicOr(a.err, WORKER_TIMEOUT);
@@ -153,187 +151,160 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
     };
     bool ok = true;  // no wait of this warp ran out
 
-    // Every role goes over the units of the range, and in each over its tiles; tile `done` + t of the range has place
-    // (done + t) % NR of the codes, 2 (done + t) % NB and the one behind it of the ring.
+    // Every role goes over the units of the range, and in each over its tiles; tile `done` + t of the range has places
+    // 2 (done + t) % NB and the one behind it of the ring.
     if (warp >= 4 * MT + 1) {
         // ------------------------------------------------------------ conversions
-        const int ct = tid - (4 * MT + 1) * 32, cw = ct >> 5, r0 = ct >> 2, ch = ct & 3;  // row of 32, chunk of a half
-        float* const rscale = reinterpret_cast<float*>(sm + L::rscale);
-        volatile int* const rvalid = reinterpret_cast<volatile int*>(sm + L::rvalid);
-        const uint32_t raw0 = sm0 + L::raw + ct * 16;
-        // the place of this thread's first 8 channels of row r0 in a tile, and of the next 8
-        const int to0 = r0 * 128 + (((ch * 2) ^ (r0 & 7)) << 4), to1 = r0 * 128 + (((ch * 2 + 1) ^ (r0 & 7)) << 4);
-        Cursor F = C;  // the tile whose codes are fetched
-        int fetched = 0;
-        // pages of this thread's rows of the tile under F and, lanes 0 .. 7 of the first warp, of the block whose
-        // scale they fetch, as the table has them
-        int page[KT / 32], spage = 0;
-        auto pages = [&]() {
-            const int32_t* const row = a.kv.table + (long long)F.r * a.kv.table_stride;
-#pragma unroll
-            for (int p = 0; p < KT / 32; ++p) {
-                const int key = F.tile * KT + p * 32 + r0;
-                page[p] = key < F.len ? row[key >> a.kv.page_shift] : -1;
-            }
-            const int key = F.tile * KT + (lane & 3) * 16;
-            spage = cw == 0 && lane < 8 && key < F.len ? row[key >> a.kv.page_shift] : -1;
+        // Jobs of 16 keys or values of a tile, in turn to the warps: job 8 t + 4 part + g of tile t.
+        const int cw = warp - (4 * MT + 1), rr = lane >> 2, cc = lane & 3;
+        const int jobs = 8 * n;
+        char* const raws = sm + L::raw + cw * (L::NF * L::RAW);
+        // this lane's i-th chunk of 16 codes: its row of the 16, its first channel
+        auto row_of = [&](int i) { return D == 96 && i == 2 ? lane >> 1 : i / (D == 96 ? 1 : L::HALVES) * 8 + rr; };
+        auto channel_of = [&](int i) { return D == 96 ? (i == 2 ? 64 + (lane & 1) * 16 : cc * 16) : i % L::HALVES * 64 + cc * 16; };
+        Cursor F = C;  // of the job that is fetched
+        int fq = cw, ft = 0, fslot = 0, page = -1;
+        // the page of job fq's keys, as the table has it
+        auto find = [&]() {
+            for (; ft < fq >> 3; ++ft) advance<KT, RM, KT>(a, F, pre);
+            const int key = F.tile * KT + (fq & 3) * 16;
+            page = key < F.len ? a.kv.table[(long long)F.r * a.kv.table_stride + (key >> a.kv.page_shift)] : -1;
         };
-        pages();
-        // the codes of the tile under F; then F goes on
+        if (fq < jobs) find();
+        // the codes of job fq, and with keys the scales of keys and values; then on to the next
         auto fetch = [&]() {
-            if (fetched < n) {
-                const int key0 = F.tile * KT, own = F.len - key0;
-                if (own > 0) {
-                    const uint32_t d = raw0 + fetched % NR * (2 * L::RAW);
+            if (fq < jobs) {
+                const int key = F.tile * KT + (fq & 3) * 16, own = F.len - key;
+                const bool values = fq & 4, valid = (unsigned)page < (unsigned)a.kv.pages;
+                const uint32_t d = smem_addr(raws) + fslot * L::RAW;
+                const int at = key & (a.kv.page - 1);
+                const char* const src = (values ? a.kv.v : a.kv.k) +
+                                        (valid ? page * a.kv.page_stride + F.h * a.kv.head_stride + at * a.kv.token_stride : 0);
+                // (weights of 0 meet the codes of rows that hold no key: zeros)
 #pragma unroll
-                    for (int p = 0; p < KT / 32; ++p) {
-                        const bool in = (unsigned)page[p] < (unsigned)a.kv.pages;
-                        const long long e = in ? page[p] * a.kv.page_stride + F.h * a.kv.head_stride +
-                                                     ((key0 + p * 32 + r0) & (a.kv.page - 1)) * a.kv.token_stride + ch * 16
-                                               : 0;
-                        // (weights of 0 meet the codes of rows that hold no key: zeros)
-#pragma unroll
-                        for (int h = 0; h < L::HALVES; ++h) {
-                            if (D % 64 == 0 || h * 64 + ch * 16 < D) {
-                                cp16(d + (p * L::HALVES + h) * 2048, a.kv.k + e + (in ? h * 64 : 0), in);
-                                cp16(d + L::RAW + (p * L::HALVES + h) * 2048, a.kv.v + e + (in ? h * 64 : 0), in);
-                            }
-                        }
-                    }
-                    if (cw == 0) {
-                        const int x = lane & 3, key = key0 + x * 16;
-                        const bool in = (unsigned)spage < (unsigned)a.kv.pages;
-                        if (lane < 4 && x * 16 < own && !in) atomicOr(a.err, WORKER_BAD_INPUT);
-                        const long long e = in ? ((long long)spage * H + F.h) * a.scales.per_page +
-                                                     ((key & (a.kv.page - 1)) >> a.scales.block_shift)
-                                               : 0;
-                        if (lane < 8) cp4(sm0 + L::rscale + (fetched & 7) * 32 + lane * 4, (lane < 4 ? a.scales.k : a.scales.v) + e, in);
-                        const unsigned valid = __ballot_sync(0xffffffffu, in) & 15;
-                        if (lane == 0) rvalid[fetched & 7] = (int)valid;
-                    }
+                for (int i = 0; i < L::CPL; ++i) {
+                    const bool in = valid && row_of(i) < own;
+                    cp16(d + i * 512 + lane * 16, src + (in ? row_of(i) * a.kv.token_stride + channel_of(i) : 0), in);
                 }
-                if (++fetched < n) {
-                    advance<KT, RM, KT>(a, F, pre);
-                    pages();
+                if (!values && lane < 2) {
+                    const long long e = valid ? ((long long)page * H + F.h) * a.scales.per_page + (at >> a.scales.block_shift) : 0;
+                    cp4(d + L::CPL * 512 + lane * 4, (lane ? a.scales.v : a.scales.k) + e, valid);
+                    if (lane == 0) *reinterpret_cast<int*>(raws + fslot * L::RAW + L::CPL * 512 + 8) = valid;
+                    if (!valid && own > 0) atomicOr(a.err, WORKER_BAD_INPUT);
                 }
+                fq += L::CONV;
+                if (fq < jobs) find();
+                if (++fslot == L::NF) fslot = 0;
             }
             cp_commit();
         };
-        int units = 0, i = -(NR - 1);  // the tile that is converted
+#pragma unroll 1
+        for (int i = 0; i < L::NF - 1; ++i) fetch();
         Cursor u = C;
+        int ut = 0, slot = 0, units = 0;
 #pragma unroll 1
-        for (; i < n; ++i) {
+        for (int q = cw; q < jobs; q += L::CONV) {
             fetch();
-            if (i < 0) continue;
-            const bool cached = u.tile * KT < u.len;
-            Info& info = infos[i & 7];
-            cp_wait<NR - 1>();
-            int vtop = 0;
+            for (; ut < q >> 3; ++ut) {
+                if (u.tile + 1 == u.c) ++units;
+                advance<KT, RM, KT>(a, u, pre);
+            }
+            const int part = q >> 2 & 1, g = q & 3;
+            // A place is free when its half of NB halves before has been read. That the phase before is over (a wait tells
+            // two phases apart, not three) follows from this warp's last job, at most two halves back: the half that it
+            // waited for, NB + 2 back at most, had been read, so all had that lie three or more before it, and the one
+            // two before it, which is of its kind; and no phase goes by before this warp's job is done.
+            const int half = q >> 2;
+            if (half >= NB) ok = wait(sm0 + L::empty + half % NB * 8, half / NB - 1);
+            cp_wait<L::NF - 1>();
+            __syncwarp();
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            char* const d = sm + half % NB * L::TILE + g * (16 * 128);
+            Info& info = infos[ut & 7];
+            if (u.tile * KT < u.len) {
+                const char* const src = raws + slot * L::RAW;
+                if (part == 0 && lane == 0) {
+                    const float k = *reinterpret_cast<const float*>(src + L::CPL * 512), v = *reinterpret_cast<const float*>(src + L::CPL * 512 + 4);
+                    const int valid = *reinterpret_cast<const int*>(src + L::CPL * 512 + 8);
+                    const float lv = valid && u.tile * KT + g * 16 < u.len ? log_scale(v) : -INFINITY;
+                    // (a factor that is not 0: scores of 0 stay 0, and those that do not count -inf)
+                    info.k[g] = k < 1e-30f ? 1e-30f : k;
+                    info.lv[g] = lv;
+                    info.top[g] = lv;
+                    info.valid[g] = valid;
+                }
+#pragma unroll
+                for (int i = 0; i < L::CPL; ++i) {
+                    const uint4 c = *reinterpret_cast<const uint4*>(src + i * 512 + lane * 16);
+                    const int row = row_of(i), p = channel_of(i) >> 3, e = row * 128 + (p >> 3) * (KT * 128);
+                    *reinterpret_cast<uint4*>(d + e + (((p & 7) ^ (row & 7)) << 4)) =
+                        make_uint4(half2_lo(c.x), half2_hi(c.x), half2_lo(c.y), half2_hi(c.y));
+                    *reinterpret_cast<uint4*>(d + e + ((((p & 7) + 1) ^ (row & 7)) << 4)) =
+                        make_uint4(half2_lo(c.z), half2_hi(c.z), half2_lo(c.w), half2_hi(c.w));
+                }
+            } else {
+                // new tokens g * 16 ..
+                constexpr int CH = D / 8;
+                const char* const base = part ? a.tok.v : a.tok.k;
+                const long long stride = (part ? a.tok.v_stride : a.tok.k_stride) * 2;
+                int mine = 0;  // the largest exponent of this lane's row of the part
+                if constexpr (BF16) {
+                    // of two halves of a row a lane, of keys (if they are this job's) and values, not of infinities and NaN
+                    const int row = g * 16 + (lane >> 1);
+                    int most = 0;
 #pragma unroll 1
-            for (int part = 0; part < 2; ++part) {
-                const int half = 2 * i + part, slot = half % NB;
-                if (half >= NB) ok = __all_sync(0xffffffffu, wait(sm0 + L::empty + slot * 8, half / NB - 1));
-                if (!ok) break;
-                char* const d = sm + slot * L::TILE;
-                if (cached) {
-                    if (part == 0 && cw == 0) {
-                        __syncwarp();
-                        const float s = lane < 8 ? rscale[(i & 7) * 8 + lane] : 0.0f;
-                        const int valid = rvalid[i & 7];
-                        // (a factor that is not 0: scores of 0 stay 0, and those that do not count -inf)
-                        if (lane < 4) info.k[lane] = s < 1e-30f ? 1e-30f : s;
-                        float lv = -INFINITY;
-                        if (lane >= 4 && lane < 8) {
-                            lv = valid >> (lane - 4) & 1 ? log_scale(s) : -INFINITY;
-                            info.lv[lane - 4] = lv;
-                        }
-#pragma unroll
-                        for (int x = 4; x; x >>= 1) lv = fmaxf(lv, __shfl_xor_sync(0xffffffffu, lv, x));
-                        if (lane < 4) info.top[lane] = lv;
-                        if (lane == 0) info.valid = valid;
-                    }
-                    const char* const src = sm + L::raw + (i % NR * 2 + part) * L::RAW + ct * 16;
-#pragma unroll
-                    for (int p = 0; p < KT / 32; ++p) {
-#pragma unroll
-                        for (int h = 0; h < L::HALVES; ++h) {
-                            if (D % 64 == 0 || h * 64 + ch * 16 < D) {
-                                const uint4 c = *reinterpret_cast<const uint4*>(src + (p * L::HALVES + h) * 2048);
-                                *reinterpret_cast<uint4*>(d + to0 + h * (KT * 128) + p * (32 * 128)) =
-                                    make_uint4(half2_lo(c.x), half2_hi(c.x), half2_lo(c.y), half2_hi(c.y));
-                                *reinterpret_cast<uint4*>(d + to1 + h * (KT * 128) + p * (32 * 128)) =
-                                    make_uint4(half2_lo(c.z), half2_hi(c.z), half2_lo(c.w), half2_hi(c.w));
-                            }
-                        }
-                    }
-                } else {
-                    // 16 new tokens a warp
-                    constexpr int CH = D / 8;
-                    const char* const base = part ? a.tok.v : a.tok.k;
-                    const long long stride = (part ? a.tok.v_stride : a.tok.k_stride) * 2;
-                    const char* const src = base + u.lo * stride + u.h * D * 2;
-                    if (BF16 && part == 0) {
-                        // the largest exponents of two halves of a row a lane, of keys and values, not of infinities and NaN
-                        const int row = cw * 16 + (lane >> 1);
-                        int top[2] = {0, 0};
+                    for (int e = part; e < 2; ++e) {
+                        const char* const q = (e ? a.tok.v + (u.lo + row) * a.tok.v_stride * 2 : a.tok.k + (u.lo + row) * a.tok.k_stride * 2) +
+                                              (u.h * D + (lane & 1) * (D / 2)) * 2;
+                        most = 0;
                         if (row < u.T) {
-#pragma unroll 1
-                            for (int e = 0; e < 2; ++e) {
-                                const char* const q = (e ? a.tok.v + (u.lo + row) * a.tok.v_stride * 2 : a.tok.k + (u.lo + row) * a.tok.k_stride * 2) +
-                                                      (u.h * D + (lane & 1) * (D / 2)) * 2;
-                                int most = 0;
 #pragma unroll 4
-                                for (int c = 0; c < D / 16; ++c) {
-                                    const uint4 v = *reinterpret_cast<const uint4*>(q + c * 16);
-                                    most = exponent(Num<T>::tame(v.x), exponent(Num<T>::tame(v.y), exponent(Num<T>::tame(v.z), exponent(Num<T>::tame(v.w), most))));
-                                }
-                                if (e) top[1] = most;
-                                else top[0] = most;
+                            for (int c = 0; c < D / 16; ++c) {
+                                const uint4 v = *reinterpret_cast<const uint4*>(q + c * 16);
+                                most = exponent(Num<T>::tame(v.x), exponent(Num<T>::tame(v.y), exponent(Num<T>::tame(v.z), exponent(Num<T>::tame(v.w), most))));
                             }
                         }
-                        top[0] = max(top[0], __shfl_xor_sync(0xffffffffu, top[0], 1));
-                        top[1] = max(top[1], __shfl_xor_sync(0xffffffffu, top[1], 1));
-                        float lv = row < u.T ? (float)(min(max(top[1], 15), 254) - 141) : -INFINITY;
+                        most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+                        if (e == part) mine = most;
+                    }
+                    if (part == 0) {  // (the softmax has the values' scales with the keys)
+                        float lv = row < u.T ? (float)(min(max(most, 15), 254) - 141) : -INFINITY;
                         if ((lane & 1) == 0) {
-                            info.k[row] = half_back(top[0]);
+                            info.k[row] = half_back(mine);
                             info.lv[row] = lv;
                         }
 #pragma unroll
                         for (int x = 16; x; x >>= 1) lv = fmaxf(lv, __shfl_xor_sync(0xffffffffu, lv, x));
-                        if (lane == 0) info.top[cw] = lv;
-                        vtop = top[1] | top[0] << 16;  // (the keys' is needed now, the values' in the next part)
-                    } else if (part == 0) {
-                        if (lane < 16) info.k[cw * 16 + lane] = 1.0f, info.lv[cw * 16 + lane] = 0.0f;
-                        if (lane == 0) info.top[cw] = 0.0f;
+                        if (lane == 0) info.top[g] = lv;
                     }
-                    if (part == 0 && cw == 0 && lane == 0) info.valid = 0;
-                    bool w = false;
-#pragma unroll 1
-                    for (int x = lane; x < 16 * CH; x += 32) {
-                        const int row = x / CH, c = x - row * CH, t = cw * 16 + row;
-                        uint4 v = make_uint4(0, 0, 0, 0);
-                        if (t < u.T) v = *reinterpret_cast<const uint4*>(src + t * stride + c * 16);
-                        if (part && (Num<T>::wild(v.x) || Num<T>::wild(v.y) || Num<T>::wild(v.z) || Num<T>::wild(v.w))) {
-                            w = true;
-                            v.x = Num<T>::tame(v.x), v.y = Num<T>::tame(v.y), v.z = Num<T>::tame(v.z), v.w = Num<T>::tame(v.w);
-                        }
-                        if constexpr (BF16) {
-                            static_assert(16 * CH % 32 == 0, "all lanes take part");
-                            const int both = __shfl_sync(0xffffffffu, vtop, row * 2);
-                            const float f = half_factor(part ? both & 0xffff : both >> 16);
-                            v = make_uint4(to_half(v.x, f), to_half(v.y, f), to_half(v.z, f), to_half(v.w, f));
-                        }
-                        *reinterpret_cast<uint4*>(d + (c >> 3) * (KT * 128) + t * 128 + (((c & 7) ^ (t & 7)) << 4)) = v;
-                    }
-                    if (w) wilds[units & 7] = units + 1;
+                } else if (part == 0) {
+                    if (lane < 16) info.k[g * 16 + lane] = 1.0f, info.lv[g * 16 + lane] = 0.0f;
+                    if (lane == 0) info.top[g] = 0.0f;
                 }
-                fence_async();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(sm0 + L::full + slot * 8);
+                bool w = false;
+#pragma unroll 1
+                for (int x = lane; x < 16 * CH; x += 32) {
+                    const int row = x / CH, c = x - row * CH, t = g * 16 + row;
+                    uint4 v = make_uint4(0, 0, 0, 0);
+                    if (t < u.T) v = *reinterpret_cast<const uint4*>(base + (u.lo + t) * stride + (u.h * D + c * 8) * 2);
+                    if (part && (Num<T>::wild(v.x) || Num<T>::wild(v.y) || Num<T>::wild(v.z) || Num<T>::wild(v.w))) {
+                        w = true;
+                        v.x = Num<T>::tame(v.x), v.y = Num<T>::tame(v.y), v.z = Num<T>::tame(v.z), v.w = Num<T>::tame(v.w);
+                    }
+                    if constexpr (BF16) {
+                        static_assert(16 * CH % 32 == 0, "all lanes take part");
+                        const float f = half_factor(__shfl_sync(0xffffffffu, mine, row * 2));
+                        v = make_uint4(to_half(v.x, f), to_half(v.y, f), to_half(v.z, f), to_half(v.w, f));
+                    }
+                    *reinterpret_cast<uint4*>(d + (c >> 3) * (KT * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = v;
+                }
+                if (w) wilds[units & 7] = units + 1;
             }
-            if (!ok) break;
-            if (u.tile + 1 == u.c) ++units;
-            if (i + 1 < n) advance<KT, RM, KT>(a, u, pre);
+            if (++slot == L::NF) slot = 0;
+            fence_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(sm0 + L::full + half % NB * 8);
         }
         cp_wait<0>();
     } else if (warp == 4 * MT) {
@@ -462,8 +433,8 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                     const uint32_t st = tm + lanes + L::s0 + s * KT;
                     const Info& info = infos[(done + t) & 7];
                     const int own = u.len - (u.tile + t) * KT;  // cached keys from the tile's start
-                    const int valid = info.valid;
-                    const bool special = own < KT || valid != 15;
+                    const int4 valid = *reinterpret_cast<const int4*>(info.valid);
+                    const bool special = own < KT || !(valid.x & valid.y & valid.z & valid.w);
                     if (special) {
                         // keys that are not seen or have scales of their own: scores are scaled in their place
                         const float* ks = info.k;
@@ -474,7 +445,7 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                             tmem_load16(y, st + c * 16);
                             const int left = own - c * 16;
                             const uint32_t vis = own <= 0 ? (uint32_t)(see >> (c * 16))
-                                                 : !(valid >> c & 1) ? 0u : left >= 16 ? 0xffffu : left > 0 ? (1u << left) - 1 : 0u;
+                                                 : !info.valid[c] ? 0u : left >= 16 ? 0xffffu : left > 0 ? (1u << left) - 1 : 0u;
 #pragma unroll
                             for (int i = 0; i < 16; ++i)
                                 y[i] = vis >> i & 1 ? __float_as_uint(__uint_as_float(y[i]) * (ks[i * step] * factor)) : 0xff800000u;
