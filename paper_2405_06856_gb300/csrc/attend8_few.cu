@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int rr = y * 8 + tq * 2 + e;
-                        see[y][e] = ancestors(a, C, rr < rows ? (C.rt * RM + rr) / G : 0);
+                        see[y][e] = all_ancestors(a, C, rr < rows ? (C.rt * RM + rr) / G : 0, lane);
                     }
             }
         }

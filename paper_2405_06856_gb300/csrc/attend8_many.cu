@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
     const int me = blockIdx.x;
     if (me >= ax.workers) return;
     Cursor C;
-    const int n = range<KT, RM, KT>(a, ax, C, me);
+    const int n = __shfl_sync(0xffffffffu, range<KT, RM, KT>(a, ax, C, me), 0);
     if (n == 0) return;
 
     if (warp == 0) tmem_alloc(sm0 + L::tmem, 512);
@@ -131,7 +131,7 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
     tc_before();
     __syncthreads();
     tc_after();
-    const uint32_t tm = *reinterpret_cast<volatile uint32_t*>(sm + L::tmem);
+    const uint32_t tm = __shfl_sync(0xffffffffu, *reinterpret_cast<volatile uint32_t*>(sm + L::tmem), 0);
 
     // A wait that runs out is recorded and ends its warp's part; the others' waits run
     // out after it (no warps meet at a barrier without a limit before the end), and all meet at
@@ -317,7 +317,9 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
         int asked[2] = {0, 0}, run[2] = {0, 0}, started[2] = {0, 0};
 #pragma unroll 1
         for (int done = 0; done < n && ok;) {
-            const int count = min(u.c - u.tile, n - done), act = active(u), steps = count * act;
+            // (from one lane, so that the compiler knows that all have the same)
+            const int count = __shfl_sync(0xffffffffu, min(u.c - u.tile, n - done), 0), act = __shfl_sync(0xffffffffu, active(u), 0),
+                      steps = count * act;
             if (MT == 2 && act == 2) ok = wait(sm0 + L::qready + 8, asked[1]++);
             ok = ok && wait(sm0 + L::qready, asked[0]++);
 #pragma unroll 1
@@ -416,12 +418,15 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
 #pragma unroll 1
         for (int done = 0; done < n && ok;) {
             const int count = min(u.c - u.tile, n - done), rows = u.T * G - u.rt * RM - w * 128, act = active(u);
+            const bool more = done + count < n;
             Cursor next = u;
-            if (done + count < n) next_unit(next);
             if (rows <= 0) {
-                if (done + count < n) queries(next);
+                if (more) {
+                    next_unit(next);
+                    queries(next);
+                }
             } else {
-                const unsigned long long see = ancestors(a, u, row < rows ? (u.rt * RM + w * 128 + row) / G : 0);
+                const unsigned long long see = all_ancestors(a, u, row < rows ? (u.rt * RM + w * 128 + row) / G : 0, lane);
                 float m = -INFINITY, l = 0.0f, ref = -1000.0f;
                 const int bar1 = MT == 2 && act == 2 ? 0 : 1;  // with one row tile the places alternate
 #pragma unroll 1
@@ -431,11 +436,19 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                     if (!ok) break;
                     tc_after();
                     const uint32_t st = tm + lanes + L::s0 + s * KT;
+                    uint32_t v[2][32];
+                    tmem_start(v[0], st);
+                    tmem_start(v[1], st + 32);
                     const Info& info = infos[(done + t) & 7];
                     const int own = u.len - (u.tile + t) * KT;  // cached keys from the tile's start
+                    const float4 kf = *reinterpret_cast<const float4*>(info.k), lf = *reinterpret_cast<const float4*>(info.lv),
+                                 tops = *reinterpret_cast<const float4*>(info.top);
                     const int4 valid = *reinterpret_cast<const int4*>(info.valid);
-                    const bool special = own < KT || !(valid.x & valid.y & valid.z & valid.w);
-                    if (special) {
+                    const float scale_top = fmaxf(fmaxf(tops.x, tops.y), fmaxf(tops.z, tops.w));
+                    float f[4] = {kf.x * factor, kf.y * factor, kf.z * factor, kf.w * factor};
+                    tmem_loaded(v[0]);
+                    tmem_loaded(v[1]);
+                    if (own < KT || !(valid.x & valid.y & valid.z & valid.w)) {
                         // keys that are not seen or have scales of their own: scores are scaled in their place
                         const float* ks = info.k;
                         const int step = own > 0 ? 0 : 1;
@@ -453,17 +466,10 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                             ks += step ? 16 : 1;
                         }
                         tmem_stored();
+                        f[0] = f[1] = f[2] = f[3] = 1.0f;
+                        tmem_load(v[0], st);
+                        tmem_load(v[1], st + 32);
                     }
-                    uint32_t v[2][32];
-                    tmem_start(v[0], st);
-                    tmem_start(v[1], st + 32);
-                    const float4 kf = *reinterpret_cast<const float4*>(info.k), lf = *reinterpret_cast<const float4*>(info.lv),
-                                 tops = *reinterpret_cast<const float4*>(info.top);
-                    const float scale_top = fmaxf(fmaxf(tops.x, tops.y), fmaxf(tops.z, tops.w));
-                    float f[4] = {kf.x * factor, kf.y * factor, kf.z * factor, kf.w * factor};
-                    if (special) f[0] = f[1] = f[2] = f[3] = 1.0f;
-                    tmem_loaded(v[0]);
-                    tmem_loaded(v[1]);
                     float top = -INFINITY;
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
@@ -548,8 +554,9 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                     }
                     tmem_stored();
                     tc_before();
-                    // (the products of the tile before are done, so that the arrivals before these have been seen)
-                    if (weighed) ok = __all_sync(0xffffffffu, wait(sm0 + L::odone + w * 8, weighed - 1));
+                    // (the products of the tile before are done, so that the arrivals before these have been seen; with
+                    // two row tiles they were started before this tile's scores)
+                    if (bar1 && weighed) ok = __all_sync(0xffffffffu, wait(sm0 + L::odone + w * 8, weighed - 1));
                     if (!ok) break;
                     if (lane == 0) mbar_arrive(sm0 + L::pready + w * 8);
                     ++weighed;
@@ -557,7 +564,10 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                 if (!ok) break;
                 // the next unit's queries, while the last products run: this unit's scores are done
                 const float unit = ex2(ref);
-                if (done + count < n) queries(next);
+                if (more) {
+                    next_unit(next);
+                    queries(next);
+                }
                 ok = __all_sync(0xffffffffu, wait(sm0 + L::odone + w * 8, weighed - 1));
                 if (!ok) break;
                 tc_after();
