@@ -3,13 +3,15 @@
 // Every cached byte is read once and next to nothing is computed with it: what counts is bytes in flight
 // and few instructions a byte. As in the attention over 16 bits, every warp works alone on a range of the axis of
 // all key tiles, with a few tiles of shared memory that it fills by asynchronous copies ahead, and the products
-// are formed transposed: keys by rows, then channels by rows, 8 rows an operand. The codes become half-precision operands
-// in registers, one conversion for two values. No lane needs another one's codes:
-//   scores    the index that is summed over, the channels, may be taken in any order, the same for both operands:
-//             a lane takes runs of 4 channels, so that the two halves of a word are the pairs that it needs;
-//   results   a lane takes the same channels of the tile's keys 2t, 2t + 1, 2t + 8, 2t + 9 and interleaves the bytes
-//             of two keys; which of its channels stands for which row of the operand is its own choice again, so that
-//             a lane ends with runs of channels of two rows and writes them as they are.
+// are formed transposed: keys by rows, then channels by rows, 8 rows an operand. No lane needs another one's codes:
+//   scores    the keys' codes are operands as they are, of products of e4m3 with 32-bit sums (measured: as exact as those
+//             of half precision, at four times their rate); a query is split into e4m3 parts (attend8.cuh). The index that
+//             is summed over, the channels, may be taken in any order, the same for both operands: a lane takes
+//             runs of 4 channels, a word each;
+//   results   the values' codes become half precision in registers, two in one conversion. A lane takes the same channels
+//             of 16 keys' 2t, 2t + 1, 2t + 8, 2t + 9 and interleaves the bytes of two keys; which of its channels
+//             stands for which row of the operand is its own choice again, so that a lane ends with runs of channels of
+//             two rows and writes them as they are. (Weights split into e4m3 parts would need three of them.)
 // Chunks of 16 bytes are exchanged within a tile so that the loads of both meet different banks.
 //
 // New tokens have tiles of their own, 16 bits wide. Their scores are matrix products in the worker's type; their values,
@@ -23,15 +25,17 @@ namespace {
 
 template <int D, int NB>
 struct Few8 {
-    static constexpr int TK = D == 64 ? 32 : 16;                      // cached keys of a tile
+    static constexpr int TK = D == 64 ? 64 : D == 256 ? 16 : 32;      // cached keys of a tile
     static constexpr int TN = TK / 2;                                 // new keys of a tile
-    static constexpr int WARPS = D == 256 ? 8 : NB == 2 && D == 128 ? 12 : 16;  // of a CTA, one CTA an SM
-    static constexpr int S = 3;                                       // tiles of a warp
+    static constexpr int KB = TK / 16;                                // blocks of 16 keys
+    static constexpr int WARPS = D == 256 || NB == 2 ? 8 : 12;        // of a CTA, one CTA an SM
+    static constexpr int S = WARPS == 8 ? 3 : 2;                      // tiles of a warp
     static constexpr int TILE = 2 * TK * D;                           // keys, then values
-    static constexpr int SLOT = TILE + 16;                            // and the scales of 16 keys each, then of 16 values
-    static constexpr unsigned FULL = TK == 32 ? 0xffffffffu : 0xffffu;
+    static constexpr int SLOT = TILE + 32;                            // and the scales of 16 keys each, then of 16 values
+    typedef typename std::conditional<TK == 64, unsigned long long, unsigned>::type Mask;  // a bit for each key
+    static constexpr Mask FULL = TK == 16 ? (Mask)0xffff : ~(Mask)0;
     static constexpr int oks = WARPS * S * SLOT;                      // masks of tiles
-    static constexpr int scratch = (oks + WARPS * S * 4 + 7) / 8 * 8;
+    static constexpr int scratch = oks + WARPS * S * 8;
     static constexpr int pre = scratch + 32 * 8;
     static constexpr int bytes(int n_req) { return pre + (n_req + 1) * 8; }
 
@@ -61,7 +65,7 @@ struct Few8 {
 
 // Keys of a place in calls that give every warp few tiles, and what a unit costs beside
 // its tiles, in keys.
-constexpr int PLACE_KEYS = 64, UNIT_KEYS = 32;
+constexpr int PLACE_KEYS = 64, UNIT_KEYS = 64;
 
 // The results from now on in units of 2^to.
 template <int MO, int NB>
@@ -84,14 +88,16 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
     constexpr int RM = NB * 8;
     using L = Few8<D, NB>;
     constexpr int TK = L::TK, TN = L::TN, S = L::S, NT = L::WARPS * 32;
-    constexpr int KB = TK / 16, MO = D / 16, NW = D / 32;  // blocks of 16 keys, of 16 channels; words of a value a lane
+    constexpr int KB = L::KB, MO = D / 16, NW = D / 32;  // blocks of 16 keys, of 16 channels; words of a value a lane
+    constexpr int NP = std::is_same<T, __half>::value ? 3 : 2;  // parts of a query
+    typedef typename L::Mask Mask;
     extern __shared__ __align__(128) char sm[];
     int* const pre = reinterpret_cast<int*>(sm + L::pre);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int G = a.kv.group, H = a.kv.kv_heads;
     char* const tiles = sm + warp * S * L::SLOT;
     const uint32_t tiles0 = smem_addr(tiles);
-    unsigned* const oks = reinterpret_cast<unsigned*>(sm + L::oks) + warp * S;
+    Mask* const oks = reinterpret_cast<Mask*>(sm + L::oks) + warp * S;
 
     Axis ax;
     if (!plan<NT>(a.tok.n_req, ax, pre, pre + a.tok.n_req + 1, reinterpret_cast<long long*>(sm + L::scratch),
@@ -107,52 +113,66 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
     // the pages of the tile under F, 16 keys each, as the table has them
     int page[KB];
     auto pages = [&]() {
+        const int32_t* const row = a.kv.table + (long long)F.r * a.kv.table_stride;
 #pragma unroll
         for (int g = 0; g < KB; ++g) {
             const int key = F.tile * TK + g * 16;
-            page[g] = key < F.len ? a.kv.table[(long long)F.r * a.kv.table_stride + (key >> a.kv.page_shift)] : 0;
+            page[g] = key < F.len ? row[key >> a.kv.page_shift] : -1;
         }
     };
     pages();
+    // this lane's chunks of 16 keys: rows, places in the pool and in a tile
+    constexpr int CH = D / 16, NI = CH / 2;
+    auto row_of = [&](int i) { return (lane + i * 32) / CH; };
+    auto chunk_of = [&](int i) { return (lane + i * 32) % CH; };
+    const long long from0 = row_of(0) * a.kv.token_stride + chunk_of(0) * 16;
+    auto from = [&](int i) {
+        return 32 % CH == 0 ? from0 + i * (32 / CH) * a.kv.token_stride : row_of(i) * a.kv.token_stride + chunk_of(i) * 16;
+    };
+    const long long apart = a.kv.v - a.kv.k;
     // the tile under F into place b; then F goes on
     auto fetch = [&](int b, bool more) {
         const int key0 = F.tile * TK, own = F.len - key0;  // cached keys from the tile's start
         const uint32_t d = tiles0 + b * L::SLOT;
         if (own > 0) {
-            unsigned mask = 0;
+            Mask mask = 0;
 #pragma unroll
             for (int g = 0; g < KB; ++g) {
-                if ((unsigned)page[g] < (unsigned)a.kv.pages) mask |= 0xffffu << (g * 16);
-                else if (lane == 0) atomicOr(a.err, WORKER_BAD_INPUT);
-            }
-            if (own < TK) mask &= (1u << own) - 1;
-            const long long head = (long long)F.h * a.kv.head_stride;
-            constexpr int CH = D / 16;
+                const int at = (key0 + g * 16) & (a.kv.page - 1), rows = own - g * 16;
+                const bool in = (unsigned)page[g] < (unsigned)a.kv.pages;
+                const char* const src =
+                    a.kv.k + (in ? page[g] * a.kv.page_stride + F.h * a.kv.head_stride + at * a.kv.token_stride : 0);
+                if (in && rows >= 16) {
 #pragma unroll
-            for (int i = 0; i < TK * CH / 32; ++i) {
-                const int x = lane + i * 32, row = x / CH, ch = x - row * CH;
-                const bool ok = mask >> row & 1;
-                const int p = KB == 1 || row < 16 ? page[0] : page[KB - 1];
-                const long long e = ok ? p * a.kv.page_stride + head +
-                                             ((key0 + row) & (a.kv.page - 1)) * a.kv.token_stride + ch * 16
-                                       : 0;
-                // (weights of 0 meet the codes of rows that hold no key: zeros)
-                cp16(d + L::key_at(row, ch), a.kv.k + e, ok);
-                cp16(d + TK * D + L::value_at(row, ch), a.kv.v + e, ok);
-            }
-            if (lane < 2 * KB) {
-                const int g = lane % KB, p = KB == 1 || g == 0 ? page[0] : page[KB - 1];
-                const bool ok = mask >> (g * 16) & 1;
-                const long long e = ok ? ((long long)p * H + F.h) * a.scales.per_page +
-                                             (((key0 + g * 16) & (a.kv.page - 1)) >> a.scales.block_shift)
-                                       : 0;
-                cp4(d + L::TILE + lane * 4, (lane < KB ? a.scales.k : a.scales.v) + e, ok);
+                    for (int i = 0; i < NI; ++i) {
+                        const char* const p = src + from(i);
+                        cp16(d + L::key_at(g * 16 + row_of(i), chunk_of(i)), p, true);
+                        cp16(d + TK * D + L::value_at(g * 16 + row_of(i), chunk_of(i)), p + apart, true);
+                    }
+                    mask |= (Mask)0xffff << (g * 16);
+                } else {
+                    // (weights of 0 meet the codes of rows that hold no key: zeros)
+#pragma unroll 1
+                    for (int i = 0; i < NI; ++i) {
+                        const bool ok = in && row_of(i) < rows;
+                        const char* const p = src + (ok ? row_of(i) * a.kv.token_stride + chunk_of(i) * 16 : 0);
+                        cp16(d + L::key_at(g * 16 + row_of(i), chunk_of(i)), p, ok);
+                        cp16(d + TK * D + L::value_at(g * 16 + row_of(i), chunk_of(i)), p + apart, ok);
+                    }
+                    if (in && rows > 0) mask |= (Mask)((1u << rows) - 1) << (g * 16);
+                    if (!in && rows > 0 && lane == 0) atomicOr(a.err, WORKER_BAD_INPUT);
+                }
+                if (lane < 2) {
+                    const long long e =
+                        in ? ((long long)page[g] * H + F.h) * a.scales.per_page + (at >> a.scales.block_shift) : 0;
+                    cp4(d + L::TILE + (lane * KB + g) * 4, (lane ? a.scales.v : a.scales.k) + e, in);
+                }
             }
             if (lane == 0) oks[b] = mask;
         } else {
             const int first = (F.tile - (F.len + TK - 1) / TK) * TN;
             constexpr int CH = D / 8;
-#pragma unroll 2
+#pragma unroll 1
             for (int i = 0; i < TN * CH / 32; ++i) {
                 const int x = lane + i * 32, row = x / CH, ch = x - row * CH;
                 const bool ok = first + row < F.T;
@@ -173,7 +193,7 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
     }
 
     const int gq = lane >> 2, tq = lane & 3;
-    uint32_t qf[MO][NB][2];   // row gq of every block, in half precision
+    uint32_t qf[NP][MO][NB];  // row gq of every block in parts, 4 channels a word
     float factor[NB][2];      // of the scores of rows 2 tq, 2 tq + 1, to base 2
     // this lane's channels of row gq of block y in the worker's type
     auto query = [&](const Cursor& u, int y, int x) -> uint2 {
@@ -206,14 +226,17 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                 m[y][0] = m[y][1] = -INFINITY;
                 l[y][0] = l[y][1] = 0.0f;
                 see[y][0] = see[y][1] = 1;
-                uint2 q[MO];
+                float back;
+                {
+                    uint2 q[MO];
 #pragma unroll
-                for (int x = 0; x < MO; ++x) q[x] = query(C, y, x);
-                float back = half_row<T, MO>(q);
+                    for (int x = 0; x < MO; ++x) q[x] = query(C, y, x);
+                    uint32_t p[NP][MO];
+                    back = split_row<T>(q, p);
 #pragma unroll
-                for (int x = 0; x < MO; ++x) {
-                    qf[x][y][0] = q[x].x;
-                    qf[x][y][1] = q[x].y;
+                    for (int z = 0; z < NP; ++z)
+#pragma unroll
+                        for (int x = 0; x < MO; ++x) qf[z][x][y] = p[z][x];
                 }
                 back *= a.scale_log2;
                 factor[y][0] = __shfl_sync(0xffffffffu, back, tq * 8);
@@ -237,15 +260,16 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
 
         float s[KB][NB][4];  // keys gq, gq + 8 of a block by rows 2 tq, 2 tq + 1
         float lv[KB];        // logarithms of the blocks' scales of values, relative to ref
-#pragma unroll
-        for (int x = 0; x < KB; ++x)
-#pragma unroll
-            for (int y = 0; y < NB; ++y) s[x][y][0] = s[x][y][1] = s[x][y][2] = s[x][y][3] = 0.0f;
         if (cached) {
-            const unsigned okm = oks[b];
+            const Mask okm = oks[b];
             const float* const scales = reinterpret_cast<const float*>(slot + L::TILE);
 #pragma unroll
             for (int x = 0; x < KB; ++x) {
+                float part[NP][NB][4];
+#pragma unroll
+                for (int z = 0; z < NP; ++z)
+#pragma unroll
+                    for (int y = 0; y < NB; ++y) part[z][y][0] = part[z][y][1] = part[z][y][2] = part[z][y][3] = 0.0f;
                 constexpr int CW = D == 96 ? 2 : 4;  // words of a load
 #pragma unroll
                 for (int i = 0; i < MO / CW; ++i) {
@@ -262,28 +286,42 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                         }
                     }
 #pragma unroll
-                    for (int c = 0; c < CW; ++c) {
-                        const uint32_t f[4] = {half2_lo(w[0][c]), half2_lo(w[1][c]), half2_hi(w[0][c]), half2_hi(w[1][c])};
+                    for (int c = 0; c < CW; c += 2) {
+                        const uint32_t f[4] = {w[0][c], w[1][c], w[0][c + 1], w[1][c + 1]};
 #pragma unroll
                         for (int y = 0; y < NB; ++y)
-                            Num<__half>::mma(s[x][y], f, qf[i * CW + c][y][0], qf[i * CW + c][y][1]);
+#pragma unroll
+                            for (int z = 0; z < NP; ++z)
+                                mma8(part[z][y], f, qf[z][i * CW + c][y], qf[z][i * CW + c + 1][y]);
                     }
                 }
                 const float ks = scales[x];
 #pragma unroll
                 for (int y = 0; y < NB; ++y) {
+                    const float k0 = ks * factor[y][0], k1 = ks * factor[y][1];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        s[x][y][e] *= ks * factor[y][e & 1];
-                        if (okm != L::FULL && !(okm >> (x * 16 + (e >> 1) * 8 + gq) & 1)) s[x][y][e] = -INFINITY;
+                        float v = part[NP - 1][y][e];
+#pragma unroll
+                        for (int z = NP - 2; z >= 0; --z) v = fmaf(v, 1.0f / PART, part[z][y][e]);
+                        s[x][y][e] = v * (e & 1 ? k1 : k0);
                     }
                 }
+            }
+            if (okm != L::FULL) {
+#pragma unroll
+                for (int x = 0; x < KB; ++x)
+#pragma unroll
+                    for (int y = 0; y < NB; ++y)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (!(okm >> (x * 16 + (e >> 1) * 8 + gq) & 1)) s[x][y][e] = -INFINITY;
             }
             // the reference follows scales that are more than 2^4 times it
             float grown = ref;
 #pragma unroll
             for (int x = 0; x < KB; ++x) {
-                lv[x] = log_scale(okm >> (x * 16) & 1 ? scales[KB + x] : 0.0f);
+                lv[x] = okm >> (x * 16) & 1 ? log_scale(scales[KB + x]) : -INFINITY;
                 if (lv[x] > grown + 4.0f) grown = lv[x];
             }
             if (grown > ref) rebase<MO, NB>(o, ref, grown);
@@ -294,7 +332,9 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
 #pragma unroll
             for (int x = 0; x < KB; ++x) {
                 lv[x] = 0.0f;
-#pragma unroll 4
+#pragma unroll
+                for (int y = 0; y < NB; ++y) s[x][y][0] = s[x][y][1] = s[x][y][2] = s[x][y][3] = 0.0f;
+#pragma unroll 2
                 for (int i = 0; i < MO; ++i) {
                     const uint2 v = *reinterpret_cast<const uint2*>(slot + (x * 8 + gq) * (D * 2) + L::key_channel(i, tq) * 2);
                     const uint32_t f[4] = {v.x, 0u, v.y, 0u};
