@@ -81,11 +81,39 @@ struct Axis {
     }
 };
 
+// The same axis dealt out in whole places: the first `more` workers have one place more than the others' `each`. (Two
+// 32-bit divisions once, and one to find a worker, where the ranges of Axis take 64-bit ones.)
+struct Dealt {
+    const int* pre;
+    const int* tiles;
+    int total, workers, ov, ct, each, more;
+
+    __device__ __forceinline__ void deal()
+    {
+        each = total / workers;
+        more = total - each * workers;
+    }
+    __device__ __forceinline__ int places(int c) const { return ov + (c + ct - 1) / ct; }
+    __device__ __forceinline__ int tile_at(int z) const { return z <= ov ? 0 : (z - ov) * ct; }
+    __device__ __forceinline__ int begin(int i) const { return i * each + min(i, more); }
+    __device__ __forceinline__ int worker_of(int x) const
+    {
+        const int y = x - more * (each + 1);
+        return y < 0 ? x / (each + 1) : more + y / each;
+    }
+    __device__ __forceinline__ void sharers(const Cursor& u, int& first, int& last) const
+    {
+        const int n = places(u.c), at = pre[u.r] + (u.h * u.nrt + u.rt) * n;
+        first = worker_of(at + ov);
+        last = worker_of(at + n - 1);
+    }
+};
+
 // Lays n requests on the axis, the block's threads together; pre and tiles hold n + 1
 // entries each. of(r, c) gives the units of request r and sets c to the tiles of one.
 // false: nothing to do.
-template <int NT, typename F>
-__device__ __forceinline__ bool plan(int n, Axis& x, int* pre, int* tiles, long long* scratch, int most, int ov,
+template <int NT, typename A, typename F>
+__device__ __forceinline__ bool plan(int n, A& x, int* pre, int* tiles, long long* scratch, int most, int ov,
                                      int ct, unsigned* err, F of)
 {
     const int all = plan_prefix<NT>(n, tiles, scratch, [&](int r) -> long long {
@@ -127,8 +155,8 @@ __device__ __forceinline__ int attend_units(const AttendArgs& a, int r, int& c)
 }
 
 // The cursor at place x < total; returns the tiles in front of it.
-template <int KT, int RM, int TN = 0>
-__device__ __forceinline__ int locate(const AttendArgs& a, const Axis& ax, Cursor& u, int x)
+template <int KT, int RM, int TN = 0, typename A>
+__device__ __forceinline__ int locate(const AttendArgs& a, const A& ax, Cursor& u, int x)
 {
     const int r = plan_find(ax.pre, a.tok.n_req, x);
     enter<KT, RM, TN>(a, u, r);
@@ -140,8 +168,8 @@ __device__ __forceinline__ int locate(const AttendArgs& a, const Axis& ax, Curso
 }
 
 // Worker i's first tile under u; returns the number of its tiles.
-template <int KT, int RM, int TN = 0>
-__device__ __forceinline__ int range(const AttendArgs& a, const Axis& ax, Cursor& u, int i)
+template <int KT, int RM, int TN = 0, typename A>
+__device__ __forceinline__ int range(const AttendArgs& a, const A& ax, Cursor& u, int i)
 {
     const int end = ax.begin(i + 1);
     const int t1 = end < ax.total ? locate<KT, RM, TN>(a, ax, u, end) : ax.tiles[a.tok.n_req];

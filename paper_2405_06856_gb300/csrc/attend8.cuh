@@ -46,60 +46,20 @@ __device__ __forceinline__ uint32_t to_half(uint32_t w, float f)
     return Num<__half>::pack(v.x * f, v.y * f);
 }
 
-// Products of e4m3: 16 keys of 32 channels by 8 rows.
-__device__ __forceinline__ void mma8(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+// A row of queries, 4 lanes together, to half precision; returns what its scores are multiplied by.
+template <typename T, int N>
+__device__ __forceinline__ float half_row(uint2 (&q)[N])
 {
-    asm volatile(
-        "mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-// Two e4m3 codes of two 32-bit values, the first in the lower byte.
-__device__ __forceinline__ uint32_t codes2(float lo, float hi)
-{
-    unsigned short u;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(u) : "f"(hi), "f"(lo));
-    return u;
-}
-
-// A row of queries, 4 lanes together, as the sum of N parts of e4m3, each in units of 1 / PART of the one before, times
-// the power of two that is returned. The row is scaled so that its largest channel lies in 2^7 .. 2^8; what a part
-// leaves over, at most half a step, 2^-4 of it, is exact in 32 bits. Two parts hold 9 bits of every channel
-// (bfloat16 has 8), three hold 14 (half precision has 11), where the last part's smallest step, 2^-9, is small
-// enough: of channels below 2^-13 (2^-20 with three) of the largest what is lost is less than 2^-22 (2^-27) of it.
-constexpr float PART = 32.0f;
-template <typename T, int N, int M>
-__device__ __forceinline__ float split_row(const uint2 (&q)[M], uint32_t (&p)[N][M])
-{
-    unsigned most = 0;  // magnitudes as whole numbers: infinity and NaN are the largest
+    if constexpr (std::is_same<T, __half>::value) return 1.0f;
+    int top = 0;
 #pragma unroll
-    for (int x = 0; x < M; ++x) {
-        const float2 u = Num<T>::unpack(q[x].x), v = Num<T>::unpack(q[x].y);
-        const auto bits = [](float y) { return __float_as_uint(y) & 0x7fffffffu; };
-        most = max(max(most, max(bits(u.x), bits(u.y))), max(bits(v.x), bits(v.y)));
-    }
-    most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
-    most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
-    // exponent fields from 17 (2^-110) on: the factor and its inverse are normal numbers
-    const int e = min(max((int)(most >> 23), 17), 254);
-    const float f = __uint_as_float((uint32_t)(261 - e) << 23);
+    for (int x = 0; x < N; ++x) top = exponent(q[x].y, exponent(q[x].x, top));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const float f = half_factor(top);
 #pragma unroll
-    for (int x = 0; x < M; ++x) {
-        const float2 u = Num<T>::unpack(q[x].x), v = Num<T>::unpack(q[x].y);
-        float r[4] = {u.x * f, u.y * f, v.x * f, v.y * f};
-#pragma unroll
-        for (int z = 0; z < N; ++z) {
-            const uint32_t lo = codes2(r[0], r[1]), hi = codes2(r[2], r[3]);
-            p[z][x] = lo | hi << 16;
-            if (z + 1 < N) {
-                const uint32_t a = half2_lo(lo), b = half2_lo(hi);
-                const float2 c = Num<__half>::unpack(a), d = Num<__half>::unpack(b);
-                r[0] = (r[0] - c.x) * PART, r[1] = (r[1] - c.y) * PART;
-                r[2] = (r[2] - d.x) * PART, r[3] = (r[3] - d.y) * PART;
-            }
-        }
-    }
-    return most < 0x7f800000u ? __uint_as_float((uint32_t)(e - 7) << 23) : NAN;  // (a query that is not finite has no scores)
+    for (int x = 0; x < N; ++x) q[x] = make_uint2(to_half(q[x].x, f), to_half(q[x].y, f));
+    return half_back(top);
 }
 
 // Logarithm of a block's scale: -inf of 0, NaN of what is none.

@@ -3,15 +3,14 @@
 // Every cached byte is read once and next to nothing is computed with it: what counts is bytes in flight
 // and few instructions a byte. As in the attention over 16 bits, every warp works alone on a range of the axis of
 // all key tiles, with a few tiles of shared memory that it fills by asynchronous copies ahead, and the products
-// are formed transposed: keys by rows, then channels by rows, 8 rows an operand. No lane needs another one's codes:
-//   scores    the keys' codes are operands as they are, of products of e4m3 with 32-bit sums (measured: as exact as those
-//             of half precision, at four times their rate); a query is split into e4m3 parts (attend8.cuh). The index that
-//             is summed over, the channels, may be taken in any order, the same for both operands: a lane takes
-//             runs of 4 channels, a word each;
-//   results   the values' codes become half precision in registers, two in one conversion. A lane takes the same channels
-//             of 16 keys' 2t, 2t + 1, 2t + 8, 2t + 9 and interleaves the bytes of two keys; which of its channels
-//             stands for which row of the operand is its own choice again, so that a lane ends with runs of channels of
-//             two rows and writes them as they are. (Weights split into e4m3 parts would need three of them.)
+// are formed transposed: keys by rows, then channels by rows, 8 rows an operand. The codes become half-precision operands
+// in registers, one conversion for two values (products of e4m3 take conversions and 32-bit additions of their own on
+// this GPU: 60 us for 57). No lane needs another one's codes:
+//   scores    the index that is summed over, the channels, may be taken in any order, the same for both operands:
+//             a lane takes runs of 4 channels, so that the two halves of a word are the pairs that it needs;
+//   results   a lane takes the same channels of 16 keys' 2t, 2t + 1, 2t + 8, 2t + 9 and interleaves the bytes
+//             of two keys; which of its channels stands for which row of the operand is its own choice again, so that
+//             a lane ends with runs of channels of two rows and writes them as they are.
 // Chunks of 16 bytes are exchanged within a tile so that the loads of both meet different banks.
 //
 // New tokens have tiles of their own, 16 bits wide. Their scores are matrix products in the worker's type; their values,
@@ -89,7 +88,6 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
     using L = Few8<D, NB>;
     constexpr int TK = L::TK, TN = L::TN, S = L::S, NT = L::WARPS * 32;
     constexpr int KB = L::KB, MO = D / 16, NW = D / 32;  // blocks of 16 keys, of 16 channels; words of a value a lane
-    constexpr int NP = std::is_same<T, __half>::value ? 3 : 2;  // parts of a query
     typedef typename L::Mask Mask;
     extern __shared__ __align__(128) char sm[];
     int* const pre = reinterpret_cast<int*>(sm + L::pre);
@@ -99,74 +97,97 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
     const uint32_t tiles0 = smem_addr(tiles);
     Mask* const oks = reinterpret_cast<Mask*>(sm + L::oks) + warp * S;
 
-    Axis ax;
+    Dealt ax;
     if (!plan<NT>(a.tok.n_req, ax, pre, pre + a.tok.n_req + 1, reinterpret_cast<long long*>(sm + L::scratch),
                   (int)gridDim.x * L::WARPS, UNIT_KEYS / TK, PLACE_KEYS / TK, a.err,
                   [&](int r, int& c) { return attend_units<TK, RM, TN>(a, r, c); }))
         return;
+    ax.deal();
     // neighbouring ranges lie on different SMs
     const int me = warp * gridDim.x + blockIdx.x;
     if (me >= ax.workers) return;
     Cursor C, F;  // the tile computed, the tile fetched
     const int n = range<TK, RM, TN>(a, ax, C, me);
     F = C;
-    // the pages of the tile under F, 16 keys each, as the table has them
-    int page[KB];
-    auto pages = [&]() {
-        const int32_t* const row = a.kv.table + (long long)F.r * a.kv.table_stride;
-#pragma unroll
-        for (int g = 0; g < KB; ++g) {
-            const int key = F.tile * TK + g * 16;
-            page[g] = key < F.len ? row[key >> a.kv.page_shift] : -1;
-        }
+    // of F's unit: its row of the table, its head in the pool and among the scales
+    const int32_t* row_F;
+    const char* keys_F;
+    auto unit = [&]() {
+        row_F = a.kv.table + (long long)F.r * a.kv.table_stride;
+        keys_F = a.kv.k + F.h * a.kv.head_stride;
     };
-    pages();
-    // this lane's chunks of 16 keys: rows, places in the pool and in a tile
-    constexpr int CH = D / 16, NI = CH / 2;
-    auto row_of = [&](int i) { return (lane + i * 32) / CH; };
-    auto chunk_of = [&](int i) { return (lane + i * 32) % CH; };
-    const long long from0 = row_of(0) * a.kv.token_stride + chunk_of(0) * 16;
-    auto from = [&](int i) {
-        return 32 % CH == 0 ? from0 + i * (32 / CH) * a.kv.token_stride : row_of(i) * a.kv.token_stride + chunk_of(i) * 16;
+    // the page of 16 keys of the tile under F, as the table has it: of block lane % KB
+    int page;
+    auto find = [&]() {
+        const int key = F.tile * TK + lane % KB * 16;
+        page = key < F.len ? row_F[key >> a.kv.page_shift] : -1;
     };
-    const long long apart = a.kv.v - a.kv.k;
+    unit();
+    find();
+    // this lane's chunks of a tile's rows: 16 bytes of rows row0, row0 + 32 / CH, ..
+    constexpr int CH = D / 16, NI = TK * CH / 32;
+    auto row_of = [&](int i) { return 32 % CH == 0 ? lane / CH + i * (32 / CH) : (lane + i * 32) / CH; };
+    auto chunk_of = [&](int i) { return 32 % CH == 0 ? lane % CH : (lane + i * 32) % CH; };
+    const long long from0 = row_of(0) * a.kv.token_stride + chunk_of(0) * 16, apart = a.kv.v - a.kv.k;
+    const long long rows_on = (32 % CH == 0 ? 32 / CH : 16) * a.kv.token_stride;  // (D 96: three chunks, then 16 rows on)
+    const bool one_page = a.kv.page >= TK;
     // the tile under F into place b; then F goes on
     auto fetch = [&](int b, bool more) {
         const int key0 = F.tile * TK, own = F.len - key0;  // cached keys from the tile's start
         const uint32_t d = tiles0 + b * L::SLOT;
         if (own > 0) {
-            Mask mask = 0;
-#pragma unroll
-            for (int g = 0; g < KB; ++g) {
-                const int at = (key0 + g * 16) & (a.kv.page - 1), rows = own - g * 16;
-                const bool in = (unsigned)page[g] < (unsigned)a.kv.pages;
-                const char* const src =
-                    a.kv.k + (in ? page[g] * a.kv.page_stride + F.h * a.kv.head_stride + at * a.kv.token_stride : 0);
-                if (in && rows >= 16) {
+            const int at = key0 & (a.kv.page - 1), page0 = __shfl_sync(0xffffffffu, page, 0);
+            Mask mask = L::FULL;
+            if (one_page && own >= TK && (unsigned)page0 < (unsigned)a.kv.pages) {
+                const char* k = keys_F + page0 * a.kv.page_stride + at * a.kv.token_stride;
+                if constexpr (32 % CH == 0) {
+                    k += from0;
+                    const char* v = k + apart;
 #pragma unroll
                     for (int i = 0; i < NI; ++i) {
-                        const char* const p = src + from(i);
-                        cp16(d + L::key_at(g * 16 + row_of(i), chunk_of(i)), p, true);
-                        cp16(d + TK * D + L::value_at(g * 16 + row_of(i), chunk_of(i)), p + apart, true);
+                        cp16(d + L::key_at(row_of(i), chunk_of(i)), k, true);
+                        cp16(d + TK * D + L::value_at(row_of(i), chunk_of(i)), v, true);
+                        k += rows_on;
+                        v += rows_on;
                     }
-                    mask |= (Mask)0xffff << (g * 16);
                 } else {
-                    // (weights of 0 meet the codes of rows that hold no key: zeros)
-#pragma unroll 1
-                    for (int i = 0; i < NI; ++i) {
-                        const bool ok = in && row_of(i) < rows;
-                        const char* const p = src + (ok ? row_of(i) * a.kv.token_stride + chunk_of(i) * 16 : 0);
-                        cp16(d + L::key_at(g * 16 + row_of(i), chunk_of(i)), p, ok);
-                        cp16(d + TK * D + L::value_at(g * 16 + row_of(i), chunk_of(i)), p + apart, ok);
+#pragma unroll
+                    for (int i = 0; i < 3; ++i) {
+                        const char* p = k + row_of(i) * a.kv.token_stride + chunk_of(i) * 16;
+#pragma unroll
+                        for (int g = 0; g < KB; ++g) {
+                            cp16(d + L::key_at(g * 16 + row_of(i), chunk_of(i)), p, true);
+                            cp16(d + TK * D + L::value_at(g * 16 + row_of(i), chunk_of(i)), p + apart, true);
+                            p += rows_on;
+                        }
                     }
-                    if (in && rows > 0) mask |= (Mask)((1u << rows) - 1) << (g * 16);
-                    if (!in && rows > 0 && lane == 0) atomicOr(a.err, WORKER_BAD_INPUT);
                 }
-                if (lane < 2) {
-                    const long long e =
-                        in ? ((long long)page[g] * H + F.h) * a.scales.per_page + (at >> a.scales.block_shift) : 0;
-                    cp4(d + L::TILE + (lane * KB + g) * 4, (lane ? a.scales.v : a.scales.k) + e, in);
+            } else {
+                // rows behind the last key or on other pages (weights of 0 meet the codes of rows that hold no key: zeros)
+                const bool have = (unsigned)page < (unsigned)a.kv.pages;
+                const unsigned pages = __ballot_sync(0xffffffffu, have);
+#pragma unroll 1
+                for (int i = 0; i < NI; ++i) {
+                    const int row = (lane + i * 32) / CH, ch = (lane + i * 32) % CH;
+                    const int p = __shfl_sync(0xffffffffu, page, row >> 4);
+                    const bool ok = row < own && (pages >> (row >> 4) & 1);
+                    const char* const k =
+                        ok ? keys_F + p * a.kv.page_stride + ((key0 + row) & (a.kv.page - 1)) * a.kv.token_stride + ch * 16 : a.kv.k;
+                    cp16(d + L::key_at(row, ch), k, ok);
+                    cp16(d + TK * D + L::value_at(row, ch), k + apart, ok);
                 }
+                mask = own >= TK ? L::FULL : ((Mask)1 << own) - 1;
+#pragma unroll
+                for (int g = 0; g < KB; ++g)
+                    if (!(pages >> g & 1)) mask &= ~((Mask)0xffff << (g * 16));
+                if (lane < KB && lane * 16 < own && !have) atomicOr(a.err, WORKER_BAD_INPUT);
+            }
+            if (lane < 2 * KB) {
+                const bool ok = (unsigned)page < (unsigned)a.kv.pages;
+                const long long e = ok ? ((long long)page * H + F.h) * a.scales.per_page +
+                                             (((key0 + lane % KB * 16) & (a.kv.page - 1)) >> a.scales.block_shift)
+                                       : 0;
+                cp4(d + L::TILE + lane * 4, (lane < KB ? a.scales.k : a.scales.v) + e, ok);
             }
             if (lane == 0) oks[b] = mask;
         } else {
@@ -183,7 +204,8 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
         }
         if (more) {
             advance<TK, RM, TN>(a, F, pre);
-            pages();
+            if (F.tile == 0) unit();
+            find();
         }
     };
 #pragma unroll
@@ -193,7 +215,7 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
     }
 
     const int gq = lane >> 2, tq = lane & 3;
-    uint32_t qf[NP][MO][NB];  // row gq of every block in parts, 4 channels a word
+    uint32_t qf[MO][NB][2];   // row gq of every block, in half precision
     float factor[NB][2];      // of the scores of rows 2 tq, 2 tq + 1, to base 2
     // this lane's channels of row gq of block y in the worker's type
     auto query = [&](const Cursor& u, int y, int x) -> uint2 {
@@ -226,17 +248,14 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                 m[y][0] = m[y][1] = -INFINITY;
                 l[y][0] = l[y][1] = 0.0f;
                 see[y][0] = see[y][1] = 1;
-                float back;
-                {
-                    uint2 q[MO];
+                uint2 q[MO];
 #pragma unroll
-                    for (int x = 0; x < MO; ++x) q[x] = query(C, y, x);
-                    uint32_t p[NP][MO];
-                    back = split_row<T>(q, p);
+                for (int x = 0; x < MO; ++x) q[x] = query(C, y, x);
+                float back = half_row<T, MO>(q);
 #pragma unroll
-                    for (int z = 0; z < NP; ++z)
-#pragma unroll
-                        for (int x = 0; x < MO; ++x) qf[z][x][y] = p[z][x];
+                for (int x = 0; x < MO; ++x) {
+                    qf[x][y][0] = q[x].x;
+                    qf[x][y][1] = q[x].y;
                 }
                 back *= a.scale_log2;
                 factor[y][0] = __shfl_sync(0xffffffffu, back, tq * 8);
@@ -265,11 +284,8 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
             const float* const scales = reinterpret_cast<const float*>(slot + L::TILE);
 #pragma unroll
             for (int x = 0; x < KB; ++x) {
-                float part[NP][NB][4];
 #pragma unroll
-                for (int z = 0; z < NP; ++z)
-#pragma unroll
-                    for (int y = 0; y < NB; ++y) part[z][y][0] = part[z][y][1] = part[z][y][2] = part[z][y][3] = 0.0f;
+                for (int y = 0; y < NB; ++y) s[x][y][0] = s[x][y][1] = s[x][y][2] = s[x][y][3] = 0.0f;
                 constexpr int CW = D == 96 ? 2 : 4;  // words of a load
 #pragma unroll
                 for (int i = 0; i < MO / CW; ++i) {
@@ -286,13 +302,10 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                         }
                     }
 #pragma unroll
-                    for (int c = 0; c < CW; c += 2) {
-                        const uint32_t f[4] = {w[0][c], w[1][c], w[0][c + 1], w[1][c + 1]};
+                    for (int c = 0; c < CW; ++c) {
+                        const uint32_t f[4] = {half2_lo(w[0][c]), half2_lo(w[1][c]), half2_hi(w[0][c]), half2_hi(w[1][c])};
 #pragma unroll
-                        for (int y = 0; y < NB; ++y)
-#pragma unroll
-                            for (int z = 0; z < NP; ++z)
-                                mma8(part[z][y], f, qf[z][i * CW + c][y], qf[z][i * CW + c + 1][y]);
+                        for (int y = 0; y < NB; ++y) Num<__half>::mma(s[x][y], f, qf[i * CW + c][y][0], qf[i * CW + c][y][1]);
                     }
                 }
                 const float ks = scales[x];
@@ -300,12 +313,7 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                 for (int y = 0; y < NB; ++y) {
                     const float k0 = ks * factor[y][0], k1 = ks * factor[y][1];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float v = part[NP - 1][y][e];
-#pragma unroll
-                        for (int z = NP - 2; z >= 0; --z) v = fmaf(v, 1.0f / PART, part[z][y][e]);
-                        s[x][y][e] = v * (e & 1 ? k1 : k0);
-                    }
+                    for (int e = 0; e < 4; ++e) s[x][y][e] *= e & 1 ? k1 : k0;
                 }
             }
             if (okm != L::FULL) {

@@ -99,11 +99,12 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
         if (tid == 0) atomicOr(a.err, WORKER_TIMEOUT);
         return;
     }
-    Axis ax;
+    Dealt ax;
     if (!plan<NT>(a.tok.n_req, ax, pre, pre + a.tok.n_req + 1, reinterpret_cast<long long*>(sm + L::scratch),
                   (int)gridDim.x, UNIT_KEYS / KT, 1, a.err,
                   [&](int r, int& c) { return attend_units<KT, RM, KT>(a, r, c); }))
         return;
+    ax.deal();
     const int me = blockIdx.x;
     if (me >= ax.workers) return;
     Cursor C;
