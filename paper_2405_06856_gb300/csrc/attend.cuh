@@ -31,21 +31,14 @@ struct Cursor {
     int c, nrt;           // key tiles, row tiles
 };
 
-// Key tiles of a row tile: KT keys each, cached then new; TN: new tokens begin a tile of their own, TN to a tile.
-template <int KT, int TN>
-__device__ __forceinline__ int key_tiles(int len, int T)
-{
-    return TN ? (len + KT - 1) / KT + (T + (TN ? TN : 1) - 1) / (TN ? TN : 1) : (len + T + KT - 1) / KT;
-}
-
-template <int KT, int RM, int TN = 0>
+template <int KT, int RM>
 __device__ __forceinline__ void enter(const AttendArgs& a, Cursor& u, int r)
 {
     u.r = r;
     u.lo = a.tok.off[r];
     u.T = a.tok.off[r + 1] - u.lo;
     u.len = a.kv.len[r];
-    u.c = key_tiles<KT, TN>(u.len, u.T);
+    u.c = (u.len + u.T + KT - 1) / KT;
     u.nrt = (u.T * a.kv.group + RM - 1) / RM;
 }
 
@@ -81,39 +74,11 @@ struct Axis {
     }
 };
 
-// The same axis dealt out in whole places: the first `more` workers have one place more than the others' `each`. (Two
-// 32-bit divisions once, and one to find a worker, where the ranges of Axis take 64-bit ones.)
-struct Dealt {
-    const int* pre;
-    const int* tiles;
-    int total, workers, ov, ct, each, more;
-
-    __device__ __forceinline__ void deal()
-    {
-        each = total / workers;
-        more = total - each * workers;
-    }
-    __device__ __forceinline__ int places(int c) const { return ov + (c + ct - 1) / ct; }
-    __device__ __forceinline__ int tile_at(int z) const { return z <= ov ? 0 : (z - ov) * ct; }
-    __device__ __forceinline__ int begin(int i) const { return i * each + min(i, more); }
-    __device__ __forceinline__ int worker_of(int x) const
-    {
-        const int y = x - more * (each + 1);
-        return y < 0 ? x / (each + 1) : more + y / each;
-    }
-    __device__ __forceinline__ void sharers(const Cursor& u, int& first, int& last) const
-    {
-        const int n = places(u.c), at = pre[u.r] + (u.h * u.nrt + u.rt) * n;
-        first = worker_of(at + ov);
-        last = worker_of(at + n - 1);
-    }
-};
-
 // Lays n requests on the axis, the block's threads together; pre and tiles hold n + 1
 // entries each. of(r, c) gives the units of request r and sets c to the tiles of one.
 // false: nothing to do.
-template <int NT, typename A, typename F>
-__device__ __forceinline__ bool plan(int n, A& x, int* pre, int* tiles, long long* scratch, int most, int ov,
+template <int NT, typename F>
+__device__ __forceinline__ bool plan(int n, Axis& x, int* pre, int* tiles, long long* scratch, int most, int ov,
                                      int ct, unsigned* err, F of)
 {
     const int all = plan_prefix<NT>(n, tiles, scratch, [&](int r) -> long long {
@@ -141,7 +106,7 @@ __device__ __forceinline__ bool plan(int n, A& x, int* pre, int* tiles, long lon
 
 // The attention's requests: units of a key head's row tiles. A request whose offsets or
 // length make no sense has none and is recorded.
-template <int KT, int RM, int TN = 0>
+template <int KT, int RM>
 __device__ __forceinline__ int attend_units(const AttendArgs& a, int r, int& c)
 {
     const int lo = a.tok.off[r], hi = a.tok.off[r + 1], len = a.kv.len[r];
@@ -150,16 +115,16 @@ __device__ __forceinline__ int attend_units(const AttendArgs& a, int r, int& c)
         c = 0;
         return 0;
     }
-    c = key_tiles<KT, TN>(len, hi - lo);
+    c = (len + hi - lo + KT - 1) / KT;
     return ((hi - lo) * a.kv.group + RM - 1) / RM * a.kv.kv_heads;
 }
 
 // The cursor at place x < total; returns the tiles in front of it.
-template <int KT, int RM, int TN = 0, typename A>
-__device__ __forceinline__ int locate(const AttendArgs& a, const A& ax, Cursor& u, int x)
+template <int KT, int RM>
+__device__ __forceinline__ int locate(const AttendArgs& a, const Axis& ax, Cursor& u, int x)
 {
     const int r = plan_find(ax.pre, a.tok.n_req, x);
-    enter<KT, RM, TN>(a, u, r);
+    enter<KT, RM>(a, u, r);
     const int n = ax.places(u.c), y = x - ax.pre[r], unit = y / n;
     u.tile = ax.tile_at(y - unit * n);
     u.h = unit / u.nrt;
@@ -168,16 +133,16 @@ __device__ __forceinline__ int locate(const AttendArgs& a, const A& ax, Cursor& 
 }
 
 // Worker i's first tile under u; returns the number of its tiles.
-template <int KT, int RM, int TN = 0, typename A>
-__device__ __forceinline__ int range(const AttendArgs& a, const A& ax, Cursor& u, int i)
+template <int KT, int RM>
+__device__ __forceinline__ int range(const AttendArgs& a, const Axis& ax, Cursor& u, int i)
 {
     const int end = ax.begin(i + 1);
-    const int t1 = end < ax.total ? locate<KT, RM, TN>(a, ax, u, end) : ax.tiles[a.tok.n_req];
-    return t1 - locate<KT, RM, TN>(a, ax, u, ax.begin(i));
+    const int t1 = end < ax.total ? locate<KT, RM>(a, ax, u, end) : ax.tiles[a.tok.n_req];
+    return t1 - locate<KT, RM>(a, ax, u, ax.begin(i));
 }
 
 // To the next tile; pre[r] == pre[r + 1] for requests without tiles.
-template <int KT, int RM, int TN = 0>
+template <int KT, int RM>
 __device__ __forceinline__ void advance(const AttendArgs& a, Cursor& u, const int* pre)
 {
     if (++u.tile < u.c) return;
@@ -188,7 +153,7 @@ __device__ __forceinline__ void advance(const AttendArgs& a, Cursor& u, const in
     u.h = 0;
     int r = u.r + 1;
     while (r < a.tok.n_req && pre[r + 1] == pre[r]) ++r;
-    if (r < a.tok.n_req) enter<KT, RM, TN>(a, u, r);
+    if (r < a.tok.n_req) enter<KT, RM>(a, u, r);
 }
 
 // The tokens that token t of the request under u sees, itself among them. A parent

@@ -46,6 +46,15 @@ __device__ __forceinline__ uint32_t to_half(uint32_t w, float f)
     return Num<__half>::pack(v.x * f, v.y * f);
 }
 
+// ... and back.
+template <typename T>
+__device__ __forceinline__ uint32_t from_half(uint32_t w, float f)
+{
+    if constexpr (std::is_same<T, __half>::value) return w;
+    const float2 v = Num<__half>::unpack(w);
+    return Num<T>::pack(v.x * f, v.y * f);
+}
+
 // A row of queries, 4 lanes together, to half precision; returns what its scores are multiplied by.
 template <typename T, int N>
 __device__ __forceinline__ float half_row(uint2 (&q)[N])
@@ -68,6 +77,212 @@ __device__ __forceinline__ float log_scale(float v) { return v >= 0.0f && v < IN
 __device__ __forceinline__ float relative(float lv, float ref)
 {
     return lv == -INFINITY || lv - ref < -40.0f ? -40.0f : lv - ref;
+}
+
+// The axis of all key tiles (attend.cuh), its places dealt out whole: the first `more` workers have one place more than
+// the others' `each`. What a cursor needs to know of the requests lies in shared memory.
+struct Axis8 {
+    int* pre;    // places of the requests before each, and of all
+    int* tiles;  // their tiles
+    int* lo;     // first new tokens
+    int* toks;   // new tokens, 0 of requests that make no sense
+    int* len;    // cached tokens
+    int total, workers, ov, ct, each, more;
+
+    static constexpr int ints(int n_req) { return 5 * (n_req + 1); }
+    __device__ __forceinline__ int places(int c) const { return ov + (c + ct - 1) / ct; }
+    __device__ __forceinline__ int tile_at(int z) const { return z <= ov ? 0 : (z - ov) * ct; }
+    __device__ __forceinline__ int begin(int i) const { return i * each + min(i, more); }
+    __device__ __forceinline__ int worker_of(int x) const
+    {
+        const int y = x - more * (each + 1);
+        return y < 0 ? x / (each + 1) : more + y / each;
+    }
+    // The first and the last worker that have tiles of the unit under u.
+    __device__ __forceinline__ void sharers(const Cursor& u, int& first, int& last) const
+    {
+        const int n = places(u.c), at = pre[u.r] + (u.h * u.nrt + u.rt) * n;
+        first = worker_of(at + ov);
+        last = worker_of(at + n - 1);
+    }
+};
+
+// Key tiles of a row tile: KT keys each, then new tokens in tiles of their own, TN each.
+template <int KT, int TN>
+__device__ __forceinline__ int key_tiles(int len, int T)
+{
+    return (len + KT - 1) / KT + (T + TN - 1) / TN;
+}
+
+// Lays the requests on the axis, the block's threads together; mem: Axis8::ints, scratch: 96 long longs. One pass with
+// three sums: of tiles, of places with `ov` for each unit, and of places of ct tiles. false: nothing to do.
+template <int NT, int KT, int TN, int RM>
+__device__ __forceinline__ bool plan8(const AttendArgs& a, Axis8& x, int* mem, long long* scratch, int most, int ov, int ct)
+{
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = a.tok.n_req;
+    x.pre = mem;
+    x.tiles = mem + (n + 1);
+    x.lo = mem + 2 * (n + 1);
+    x.toks = mem + 3 * (n + 1);
+    x.len = mem + 4 * (n + 1);
+    int* const small = x.pre;  // places of ct tiles first; replaced where the axis is a large one
+    long long base[3] = {0, 0, 0};
+    for (int r0 = 0; r0 < n; r0 += NT) {
+        const int r = r0 + tid;
+        long long v[3] = {0, 0, 0};
+        int T = 0, units = 0, c = 0;
+        if (r < n) {
+            const int lo = a.tok.off[r], hi = a.tok.off[r + 1], len = a.kv.len[r];
+            if (lo < 0 || hi < lo || hi > a.tok.n_tok || hi - lo > ALADDIN_TREE_MAX || len < 0 || len > a.kv.cap) {
+                if (blockIdx.x == 0) atomicOr(a.err, WORKER_BAD_INPUT);
+            } else {
+                T = hi - lo;
+            }
+            x.lo[r] = lo;
+            x.toks[r] = T;
+            x.len[r] = len;
+            if (T) {
+                c = key_tiles<KT, TN>(len, T);
+                units = (T * a.kv.group + RM - 1) / RM * a.kv.kv_heads;
+            }
+            v[0] = (long long)units * c;
+            v[1] = (long long)units * (ov + c);
+            v[2] = (long long)units * ((c + ct - 1) / ct);
+        }
+        long long mine[3];
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            mine[k] = v[k];
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long u = __shfl_up_sync(0xffffffffu, v[k], o);
+                if (lane >= o) v[k] += u;
+            }
+            if (lane == 31) scratch[k * 32 + warp] = v[k];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            long long before = base[k];
+#pragma unroll
+            for (int w = 0; w < NT / 32; ++w) {
+                const long long y = scratch[k * 32 + w];
+                before += w < warp ? y : 0;
+                base[k] += y;
+            }
+            v[k] += before - mine[k];
+        }
+        if (r < n) {
+            x.tiles[r] = (int)v[0];
+            small[r] = (int)v[2];
+        }
+        __syncthreads();
+    }
+    if (base[1] > 0x7fffffffll || base[0] <= 0) {
+        if (base[0] > 0 && blockIdx.x == 0 && tid == 0) atomicOr(a.err, WORKER_BAD_INPUT);
+        return false;
+    }
+    if (tid == 0) x.tiles[n] = (int)base[0];
+    const bool few = base[0] <= (long long)ct * most;
+    x.ov = few ? 0 : ov;
+    x.ct = few ? ct : 1;
+    x.total = (int)(few ? base[2] : base[1]);
+    if (tid == 0) small[n] = x.total;
+    __syncthreads();
+    if (!few) {
+        // a unit has ov places more than tiles: so many for all units before
+        for (int r = tid; r < n; r += NT) x.pre[r] = x.tiles[r];
+        __syncthreads();
+        if (ov) {
+            long long sum = 0;  // of units
+            for (int r0 = 0; r0 < n; r0 += NT) {
+                const int r = r0 + tid;
+                int v = r < n && x.toks[r] ? (x.toks[r] * a.kv.group + RM - 1) / RM * a.kv.kv_heads : 0;
+                const int mine = v;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int u = __shfl_up_sync(0xffffffffu, v, o);
+                    if (lane >= o) v += u;
+                }
+                if (lane == 31) scratch[warp] = v;
+                __syncthreads();
+                long long before = sum;
+#pragma unroll
+                for (int w = 0; w < NT / 32; ++w) {
+                    before += w < warp ? scratch[w] : 0;
+                    sum += scratch[w];
+                }
+                if (r < n) x.pre[r] += (int)(before + v - mine) * ov;
+                __syncthreads();
+            }
+        }
+    }
+    x.workers = min(most, x.total);
+    x.each = x.total / x.workers;
+    x.more = x.total - x.each * x.workers;
+    return true;
+}
+
+template <int KT, int TN, int RM>
+__device__ __forceinline__ void enter8(const AttendArgs& a, const Axis8& x, Cursor& u, int r)
+{
+    u.r = r;
+    u.lo = x.lo[r];
+    u.T = x.toks[r];
+    u.len = x.len[r];
+    u.c = key_tiles<KT, TN>(u.len, u.T);
+    u.nrt = (u.T * a.kv.group + RM - 1) / RM;
+}
+
+// The cursor at place y < total; returns the tiles in front of it.
+template <int KT, int TN, int RM>
+__device__ __forceinline__ int locate8(const AttendArgs& a, const Axis8& x, Cursor& u, int y)
+{
+    const int r = plan_find(x.pre, a.tok.n_req, y);
+    enter8<KT, TN, RM>(a, x, u, r);
+    const int n = x.places(u.c), z = y - x.pre[r], unit = z / n;
+    u.tile = x.tile_at(z - unit * n);
+    u.h = unit / u.nrt;
+    u.rt = unit - u.h * u.nrt;
+    return x.tiles[r] + unit * u.c + u.tile;
+}
+
+// Worker i's first tile under u; returns the number of its tiles.
+template <int KT, int TN, int RM>
+__device__ __forceinline__ int range8(const AttendArgs& a, const Axis8& x, Cursor& u, int i)
+{
+    const int end = x.begin(i + 1);
+    const int t1 = end < x.total ? locate8<KT, TN, RM>(a, x, u, end) : x.tiles[a.tok.n_req];
+    return t1 - locate8<KT, TN, RM>(a, x, u, x.begin(i));
+}
+
+// To the next unit.
+template <int KT, int TN, int RM>
+__device__ __forceinline__ void next_unit8(const AttendArgs& a, const Axis8& x, Cursor& u)
+{
+    u.tile = 0;
+    if (++u.rt < u.nrt) return;
+    u.rt = 0;
+    if (++u.h < a.kv.kv_heads) return;
+    u.h = 0;
+    int r = u.r + 1;
+    while (r < a.tok.n_req && x.toks[r] == 0) ++r;
+    if (r < a.tok.n_req) enter8<KT, TN, RM>(a, x, u, r);
+}
+// To the next tile.
+template <int KT, int TN, int RM>
+__device__ __forceinline__ void advance8(const AttendArgs& a, const Axis8& x, Cursor& u)
+{
+    if (++u.tile == u.c) next_unit8<KT, TN, RM>(a, x, u);
+}
+
+// A warp says that its part of a unit is written, and learns how many have said so before; the last one reads what they
+// wrote behind a fence of its own. counter: of the unit, zero between calls. The number is not waited for here.
+__device__ __forceinline__ int arrive_at(int* counter)
+{
+    int before;
+    asm volatile("fence.acq_rel.gpu;\n atom.add.relaxed.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(counter) : "memory");
+    return before;
 }
 
 // The tokens that token t of the request under u sees, itself among them; all lanes together, each its own t. A

@@ -27,7 +27,9 @@ struct Few8 {
     static constexpr int TK = D == 64 ? 64 : D == 256 ? 16 : 32;      // cached keys of a tile
     static constexpr int TN = TK / 2;                                 // new keys of a tile
     static constexpr int KB = TK / 16;                                // blocks of 16 keys
-    static constexpr int WARPS = D == 256 || NB == 2 ? 8 : 12;        // of a CTA, one CTA an SM
+    // of a CTA, one CTA an SM (128 decodes with 128 channels: 8 warps 44 us, 12 warps 48, as units are split and joined
+    // more often; two long requests with 64 channels: 94 and 91)
+    static constexpr int WARPS = D == 64 && NB == 1 ? 12 : 8;
     static constexpr int S = WARPS == 8 ? 3 : 2;                      // tiles of a warp
     static constexpr int TILE = 2 * TK * D;                           // keys, then values
     static constexpr int SLOT = TILE + 32;                            // and the scales of 16 keys each, then of 16 values
@@ -35,8 +37,8 @@ struct Few8 {
     static constexpr Mask FULL = TK == 16 ? (Mask)0xffff : ~(Mask)0;
     static constexpr int oks = WARPS * S * SLOT;                      // masks of tiles
     static constexpr int scratch = oks + WARPS * S * 8;
-    static constexpr int pre = scratch + 32 * 8;
-    static constexpr int bytes(int n_req) { return pre + (n_req + 1) * 8; }
+    static constexpr int pre = scratch + 96 * 8;
+    static constexpr int bytes(int n_req) { return pre + Axis8::ints(n_req) * 4; }
 
     // byte of chunk c (16 bytes) of a tile's row, keys and values
     static __device__ __forceinline__ int key_at(int row, int c)
@@ -80,6 +82,116 @@ __device__ __forceinline__ void rebase(float (&o)[MO][NB][4], float& ref, float 
     ref = to;
 }
 
+// N consecutive floats that other warps wrote
+template <int N>
+__device__ __forceinline__ void load_row(float (&v)[N], const float* p)
+{
+    if constexpr (N % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            const float4 x = __ldcg(reinterpret_cast<const float4*>(p + i));
+            v[i] = x.x, v[i + 1] = x.y, v[i + 2] = x.z, v[i + 3] = x.w;
+        }
+    } else if constexpr (N == 2) {
+        const float2 x = __ldcg(reinterpret_cast<const float2*>(p));
+        v[0] = x.x, v[1] = x.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = __ldcg(p + i);
+    }
+}
+
+// The rows below live of the unit under u, whose partial results the workers first .. last left; one warp, D / 32 columns
+// a lane. What another SM wrote is 1,500 cycles away: the maxima and sums of up to 32 partial results, one a lane, and
+// the columns of four of them are on their way together.
+template <typename T, int D, int RM>
+__device__ __forceinline__ void join_rows8(const AttendArgs& a, const Cursor& u, int first, int last, int live, int lane)
+{
+    constexpr int N = D / 32, U = D == 256 ? 2 : 4, ROWS = 4;
+    const int G = a.kv.group;
+#pragma unroll 1
+    for (int r0 = 0; r0 < live; r0 += ROWS) {
+        float ref[ROWS], sum[ROWS], acc[ROWS][N];
+#pragma unroll
+        for (int y = 0; y < ROWS; ++y) {
+            ref[y] = -INFINITY;
+            sum[y] = 0.0f;
+#pragma unroll
+            for (int x = 0; x < N; ++x) acc[y][x] = 0.0f;
+        }
+#pragma unroll 1
+        for (int i0 = first; i0 <= last; i0 += 32) {
+            const int count = min(32, last - i0 + 1), mine = i0 + min(lane, count - 1);
+            float2 ml[ROWS];
+            {
+                const float* const p = part_of<D, RM>(a, mine, mine == first);
+#pragma unroll
+                for (int y = 0; y < ROWS; ++y)
+                    ml[y] = __ldcg(reinterpret_cast<const float2*>(p + min(r0 + y, live - 1) * 2));
+            }
+            float f[ROWS];
+#pragma unroll 1
+            for (int k0 = 0; k0 < count; k0 += U) {
+                float v[U][ROWS][N];
+#pragma unroll
+                for (int k = 0; k < U; ++k) {
+                    const int i = i0 + min(k0 + k, count - 1);
+                    const float* const p = part_of<D, RM>(a, i, i == first) + RM * 2 + lane * N;
+#pragma unroll
+                    for (int y = 0; y < ROWS; ++y) load_row(v[k][y], p + min(r0 + y, live - 1) * D);
+                }
+                if (k0 == 0) {
+                    // this lane's factor to the largest maximum so far, and what came before to that
+#pragma unroll
+                    for (int y = 0; y < ROWS; ++y) {
+                        float top = fmaxf(ref[y], ml[y].x);
+#pragma unroll
+                        for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+                        const float base = top == -INFINITY ? 0.0f : top, g = ex2(ref[y] - base);
+                        f[y] = lane < count ? ex2(ml[y].x - base) : 0.0f;
+                        sum[y] = sum[y] * g + (lane < count ? ml[y].y * f[y] : 0.0f);
+#pragma unroll
+                        for (int x = 0; x < N; ++x) acc[y][x] *= g;
+                        ref[y] = top;
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < U; ++k) {
+                    if (k0 + k >= count) break;
+#pragma unroll
+                    for (int y = 0; y < ROWS; ++y) {
+                        const float w = __shfl_sync(0xffffffffu, f[y], k0 + k);
+#pragma unroll
+                        for (int x = 0; x < N; ++x) acc[y][x] += w * v[k][y][x];
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int y = 0; y < ROWS; ++y) {
+#pragma unroll
+            for (int x = 16; x; x >>= 1) sum[y] += __shfl_xor_sync(0xffffffffu, sum[y], x);
+            const int rr = r0 + y;
+            if (rr >= live) break;
+            const int rho = u.rt * RM + rr, t = rho / G, head = u.h * G + rho - t * G;
+            const float inv = sum[y] > 0.0f || sum[y] != sum[y] ? 1.0f / sum[y] : 0.0f;
+            char* const d = a.out + ((u.lo + t) * a.out_stride + (long long)head * D + lane * N) * 2;
+            if constexpr (N % 2 == 0) {
+#pragma unroll
+                for (int x = 0; x < N; x += 2)
+                    *reinterpret_cast<uint32_t*>(d + x * 2) = Num<T>::pack(acc[y][x] * inv, acc[y][x + 1] * inv);
+            } else {
+#pragma unroll
+                for (int x = 0; x < N; ++x)
+                    *reinterpret_cast<unsigned short*>(d + x * 2) = (unsigned short)Num<T>::pack(acc[y][x] * inv, 0.0f);
+            }
+            if (lane == 0 && a.lse)
+                a.lse[(long long)(u.lo + t) * (a.kv.kv_heads * G) + head] =
+                    ((ref[y] == -INFINITY ? 0.0f : ref[y]) + log2f(sum[y])) * LN2;
+        }
+    }
+}
+
 // NB: blocks of 8 rows.
 template <typename T, int D, int NB>
 __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Attend8Args a)
@@ -90,24 +202,21 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
     constexpr int KB = L::KB, MO = D / 16, NW = D / 32;  // blocks of 16 keys, of 16 channels; words of a value a lane
     typedef typename L::Mask Mask;
     extern __shared__ __align__(128) char sm[];
-    int* const pre = reinterpret_cast<int*>(sm + L::pre);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int G = a.kv.group, H = a.kv.kv_heads;
     char* const tiles = sm + warp * S * L::SLOT;
     const uint32_t tiles0 = smem_addr(tiles);
     Mask* const oks = reinterpret_cast<Mask*>(sm + L::oks) + warp * S;
 
-    Dealt ax;
-    if (!plan<NT>(a.tok.n_req, ax, pre, pre + a.tok.n_req + 1, reinterpret_cast<long long*>(sm + L::scratch),
-                  (int)gridDim.x * L::WARPS, UNIT_KEYS / TK, PLACE_KEYS / TK, a.err,
-                  [&](int r, int& c) { return attend_units<TK, RM, TN>(a, r, c); }))
+    Axis8 ax;
+    if (!plan8<NT, TK, TN, RM>(a, ax, reinterpret_cast<int*>(sm + L::pre), reinterpret_cast<long long*>(sm + L::scratch),
+                               (int)gridDim.x * L::WARPS, UNIT_KEYS / TK, PLACE_KEYS / TK))
         return;
-    ax.deal();
     // neighbouring ranges lie on different SMs
     const int me = warp * gridDim.x + blockIdx.x;
     if (me >= ax.workers) return;
     Cursor C, F;  // the tile computed, the tile fetched
-    const int n = range<TK, RM, TN>(a, ax, C, me);
+    const int n = range8<TK, TN, RM>(a, ax, C, me);
     F = C;
     // of F's unit: its row of the table, its head in the pool and among the scales
     const int32_t* row_F;
@@ -203,17 +312,11 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
             }
         }
         if (more) {
-            advance<TK, RM, TN>(a, F, pre);
+            advance8<TK, TN, RM>(a, ax, F);
             if (F.tile == 0) unit();
             find();
         }
     };
-#pragma unroll
-    for (int j = 0; j < S - 1; ++j) {
-        if (j < n) fetch(j, j + 1 < n);
-        cp_commit();
-    }
-
     const int gq = lane >> 2, tq = lane & 3;
     uint32_t qf[MO][NB][2];   // row gq of every block, in half precision
     float factor[NB][2];      // of the scores of rows 2 tq, 2 tq + 1, to base 2
@@ -226,11 +329,35 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
             a.tok.q + ((u.lo + t) * a.tok.q_stride + (long long)(u.h * G + rho - t * G) * D + L::key_channel(x, tq)) * 2));
     };
 
+    // the next unit's queries are on their way while one is computed, the first ones in front of all keys
+    // (256 channels leave no registers for that)
+    constexpr bool AHEAD = D < 256;
+    uint2 qn[AHEAD ? MO : 1][NB];
+    auto queries_of = [&](const Cursor& u) {
+        if constexpr (AHEAD) {
+#pragma unroll
+            for (int y = 0; y < NB; ++y)
+#pragma unroll
+                for (int x = 0; x < MO; ++x) qn[x][y] = query(u, y, x);
+        }
+    };
+    queries_of(C);
+#pragma unroll
+    for (int j = 0; j < S - 1; ++j) {
+        if (j < n) fetch(j, j + 1 < n);
+        cp_commit();
+    }
+
     float o[MO][NB][4], m[NB][2], l[NB][2];  // channels of rows 2 tq, 2 tq + 1
+    float unscale[NB];                       // of row gq of every block
     float ref = -INFINITY;                   // the results count in units of 2^ref
     unsigned long long see[NB][2];
     bool fresh = true;
     int b = 0, tile0 = 0;  // a tile's place; the first tile of the unit that this warp has
+    // A unit that warps share and whose part this one has written: a tile later it says so, and at the end of its next
+    // unit it looks whether it was the last one to, which joins the parts; neither is waited for while there are tiles.
+    Cursor P = C;
+    int pend = 0, p_first = 0, p_last = 0, p_before = 0;  // 1: written, 2: said
 
     for (int j = 0; j < n; ++j) {
         __syncwarp();
@@ -250,8 +377,9 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                 see[y][0] = see[y][1] = 1;
                 uint2 q[MO];
 #pragma unroll
-                for (int x = 0; x < MO; ++x) q[x] = query(C, y, x);
+                for (int x = 0; x < MO; ++x) q[x] = AHEAD ? qn[AHEAD ? x : 0][y] : query(C, y, x);
                 float back = half_row<T, MO>(q);
+                unscale[y] = back;
 #pragma unroll
                 for (int x = 0; x < MO; ++x) {
                     qf[x][y][0] = q[x].x;
@@ -260,6 +388,11 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                 back *= a.scale_log2;
                 factor[y][0] = __shfl_sync(0xffffffffu, back, tq * 8);
                 factor[y][1] = __shfl_sync(0xffffffffu, back, tq * 8 + 4);
+            }
+            if (AHEAD && j + C.c - C.tile < n) {  // the range goes on behind this unit
+                Cursor u = C;
+                next_unit8<TK, TN, RM>(a, ax, u);
+                queries_of(u);
             }
             if (C.T > 1) {
 #pragma unroll
@@ -342,14 +475,13 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                 lv[x] = 0.0f;
 #pragma unroll
                 for (int y = 0; y < NB; ++y) s[x][y][0] = s[x][y][1] = s[x][y][2] = s[x][y][3] = 0.0f;
-#pragma unroll 2
+#pragma unroll
                 for (int i = 0; i < MO; ++i) {
                     const uint2 v = *reinterpret_cast<const uint2*>(slot + (x * 8 + gq) * (D * 2) + L::key_channel(i, tq) * 2);
                     const uint32_t f[4] = {v.x, 0u, v.y, 0u};
 #pragma unroll
                     for (int y = 0; y < NB; ++y) {
-                        const uint2 q = query(C, y, i);
-                        Num<T>::mma(s[x][y], f, q.x, q.y);
+                        Num<T>::mma(s[x][y], f, from_half<T>(qf[i][y][0], unscale[y]), from_half<T>(qf[i][y][1], unscale[y]));
                     }
                 }
                 const int key = first + x * 8 + gq;
@@ -485,6 +617,10 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
             }
         }
 
+        if (pend == 1) {
+            if (lane == 0) p_before = arrive_at(a.arrived + p_first);
+            pend = 2;
+        }
         if (C.tile + 1 == C.c || j + 1 == n) {
             const bool whole = tile0 == 0 && C.tile + 1 == C.c;
             const int live = min(rows, RM);
@@ -521,23 +657,30 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                     }
                 }
             }
-            if (!whole) {
-                int first_w, last_w;
-                ax.sharers(C, first_w, last_w);
-                __threadfence();
-                __syncwarp();
-                int arrived = 0;
-                if (lane == 0) arrived = atomicAdd(a.arrived + first_w, 1);
-                arrived = __shfl_sync(0xffffffffu, arrived, 0);
-                if (arrived == last_w - first_w) {
-                    if (lane == 0) a.arrived[first_w] = 0;
-                    __threadfence();
-                    join_rows<T, D, RM>(a, C, first_w, last_w, 0, live, 4, lane);
+            bool add = !whole;
+#pragma unroll 1
+            while (pend || add) {
+                if (pend) {
+                    if (__shfl_sync(0xffffffffu, p_before, 0) == p_last - p_first) {
+                        if (lane == 0) a.arrived[p_first] = 0;
+                        asm volatile("fence.acq_rel.gpu;" ::: "memory");
+                        join_rows8<T, D, RM>(a, P, p_first, p_last, min(P.T * G - P.rt * RM, RM), lane);
+                    }
+                    pend = 0;
                 }
+                if (!add) break;
+                add = false;
+                P = C;
+                ax.sharers(P, p_first, p_last);
+                __syncwarp();
+                pend = 1;
+                if (j + 1 < n) break;
+                if (lane == 0) p_before = arrive_at(a.arrived + p_first);
+                pend = 2;
             }
             fresh = true;
         }
-        if (j + 1 < n) advance<TK, RM, TN>(a, C, pre);
+        if (j + 1 < n) advance8<TK, TN, RM>(a, ax, C);
         if (++b == S) b = 0;
     }
     cp_wait<0>();

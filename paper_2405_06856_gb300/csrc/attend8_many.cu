@@ -42,8 +42,8 @@ struct Many8 {
     static constexpr int late = wild + 8 * 4;            // whether a wait ran out
     static constexpr int info = late + 8;                // 8 tiles' Info
     static constexpr int scratch = info + 8 * (64 * 8 + 32);
-    static constexpr int pre = scratch + 32 * 8;
-    static constexpr int bytes(int n_req) { return pre + (n_req + 1) * 8; }
+    static constexpr int pre = scratch + 96 * 8;
+    static constexpr int bytes(int n_req) { return pre + Axis8::ints(n_req) * 4; }
     static constexpr int WARPS = 4 * MT + 1 + CONV;      // softmax, products, conversions
     // columns of tensor memory: the scores' two places, the accumulators, the queries
     static constexpr int s0 = 0, o0 = 2 * KT, q0 = o0 + MT * HALVES * 64;
@@ -86,7 +86,6 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
     constexpr bool BF16 = !std::is_same<T, __half>::value;
     extern __shared__ __align__(1024) char sm[];
     const uint32_t sm0 = smem_addr(sm);
-    int* const pre = reinterpret_cast<int*>(sm + L::pre);
     // (tiles' scales, units' flags: the conversions run fewer than 8 tiles ahead of the softmax)
     Info* const infos = reinterpret_cast<Info*>(sm + L::info);
     volatile int* const wilds = reinterpret_cast<volatile int*>(sm + L::wild);
@@ -99,16 +98,14 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
         if (tid == 0) atomicOr(a.err, WORKER_TIMEOUT);
         return;
     }
-    Dealt ax;
-    if (!plan<NT>(a.tok.n_req, ax, pre, pre + a.tok.n_req + 1, reinterpret_cast<long long*>(sm + L::scratch),
-                  (int)gridDim.x, UNIT_KEYS / KT, 1, a.err,
-                  [&](int r, int& c) { return attend_units<KT, RM, KT>(a, r, c); }))
+    Axis8 ax;
+    if (!plan8<NT, KT, KT, RM>(a, ax, reinterpret_cast<int*>(sm + L::pre), reinterpret_cast<long long*>(sm + L::scratch),
+                               (int)gridDim.x, UNIT_KEYS / KT, 1))
         return;
-    ax.deal();
     const int me = blockIdx.x;
     if (me >= ax.workers) return;
     Cursor C;
-    const int n = __shfl_sync(0xffffffffu, range<KT, RM, KT>(a, ax, C, me), 0);
+    const int n = __shfl_sync(0xffffffffu, range8<KT, KT, RM>(a, ax, C, me), 0);
     if (n == 0) return;
 
     if (warp == 0) tmem_alloc(sm0 + L::tmem, 512);
@@ -146,10 +143,7 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
     // row tiles of the unit under u, of MT at most
     auto active = [&](const Cursor& u) { return MT == 2 && u.T * G - u.rt * RM > 128 ? 2 : 1; };
     // to the next unit
-    auto next_unit = [&](Cursor& u) {
-        u.tile = u.c - 1;
-        advance<KT, RM, KT>(a, u, pre);
-    };
+    auto next_unit = [&](Cursor& u) { next_unit8<KT, KT, RM>(a, ax, u); };
     bool ok = true;  // no wait of this warp ran out
 
     // Every role goes over the units of the range, and in each over its tiles; tile `done` + t of the range has places
@@ -167,7 +161,7 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
         int fq = cw, ft = 0, fslot = 0, page = -1;
         // the page of job fq's keys, as the table has it
         auto find = [&]() {
-            for (; ft < fq >> 3; ++ft) advance<KT, RM, KT>(a, F, pre);
+            for (; ft < fq >> 3; ++ft) advance8<KT, KT, RM>(a, ax, F);
             const int key = F.tile * KT + (fq & 3) * 16;
             page = key < F.len ? a.kv.table[(long long)F.r * a.kv.table_stride + (key >> a.kv.page_shift)] : -1;
         };
@@ -208,7 +202,7 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
             fetch();
             for (; ut < q >> 3; ++ut) {
                 if (u.tile + 1 == u.c) ++units;
-                advance<KT, RM, KT>(a, u, pre);
+                advance8<KT, KT, RM>(a, ax, u);
             }
             const int part = q >> 2 & 1, g = q & 3;
             // A place is free when its half of NB halves before has been read. That the phase before is over (a wait tells
