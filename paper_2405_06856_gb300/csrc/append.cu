@@ -2,24 +2,25 @@
 // on the way (rope.cuh).
 //
 // Request r appends tokens i = 0 .. A: token i takes slot len + i and position next + i. In 16 bits a unit is some rows
-// (heads' keys or values) of one token. In 8 bits it is a block of slots of one head, keys or values, by one warp: of the
+// (heads' keys or values) of one token, a warp's. In 8 bits it is a block of slots of one head, keys or values: of the
 // new values x of the block
 //     scale = 2^j, the least j >= -126 with max |x| <= 448 2^j (finite values), or the scale that the block
 //     has for the tokens that it holds, where that is larger;  code = e4m3(x / scale).
 // With scales that are powers of two e4m3, a floating type, loses nothing but below its smallest normal
 // number, 2^-6 of the scale: a scale that grows lets codes be rounded again without loss, and blocks do
-// not depend on how their tokens came in. The two passes, for the maximum and for the codes, both
-// read the new rows; the second finds them in the first-level cache.
+// not depend on how their tokens came in. A warp has a few rows of a block, four chunks of 8 channels a lane, and keeps
+// them, rotated, in registers from the maximum to the codes; the warps of a block exchange their maxima. Instructions are
+// what it spends most of: so a lane forms the angles of its first row and turns them on from row to row.
 //
-// The kernels lay the requests' units on one axis (a prefix sum by each CTA) and go over it with all warps of the GPU. The
-// last CTA to finish advances the lengths.
+// The kernels lay the requests' units on one axis (a prefix sum by each CTA, which keeps what the units need of them) and
+// go over it with all warps of the GPU. The last CTA to finish advances the lengths.
 #include "rope.cuh"
 
 namespace aladdin {
 namespace wk {
 namespace {
 
-constexpr int WARPS = 8, NT = WARPS * 32;
+constexpr int WARPS = 8, NT = WARPS * 32, PER_SM = 2;  // of a CTA; CTAs of an SM
 
 // Tokens that request r appends; -1 where its offsets, length or choice make no sense.
 __device__ __forceinline__ int appended(const AppendArgs& a, int r)
@@ -35,21 +36,40 @@ __device__ __forceinline__ int appended(const AppendArgs& a, int r)
     return ok ? a1 - a0 : -1;
 }
 
-// Lays the requests on the axis, per(r, A) units each; returns the number of all.
+// What the units need of the requests, in shared memory.
+struct Requests {
+    int* pre;   // units of the requests before each, and of all
+    int* len;
+    int* next;
+    int* lo;    // first new tokens
+    int* a0;    // first entries of acc
+    int* count; // tokens that they append
+
+    static size_t bytes(int n) { return (size_t)(n + 1) * 6 * sizeof(int); }
+};
+
+// Lays the requests on the axis, per(len, A) units each; returns the number of all.
 template <typename F>
-__device__ __forceinline__ int lay(const AppendArgs& a, int* pre, long long* scratch, F per)
+__device__ __forceinline__ int lay(const AppendArgs& a, Requests& q, int* mem, long long* scratch, F per)
 {
-    const int all = plan_prefix<NT>(a.tok.n_req, pre, scratch, [&](int r) -> long long {
+    const int n = a.tok.n_req + 1;
+    q.pre = mem, q.len = mem + n, q.next = mem + 2 * n, q.lo = mem + 3 * n, q.a0 = mem + 4 * n, q.count = mem + 5 * n;
+    const int all = plan_prefix<NT>(a.tok.n_req, q.pre, scratch, [&](int r) -> long long {
         const int A = appended(a, r);
         if (A < 0 && blockIdx.x == 0) atomicOr(a.err, WORKER_BAD_INPUT);
-        return A > 0 ? per(r, A) : 0;
+        q.len[r] = a.kv.len[r];
+        q.next[r] = a.kv.next ? a.kv.next[r] : q.len[r];
+        q.lo[r] = a.tok.off[r];
+        q.a0[r] = a.acc_off ? a.acc_off[r] : 0;
+        q.count[r] = A;
+        return A > 0 ? per(q.len[r], A) : 0;
     });
     if (all < 0 && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.err, WORKER_BAD_INPUT);
     return all;
 }
 
 // Every CTA has read the lengths: the last one to come here advances those of the requests with units.
-__device__ __forceinline__ void leave(const AppendArgs& a, const int* pre, int all, int* last)
+__device__ __forceinline__ void leave(const AppendArgs& a, const Requests& q, int all, int* last)
 {
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -61,82 +81,109 @@ __device__ __forceinline__ void leave(const AppendArgs& a, const int* pre, int a
     if (threadIdx.x == 0) *a.arrived = 0;
     if (all <= 0) return;
     for (int r = threadIdx.x; r < a.tok.n_req; r += NT) {
-        if (pre[r + 1] == pre[r]) continue;
-        const int A = a.acc_off ? a.acc_off[r + 1] - a.acc_off[r] : a.tok.off[r + 1] - a.tok.off[r];
-        a.kv.len[r] += A;
-        if (a.kv.next) a.kv.next[r] += A;
+        if (q.count[r] <= 0) continue;
+        a.kv.len[r] = q.len[r] + q.count[r];
+        if (a.kv.next) a.kv.next[r] = q.next[r] + q.count[r];
     }
 }
 
 // Index of the i-th token that request r appends among all new tokens.
-__device__ __forceinline__ long long source(const AppendArgs& a, int r, int i)
+__device__ __forceinline__ long long source(const AppendArgs& a, const Requests& q, int r, int i)
 {
-    return a.tok.off[r] + (a.acc_off ? a.acc[a.acc_off[r] + i] : i);
+    return q.lo[r] + (a.acc ? a.acc[q.a0[r] + i] : i);
 }
 
-constexpr int ROWS = 4;  // rows in flight of a lane
+constexpr int ROWS = 4;  // rows of keys, and of values, in flight of a lane
 
-// 16 bits: 2 H rows a token, in `parts` parts.
+// 16 bits: a unit is `heads` heads of one token. A warp has neighbouring units.
 template <typename T, int D, bool INTERLEAVED>
-__global__ void __launch_bounds__(NT) k_append(AppendArgs a, int parts)
+__global__ void __launch_bounds__(NT, PER_SM) k_append(AppendArgs a, int heads)
 {
     constexpr int CH = D / 8, RPW = 32 / CH;
-    extern __shared__ int pre[];
+    extern __shared__ int mem[];
     __shared__ long long scratch[32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, H = a.kv.kv_heads;
-    const int all = lay(a, pre, scratch, [&](int, int A) { return (long long)A * parts; });
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, H = a.kv.kv_heads, parts = (H + heads - 1) / heads;
+    Requests q;
+    const int all = lay(a, q, mem, scratch, [&](int, int A) { return (long long)A * parts; });
     const int sub = lane / CH, ch = lane - sub * CH;
-    Turns<INTERLEAVED> turns;
-    if (a.rope.half) turns.load(a.rope, ch);
-    const int per = ((2 * H + parts - 1) / parts + RPW - 1) / RPW * RPW;
-    for (long long u = blockIdx.x * WARPS + warp; u < all; u += gridDim.x * WARPS) {
-        const int r = plan_find(pre, a.tok.n_req, (int)u), y = (int)u - pre[r], i = y / parts, part = y - i * parts;
-        const int slot = a.kv.len[r] + i, at = slot & (a.kv.page - 1);
-        const int p = (int)((unsigned)(a.kv.next ? a.kv.next[r] : a.kv.len[r]) + (unsigned)i);
+    const bool on = sub < RPW;
+    Rotor<INTERLEAVED> rotor, one;
+    if (a.rope.half) {
+        rotor.load(a.rope, ch);
+        one = rotor;
+        one.scale = 1.0f;
+        one.at(1);
+    }
+    const int workers = (int)gridDim.x * WARPS, each = (max(all, 0) + workers - 1) / workers;
+    const int begin = (int)min((long long)(blockIdx.x * WARPS + warp) * each, (long long)max(all, 0)),
+              end = (int)min((long long)begin + each, (long long)max(all, 0));
+    int r = begin < end ? plan_find(q.pre, a.tok.n_req, begin) : 0;
+    int at_p = 0, turned = 0;  // where the rotor is, how often it has been turned on to there
+    bool fresh = true;
+    for (int u = begin; u < end; ++u) {
+        while (u >= q.pre[r + 1]) ++r;
+        const int y = u - q.pre[r], i = parts == 1 ? y : y / parts, part = y - i * parts;
+        const int slot = q.len[r] + i, at = slot & (a.kv.page - 1);
+        const int p = (int)((unsigned)q.next[r] + (unsigned)i);
+        // (the page is looked up while the rows are on their way)
         const int page = a.kv.table[r * a.kv.table_stride + (slot >> a.kv.page_shift)];
-        if ((unsigned)page >= (unsigned)a.kv.pages) {
-            if (lane == 0) atomicOr(a.err, WORKER_BAD_INPUT);
-            continue;
+        const long long t = source(a, q, r, i);
+        const int h0 = part * heads + sub, h1 = min(H, part * heads + heads);
+        const char* k = a.tok.k + (t * a.tok.k_stride + h0 * D + ch * 8) * 2;
+        const char* v = a.tok.v + (t * a.tok.v_stride + h0 * D + ch * 8) * 2;
+        if (a.rope.half && (fresh || p != at_p)) {
+            if (!fresh && p == at_p + 1 && turned < 3) {
+                rotor.on(one);
+                ++turned;
+            } else {
+                rotor.at(p);
+                turned = 0;
+            }
+            fresh = false;
+            at_p = p;
         }
-        const long long t = source(a, r, i);
-        const char* const k = a.tok.k + t * a.tok.k_stride * 2;
-        const char* const v = a.tok.v + t * a.tok.v_stride * 2;
-        const long long dst = page * a.kv.page_stride + at * a.kv.token_stride;
-        const int row0 = part * per, row1 = min(2 * H, row0 + per);
-        for (int row = row0; row < row1; row += RPW * ROWS) {
-            uint4 x[ROWS], z[ROWS];
+        const bool have = (unsigned)page < (unsigned)a.kv.pages;
+        long long dst = (have ? page * a.kv.page_stride + at * a.kv.token_stride + h0 * a.kv.head_stride : 0) + ch * 8;
+        long long m = have ? ((long long)page * H + h0) * a.kv.page + at : 0;
+        for (int h = h0; h - sub < h1; h += RPW * ROWS) {
+            uint4 x[ROWS], z[ROWS], w[ROWS];
 #pragma unroll
             for (int e = 0; e < ROWS; ++e) {
-                const int h = row + e * RPW + sub;
-                if (sub < RPW && h < row1) {
-                    const char* const src = h < H ? k + (long long)h * D * 2 : v + (long long)(h - H) * D * 2;
-                    x[e] = *reinterpret_cast<const uint4*>(src + ch * 16);
-                    if (!INTERLEAVED && a.rope.half && h < H) z[e] = partners<T>(a.rope, src, ch);
+                if (on && h + e * RPW < h1) {
+                    x[e] = *reinterpret_cast<const uint4*>(k + e * RPW * D * 2);
+                    if (!INTERLEAVED && a.rope.half) z[e] = partners<T>(a.rope, k + (e * RPW * D - ch * 8) * 2, ch);
+                    w[e] = *reinterpret_cast<const uint4*>(v + e * RPW * D * 2);
                 }
+            }
+            if (!have) {
+                if (lane == 0) atomicOr(a.err, WORKER_BAD_INPUT);
+                break;
             }
 #pragma unroll
             for (int e = 0; e < ROWS; ++e) {
-                const int h = row + e * RPW + sub;
-                if (sub < RPW && h < row1) {
-                    if (a.rope.half && h < H) {
+                if (on && h + e * RPW < h1) {
+                    if (a.rope.half) {
                         float f[8], g[8];
                         widen<T>(x[e], f);
                         if (!INTERLEAVED) widen<T>(z[e], g);
-                        turn<INTERLEAVED>(a.rope, turns, p, ch, f, g);
+                        rotor.turn(f, g);
                         x[e] = narrow<T>(f);
                     }
-                    const int head = h < H ? h : h - H;
-                    *reinterpret_cast<uint4*>((h < H ? a.kv.k : a.kv.v) + (dst + head * a.kv.head_stride + ch * 8) * 2) = x[e];
-                    if (h < H && ch == 0) {
-                        const long long m = ((long long)page * H + h) * a.kv.page + at;
+                    *reinterpret_cast<uint4*>(a.kv.k + dst * 2) = x[e];
+                    *reinterpret_cast<uint4*>(a.kv.v + dst * 2) = w[e];
+                    if (ch == 0) {
                         if (a.kv.pos) a.kv.pos[m] = p;
                         if (a.kv.weight) a.kv.weight[m] = 0.0f;
                     }
+                    dst += RPW * a.kv.head_stride;
+                    m += RPW * a.kv.page;
                 }
             }
+            k += ROWS * RPW * D * 2;
+            v += ROWS * RPW * D * 2;
         }
     }
-    leave(a, pre, all, reinterpret_cast<int*>(scratch));
+    leave(a, q, all, reinterpret_cast<int*>(scratch));
 }
 
 // ---- 8 bits
@@ -163,120 +210,181 @@ __device__ __forceinline__ float scale_of(float m)
     return __uint_as_float((uint32_t)max(e, 1) << 23);
 }
 
+// Rows of a block that a warp has at a time: four chunks a lane.
+template <int D>
+constexpr int ROWS8 = 4 * (32 / (D / 8));
+
+// `wpu` warps a unit: as many as have its rows, at most all of a CTA. A unit is a block and `many` of its 2 H rows of keys and
+// values.
 template <typename T, int D, bool INTERLEAVED>
-__global__ void __launch_bounds__(NT) k_append8(AppendArgs a)
+__global__ void __launch_bounds__(NT, PER_SM) k_append8(AppendArgs a, int wpu, int many)
 {
-    constexpr int CH = D / 8, RPW = 32 / CH;
-    extern __shared__ int pre[];
+    constexpr int CH = D / 8, RPW = 32 / CH, N = 4, RW = ROWS8<D>;
+    extern __shared__ int mem[];
     __shared__ long long scratch[32];
+    __shared__ float tops[2][WARPS];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, H = a.kv.kv_heads;
-    const int shift = a.scales.block_shift, block = 1 << shift;
-    const int all = lay(a, pre, scratch, [&](int r, int A) {
-        const int len = a.kv.len[r];
-        return (long long)(((len + A - 1) >> shift) - (len >> shift) + 1) * (2 * H);
+    const int shift = a.scales.block_shift, block = 1 << shift, parts = (2 * H + many - 1) / many;
+    Requests q;
+    const int all = lay(a, q, mem, scratch, [&](int len, int A) {
+        return (long long)(((len + A - 1) >> shift) - (len >> shift) + 1) * parts;
     });
     const int sub = lane / CH, ch = lane - sub * CH;
-    Turns<INTERLEAVED> turns;
-    if (a.rope.half) turns.load(a.rope, ch);
-    for (long long u = blockIdx.x * WARPS + warp; u < all; u += gridDim.x * WARPS) {
-        const int r = plan_find(pre, a.tok.n_req, (int)u), y = (int)u - pre[r], b = y / (2 * H), hv = y - b * (2 * H);
-        const bool values = hv >= H;
-        const int h = values ? hv - H : hv, len = a.kv.len[r];
-        const int A = a.acc_off ? a.acc_off[r + 1] - a.acc_off[r] : a.tok.off[r + 1] - a.tok.off[r];
-        const int first = ((len >> shift) + b) << shift;               // the block's first slot
-        const int lo = max(first, len), hi = min(first + block, len + A);  // its new slots
-        const int page = a.kv.table[r * a.kv.table_stride + (first >> a.kv.page_shift)];
-        if ((unsigned)page >= (unsigned)a.kv.pages) {
-            if (lane == 0) atomicOr(a.err, WORKER_BAD_INPUT);
-            continue;
-        }
-        const int at = first & (a.kv.page - 1), p0 = a.kv.next ? a.kv.next[r] : len;
-        const char* const src = (values ? a.tok.v : a.tok.k) + (h * D + ch * 8) * 2;
-        const long long stride = values ? a.tok.v_stride : a.tok.k_stride;
-        const bool turned = !values && a.rope.half;
-        // row `slot` of the new ones in 32 bits
-        auto load = [&](int slot, float (&x)[8]) {
-            const char* const row = src + source(a, r, slot - len) * stride * 2;
-            widen<T>(*reinterpret_cast<const uint4*>(row), x);
-            if (turned) {
-                float z[8];
-                if (!INTERLEAVED) widen<T>(partners<T>(a.rope, row - ch * 16, ch), z);
-                turn<INTERLEAVED>(a.rope, turns, (int)((unsigned)p0 + (unsigned)(slot - len)), ch, x, z);
-            }
-        };
-        float most = 0.0f;
-#pragma unroll 2
-        for (int slot = lo + sub; slot < hi; slot += RPW) {
-            if (sub >= RPW) break;
-            float x[8];
-            load(slot, x);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float m = fabsf(x[j]);
-                if (m < INFINITY) most = fmaxf(most, m);
-            }
-        }
-#pragma unroll
-        for (int x = 16; x; x >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, x));
-        float* const held = (values ? a.scales.v : a.scales.k) +
-                            (((long long)page * H + h) * a.scales.per_page + (at >> shift));
-        float scale = scale_of(most);
-        char* const dst = (values ? a.kv.v : a.kv.k) + page * a.kv.page_stride + h * a.kv.head_stride +
-                          at * a.kv.token_stride + ch * 8;
-        if (lo > first) {
-            const float old = *held;
-            if (scale > old) {
-                const float f = old / scale;
-                for (int slot = first + sub; slot < lo && sub < RPW; slot += RPW) {
-                    uint2* const d = reinterpret_cast<uint2*>(dst + (slot - first) * a.kv.token_stride);
-                    const uint2 c = *d;
-                    uint32_t w[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float2 z = values2((j < 2 ? c.x : c.y) >> (j & 1) * 16);
-                        w[j] = codes2(z.x * f, z.y * f);
-                    }
-                    *d = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
-                }
-            } else {
-                scale = old;
-            }
-        }
-        const float inv = 1.0f / scale;
-#pragma unroll 2
-        for (int slot = lo + sub; slot < hi; slot += RPW) {
-            if (sub >= RPW) break;
-            float x[8];
-            load(slot, x);
-            // (x - x: nothing, or NaN for what is not finite)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = fmaf(x[j], inv, x[j] - x[j]);
-            *reinterpret_cast<uint2*>(dst + (slot - first) * a.kv.token_stride) =
-                make_uint2(codes2(x[0], x[1]) | codes2(x[2], x[3]) << 16, codes2(x[4], x[5]) | codes2(x[6], x[7]) << 16);
-        }
-        __syncwarp();
-        if (lane == 0) *held = scale;
+    const int groups = WARPS / wpu, group = warp / wpu, member = warp - group * wpu, span = wpu * RW;
+    Rotor<INTERLEAVED> rotor, by;  // at a row's position; from a lane's row to its next
+    if (a.rope.half) {
+        rotor.load(a.rope, ch);
+        by = rotor;
+        by.scale = 1.0f;
+        by.at(RPW);
     }
-    leave(a, pre, all, reinterpret_cast<int*>(scratch));
+    int round = 0;
+    for (long long u0 = (long long)blockIdx.x * groups; u0 < all; u0 += (long long)gridDim.x * groups) {
+        const bool any = u0 + group < all;
+        const int u = any ? (int)(u0 + group) : 0;
+        const int r = plan_find(q.pre, a.tok.n_req, u), y = u - q.pre[r], b = y / parts, hv0 = (y - b * parts) * many;
+        const int len = q.len[r];
+        const int first = ((len >> shift) + b) << shift;                            // the block's first slot
+        const int lo = max(first, len), hi = any ? min(first + block, len + q.count[r]) : lo;  // its new slots
+        const int page = a.kv.table[r * a.kv.table_stride + (first >> a.kv.page_shift)];
+        const int at = first & (a.kv.page - 1), mine = member * RW + sub;  // this lane's first row
+        const bool have = any && (unsigned)page < (unsigned)a.kv.pages;
+        if (any && !have && lane == 0 && member == 0) atomicOr(a.err, WORKER_BAD_INPUT);
+#pragma unroll 1
+        for (int hv = hv0; hv < hv0 + many; ++hv, ++round) {  // (all warps of a CTA, the same number of times)
+            const bool live = have && hv < 2 * H, values = hv >= H;
+            const int h = values ? hv - H : hv, end = live ? hi : lo;
+            const long long stride = (values ? a.tok.v_stride : a.tok.k_stride) * 2;
+            const char* const src = (values ? a.tok.v : a.tok.k) + h * D * 2 + q.lo[r] * stride;
+            const bool turned = !values && a.rope.half;
+            // this warp's rows from slot s0 on, in 32 bits
+            float x[N][8];
+            auto load = [&](int s0) {
+                uint4 raw[N], mates[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const int slot = s0 + mine + i * RPW;
+                    raw[i] = mates[i] = make_uint4(0, 0, 0, 0);
+                    if (sub < RPW && slot < end) {
+                        const char* const row = src + (a.acc ? a.acc[q.a0[r] + slot - len] : slot - len) * stride;
+                        raw[i] = *reinterpret_cast<const uint4*>(row + ch * 16);
+                        if (!INTERLEAVED && turned) mates[i] = partners<T>(a.rope, row, ch);
+                    }
+                }
+                if (turned && s0 + member * RW < end) rotor.at((int)((unsigned)q.next[r] + (unsigned)(s0 + mine - len)));
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    widen<T>(raw[i], x[i]);
+                    if (turned && s0 + member * RW + i * RPW < end) {
+                        float z[8];
+                        if (!INTERLEAVED) widen<T>(mates[i], z);
+                        rotor.turn(x[i], z);
+                        if (i + 1 < N) rotor.on(by);
+                    }
+                }
+            };
+            // their largest magnitude; infinity where it is not to be left out
+            auto largest = [&](bool finite) {
+                float most = 0.0f;
+#pragma unroll 1
+                for (int s0 = lo; s0 < end; s0 += span) {
+                    load(s0);
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const float m = fabsf(x[i][j]);
+                            most = fmaxf(most, finite && m == INFINITY ? 0.0f : m);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+                return most;
+            };
+            float most = largest(false);
+            bool wild = most == INFINITY;  // of this warp's rows
+            if (wild) most = largest(true);
+            float* const held = (values ? a.scales.v : a.scales.k) +
+                                (live ? ((long long)page * H + h) * a.scales.per_page + (at >> shift) : 0);
+            const float old = live && lo > first ? *held : 0.0f;
+            if (wpu > 1) {
+                if (lane == 0) tops[round & 1][warp] = most;
+                __syncthreads();  // (the scale has been read by all when the first writes it; two sets: one round may be behind)
+                for (int w = 0; w < wpu; ++w) most = fmaxf(most, tops[round & 1][group * wpu + w]);
+            }
+            if (!live) continue;
+            float scale = scale_of(most);
+            char* const dst = (values ? a.kv.v : a.kv.k) + page * a.kv.page_stride + h * a.kv.head_stride +
+                              at * a.kv.token_stride + ch * 8;
+            if (lo > first) {
+                if (scale > old) {
+                    const float f = old / scale;
+                    for (int slot = first + member * RPW + sub; slot < lo && sub < RPW; slot += wpu * RPW) {
+                        uint2* const d = reinterpret_cast<uint2*>(dst + (slot - first) * a.kv.token_stride);
+                        const uint2 c = *d;
+                        uint32_t w[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float2 z = values2((j < 2 ? c.x : c.y) >> (j & 1) * 16);
+                            w[j] = codes2(z.x * f, z.y * f);
+                        }
+                        *d = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+                    }
+                } else {
+                    scale = old;
+                }
+            }
+            const float inv = 1.0f / scale;
+#pragma unroll 1
+            for (int s0 = lo; s0 < end; s0 += span) {
+                if (end - lo > span) load(s0);
+                if (wild) {  // what is infinite becomes NaN, as conversions of NaN are, not the largest number
+#pragma unroll
+                    for (int i = 0; i < N; ++i)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) x[i][j] += x[i][j] - x[i][j];
+                }
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const int slot = s0 + mine + i * RPW;
+                    if (sub < RPW && slot < end)
+                        *reinterpret_cast<uint2*>(dst + (slot - first) * a.kv.token_stride) =
+                            make_uint2(codes2(x[i][0] * inv, x[i][1] * inv) | codes2(x[i][2] * inv, x[i][3] * inv) << 16,
+                                       codes2(x[i][4] * inv, x[i][5] * inv) | codes2(x[i][6] * inv, x[i][7] * inv) << 16);
+                }
+            }
+            if (lane == 0 && member == 0) *held = scale;
+        }
+    }
+    leave(a, q, all, reinterpret_cast<int*>(scratch));
 }
 
 template <typename T, int D, bool INTERLEAVED>
 cudaError_t launch_kind(const AppendArgs& a, int sms, cudaStream_t st)
 {
     constexpr int RPW = 32 / (D / 8);
-    const int smem = (a.tok.n_req + 1) * (int)sizeof(int), H = a.kv.kv_heads;
-    // CTAs that have a unit, 4 an SM at most
-    auto ctas = [&](long long units) {
-        const long long want = (units + WARPS - 1) / WARPS;
-        return (int)(want < 4ll * sms ? want : 4ll * sms);
+    const size_t smem = Requests::bytes(a.tok.n_req);
+    const int H = a.kv.kv_heads;
+    // CTAs that have a unit, as many as run at once at most
+    auto ctas = [&](long long units, int a_cta) {
+        const long long want = (units + a_cta - 1) / a_cta;
+        return (int)(want < (long long)PER_SM * sms ? want : PER_SM * sms);
     };
     if (a.scales.k) {
+        const int need = (1 << a.scales.block_shift) / ROWS8<D>, wpu = need < WARPS ? need : WARPS;
         // (a request's tokens enter two blocks more than they fill, at most)
-        k_append8<T, D, INTERLEAVED><<<ctas((((long long)a.n_acc >> a.scales.block_shift) + 2ll * a.tok.n_req) * 2 * H), NT, smem, st>>>(a);
+        const long long blocks = ((long long)a.n_acc >> a.scales.block_shift) + 2ll * a.tok.n_req;
+        // several rows of heads a unit where there are 8 units for every group of warps all the same
+        long long many = blocks * 2 * H * wpu / (8ll * WARPS * PER_SM * sms);
+        many = many < 1 ? 1 : many < 2 * H ? many : 2 * H;
+        k_append8<T, D, INTERLEAVED><<<ctas(blocks * ((2 * H + many - 1) / many), WARPS / wpu), NT, smem, st>>>(a, wpu, (int)many);
     } else {
-        const long long want = ((long long)sms * 32 + a.n_acc - 1) / a.n_acc;
-        const int most = (2 * H + RPW * ROWS - 1) / (RPW * ROWS), parts = (int)(want < most ? want : most);
-        k_append<T, D, INTERLEAVED><<<ctas((long long)a.n_acc * parts), NT, smem, st>>>(a, parts);
+        // heads of a unit: all, or as few as give every warp a unit, a warp's loads at least
+        const long long want = ((long long)PER_SM * sms * WARPS + a.n_acc - 1) / a.n_acc;
+        int heads = (int)((H + want - 1) / want);
+        heads = (heads + RPW - 1) / RPW * RPW;
+        k_append<T, D, INTERLEAVED><<<ctas((long long)a.n_acc * ((H + heads - 1) / heads), WARPS), NT, smem, st>>>(a, heads);
     }
     return cudaGetLastError();
 }

@@ -12,37 +12,78 @@
 namespace aladdin {
 namespace wk {
 
-// What turns channels [8 ch, 8 ch + 8) of a head: the frequencies of their pairs.
+// What turns channels [8 ch, 8 ch + 8) of a head: cosine and sine of each of their pairs at one position, times the
+// factor. In the half layout a channel has its pair's sine with the sign of its partner's part: x' = x c + y s.
+// Channels that are not turned have 1 and 0.
 template <bool INTERLEAVED>
-struct Turns {
+struct Rotor {
     static constexpr int N = INTERLEAVED ? 4 : 8;
-    uint32_t hi[N], lo[N];
+    uint32_t hi[N], lo[N];  // frequencies
+    float c[N], s[N];
+    float scale;
+    unsigned turned, minus;  // bits of the pairs (channels) that are turned, whose sine is taken negative
 
     __device__ __forceinline__ void load(const RopeDev& rope, int ch)
     {
+        scale = rope.scale;
+        turned = minus = 0;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            const int c = ch * 8 + j, p = INTERLEAVED ? ch * 4 + j : c < rope.half ? c : c - rope.half;
+            const int at = ch * 8 + j, p = INTERLEAVED ? ch * 4 + j : at < rope.half ? at : at - rope.half;
+            if (p < rope.half) turned |= 1u << j;
+            if (!INTERLEAVED && at < rope.half) minus |= 1u << j;
             const unsigned long long t = p < rope.half ? __ldg(rope.turn + p) : 0;
             hi[j] = (uint32_t)(t >> 32);
             lo[j] = (uint32_t)t;
         }
     }
-    // cosine and sine of pair j at position p, times the factor
-    __device__ __forceinline__ void at(const RopeDev& rope, int p, int j, float& c, float& s) const
+    // to position p
+    __device__ __forceinline__ void at(int p)
     {
-        // the upper word of p (hi, lo), p signed
-        const uint32_t turn = (uint32_t)p * hi[j] + __umulhi((uint32_t)p, lo[j]) - (p < 0 ? lo[j] : 0u);
-        const uint32_t quarter = (turn + 0x20000000u) & 0xc0000000u;
-        const float x = (float)(int)(turn - quarter) * 1.46291807927e-9f;  // 2 pi / 2^32
-        const float x2 = x * x;
-        const float a = fmaf(x * x2, fmaf(x2, fmaf(x2, fmaf(x2, 1.0f / 362880, -1.0f / 5040), 1.0f / 120), -1.0f / 6), x);
-        const float b = fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, 1.0f / 40320, -1.0f / 720), 1.0f / 24), -0.5f), 1.0f);
-        // of 0, 1, 2, 3 quarters more: (b, a), (-a, b), (-b, -a), (a, -b)
-        const bool odd = quarter & 0x40000000u;
-        const float u = odd ? a : b, v = odd ? b : a;
-        c = __uint_as_float(__float_as_uint(u) ^ ((quarter + 0x40000000u) & 0x80000000u)) * rope.scale;
-        s = __uint_as_float(__float_as_uint(v) ^ (quarter & 0x80000000u)) * rope.scale;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            // the upper word of p (hi, lo), p signed
+            const uint32_t turn = (uint32_t)p * hi[j] + __umulhi((uint32_t)p, lo[j]) - (p < 0 ? lo[j] : 0u);
+            const uint32_t quarter = (turn + 0x20000000u) & 0xc0000000u;
+            const float x = (float)(int)(turn - quarter) * 1.46291807927e-9f;  // 2 pi / 2^32
+            const float x2 = x * x;
+            const float a = fmaf(x * x2, fmaf(x2, fmaf(x2, fmaf(x2, 1.0f / 362880, -1.0f / 5040), 1.0f / 120), -1.0f / 6), x);
+            const float b = fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, 1.0f / 40320, -1.0f / 720), 1.0f / 24), -0.5f), 1.0f);
+            // of 0, 1, 2, 3 quarters more: (b, a), (-a, b), (-b, -a), (a, -b)
+            const bool odd = quarter & 0x40000000u;
+            const float u = odd ? a : b, v = odd ? b : a;
+            const uint32_t sign = (quarter & 0x80000000u) ^ (minus >> j << 31);
+            c[j] = __uint_as_float(__float_as_uint(u) ^ ((quarter + 0x40000000u) & 0x80000000u)) * scale;
+            s[j] = __uint_as_float(__float_as_uint(v) ^ sign) * scale;
+            if (!(turned >> j & 1)) c[j] = 1.0f, s[j] = 0.0f;
+        }
+    }
+    // on by as many positions as `by`, a rotor at them with factor 1, stands for: an error of 2^-24 more
+    __device__ __forceinline__ void on(const Rotor& by)
+    {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float t = fmaf(c[j], by.c[j], -s[j] * by.s[j]);
+            s[j] = fmaf(s[j], by.c[j], c[j] * by.s[j]);
+            c[j] = t;
+        }
+    }
+    // x, 8 channels; y: their partners (half layout; 0 for channels that are not turned)
+    __device__ __forceinline__ void turn(float (&x)[8], const float (&y)[8]) const
+    {
+        if constexpr (INTERLEAVED) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float a = x[2 * j], b = x[2 * j + 1];
+                if (turned >> j & 1) {
+                    x[2 * j] = fmaf(a, c[j], -b * s[j]);
+                    x[2 * j + 1] = fmaf(a, s[j], b * c[j]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = fmaf(x[j], c[j], y[j] * s[j]);
+        }
     }
 };
 
@@ -66,7 +107,7 @@ __device__ __forceinline__ uint4 narrow(const float (&x)[8])
 }
 
 // The partners of channels [8 ch, 8 ch + 8) in the half layout, from the head's row in global memory (16 bytes at a
-// time where the halves begin at multiples of 8 channels); anything for channels that are not turned.
+// time where the halves begin at multiples of 8 channels); 0 for channels that are not turned.
 template <typename T>
 __device__ __forceinline__ uint4 partners(const RopeDev& rope, const char* row, int ch)
 {
@@ -79,41 +120,12 @@ __device__ __forceinline__ uint4 partners(const RopeDev& rope, const char* row, 
         uint32_t u[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const int c = c0 + 2 * i + e, p = c < h ? c + h : c < 2 * h ? c - h : c;
-            u[e] = *reinterpret_cast<const unsigned short*>(row + p * 2);
+            const int c = c0 + 2 * i + e;
+            u[e] = c < 2 * h ? *reinterpret_cast<const unsigned short*>(row + (c < h ? c + h : c - h) * 2) : 0;
         }
         w[i] = u[0] | u[1] << 16;
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-// x, channels [8 ch, 8 ch + 8) of a head, turned to position p; y: their partners (half layout).
-template <bool INTERLEAVED>
-__device__ __forceinline__ void turn(const RopeDev& rope, const Turns<INTERLEAVED>& t, int p, int ch, float (&x)[8],
-                                     const float (&y)[8])
-{
-    if constexpr (INTERLEAVED) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (ch * 4 + j < rope.half) {
-                float c, s;
-                t.at(rope, p, j, c, s);
-                const float a = x[2 * j], b = x[2 * j + 1];
-                x[2 * j] = a * c - b * s;
-                x[2 * j + 1] = a * s + b * c;
-            }
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int at = ch * 8 + j;
-            if (at < 2 * rope.half) {
-                float c, s;
-                t.at(rope, p, j, c, s);
-                x[j] = x[j] * c + (at < rope.half ? -y[j] : y[j]) * s;
-            }
-        }
-    }
 }
 
 }  // namespace wk

@@ -73,12 +73,13 @@ __global__ void __launch_bounds__(WARPS * 32) k_rotate(RotateArgs a, int parts)
                 at = at < 32 ? x : y;
             }
         }
-        p = (a.next ? a.next[r] : 0) + depth;
+        p = (int)((unsigned)(a.next ? a.next[r] : 0) + (unsigned)depth);
     }
 
     const int sub = lane / CH, ch = lane - sub * CH;
-    Turns<INTERLEAVED> turns;
-    turns.load(a.rope, ch);
+    Rotor<INTERLEAVED> rotor;
+    rotor.load(a.rope, ch);
+    rotor.at(p);
     const int nq = a.q_out ? a.q_heads : 0, rows = nq + (a.k_out ? a.kv_heads : 0);
     const int per = ((rows + parts - 1) / parts + RPW - 1) / RPW * RPW;
     const int row0 = part * per, row1 = min(rows, row0 + per);
@@ -105,7 +106,7 @@ __global__ void __launch_bounds__(WARPS * 32) k_rotate(RotateArgs a, int parts)
                 float u[8], v[8];
                 widen<T>(x[i], u);
                 if (!INTERLEAVED) widen<T>(y[i], v);
-                turn<INTERLEAVED>(a.rope, turns, p, ch, u, v);
+                rotor.turn(u, v);
                 char* const dst = h < nq ? qo + (long long)h * D * 2 : ko + (long long)(h - nq) * D * 2;
                 *reinterpret_cast<uint4*>(dst + ch * 16) = narrow<T>(u);
             }
