@@ -2,15 +2,15 @@
 // products run on the fifth-generation tensor cores (tcgen05). See attend8.cuh for the operator.
 //
 // A CTA runs through a range of the axis of all key tiles, up to MT tiles of 128 rows at a time. Its warps have roles:
-//   four warps for each row tile do the softmax, one thread a row. A thread brings its row of queries into tensor memory,
-//   in half precision and scaled for it, reads a tile's scores once, and leaves the weights in the place of the scores;
-//   one thread issues the products: scores S = Q K' and out += P V, both with the first operand, Q or P, from tensor
-//   memory, so that shared memory, which the copies and conversions use too, is read for K and V only;
+//   four warps for each row tile do the softmax, one thread a row. A thread brings its row of queries into shared memory
+//   (256 channels: tensor memory), in half precision and scaled for it, reads a tile's scores once, and leaves the weights
+//   in the place of the scores;
+//   one thread issues the products: scores S = Q K' and out += P V, P from tensor memory;
 //   seven warps convert, 16 keys or values at a time in turn: codes come by asynchronous copies a few of those ahead, each
 //   lane's own, and go as half precision into a ring of shared memory, K0 V0 K1 V1 ..., in the 128-byte-swizzled layout of
 //   the matrix descriptors. New tokens have a tile of their own; those of bfloat16 are scaled by a power of two for each.
-// With two row tiles the tensor cores work on one while the softmax works on the other; with one, the scores of the next
-// tile are formed ahead into the second place. The accumulator stays in tensor memory; it is rescaled only when a row's
+// A row tile's scores have two places: the next ones are formed while the softmax works on those before. The accumulator
+// stays in tensor memory; it is rescaled only when a row's
 // maximum has grown by more than 2^8 over the one that its weights refer to, or a scale by more than 2^4.
 //
 // New tokens' values that are not finite would reach rows that do not see them (0 times infinity): they are replaced by
@@ -28,26 +28,31 @@ struct Many8 {
     static constexpr int RM = 128 * MT;                  // rows of a unit
     static constexpr int HALVES = (D + 63) / 64;         // blocks of 64 channels
     static constexpr int TILE = HALVES * KT * 128;       // keys or values of a tile, half precision
-    static constexpr int NB = D == 256 ? 4 : 8;          // of them in the ring
+    // the queries: 128 rows a row tile in shared memory, in tensor memory where 256 channels leave no room for that
+    static constexpr bool QS = D < 256;
+    static constexpr int QT = QS ? HALVES * 128 * 128 : 0;
+    static constexpr int PLACES = MT == 2 ? 4 : 2;       // of scores: two for each row tile
+    static constexpr int NB = D == 256 ? 4 : D == 64 ? 8 : 6;  // of them in the ring
     static constexpr int CONV = 7;                       // warps that convert, 16 keys or values at a time
     static constexpr int CPL = D / 32;                   // 16 codes each: what a lane has of those
-    static constexpr int NF = D == 256 ? 2 : 4;          // of them in flight, a warp
+    static constexpr int NF = D == 64 ? 4 : D == 96 ? 3 : 2;  // of them in flight, a warp
     static constexpr int RAW = CPL * 512 + 16;           // their codes, scales, whether their page is one of the pool
-    static constexpr int raw = NB * TILE;
+    static constexpr int q = NB * TILE;
+    static constexpr int raw = q + MT * QT;
     static constexpr int bars = (raw + CONV * NF * RAW + 15) / 16 * 16;
     static constexpr int full = bars, empty = full + NB * 8, qready = empty + NB * 8, sready = qready + 16,
-                         pready = sready + 24, odone = pready + 16, ofree = odone + 16, over = ofree + 16,
+                         pready = sready + 48, odone = pready + 32, ofree = odone + 32, over = ofree + 16,
                          tmem = over + 8;
     static constexpr int wild = tmem + 8;                // 8 flags of units
     static constexpr int late = wild + 8 * 4;            // whether a wait ran out
-    static constexpr int info = late + 8;                // 8 tiles' Info
+    static constexpr int info = (late + 8 + 15) / 16 * 16;  // 8 tiles' Info
     static constexpr int scratch = info + 8 * (64 * 8 + 32);
     static constexpr int pre = scratch + 96 * 8;
     static constexpr int bytes(int n_req) { return pre + Axis8::ints(n_req) * 4; }
     static constexpr int WARPS = 4 * MT + 1 + CONV;      // softmax, products, conversions
-    // columns of tensor memory: the scores' two places, the accumulators, the queries
-    static constexpr int s0 = 0, o0 = 2 * KT, q0 = o0 + MT * HALVES * 64;
-    static_assert(q0 + MT * (D / 2) <= 512, "tensor memory");
+    // columns of tensor memory: the scores' places, the accumulators, queries
+    static constexpr int s0 = 0, o0 = PLACES * KT, q0 = o0 + MT * HALVES * 64;
+    static_assert(q0 + (QS ? 0 : MT * (D / 2)) <= 512, "tensor memory");
     static_assert(info % 16 == 0 && scratch % 8 == 0 && TILE % 1024 == 0, "alignment");
 };
 
@@ -116,11 +121,13 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
         }
         for (int w = 0; w < 2; ++w) {
             mbar_init(sm0 + L::qready + w * 8, 4);
-            mbar_init(sm0 + L::pready + w * 8, 4);
-            mbar_init(sm0 + L::odone + w * 8, 1);
+            mbar_init(sm0 + L::pready + w * 16, 4);
+            mbar_init(sm0 + L::pready + w * 16 + 8, 4);
+            mbar_init(sm0 + L::odone + w * 16, 1);
+            mbar_init(sm0 + L::odone + w * 16 + 8, 1);
             mbar_init(sm0 + L::ofree + w * 8, 4);
         }
-        for (int w = 0; w < 3; ++w) mbar_init(sm0 + L::sready + w * 8, 1);
+        for (int w = 0; w < 6; ++w) mbar_init(sm0 + L::sready + w * 8, 1);
         mbar_init(sm0 + L::over, 1);
         for (int u = 0; u < 8; ++u) wilds[u] = 0;
         *late = 0;
@@ -134,7 +141,7 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
     // A wait that runs out is recorded and ends its warp's part; the others' waits run
     // out after it (no warps meet at a barrier without a limit before the end), and all meet at
     // the end, where what is in flight is waited for and tensor memory is freed. Whoever waits for a
-    // barrier waits for all of its phases (the conversions: see there).
+    // barrier waits for all of its phases, or knows that the one before is over: a wait tells two apart, not three.
     auto wait = [&](uint32_t bar, int phase) -> bool {
         if (mbar_wait(bar, phase & 1)) return true;
         atomicOr(a.err, WORKER_TIMEOUT);
@@ -304,25 +311,26 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
         cp_wait<0>();
     } else if (warp == 4 * MT) {
         // ------------------------------------------------------------ products
-        // Steps of a tile and a row tile each. The scores of a step go to place step % 2; they are formed when the
-        // products with values of the step two before have been started.
+        // Steps of a tile and a row tile each. With two row tiles the scores of step k go to place k % 4 and are formed when
+        // the products with values of the step four before have been started, with one to place k % 2, two before: a row
+        // tile's next scores are formed while its softmax works on those before.
         constexpr uint32_t qk = product<__half>(KT, false), pv = product<__half>(D, true);
         const bool leader = elected();
         Cursor u = C;
-        int asked[2] = {0, 0}, run[2] = {0, 0}, started[2] = {0, 0};
+        int asked[2] = {0, 0}, run[4] = {0, 0, 0, 0}, started[2] = {0, 0};
 #pragma unroll 1
         for (int done = 0; done < n && ok;) {
             // (from one lane, so that the compiler knows that all have the same)
-            const int count = __shfl_sync(0xffffffffu, min(u.c - u.tile, n - done), 0), act = __shfl_sync(0xffffffffu, active(u), 0),
-                      steps = count * act;
-            if (MT == 2 && act == 2) ok = wait(sm0 + L::qready + 8, asked[1]++);
+            const int count = __shfl_sync(0xffffffffu, min(u.c - u.tile, n - done), 0), act = __shfl_sync(0xffffffffu, active(u), 0);
+            const int steps = count * act, ahead = 2 * act, two = MT == 2 && act == 2;
+            if (two) ok = wait(sm0 + L::qready + 8, asked[1]++);
             ok = ok && wait(sm0 + L::qready, asked[0]++);
 #pragma unroll 1
-            for (int k = -2; k < steps; ++k) {
+            for (int k = -ahead; k < steps; ++k) {
                 if (k >= 0) {
                     // out += P V of step k
-                    const int w = MT == 2 && act == 2 ? k & 1 : 0, t = MT == 2 && act == 2 ? k >> 1 : k, v = 2 * (done + t) + 1;
-                    ok = ok && wait(sm0 + L::pready + w * 8, w ? run[1]++ : run[0]++);
+                    const int w = two ? k & 1 : 0, t = two ? k >> 1 : k, v = 2 * (done + t) + 1, x2 = w * 2 + (t & 1);
+                    ok = ok && wait(sm0 + L::pready + x2 * 8, x2 == 0 ? run[0]++ : x2 == 1 ? run[1]++ : x2 == 2 ? run[2]++ : run[3]++);
                     if (w == 0) ok = ok && wait(sm0 + L::full + v % NB * 8, v / NB);
                     if (t == 0) {
                         const int before = w ? started[1]++ : started[0]++;
@@ -331,30 +339,38 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
                     tc_after();
-                    const uint32_t v0 = operand_lo(sm0 + v % NB * L::TILE, KT * 128), at = tm + L::s0 + (k & 1) * KT,
-                                   o = tm + L::o0 + w * (L::HALVES * 64);
+                    const uint32_t v0 = operand_lo(sm0 + v % NB * L::TILE, KT * 128),
+                                   at = tm + L::s0 + (k & (ahead - 1)) * KT, o = tm + L::o0 + w * (L::HALVES * 64);
                     if (leader) {
 #pragma unroll
                         for (int x = 0; x < KT / 16; ++x)
                             tc_mma_ts(o, at + x * 8, whole(v0 + x * 2048 / 16, OPERAND_HI), pv, t > 0 || x > 0);
-                        tc_commit(sm0 + L::odone + w * 8);
+                        tc_commit(sm0 + L::odone + x2 * 8);
                         if (w == act - 1) tc_commit(sm0 + L::empty + v % NB * 8);
                     }
                     __syncwarp();
                 }
-                if (k + 2 < steps) {
-                    // S = Q K' of step k + 2
-                    const int y = k + 2, w = MT == 2 && act == 2 ? y & 1 : 0, t = MT == 2 && act == 2 ? y >> 1 : y, i = 2 * (done + t);
+                if (k + ahead < steps) {
+                    // S = Q K' of step y
+                    const int y = k + ahead, w = two ? y & 1 : 0, t = two ? y >> 1 : y, i = 2 * (done + t);
                     if (w == 0) ok = __all_sync(0xffffffffu, ok && wait(sm0 + L::full + i % NB * 8, i / NB));
                     if (!ok) break;
                     tc_after();
-                    const uint32_t k0 = operand_lo(sm0 + i % NB * L::TILE, 0), at = tm + L::s0 + (y & 1) * KT,
-                                   q = tm + L::q0 + w * (D / 2);
+                    const uint32_t k0 = operand_lo(sm0 + i % NB * L::TILE, 0), at = tm + L::s0 + (y & (ahead - 1)) * KT;
                     if (leader) {
+                        if constexpr (L::QS) {
+                            const uint32_t q0 = operand_lo(sm0 + L::q + w * L::QT, 0);
 #pragma unroll
-                        for (int x = 0; x < D / 16; ++x)
-                            tc_mma_ts(at, q + x * 8, whole(k0 + ((x >> 2) * KT * 128 + (x & 3) * 32) / 16, OPERAND_HI), qk, x > 0);
-                        tc_commit(sm0 + L::sready + ((y & 1) + w) * 8);
+                            for (int x = 0; x < D / 16; ++x)
+                                tc_mma_ss(at, whole(q0 + ((x >> 2) * 128 * 128 + (x & 3) * 32) / 16, OPERAND_HI),
+                                          whole(k0 + ((x >> 2) * KT * 128 + (x & 3) * 32) / 16, OPERAND_HI), qk, x > 0);
+                        } else {
+                            const uint32_t q0 = tm + L::q0 + w * (D / 2);
+#pragma unroll
+                            for (int x = 0; x < D / 16; ++x)
+                                tc_mma_ts(at, q0 + x * 8, whole(k0 + ((x >> 2) * KT * 128 + (x & 3) * 32) / 16, OPERAND_HI), qk, x > 0);
+                        }
+                        tc_commit(sm0 + L::sready + (two ? y & 3 : 4 + (y & 1)) * 8);
                         if (w == act - 1) tc_commit(sm0 + L::empty + i % NB * 8);
                     }
                     __syncwarp();
@@ -369,8 +385,8 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
         const int w = warp >> 2, row = tid & 127;
         const uint32_t lanes = (uint32_t)(warp & 3) * 32u << 16, om = tm + lanes + L::o0 + w * (L::HALVES * 64);
         float factor = 0.0f;  // of this row's scores
-        int scored[3] = {0, 0, 0}, weighed = 0;
-        // this row's queries of the unit under u, 32 channels a time, into tensor memory
+        int scored[4] = {0, 0, 0, 0}, weighed[2] = {0, 0};  // phases of the barriers of two row tiles, of one; even and odd tiles
+        // this row's queries of the unit under u, 32 channels a time, into shared (tensor) memory
         auto queries = [&](const Cursor& u) {
             if (u.T * G - u.rt * RM <= w * 128) return;
             const int rho = u.rt * RM + w * 128 + row, t = rho / G;
@@ -400,10 +416,23 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
 #pragma unroll
                     for (int i = 0; i < 16; ++i) x[i] = to_half(x[i], f);
                 }
-                tmem_store16(tm + lanes + L::q0 + w * (D / 2) + c * 16, x);
+                if constexpr (L::QS) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int p = c * 4 + i;
+                        *reinterpret_cast<uint4*>(sm + L::q + w * L::QT + (p >> 3) * (128 * 128) + row * 128 + (((p & 7) ^ (row & 7)) << 4)) =
+                            make_uint4(x[i * 4], x[i * 4 + 1], x[i * 4 + 2], x[i * 4 + 3]);
+                    }
+                } else {
+                    tmem_store16(tm + lanes + L::q0 + w * (D / 2) + c * 16, x);
+                }
             }
-            tmem_stored();
-            tc_before();
+            if constexpr (L::QS) {
+                fence_async();
+            } else {
+                tmem_stored();
+                tc_before();
+            }
             __syncwarp();
             if (lane == 0) mbar_arrive(sm0 + L::qready + w * 8);
         };
@@ -423,11 +452,11 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
             } else {
                 const unsigned long long see = all_ancestors(a, u, row < rows ? (u.rt * RM + w * 128 + row) / G : 0, lane);
                 float m = -INFINITY, l = 0.0f, ref = -1000.0f;
-                const int bar1 = MT == 2 && act == 2 ? 0 : 1;  // with one row tile the places alternate
+                const bool two = MT == 2 && act == 2;
 #pragma unroll 1
                 for (int t = 0; t < count; ++t) {
-                    const int s = bar1 ? t & 1 : w, bar = s + w;
-                    ok = __all_sync(0xffffffffu, wait(sm0 + L::sready + bar * 8, bar == 2 ? scored[2]++ : bar ? scored[1]++ : scored[0]++));
+                    const int s = two ? (t & 1) * 2 + w : t & 1, phase = two ? (t & 1 ? scored[1]++ : scored[0]++) : t & 1 ? scored[3]++ : scored[2]++;
+                    ok = __all_sync(0xffffffffu, wait(sm0 + L::sready + (two ? s : 4 + s) * 8, phase));
                     if (!ok) break;
                     tc_after();
                     const uint32_t st = tm + lanes + L::s0 + s * KT;
@@ -484,8 +513,9 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                         const bool grown = top > m + 8.0f;  // (always where m is -inf and top is not)
                         const bool larger = scale_top > ref + 4.0f;
                         if (larger || __any_sync(0xffffffffu, grown)) {
-                            // the weights of the tiles before are in the accumulator
-                            ok = __all_sync(0xffffffffu, wait(sm0 + L::odone + w * 8, weighed - 1));
+                            // the weights of the tile before are in the accumulator (those of the one before it were when
+                            // these scores were formed)
+                            ok = __all_sync(0xffffffffu, wait(sm0 + L::odone + (w * 2 + (t + 1 & 1)) * 8, (t & 1 ? weighed[0] : weighed[1]) - 1));
                             if (!ok) break;
                             tc_after();
                             float g = grown ? ex2(m - top) : 1.0f;
@@ -549,12 +579,10 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                     }
                     tmem_stored();
                     tc_before();
-                    // (the products of the tile before are done, so that the arrivals before these have been seen; with
-                    // two row tiles they were started before this tile's scores)
-                    if (bar1 && weighed) ok = __all_sync(0xffffffffu, wait(sm0 + L::odone + w * 8, weighed - 1));
-                    if (!ok) break;
-                    if (lane == 0) mbar_arrive(sm0 + L::pready + w * 8);
-                    ++weighed;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(sm0 + L::pready + (w * 2 + (t & 1)) * 8);
+                    if (t & 1) ++weighed[1];
+                    else ++weighed[0];
                 }
                 if (!ok) break;
                 // the next unit's queries, while the last products run: this unit's scores are done
@@ -563,7 +591,7 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                     next_unit(next);
                     queries(next);
                 }
-                ok = __all_sync(0xffffffffu, wait(sm0 + L::odone + w * 8, weighed - 1));
+                ok = __all_sync(0xffffffffu, wait(sm0 + L::odone + (w * 2 + (count - 1 & 1)) * 8, (count & 1 ? weighed[0] : weighed[1]) - 1));
                 if (!ok) break;
                 tc_after();
                 const bool whole = u.tile == 0 && count == u.c;
