@@ -41,11 +41,13 @@ struct Many8 {
     static constexpr int raw = q + MT * QT;
     static constexpr int bars = (raw + CONV * NF * RAW + 15) / 16 * 16;
     static constexpr int full = bars, empty = full + NB * 8, qready = empty + NB * 8, sready = qready + 16,
-                         pready = sready + 48, odone = pready + 32, ofree = odone + 32, over = ofree + 16,
+                         pready = sready + 32, odone = pready + 32, ofree = odone + 32, merged = ofree + 16, over = merged + 8,
                          tmem = over + 8;
     static constexpr int wild = tmem + 8;                // 8 flags of units
     static constexpr int late = wild + 8 * 4;            // whether a wait ran out
-    static constexpr int info = (late + 8 + 15) / 16 * 16;  // 8 tiles' Info
+    static constexpr int factors = late + 8;             // of the rows' scores, for two units in turn
+    static constexpr int other = (factors + 2 * 128 * 4 + 15) / 16 * 16;  // what the second half of the tiles gave a row
+    static constexpr int info = other + 128 * 16;        // 8 tiles' Info
     static constexpr int scratch = info + 8 * (64 * 8 + 32);
     static constexpr int pre = scratch + 96 * 8;
     static constexpr int bytes(int n_req) { return pre + Axis8::ints(n_req) * 4; }
@@ -127,7 +129,8 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
             mbar_init(sm0 + L::odone + w * 16 + 8, 1);
             mbar_init(sm0 + L::ofree + w * 8, 4);
         }
-        for (int w = 0; w < 6; ++w) mbar_init(sm0 + L::sready + w * 8, 1);
+        for (int w = 0; w < 4; ++w) mbar_init(sm0 + L::sready + w * 8, 1);
+        mbar_init(sm0 + L::merged, 4);
         mbar_init(sm0 + L::over, 1);
         for (int u = 0; u < 8; ++u) wilds[u] = 0;
         *late = 0;
@@ -164,6 +167,7 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
         // this lane's i-th chunk of 16 codes: its row of the 16, its first channel
         auto row_of = [&](int i) { return D == 96 && i == 2 ? lane >> 1 : i / (D == 96 ? 1 : L::HALVES) * 8 + rr; };
         auto channel_of = [&](int i) { return D == 96 ? (i == 2 ? 64 + (lane & 1) * 16 : cc * 16) : i % L::HALVES * 64 + cc * 16; };
+        const long long row0 = row_of(0) * a.kv.token_stride + channel_of(0), eight = 8 * a.kv.token_stride;
         Cursor F = C;  // of the job that is fetched
         int fq = cw, ft = 0, fslot = 0, page = -1;
         // the page of job fq's keys, as the table has it
@@ -183,10 +187,19 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                 const char* const src = (values ? a.kv.v : a.kv.k) +
                                         (valid ? page * a.kv.page_stride + F.h * a.kv.head_stride + at * a.kv.token_stride : 0);
                 // (weights of 0 meet the codes of rows that hold no key: zeros)
+                if (D != 96 && valid && own >= 16) {
+                    const char* p = src + row0;
 #pragma unroll
-                for (int i = 0; i < L::CPL; ++i) {
-                    const bool in = valid && row_of(i) < own;
-                    cp16(d + i * 512 + lane * 16, src + (in ? row_of(i) * a.kv.token_stride + channel_of(i) : 0), in);
+                    for (int i = 0; i < L::CPL; ++i) {
+                        cp16(d + i * 512 + lane * 16, p + (i % L::HALVES) * 64, true);
+                        if (i % L::HALVES == L::HALVES - 1) p += eight;
+                    }
+                } else {
+#pragma unroll 1
+                    for (int i = 0; i < L::CPL; ++i) {
+                        const bool in = valid && row_of(i) < own;
+                        cp16(d + i * 512 + lane * 16, src + (in ? row_of(i) * a.kv.token_stride + channel_of(i) : 0), in);
+                    }
                 }
                 if (!values && lane < 2) {
                     const long long e = valid ? ((long long)page * H + F.h) * a.scales.per_page + (at >> a.scales.block_shift) : 0;
@@ -311,84 +324,87 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
         cp_wait<0>();
     } else if (warp == 4 * MT) {
         // ------------------------------------------------------------ products
-        // Steps of a tile and a row tile each. With two row tiles the scores of step k go to place k % 4 and are formed when
-        // the products with values of the step four before have been started, with one to place k % 2, two before: a row
-        // tile's next scores are formed while its softmax works on those before.
+        // Steps of a tile and a row tile each; of a unit with one row tile the even and the odd tiles have an accumulator and
+        // softmax warps each, as two row tiles would. The scores of step k go to place k % 4 (256 channels: 2), and are
+        // formed when the products with values of the step `ahead` before have been started: a step's scores are formed
+        // while the softmax works on those before.
         constexpr uint32_t qk = product<__half>(KT, false), pv = product<__half>(D, true);
-        const bool leader = elected();
-        Cursor u = C;
-        int asked[2] = {0, 0}, run[4] = {0, 0, 0, 0}, started[2] = {0, 0};
+        constexpr int PL = L::PLACES;
+        if (elected()) {  // (one thread waits and issues)
+            Cursor u = C;
+            int asked[2] = {0, 0}, run[4] = {0, 0, 0, 0}, started[2] = {0, 0};
 #pragma unroll 1
-        for (int done = 0; done < n && ok;) {
-            // (from one lane, so that the compiler knows that all have the same)
-            const int count = __shfl_sync(0xffffffffu, min(u.c - u.tile, n - done), 0), act = __shfl_sync(0xffffffffu, active(u), 0);
-            const int steps = count * act, ahead = 2 * act, two = MT == 2 && act == 2;
-            if (two) ok = wait(sm0 + L::qready + 8, asked[1]++);
-            ok = ok && wait(sm0 + L::qready, asked[0]++);
+            for (int done = 0; done < n && ok;) {
+                const int count = min(u.c - u.tile, n - done), two = active(u) == 2;
+                // (of single tiles as many ahead as the ring holds)
+                const int steps = two ? 2 * count : count, ahead = two || NB >= 2 * PL ? PL : MT == 2 ? NB / 2 : 2;
+                if (two) ok = wait(sm0 + L::qready + 8, asked[1]++);
+                ok = ok && wait(sm0 + L::qready, asked[0]++);
 #pragma unroll 1
-            for (int k = -ahead; k < steps; ++k) {
-                if (k >= 0) {
-                    // out += P V of step k
-                    const int w = two ? k & 1 : 0, t = two ? k >> 1 : k, v = 2 * (done + t) + 1, x2 = w * 2 + (t & 1);
-                    ok = ok && wait(sm0 + L::pready + x2 * 8, x2 == 0 ? run[0]++ : x2 == 1 ? run[1]++ : x2 == 2 ? run[2]++ : run[3]++);
-                    if (w == 0) ok = ok && wait(sm0 + L::full + v % NB * 8, v / NB);
-                    if (t == 0) {
-                        const int before = w ? started[1]++ : started[0]++;
-                        if (before > 0) ok = ok && wait(sm0 + L::ofree + w * 8, before - 1);
-                    }
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
-                    tc_after();
-                    const uint32_t v0 = operand_lo(sm0 + v % NB * L::TILE, KT * 128),
-                                   at = tm + L::s0 + (k & (ahead - 1)) * KT, o = tm + L::o0 + w * (L::HALVES * 64);
-                    if (leader) {
+                for (int k = -ahead; k < steps; ++k) {
+                    if (k >= 0) {
+                        // out += P V of step k
+                        const int w = MT == 2 ? k & 1 : 0, y = MT == 2 ? k >> 1 : k, v = 2 * (done + (two ? y : k)) + 1, x2 = w * 2 + (y & 1);
+                        ok = ok && wait(sm0 + L::pready + x2 * 8, x2 == 0 ? run[0]++ : x2 == 1 ? run[1]++ : x2 == 2 ? run[2]++ : run[3]++);
+                        if (w == 0 || !two) ok = ok && wait(sm0 + L::full + v % NB * 8, v / NB);
+                        if (y == 0) {
+                            const int before = w ? started[1]++ : started[0]++;
+                            if (before > 0) ok = ok && wait(sm0 + L::ofree + w * 8, before - 1);
+                        }
+                        if (!ok) break;
+                        tc_after();
+                        const uint32_t v0 = operand_lo(sm0 + v % NB * L::TILE, KT * 128), at = tm + L::s0 + (k & (PL - 1)) * KT,
+                                       o = tm + L::o0 + w * (L::HALVES * 64);
 #pragma unroll
                         for (int x = 0; x < KT / 16; ++x)
-                            tc_mma_ts(o, at + x * 8, whole(v0 + x * 2048 / 16, OPERAND_HI), pv, t > 0 || x > 0);
+                            tc_mma_ts(o, at + x * 8, whole(v0 + x * 2048 / 16, OPERAND_HI), pv, y > 0 || x > 0);
                         tc_commit(sm0 + L::odone + x2 * 8);
-                        if (w == act - 1) tc_commit(sm0 + L::empty + v % NB * 8);
+                        if (w == 1 || !two) tc_commit(sm0 + L::empty + v % NB * 8);
                     }
-                    __syncwarp();
-                }
-                if (k + ahead < steps) {
-                    // S = Q K' of step y
-                    const int y = k + ahead, w = two ? y & 1 : 0, t = two ? y >> 1 : y, i = 2 * (done + t);
-                    if (w == 0) ok = __all_sync(0xffffffffu, ok && wait(sm0 + L::full + i % NB * 8, i / NB));
-                    if (!ok) break;
-                    tc_after();
-                    const uint32_t k0 = operand_lo(sm0 + i % NB * L::TILE, 0), at = tm + L::s0 + (y & (ahead - 1)) * KT;
-                    if (leader) {
+                    const int z = k + ahead;
+                    if (z < steps) {
+                        // S = Q K' of step z
+                        const int w = MT == 2 ? z & 1 : 0, i = 2 * (done + (two ? z >> 1 : z));
+                        if (w == 0 || !two) ok = ok && wait(sm0 + L::full + i % NB * 8, i / NB);
+                        if (!ok) break;
+                        tc_after();
+                        const uint32_t k0 = operand_lo(sm0 + i % NB * L::TILE, 0), at = tm + L::s0 + (z & (PL - 1)) * KT;
                         if constexpr (L::QS) {
-                            const uint32_t q0 = operand_lo(sm0 + L::q + w * L::QT, 0);
+                            const uint32_t q0 = operand_lo(sm0 + L::q + (two ? w : 0) * L::QT, 0);
 #pragma unroll
                             for (int x = 0; x < D / 16; ++x)
                                 tc_mma_ss(at, whole(q0 + ((x >> 2) * 128 * 128 + (x & 3) * 32) / 16, OPERAND_HI),
                                           whole(k0 + ((x >> 2) * KT * 128 + (x & 3) * 32) / 16, OPERAND_HI), qk, x > 0);
                         } else {
-                            const uint32_t q0 = tm + L::q0 + w * (D / 2);
+                            const uint32_t q0 = tm + L::q0;
 #pragma unroll
                             for (int x = 0; x < D / 16; ++x)
                                 tc_mma_ts(at, q0 + x * 8, whole(k0 + ((x >> 2) * KT * 128 + (x & 3) * 32) / 16, OPERAND_HI), qk, x > 0);
                         }
-                        tc_commit(sm0 + L::sready + (two ? y & 3 : 4 + (y & 1)) * 8);
-                        if (w == act - 1) tc_commit(sm0 + L::empty + i % NB * 8);
+                        tc_commit(sm0 + L::sready + (z & (PL - 1)) * 8);
+                        if (w == 1 || !two) tc_commit(sm0 + L::empty + i % NB * 8);
                     }
-                    __syncwarp();
                 }
+                done += count;
+                if (done < n) next_unit(u);
             }
-            done += count;
-            if (done < n) next_unit(u);
         }
         __syncwarp();
     } else {
         // ------------------------------------------------------------ softmax
-        const int w = warp >> 2, row = tid & 127;
+        const int w = warp >> 2, row = tid & 127, first_row = warp * 32;
         const uint32_t lanes = (uint32_t)(warp & 3) * 32u << 16, om = tm + lanes + L::o0 + w * (L::HALVES * 64);
         float factor = 0.0f;  // of this row's scores
-        int scored[4] = {0, 0, 0, 0}, weighed[2] = {0, 0};  // phases of the barriers of two row tiles, of one; even and odd tiles
+        int weighed[2] = {0, 0}, merges = 0;  // this row tile's steps so far, even and odd ones; units whose halves were joined
+        float* const factors = reinterpret_cast<float*>(sm + L::factors);
+        float4* const other = reinterpret_cast<float4*>(sm + L::other);
         // this row's queries of the unit under u, 32 channels a time, into shared (tensor) memory
-        auto queries = [&](const Cursor& u) {
+        auto queries = [&](const Cursor& u, int number) {
             if (u.T * G - u.rt * RM <= w * 128) return;
+            if (u.T * G - u.rt * RM <= first_row) {  // (none of this warp's rows: whatever lies there meets no other row)
+                if (lane == 0) mbar_arrive(sm0 + L::qready + w * 8);
+                return;
+            }
             const int rho = u.rt * RM + w * 128 + row, t = rho / G;
             const bool live = rho < u.T * G;
             const uint4* const src = reinterpret_cast<const uint4*>(
@@ -404,6 +420,7 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
             }
             const float f = half_factor(top);
             factor = (BF16 ? half_back(top) : 1.0f) * a.scale_log2;
+            if (MT == 2 && w == 0) factors[(number & 1) * 128 + row] = factor;
 #pragma unroll 1
             for (int c = 0; c < D / 32; ++c) {
                 uint32_t x[16];
@@ -437,27 +454,36 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
             if (lane == 0) mbar_arrive(sm0 + L::qready + w * 8);
         };
         Cursor u = C;
-        queries(u);
+        queries(u, 0);
         int units = 0;
 #pragma unroll 1
         for (int done = 0; done < n && ok;) {
-            const int count = min(u.c - u.tile, n - done), rows = u.T * G - u.rt * RM - w * 128, act = active(u);
-            const bool more = done + count < n;
+            const int count = min(u.c - u.tile, n - done);
+            const bool more = done + count < n, two = active(u) == 2, split = MT == 2 && !two;
+            // this warp's rows of the unit, from row0 on, and how many of the tiles are its own: all, or every other one
+            const int row0 = two ? w * 128 : 0, rows = u.T * G - u.rt * RM - row0, mine = split ? (count + 1 - w) / 2 : count;
+            const bool idle = rows <= (warp & 3) * 32;
             Cursor next = u;
-            if (rows <= 0) {
+            if (mine == 0) {
                 if (more) {
                     next_unit(next);
-                    queries(next);
+                    queries(next, units + 1);
                 }
             } else {
-                const unsigned long long see = all_ancestors(a, u, row < rows ? (u.rt * RM + w * 128 + row) / G : 0, lane);
+                const unsigned long long see = all_ancestors(a, u, row < rows ? (u.rt * RM + row0 + row) / G : 0, lane);
                 float m = -INFINITY, l = 0.0f, ref = -1000.0f;
-                const bool two = MT == 2 && act == 2;
 #pragma unroll 1
-                for (int t = 0; t < count; ++t) {
-                    const int s = two ? (t & 1) * 2 + w : t & 1, phase = two ? (t & 1 ? scored[1]++ : scored[0]++) : t & 1 ? scored[3]++ : scored[2]++;
-                    ok = __all_sync(0xffffffffu, wait(sm0 + L::sready + (two ? s : 4 + s) * 8, phase));
+                for (int y = 0; y < mine; ++y) {
+                    const int t = split ? 2 * y + w : y, s = MT == 2 ? (y & 1) * 2 + w : y & 1;
+                    ok = __all_sync(0xffffffffu, wait(sm0 + L::sready + s * 8, y & 1 ? weighed[1] : weighed[0]));
                     if (!ok) break;
+                    if (y & 1) ++weighed[1];
+                    else ++weighed[0];
+                    if (idle) {
+                        if (lane == 0) mbar_arrive(sm0 + L::pready + (w * 2 + (y & 1)) * 8);
+                        continue;
+                    }
+                    if (split && w && y == 0) factor = factors[(units & 1) * 128 + row];
                     tc_after();
                     const uint32_t st = tm + lanes + L::s0 + s * KT;
                     uint32_t v[2][32];
@@ -478,15 +504,15 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                         const int step = own > 0 ? 0 : 1;
 #pragma unroll 1
                         for (int c = 0; c < 4; ++c) {
-                            uint32_t y[16];
-                            tmem_load16(y, st + c * 16);
+                            uint32_t z[16];
+                            tmem_load16(z, st + c * 16);
                             const int left = own - c * 16;
                             const uint32_t vis = own <= 0 ? (uint32_t)(see >> (c * 16))
                                                  : !info.valid[c] ? 0u : left >= 16 ? 0xffffu : left > 0 ? (1u << left) - 1 : 0u;
 #pragma unroll
                             for (int i = 0; i < 16; ++i)
-                                y[i] = vis >> i & 1 ? __float_as_uint(__uint_as_float(y[i]) * (ks[i * step] * factor)) : 0xff800000u;
-                            tmem_store16(st + c * 16, y);
+                                z[i] = vis >> i & 1 ? __float_as_uint(__uint_as_float(z[i]) * (ks[i * step] * factor)) : 0xff800000u;
+                            tmem_store16(st + c * 16, z);
                             ks += step ? 16 : 1;
                         }
                         tmem_stored();
@@ -500,13 +526,13 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                         float t0 = -INFINITY, t1 = -INFINITY;
 #pragma unroll
                         for (int i = 0; i < 16; i += 4) {
-                            const uint32_t* const y = &v[x / 2][x % 2 * 16 + i];
-                            t0 = fmaxf(fmaxf(t0, __uint_as_float(y[0])), __uint_as_float(y[1]));
-                            t1 = fmaxf(fmaxf(t1, __uint_as_float(y[2])), __uint_as_float(y[3]));
+                            const uint32_t* const e = &v[x / 2][x % 2 * 16 + i];
+                            t0 = fmaxf(fmaxf(t0, __uint_as_float(e[0])), __uint_as_float(e[1]));
+                            t1 = fmaxf(fmaxf(t1, __uint_as_float(e[2])), __uint_as_float(e[3]));
                         }
                         top = fmaxf(top, fmaxf(t0, t1) * f[x]);
                     }
-                    if (t == 0) {
+                    if (y == 0) {
                         m = top;
                         ref = fmaxf(scale_top, -1000.0f);
                     } else {
@@ -515,7 +541,7 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                         if (larger || __any_sync(0xffffffffu, grown)) {
                             // the weights of the tile before are in the accumulator (those of the one before it were when
                             // these scores were formed)
-                            ok = __all_sync(0xffffffffu, wait(sm0 + L::odone + (w * 2 + (t + 1 & 1)) * 8, (t & 1 ? weighed[0] : weighed[1]) - 1));
+                            ok = __all_sync(0xffffffffu, wait(sm0 + L::odone + (w * 2 + (y + 1 & 1)) * 8, (y & 1 ? weighed[0] : weighed[1]) - 1));
                             if (!ok) break;
                             tc_after();
                             float g = grown ? ex2(m - top) : 1.0f;
@@ -546,8 +572,8 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                             uint64_t sum = 0;
 #pragma unroll
                             for (int i = 0; i < 16; i += 2) {
-                                const uint32_t* const y = &v[x / 2][x % 2 * 16 + i];
-                                const uint64_t z = fma2(pair2(y[0], y[1]), ff, bb);
+                                const uint32_t* const e = &v[x / 2][x % 2 * 16 + i];
+                                const uint64_t z = fma2(pair2(e[0], e[1]), ff, bb);
                                 const float e0 = ex2(low2(z)), e1 = ex2(high2(z));
                                 sum = add2(sum, pair2(__float_as_uint(e0), __float_as_uint(e1)));
                                 v[x / 2][x % 2 * 8 + i / 2] = Num<__half>::pack(e0, e1);
@@ -561,15 +587,15 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                         // new tokens: a scale each; weights lie where scores were that have been read
 #pragma unroll 1
                         for (int c = 0; c < 4; ++c) {
-                            uint32_t y[16], p[8];
-                            tmem_load16(y, st + c * 16);
+                            uint32_t z[16], p[8];
+                            tmem_load16(z, st + c * 16);
 #pragma unroll
                             for (int i = 0; i < 16; i += 2) {
                                 float e[2];
 #pragma unroll
                                 for (int k = 0; k < 2; ++k) {
                                     const float at = relative(info.lv[c * 16 + i + k], ref);
-                                    e[k] = ex2(__uint_as_float(y[i + k]) - base + at);
+                                    e[k] = ex2(__uint_as_float(z[i + k]) - base + at);
                                     l += e[k] * ex2(-at);
                                 }
                                 p[i / 2] = Num<__half>::pack(e[0], e[1]);
@@ -580,22 +606,58 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                     tmem_stored();
                     tc_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(sm0 + L::pready + (w * 2 + (t & 1)) * 8);
-                    if (t & 1) ++weighed[1];
-                    else ++weighed[0];
+                    if (lane == 0) mbar_arrive(sm0 + L::pready + (w * 2 + (y & 1)) * 8);
                 }
                 if (!ok) break;
+                const int last_done = L::odone + (w * 2 + (mine - 1 & 1)) * 8, last_phase = (mine & 1 ? weighed[0] : weighed[1]) - 1;
+                const bool joins = split && count > 1;
+                if (joins && w) {
+                    // the odd tiles: their accumulator stays where it is, the other warps take it from there
+                    ok = __all_sync(0xffffffffu, wait(sm0 + last_done, last_phase));
+                    if (!ok) break;
+                    if (!idle) other[row] = make_float4(m, l, ref, 0.0f);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(sm0 + L::merged);
+                    if (more) {
+                        next_unit(next);
+                        queries(next, units + 1);
+                    }
+                    done += count;
+                    ++units;
+                    u = next;
+                    continue;
+                }
                 // the next unit's queries, while the last products run: this unit's scores are done
-                const float unit = ex2(ref);
+                if (joins) {
+                    ok = __all_sync(0xffffffffu, wait(sm0 + L::merged, merges++));
+                    if (!ok) break;
+                }
                 if (more) {
                     next_unit(next);
-                    queries(next);
+                    queries(next, units + 1);
                 }
-                ok = __all_sync(0xffffffffu, wait(sm0 + L::odone + (w * 2 + (count - 1 & 1)) * 8, (count & 1 ? weighed[0] : weighed[1]) - 1));
+                ok = __all_sync(0xffffffffu, wait(sm0 + last_done, last_phase));
                 if (!ok) break;
+                if (idle) {
+                    if (lane == 0) mbar_arrive(sm0 + L::ofree + w * 8);
+                    if (joins && lane == 0) mbar_arrive(sm0 + L::ofree + 8);
+                    done += count;
+                    ++units;
+                    u = next;
+                    continue;
+                }
                 tc_after();
+                float unit = ex2(ref), unit1 = 0.0f;
+                if (joins) {
+                    const float4 x = other[row];
+                    const float top = fmaxf(m, x.x), base = top == -INFINITY ? 0.0f : top, g0 = ex2(m - base), g1 = ex2(x.x - base);
+                    l = l * g0 + x.y * g1;
+                    unit *= g0;
+                    unit1 = ex2(x.z) * g1;
+                    m = top;
+                }
                 const bool whole = u.tile == 0 && count == u.c;
-                const int rr = w * 128 + row, rho = u.rt * RM + rr, t = rho / G, hd = u.h * G + rho - t * G;
+                const int rr = row0 + row, rho = u.rt * RM + rr, t = rho / G, hd = u.h * G + rho - t * G;
                 float* const part = part_of<D, RM>(a, me, u.tile == 0 ? 1 : 0);
                 const float scale = whole ? (l > 0.0f || l != l ? 1.0f / l : 0.0f) : 1.0f;
                 const bool wild = wilds[units & 7] == units + 1;
@@ -603,9 +665,16 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                 for (int c = 0; c < D / 32; ++c) {
                     uint32_t o[32];
                     tmem_load(o, om + c * 32);
-                    if (row < rows) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * unit * scale);
+                    for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * unit * scale);
+                    if (joins) {
+                        uint32_t o1[32];
+                        tmem_load(o1, om + L::HALVES * 64 + c * 32);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            o[i] = __float_as_uint(fmaf(__uint_as_float(o1[i]) * unit1, scale, __uint_as_float(o[i])));
+                    }
+                    if (row < rows) {
                         if (wild) {
                             // values that are not finite, of the tokens that this row sees
                             for (int x = 0; x < u.T; ++x) {
@@ -642,6 +711,7 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                 tc_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(sm0 + L::ofree + w * 8);
+                if (joins && lane == 0) mbar_arrive(sm0 + L::ofree + 8);
                 if (row < rows) {
                     if (!whole) *reinterpret_cast<float2*>(part + rr * 2) = make_float2(m, l);
                     else if (a.lse) a.lse[(long long)(u.lo + t) * (H * G) + hd] = (m + log2f(l)) * LN2;
