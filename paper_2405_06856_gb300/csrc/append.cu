@@ -372,11 +372,14 @@ cudaError_t launch_kind(const AppendArgs& a, int sms, cudaStream_t st)
         return (int)(want < (long long)PER_SM * sms ? want : PER_SM * sms);
     };
     if (a.scales.k) {
-        const int need = (1 << a.scales.block_shift) / ROWS8<D>, wpu = need < WARPS ? need : WARPS;
+        // as many warps a unit as have the rows that a request's new tokens, on average, bring to a block
+        const long long mean = ((long long)a.n_acc + a.tok.n_req - 1) / a.tok.n_req, rows = mean < 1 << a.scales.block_shift ? mean : 1 << a.scales.block_shift;
+        int wpu = 1;
+        while (wpu < WARPS && wpu * ROWS8<D> < rows) wpu *= 2;
         // (a request's tokens enter two blocks more than they fill, at most)
         const long long blocks = ((long long)a.n_acc >> a.scales.block_shift) + 2ll * a.tok.n_req;
-        // several rows of heads a unit where there are 8 units for every group of warps all the same
-        long long many = blocks * 2 * H * wpu / (8ll * WARPS * PER_SM * sms);
+        // several rows of heads a unit where there are 4 units for every group of warps all the same
+        long long many = blocks * 2 * H * wpu / (4ll * WARPS * PER_SM * sms);
         many = many < 1 ? 1 : many < 2 * H ? many : 2 * H;
         k_append8<T, D, INTERLEAVED><<<ctas(blocks * ((2 * H + many - 1) / many), WARPS / wpu), NT, smem, st>>>(a, wpu, (int)many);
     } else {
