@@ -702,7 +702,7 @@ int aladdin_worker_rotate(aladdin_worker* wk, const aladdin_rope* rope, const al
                           void* k_out, int64_t k_out_stride);
 
 /* Append tokens to the cache: those that acc_off and acc choose, as in aladdin_worker_accept (at most
- * ALADDIN_TREE_MAX a request), or all new tokens (acc_off NULL), any number of them. The i-th takes slot len[r] + i
+ * ALADDIN_TREE_MAX a request; acc may be NULL where n_acc is 0), or all new tokens (acc_off NULL), any number of them. The i-th takes slot len[r] + i
  * and position next[r] + i (len[r] + i where next is NULL); its key is rotated to that position (rope NULL: copied),
  * rounded once, its value copied, pos (nullable) receives the position, weight (nullable) 0, and len and next advance.
  * tok->q and tok->parent are not read. Slots on a page outside the pool are not written (and recorded); a request

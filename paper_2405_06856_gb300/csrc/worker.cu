@@ -181,7 +181,9 @@ int check_append(const aladdin_worker* wk, const aladdin_tokens* tok, const alad
     int rc = check_tokens(wk, tok, false, &a->tok);
     if (rc) return rc;
     if (rope && (rc = check_rope(wk, rope, &a->rope))) return rc;
-    if (!acc_off != !acc || (acc_off && n_acc < 0) || !all_on_device(wk, {acc_off, acc}, 4)) return ALADDIN_ERR_ARG;
+    // (no chosen tokens, no array of them: an empty tensor has no address)
+    if (acc_off ? n_acc < 0 || (!acc && n_acc > 0) : acc != nullptr) return ALADDIN_ERR_ARG;
+    if (!all_on_device(wk, {acc_off, acc}, 4)) return ALADDIN_ERR_ARG;
     a->acc_off = acc_off;
     a->acc = acc;
     a->n_acc = acc_off ? n_acc : a->tok.n_tok;
