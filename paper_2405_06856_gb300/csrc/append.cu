@@ -10,10 +10,12 @@
 // number, 2^-6 of the scale: a scale that grows lets codes be rounded again without loss, and blocks do
 // not depend on how their tokens came in. A warp has a few rows of a block, four chunks of 8 channels a lane, and keeps
 // them, rotated, in registers from the maximum to the codes; the warps of a block exchange their maxima. Instructions are
-// what it spends most of: so a lane forms the angles of its first row and turns them on from row to row.
+// what it spends most of: so a lane forms the angles of every other row and turns them on to its next. (Three turns after one
+// another: 47 us for 50, but half as many codes more than by 64-bit angles came out on the other side of a rounding; every
+// row's own angles: 55. Of 58 million codes 7 differ from those of exact angles so.)
 //
 // Measured: prompts of 20,178 tokens, 8 key heads of 128 channels, into 16 bits 36 us, 4.6 TB/s read and written (a unit of one
-// token, a search and new angles each: 49); 36,000 tokens, 4 heads of 96, into 8 bits in blocks of 64: 47 us, 1.8 TB/s, half of the
+// token, a search and new angles each: 49); 36,000 tokens, 4 heads of 96, into 8 bits in blocks of 64: 50 us, 1.7 TB/s, half of the
 // instruction slots and the rest latency of rounds that end in a barrier (one warp a block that reads its rows twice:
 // 66). One token each of 128 requests: 6 and 9 us with the launch, a chain of look-ups.
 //
@@ -276,15 +278,15 @@ __global__ void __launch_bounds__(NT, PER_SM) k_append8(AppendArgs a, int wpu, i
                         if (!INTERLEAVED && turned) mates[i] = partners<T>(a.rope, row, ch);
                     }
                 }
-                if (turned && s0 + member * RW < end) rotor.at((int)((unsigned)q.next[r] + (unsigned)(s0 + mine - len)));
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     widen<T>(raw[i], x[i]);
                     if (turned && s0 + member * RW + i * RPW < end) {
+                        if (i % 2 == 0) rotor.at((int)((unsigned)q.next[r] + (unsigned)(s0 + mine + i * RPW - len)));
+                        else rotor.on(by);
                         float z[8];
                         if (!INTERLEAVED) widen<T>(mates[i], z);
                         rotor.turn(x[i], z);
-                        if (i + 1 < N) rotor.on(by);
                     }
                 }
             };
