@@ -19,7 +19,7 @@
 // unrolled into the roles' loops (145 KB of code) a quarter of the warps' time went into fetching instructions. Measured,
 // 24 requests of 60,854 cached tokens with trees of up to 64 tokens, 64 query and 8 key heads of 128 channels: 324 us so,
 // 219 with a loop over units and one over tiles in each role, 205 with queries in shared memory and two places of
-// scores, 500 TFLOP/s of 1,932 that a large product reaches; 37 requests of 57,837 tokens with trees of up to 5, 28 and
+// scores, 500 TFLOP/s of 1,888 that a large product reaches; 37 requests of 57,837 tokens with trees of up to 5, 28 and
 // 4 heads of 96: 63 us, and 50 since seven warps convert in turn.
 //
 // New tokens' values that are not finite would reach rows that do not see them (0 times infinity): they are replaced by
