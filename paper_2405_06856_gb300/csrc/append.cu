@@ -14,10 +14,10 @@
 // another: 47 us for 50, but half as many codes more than by 64-bit angles came out on the other side of a rounding; every
 // row's own angles: 55. Of 58 million codes 7 differ from those of exact angles so.)
 //
-// Measured: prompts of 20,178 tokens, 8 key heads of 128 channels, into 16 bits 36 us, 4.6 TB/s read and written (a unit of one
+// Measured: prompts of 20,178 tokens, 8 key heads of 128 channels, into 16 bits 34 us, 4.9 TB/s read and written (a unit of one
 // token, a search and new angles each: 49); 36,000 tokens, 4 heads of 96, into 8 bits in blocks of 64: 50 us, 1.7 TB/s, half of the
 // instruction slots and the rest latency of rounds that end in a barrier (one warp a block that reads its rows twice:
-// 66). One token each of 128 requests: 6 and 9 us with the launch, a chain of look-ups.
+// 66; in blocks of 16 with 8 heads of 128 in the half layout, 222 MB: 129 us, 162 where all warps of a CTA wait for one another). One token each of 128 requests: 6 and 9 us with the launch, a chain of look-ups.
 //
 // The kernels lay the requests' units on one axis (a prefix sum by each CTA, which keeps what the units need of them) and
 // go over it with all warps of the GPU. The last CTA to finish advances the lengths.
@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(NT, PER_SM) k_append8(AppendArgs a, int wpu, i
         const bool have = any && (unsigned)page < (unsigned)a.kv.pages;
         if (any && !have && lane == 0 && member == 0) atomicOr(a.err, WORKER_BAD_INPUT);
 #pragma unroll 1
-        for (int hv = hv0; hv < hv0 + many; ++hv, ++round) {  // (all warps of a CTA, the same number of times)
+        for (int hv = hv0; hv < hv0 + many; ++hv, ++round) {  // (all warps of a group, the same number of times)
             const bool live = have && hv < 2 * H, values = hv >= H;
             const int h = values ? hv - H : hv, end = live ? hi : lo;
             const long long stride = (values ? a.tok.v_stride : a.tok.k_stride) * 2;
@@ -317,7 +317,8 @@ __global__ void __launch_bounds__(NT, PER_SM) k_append8(AppendArgs a, int wpu, i
             const float old = live && lo > first ? *held : 0.0f;
             if (wpu > 1) {
                 if (lane == 0) tops[round & 1][warp] = most;
-                __syncthreads();  // (the scale has been read by all when the first writes it; two sets: one round may be behind)
+                // the group's warps alone (the scale has been read by all when the first writes it; two sets: one may be a round behind)
+                asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(wpu * 32) : "memory");
                 for (int w = 0; w < wpu; ++w) most = fmaxf(most, tops[round & 1][group * wpu + w]);
             }
             if (!live) continue;
@@ -388,6 +389,8 @@ cudaError_t launch_kind(const AppendArgs& a, int sms, cudaStream_t st)
         // several rows of heads a unit where there are 4 units for every group of warps all the same
         long long many = blocks * 2 * H * wpu / (4ll * WARPS * PER_SM * sms);
         many = many < 1 ? 1 : many < 2 * H ? many : 2 * H;
+        const long long of = (2 * H + many - 1) / many;  // units of a block, of even size
+        many = (2 * H + of - 1) / of;
         k_append8<T, D, INTERLEAVED><<<ctas(blocks * ((2 * H + many - 1) / many), WARPS / wpu), NT, smem, st>>>(a, wpu, (int)many);
     } else {
         // heads of a unit: all, or as few as give every warp a unit, a warp's loads at least

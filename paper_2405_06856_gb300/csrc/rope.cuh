@@ -19,32 +19,47 @@ namespace wk {
 template <bool INTERLEAVED>
 struct Rotor {
     static constexpr int N = INTERLEAVED ? 4 : 8;
-    uint32_t hi[N], lo[N];  // frequencies
+    const unsigned long long* turn_of;
+    uint32_t hi[4], lo[4];  // frequencies of the pairs whose angles this lane forms
     float c[N], s[N];
     float scale;
-    unsigned turned, minus;  // bits of the pairs (channels) that are turned, whose sine is taken negative
+    int half, ch;
 
-    __device__ __forceinline__ void load(const RopeDev& rope, int ch)
+    __device__ __forceinline__ void load(const RopeDev& rope, int chunk)
     {
+        turn_of = rope.turn;
         scale = rope.scale;
-        turned = minus = 0;
+        half = rope.half;
+        ch = chunk;
+        frequencies(hi, lo, upper() ? 4 : 0);
+    }
+    // Half layout, halves that begin at multiples of 8 channels: the lanes of a pair of chunks form the angles of 4 of their
+    // pairs each, the one of the upper half the last 4, and exchange them (all 8 each: 36 us for 34 in append.cu, 16 bits).
+    __device__ __forceinline__ bool shared() const { return (half & 7) == 0; }
+    __device__ __forceinline__ bool upper() const { return !INTERLEAVED && shared() && ch * 8 >= half; }
+    __device__ __forceinline__ int pair(int j) const
+    {
+        const int at = ch * 8 + j;
+        return INTERLEAVED ? ch * 4 + j : at < half ? at : at - half;
+    }
+    __device__ __forceinline__ void frequencies(uint32_t (&h)[4], uint32_t (&l)[4], int j0) const
+    {
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const int at = ch * 8 + j, p = INTERLEAVED ? ch * 4 + j : at < rope.half ? at : at - rope.half;
-            if (p < rope.half) turned |= 1u << j;
-            if (!INTERLEAVED && at < rope.half) minus |= 1u << j;
-            const unsigned long long t = p < rope.half ? __ldg(rope.turn + p) : 0;
-            hi[j] = (uint32_t)(t >> 32);
-            lo[j] = (uint32_t)t;
+        for (int j = 0; j < 4; ++j) {
+            const int p = pair(j0 + j);
+            const unsigned long long t = p < half ? __ldg(turn_of + p) : 0;
+            h[j] = (uint32_t)(t >> 32);
+            l[j] = (uint32_t)t;
         }
     }
-    // to position p
-    __device__ __forceinline__ void at(int p)
+    // Cosine and sine of 4 pairs at position p.
+    static __device__ __forceinline__ void angles(int p, const uint32_t (&h)[4], const uint32_t (&l)[4], float (&cs)[4],
+                                                  float (&sn)[4])
     {
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            // the upper word of p (hi, lo), p signed
-            const uint32_t turn = (uint32_t)p * hi[j] + __umulhi((uint32_t)p, lo[j]) - (p < 0 ? lo[j] : 0u);
+        for (int j = 0; j < 4; ++j) {
+            // the upper word of p (h, l), p signed
+            const uint32_t turn = (uint32_t)p * h[j] + __umulhi((uint32_t)p, l[j]) - (p < 0 ? l[j] : 0u);
             const uint32_t quarter = (turn + 0x20000000u) & 0xc0000000u;
             // the angle is x + y: 2 pi / 2^32 comes in two parts, and the series' leading terms are added last
             const float f = (float)(int)(turn - quarter), x = f * 1.462918119976564e-9f, x2 = x * x;
@@ -55,10 +70,43 @@ struct Rotor {
             // of 0, 1, 2, 3 quarters more: (b, a), (-a, b), (-b, -a), (a, -b)
             const bool odd = quarter & 0x40000000u;
             const float u = odd ? a : b, v = odd ? b : a;
-            const uint32_t sign = (quarter & 0x80000000u) ^ (minus >> j << 31);
-            c[j] = __uint_as_float(__float_as_uint(u) ^ ((quarter + 0x40000000u) & 0x80000000u)) * scale;
-            s[j] = __uint_as_float(__float_as_uint(v) ^ sign) * scale;
-            if (!(turned >> j & 1)) c[j] = 1.0f, s[j] = 0.0f;
+            cs[j] = __uint_as_float(__float_as_uint(u) ^ ((quarter + 0x40000000u) & 0x80000000u));
+            sn[j] = __uint_as_float(__float_as_uint(v) ^ (quarter & 0x80000000u));
+        }
+    }
+    // to position p; all lanes of a warp, those of a row with the same p
+    __device__ __forceinline__ void at(int p)
+    {
+        float cs[4], sn[4];
+        angles(p, hi, lo, cs, sn);
+        if constexpr (INTERLEAVED) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool turned = ch * 4 + j < half;
+                c[j] = turned ? cs[j] * scale : 1.0f;
+                s[j] = turned ? sn[j] * scale : 0.0f;
+            }
+        } else {
+            float co[4], so[4];
+            if (shared()) {
+                const int mate = (threadIdx.x & 31) + (upper() ? -half / 8 : half / 8);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    co[j] = __shfl_sync(0xffffffffu, cs[j], mate);
+                    so[j] = __shfl_sync(0xffffffffu, sn[j], mate);
+                }
+            } else {
+                uint32_t h[4], l[4];
+                frequencies(h, l, 4);
+                angles(p, h, l, co, so);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int at = ch * 8 + j;
+                const float x = (j < 4) != upper() ? cs[j & 3] : co[j & 3], y = (j < 4) != upper() ? sn[j & 3] : so[j & 3];
+                c[j] = at < 2 * half ? x * scale : 1.0f;
+                s[j] = at < 2 * half ? y * (at < half ? -scale : scale) : 0.0f;
+            }
         }
     }
     // on by as many positions as `by`, a rotor at them with factor 1, stands for: an error of 2^-24 more
@@ -78,7 +126,7 @@ struct Rotor {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float a = x[2 * j], b = x[2 * j + 1];
-                if (turned >> j & 1) {
+                if (ch * 4 + j < half) {
                     x[2 * j] = fmaf(a, c[j], -b * s[j]);
                     x[2 * j + 1] = fmaf(a, s[j], b * c[j]);
                 }
