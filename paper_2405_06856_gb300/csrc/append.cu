@@ -12,12 +12,13 @@
 // them, rotated, in registers from the maximum to the codes; the warps of a block exchange their maxima. Instructions are
 // what it spends most of: so a lane forms the angles of every other row and turns them on to its next. (Three turns after one
 // another: 47 us for 50, but half as many codes more than by 64-bit angles came out on the other side of a rounding; every
-// row's own angles: 55. Of 58 million codes 7 differ from those of exact angles so.)
+// row's own angles: 55. Of 14 million keys' codes 7 differ from those of 64-bit arithmetic so, as many as with 64-bit angles.)
 //
 // Measured: prompts of 20,178 tokens, 8 key heads of 128 channels, into 16 bits 34 us, 4.9 TB/s read and written (a unit of one
-// token, a search and new angles each: 49); 36,000 tokens, 4 heads of 96, into 8 bits in blocks of 64: 50 us, 1.7 TB/s, half of the
+// token, a search and new angles each: 49); 36,000 tokens, 4 heads of 96, into 8 bits in blocks of 64: 51 us, 1.6 TB/s, half of the
 // instruction slots and the rest latency of rounds that end in a barrier (one warp a block that reads its rows twice:
-// 66; in blocks of 16 with 8 heads of 128 in the half layout, 222 MB: 129 us, 162 where all warps of a CTA wait for one another). One token each of 128 requests: 6 and 9 us with the launch, a chain of look-ups.
+// 66). In blocks of 16 with 8 heads of 128 in the half layout, 222 MB: 129 us (all warps of a CTA waiting for one another: 45
+// more). One token each of 128 requests: 6 and 9 us with the launch, a chain of look-ups.
 //
 // The kernels lay the requests' units on one axis (a prefix sum by each CTA, which keeps what the units need of them) and
 // go over it with all warps of the GPU. The last CTA to finish advances the lengths.
@@ -317,7 +318,8 @@ __global__ void __launch_bounds__(NT, PER_SM) k_append8(AppendArgs a, int wpu, i
             const float old = live && lo > first ? *held : 0.0f;
             if (wpu > 1) {
                 if (lane == 0) tops[round & 1][warp] = most;
-                // the group's warps alone (the scale has been read by all when the first writes it; two sets: one may be a round behind)
+                // the group's warps alone (the scale has been read by all when the first writes it; two sets of maxima: one may
+                // be a round behind)
                 asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(wpu * 32) : "memory");
                 for (int w = 0; w < wpu; ++w) most = fmaxf(most, tops[round & 1][group * wpu + w]);
             }
@@ -381,7 +383,8 @@ cudaError_t launch_kind(const AppendArgs& a, int sms, cudaStream_t st)
     };
     if (a.scales.k) {
         // as many warps a unit as have the rows that a request's new tokens, on average, bring to a block
-        const long long mean = ((long long)a.n_acc + a.tok.n_req - 1) / a.tok.n_req, rows = mean < 1 << a.scales.block_shift ? mean : 1 << a.scales.block_shift;
+        const long long mean = ((long long)a.n_acc + a.tok.n_req - 1) / a.tok.n_req, block = 1 << a.scales.block_shift;
+        const long long rows = mean < block ? mean : block;
         int wpu = 1;
         while (wpu < WARPS && wpu * ROWS8<D> < rows) wpu *= 2;
         // (a request's tokens enter two blocks more than they fill, at most)
