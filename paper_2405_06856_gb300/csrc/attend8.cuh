@@ -71,6 +71,9 @@ __device__ __forceinline__ float half_row(uint2 (&q)[N])
     return half_back(top);
 }
 
+// A block's scale; NaN of one that is not finite (infinity would make scores of -inf, which count as not seen).
+__device__ __forceinline__ float finite_scale(float k) { return k < INFINITY ? k : NAN; }
+
 // Logarithm of a block's scale: -inf of 0, NaN of what is none.
 __device__ __forceinline__ float log_scale(float v) { return v >= 0.0f && v < INFINITY ? __log2f(v) : NAN; }
 // ... relative to the reference

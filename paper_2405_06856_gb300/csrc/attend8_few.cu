@@ -447,7 +447,7 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                         for (int y = 0; y < NB; ++y) Num<__half>::mma(s[x][y], f, qf[i * CW + c][y][0], qf[i * CW + c][y][1]);
                     }
                 }
-                const float ks = scales[x];
+                const float ks = finite_scale(scales[x]);
 #pragma unroll
                 for (int y = 0; y < NB; ++y) {
                     const float k0 = ks * factor[y][0], k1 = ks * factor[y][1];

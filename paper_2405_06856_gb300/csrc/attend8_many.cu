@@ -253,7 +253,8 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                     const float k = *reinterpret_cast<const float*>(src + L::CPL * 512), v = *reinterpret_cast<const float*>(src + L::CPL * 512 + 4);
                     const int valid = *reinterpret_cast<const int*>(src + L::CPL * 512 + 8);
                     const float lv = valid && u.tile * KT + g * 16 < u.len ? log_scale(v) : -INFINITY;
-                    info.k[g] = k;  // (as it is, 0 too: the products that it meets are finite, and -inf only where it is not used)
+                    // (0 too as it is: the products that it meets are finite, and -inf only where it is not used)
+                    info.k[g] = finite_scale(k);
                     info.lv[g] = lv;
                     info.top[g] = lv;
                     info.valid[g] = valid;

@@ -27,3 +27,24 @@ def test_attend8_small_key_scales(A, q_heads, toks):  # noqa: F811
     case["k_scale"][case["table"][0, 1]] = 0.0
     d = Dev8(A, case)
     check_attend8(case, *d.worker.attend(d.kv, d.tok))
+
+
+@pytest.mark.parametrize("q_heads,toks", FEW_MANY)
+@pytest.mark.parametrize("held", [1, 16, 100])
+def test_attend8_infinite_key_scales(A, q_heads, toks, held):  # noqa: F811
+    """A key scale that is not finite makes the rows of its head and request not finite, also where all of its block's
+    products with the queries are negative."""
+    import torch
+    case = make8("bf16", q_heads, 2, 64, 16, [held, 40], toks)
+    case["q"] = -np.abs(case["q"])
+    case["k"] = np.where(case["k"] & 127 == 127, case["k"], case["k"] & 127)  # keys > 0
+    good = Dev8(A, case)
+    want, want_lse = good.worker.attend(good.kv, good.tok)
+    for x in (math.inf, math.nan):
+        d = Dev8(A, case)
+        d.k_scale[int(case["table"][0, 0]), 1, 0] = x
+        out, lse = d.worker.attend(d.kv, d.tok)
+        bad = torch.zeros_like(out, dtype=torch.bool)
+        bad[:toks[0], q_heads // 2:] = True
+        assert not out[bad].isfinite().any() and not lse[bad[..., 0]].isfinite().any()
+        assert torch.equal(out[~bad], want[~bad]) and torch.equal(lse[~bad[..., 0]], want_lse[~bad[..., 0]])
