@@ -7,11 +7,16 @@
 // for each row that brings its largest channel to 2^14 .. 2^15: half precision then holds every channel above 2^-28
 // of the largest without loss. Products and sums are 32-bit, and the scales and the row's power multiply the sums.
 //
-// The second product's weights e^(s_j - m) e_b are rounded to half precision (2^-12 of each, below 2^-14 of the
-// largest 2^-25 of that). For them to fit, results count in units of 2^ref: ref is the logarithm of a block's
-// scale, changed (and the results so far with it) where one comes that is more than 2^4 times as large, and the weight's
-// exponent takes the difference in, for nothing. Scales below 2^-40 of the reference count as that much, of
-// which half precision makes 0 again.
+// The second product's weights are rounded to half precision, 2^-11 of each, so what counts is what they refer to: not to
+// the largest scale, which may belong to a block without any weight, nor to the largest weight, whose block may have
+// next to no scale, but to the largest product of the two. A row keeps M, the maximum of t_j = s_j + log2 e_b (to base 2)
+// so far; its weights are 2^(t_j - M + UP), with UP as large as half precision and what M may lag behind allow, results
+// count in units of 2^(M - UP), and sums l of the weights without scales in units of 2^(M - d). So a weight is good to 2^-11 of
+// itself down to 2^-14 - UP of the largest, and 0 below 2^-25 - UP of it. Any d does that keeps the sums within 32 bits'
+// range: it is the logarithm of a scale, and while those of a tile are within 2^FAR of it, as nearly always, a tile
+// costs what it would with one scale for all. Others (and new tokens, each of which has a logarithm of its own) take a
+// longer way, on which d becomes what M has above the largest s_j. A scale of 0 has the logarithm LOG_ZERO.
+// Where scores are so large that logarithms next to them round, sums are rounded such that no weight passes 2^UP.
 #pragma once
 
 #include "attend.cuh"
@@ -33,16 +38,34 @@ __device__ __forceinline__ uint32_t half2_hi(uint32_t u)
     return h;
 }
 
-// The power of two that bfloat16 values of which `top` is the largest exponent field are multiplied by, and the one
+// The power of two that values of which `top` is the largest exponent field in 32 bits are multiplied by, and the one
 // that takes it back.
 __device__ __forceinline__ float half_factor(int top) { return __uint_as_float((uint32_t)(268 - min(max(top, 15), 254)) << 23); }
 __device__ __forceinline__ float half_back(int top) { return __uint_as_float((uint32_t)(min(max(top, 15), 254) - 14) << 23); }
 
-// The largest exponent field of two bfloat16 values and `top`.
-__device__ __forceinline__ int exponent(uint32_t w, int top) { return max(top, max((int)(w >> 7 & 0xff), (int)(w >> 23 & 0xff))); }
+// The largest magnitudes of the lower and of the upper values of words, as bits, and the exponent field in 32 bits of the
+// larger one (of half-precision numbers below 2^-14 that of 2^-14).
+__device__ __forceinline__ uint32_t largest2(uint32_t top, uint32_t w) { return __vmaxu2(top, w & 0x7fff7fffu); }
+template <typename T>
+__device__ __forceinline__ int exponent(uint32_t top)
+{
+    const uint32_t u = max(top & 0xffff, top >> 16);
+    if constexpr (std::is_same<T, __half>::value) return (int)max(u >> 10, 1u) + 112;
+    return (int)(u >> 7);
+}
+// The largest exponent field of finite values and `top`.
+template <typename T>
+__device__ __forceinline__ int finite_exponent(uint32_t w, int top)
+{
+    w = Num<T>::tame(w);
+    if constexpr (!std::is_same<T, __half>::value) return max(top, max((int)(w >> 7 & 0xff), (int)(w >> 23 & 0xff)));
+    const float2 v = Num<T>::unpack(w);
+    return max(top, max((int)(__float_as_uint(v.x) >> 23 & 0xff), (int)(__float_as_uint(v.y) >> 23 & 0xff)));
+}
+template <typename T>
 __device__ __forceinline__ uint32_t to_half(uint32_t w, float f)
 {
-    const float2 v = Num<__nv_bfloat16>::unpack(w);
+    const float2 v = Num<T>::unpack(w);
     return Num<__half>::pack(v.x * f, v.y * f);
 }
 
@@ -60,26 +83,33 @@ template <typename T, int N>
 __device__ __forceinline__ float half_row(uint2 (&q)[N])
 {
     if constexpr (std::is_same<T, __half>::value) return 1.0f;
-    int top = 0;
+    uint32_t most = 0;
 #pragma unroll
-    for (int x = 0; x < N; ++x) top = exponent(q[x].y, exponent(q[x].x, top));
+    for (int x = 0; x < N; ++x) most = largest2(largest2(most, q[x].x), q[x].y);
+    int top = exponent<T>(most);
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
     const float f = half_factor(top);
 #pragma unroll
-    for (int x = 0; x < N; ++x) q[x] = make_uint2(to_half(q[x].x, f), to_half(q[x].y, f));
+    for (int x = 0; x < N; ++x) q[x] = make_uint2(to_half<T>(q[x].x, f), to_half<T>(q[x].y, f));
     return half_back(top);
 }
 
 // A block's scale; NaN of one that is not finite (infinity would make scores of -inf, which count as not seen).
 __device__ __forceinline__ float finite_scale(float k) { return k < INFINITY ? k : NAN; }
 
-// Logarithm of a block's scale: -inf of 0, NaN of what is none.
-__device__ __forceinline__ float log_scale(float v) { return v >= 0.0f && v < INFINITY ? __log2f(v) : NAN; }
-// ... relative to the reference
-__device__ __forceinline__ float relative(float lv, float ref)
+constexpr float FAR = 40.0f, LOG_ZERO = -256.0f;
+
+// Logarithm of a block's scale, NaN of what is none.
+__device__ __forceinline__ float log_scale(float v)
 {
-    return lv == -INFINITY || lv - ref < -40.0f ? -40.0f : lv - ref;
+    return v > 0.0f && v < INFINITY ? __log2f(v) : v == 0.0f ? LOG_ZERO : NAN;
+}
+// 2^d in two factors, neither of which is lost below 2^-126 where the whole is not.
+__device__ __forceinline__ float2 unit_of(float d)
+{
+    const float x = fmaxf(d, -100.0f);
+    return make_float2(ex2(x), ex2(d - x));
 }
 
 // The axis of all key tiles (attend.cuh), its places dealt out whole: the first `more` workers have one place more than

@@ -73,18 +73,15 @@ struct Few8 {
 // its tiles, in keys.
 constexpr int PLACE_KEYS = 64, UNIT_KEYS = 64;
 
-// The results from now on in units of 2^to.
-template <int MO, int NB>
-__device__ __forceinline__ void rebase(float (&o)[MO][NB][4], float& ref, float to)
+// Room of the weights in half precision (attend8.cuh): a row's maximum does not lag.
+constexpr float UP = 15.0f;
+
+// The largest of the 8 lanes that hold a row.
+__device__ __forceinline__ float row_max(float v)
 {
-    const float f = ex2(ref - to);
 #pragma unroll
-    for (int x = 0; x < MO; ++x)
-#pragma unroll
-        for (int y = 0; y < NB; ++y)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[x][y][e] *= f;
-    ref = to;
+    for (int x = 4; x < 32; x <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, x));
+    return v;
 }
 
 // N consecutive floats that other warps wrote
@@ -354,9 +351,9 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
         cp_commit();
     }
 
-    float o[MO][NB][4], m[NB][2], l[NB][2];  // channels of rows 2 tq, 2 tq + 1
+    float o[MO][NB][4], M[NB][2], l[NB][2], d[NB][2];  // channels of rows 2 tq, 2 tq + 1, and what attend8.cuh says
+    float d_least = 0.0f, d_most = 0.0f;     // of all rows
     float unscale[NB];                       // of row gq of every block
-    float ref = -INFINITY;                   // the results count in units of 2^ref
     unsigned long long see[NB][2];
     bool fresh = true;
     int b = 0, tile0 = 0;  // a tile's place; the first tile of the unit that this warp has
@@ -373,13 +370,13 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
         if (fresh) {
             fresh = false;
             tile0 = C.tile;
-            ref = -INFINITY;
 #pragma unroll
             for (int y = 0; y < NB; ++y) {
 #pragma unroll
                 for (int x = 0; x < MO; ++x) o[x][y][0] = o[x][y][1] = o[x][y][2] = o[x][y][3] = 0.0f;
-                m[y][0] = m[y][1] = -INFINITY;
+                M[y][0] = M[y][1] = -INFINITY;
                 l[y][0] = l[y][1] = 0.0f;
+                d[y][0] = d[y][1] = 0.0f;
                 see[y][0] = see[y][1] = 1;
                 uint2 q[MO];
 #pragma unroll
@@ -417,12 +414,44 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
         const int first = cached ? 0 : (C.tile - (C.len + TK - 1) / TK) * TN;  // the first new token
 
         float s[KB][NB][4];  // keys gq, gq + 8 of a block by rows 2 tq, 2 tq + 1
-        float lv[KB];        // logarithms of the blocks' scales of values, relative to ref
+        float lv[KB];          // logarithms of the scales of the blocks' values, or of what key gq of a block has for one
+        float hi = -INFINITY;  // the largest
+        bool odd = true;       // whether a row's d is not within reach of all of them (attend8.cuh)
+        if (cached) {
+            // (a block without keys has no part, and one whose scale is none makes its scores NaN)
+            const Mask okm = oks[b];
+            const float* const scales = reinterpret_cast<const float*>(slot + L::TILE);
+            float lo = INFINITY;
+#pragma unroll
+            for (int x = 0; x < KB; ++x) {
+                lv[x] = log_scale(scales[KB + x]);
+                hi = fmaxf(hi, lv[x]);
+                lo = fminf(lo, lv[x]);
+            }
+            if (okm != L::FULL) {
+                hi = -INFINITY, lo = INFINITY;
+#pragma unroll
+                for (int x = 0; x < KB; ++x) {
+                    if (okm >> (x * 16) & 1) hi = fmaxf(hi, lv[x]), lo = fminf(lo, lv[x]);
+                }
+                if (hi == -INFINITY) hi = C.tile == tile0 ? 0.0f : d_least;
+#pragma unroll
+                for (int x = 0; x < KB; ++x) lv[x] = okm >> (x * 16) & 1 ? lv[x] : hi;
+            }
+            if (C.tile == tile0) {
+                d_least = d_most = hi;
+#pragma unroll
+                for (int y = 0; y < NB; ++y) d[y][0] = d[y][1] = hi;
+            }
+            odd = hi > d_least + FAR || lo < d_most - FAR;
+        }
         if (cached) {
             const Mask okm = oks[b];
             const float* const scales = reinterpret_cast<const float*>(slot + L::TILE);
 #pragma unroll
             for (int x = 0; x < KB; ++x) {
+                // scores come with their scale's logarithm, from the largest one on, where that is in reach
+                const float with = lv[x] - (odd ? lv[x] : hi);
 #pragma unroll
                 for (int y = 0; y < NB; ++y) s[x][y][0] = s[x][y][1] = s[x][y][2] = s[x][y][3] = 0.0f;
                 constexpr int CW = D == 96 ? 2 : 4;  // words of a load
@@ -452,7 +481,7 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                 for (int y = 0; y < NB; ++y) {
                     const float k0 = ks * factor[y][0], k1 = ks * factor[y][1];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[x][y][e] *= e & 1 ? k1 : k0;
+                    for (int e = 0; e < 4; ++e) s[x][y][e] = fmaf(s[x][y][e], e & 1 ? k1 : k0, with);
                 }
             }
             if (okm != L::FULL) {
@@ -464,21 +493,27 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                         for (int e = 0; e < 4; ++e)
                             if (!(okm >> (x * 16 + (e >> 1) * 8 + gq) & 1)) s[x][y][e] = -INFINITY;
             }
-            // the reference follows scales that are more than 2^4 times it
-            float grown = ref;
-#pragma unroll
-            for (int x = 0; x < KB; ++x) {
-                lv[x] = okm >> (x * 16) & 1 ? log_scale(scales[KB + x]) : -INFINITY;
-                if (lv[x] > grown + 4.0f) grown = lv[x];
-            }
-            if (grown > ref) rebase<MO, NB>(o, ref, grown);
-#pragma unroll
-            for (int x = 0; x < KB; ++x) lv[x] = relative(lv[x], ref);
         } else {
             // 8 new keys in the place of 16
 #pragma unroll
             for (int x = 0; x < KB; ++x) {
-                lv[x] = 0.0f;
+                // as if their values, of which the largest finite one counts, were codes of up to 2^9
+                lv[x] = -110.0f;  // (2^110 2^UP is what 32-bit weights of them have room for)
+                if (first + x * 8 < C.T) {
+                    const uint4* const v = reinterpret_cast<const uint4*>(slot + TK * D + (x * 8 + gq) * (D * 2)) + tq;
+                    uint32_t most = 0;
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i)
+                        most = largest2(largest2(largest2(largest2(most, v[i * 4].x), v[i * 4].y), v[i * 4].z), v[i * 4].w);
+                    if (__any_sync(0xffffffffu, Num<T>::wild(most))) {
+                        most = 0;
+#pragma unroll 1
+                        for (int i = 0; i < D / 8; ++i) most = largest2(most, Num<T>::tame(reinterpret_cast<const uint32_t*>(v + i / 4 * 4)[i % 4]));
+                    }
+                    most = __vmaxu2(most, __shfl_xor_sync(0xffffffffu, most, 1));
+                    most = __vmaxu2(most, __shfl_xor_sync(0xffffffffu, most, 2));
+                    lv[x] = fmaxf((float)(exponent<T>(most) - 135), -110.0f);
+                }
 #pragma unroll
                 for (int y = 0; y < NB; ++y) s[x][y][0] = s[x][y][1] = s[x][y][2] = s[x][y][3] = 0.0f;
 #pragma unroll
@@ -500,51 +535,118 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                     }
                 }
             }
-            if (0.0f > ref + 4.0f) rebase<MO, NB>(o, ref, 0.0f);
         }
 
-        float top[NB][2];
-        bool higher = false;
-#pragma unroll
-        for (int y = 0; y < NB; ++y) {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                top[y][e] = m[y][e];
-#pragma unroll
-                for (int x = 0; x < KB; ++x) top[y][e] = fmaxf(top[y][e], fmaxf(s[x][y][e], s[x][y][e + 2]));
-                higher = higher || top[y][e] > m[y][e];
-            }
-        }
-        if (__any_sync(0xffffffffu, higher)) {
+        if (!odd) {
+            float top[NB][2];
+            bool higher = false;
 #pragma unroll
             for (int y = 0; y < NB; ++y) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
+                    float t = -INFINITY;
 #pragma unroll
-                    for (int x = 4; x < 32; x <<= 1)
-                        top[y][e] = fmaxf(top[y][e], __shfl_xor_sync(0xffffffffu, top[y][e], x));
-                    const float f = top[y][e] > m[y][e] ? ex2(m[y][e] - top[y][e]) : 1.0f;
-                    m[y][e] = top[y][e];
-                    l[y][e] *= f;
+                    for (int x = 0; x < KB; ++x) t = fmaxf(t, fmaxf(s[x][y][e], s[x][y][e + 2]));
+                    top[y][e] = __fadd_ru(t, hi);
+                    higher = higher || top[y][e] > M[y][e];
+                }
+            }
+            if (__any_sync(0xffffffffu, higher)) {
 #pragma unroll
-                    for (int x = 0; x < MO; ++x) {
-                        o[x][y][e] *= f;
-                        o[x][y][e + 2] *= f;
+                for (int y = 0; y < NB; ++y) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float to = fmaxf(M[y][e], row_max(top[y][e])), f = to > M[y][e] ? ex2(M[y][e] - to) : 1.0f;
+                        M[y][e] = to;
+                        l[y][e] *= f;
+#pragma unroll
+                        for (int x = 0; x < MO; ++x) {
+                            o[x][y][e] *= f;
+                            o[x][y][e + 2] *= f;
+                        }
                     }
                 }
             }
-        }
+            const float up = hi + UP;
+            float back[KB];
 #pragma unroll
-        for (int x = 0; x < KB; ++x) {
-            const float back = ex2(-lv[x]);
+            for (int x = 0; x < KB; ++x) back[x] = ex2(hi - lv[x]);
 #pragma unroll
             for (int y = 0; y < NB; ++y) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float base = (m[y][e] == -INFINITY ? 0.0f : m[y][e]) - lv[x];
-                    s[x][y][e] = ex2(s[x][y][e] - base);
-                    s[x][y][e + 2] = ex2(s[x][y][e + 2] - base);
-                    l[y][e] += (s[x][y][e] + s[x][y][e + 2]) * back;
+                    const float at = __fadd_ru(M[y][e] == -INFINITY ? 0.0f : M[y][e], -up);
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int x = 0; x < KB; ++x) {
+                        s[x][y][e] = ex2(s[x][y][e] - at);
+                        s[x][y][e + 2] = ex2(s[x][y][e + 2] - at);
+                        sum = fmaf(s[x][y][e] + s[x][y][e + 2], back[x], sum);
+                    }
+                    l[y][e] = fmaf(sum, ex2(d[y][e] - up), l[y][e]);
+                }
+            }
+        } else {
+            // scores as they are. (Differences first: next to scores of any size logarithms would be lost)
+            float f[NB][2];
+            bool moved = false;
+#pragma unroll
+            for (int y = 0; y < NB; ++y) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float m = M[y][e] - d[y][e];
+                    float top = -INFINITY, with = -INFINITY;
+#pragma unroll
+                    for (int x = 0; x < KB; ++x) top = fmaxf(top, fmaxf(s[x][y][e], s[x][y][e + 2]));
+                    const float to = fmaxf(m, row_max(top)), base = to == -INFINITY ? 0.0f : to;
+#pragma unroll
+                    for (int x = 0; x < KB; ++x) with = fmaxf(with, (fmaxf(s[x][y][e], s[x][y][e + 2]) - base) + lv[x]);
+                    const float by = m - base, next = fmaxf(fmaxf(d[y][e] + by, row_max(with)), 2 * LOG_ZERO);
+                    f[y][e] = ex2(by + (d[y][e] - next));
+                    moved = moved || f[y][e] != 1.0f;
+                    l[y][e] *= ex2(by);
+                    M[y][e] = to == -INFINITY ? to : __fadd_ru(to, next);
+                    d[y][e] = next;
+#pragma unroll
+                    for (int x = 0; x < KB; ++x) {
+                        if (cached) {
+#pragma unroll
+                            for (int z = 0; z < 4; z += 2) {
+                                const float t = s[x][y][e + z] - base;
+                                l[y][e] += ex2(t);
+                                s[x][y][e + z] = ex2(t + (lv[x] - next + UP));
+                            }
+                        } else {
+                            // (weights of new values stay in 32 bits, and have no scale)
+                            const float t = s[x][y][e] - base;
+                            l[y][e] += ex2(t);
+                            s[x][y][e] = ex2(t + (UP - next));
+                        }
+                    }
+                }
+            }
+            if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+                for (int y = 0; y < NB; ++y)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+#pragma unroll
+                        for (int x = 0; x < MO; ++x) {
+                            o[x][y][e] *= f[y][e];
+                            o[x][y][e + 2] *= f[y][e];
+                        }
+            }
+            if (cached) {
+                d_least = d_most = d[0][0];
+#pragma unroll
+                for (int y = 0; y < NB; ++y) {
+                    d_least = fminf(d_least, fminf(d[y][0], d[y][1]));
+                    d_most = fmaxf(d_most, fmaxf(d[y][0], d[y][1]));
+                }
+#pragma unroll
+                for (int x = 1; x < 4; x <<= 1) {
+                    d_least = fminf(d_least, __shfl_xor_sync(0xffffffffu, d_least, x));
+                    d_most = fmaxf(d_most, __shfl_xor_sync(0xffffffffu, d_most, x));
                 }
             }
         }
@@ -591,7 +693,6 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                 }
             }
         } else {
-            const float unit = ex2(-ref);
 #pragma unroll
             for (int x = 0; x < KB; ++x) {
 #pragma unroll 1
@@ -601,7 +702,7 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
 #pragma unroll
                     for (int y = 0; y < NB; ++y)
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) p[y][e] = __shfl_sync(0xffffffffu, s[x][y][e], k * 4 + tq) * unit;
+                        for (int e = 0; e < 2; ++e) p[y][e] = __shfl_sync(0xffffffffu, s[x][y][e], k * 4 + tq);
 #pragma unroll
                     for (int w = 0; w < NW; ++w) {
                         const uint2 z = *reinterpret_cast<const uint2*>(v + L::value_channel(w, gq) * 2);
@@ -631,7 +732,6 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
             const bool whole = tile0 == 0 && C.tile + 1 == C.c;
             const int live = min(rows, RM);
             float* const part = part_of<D, RM>(a, me, tile0 == 0 ? 1 : 0);
-            const float unit = ex2(ref);
 #pragma unroll
             for (int y = 0; y < NB; ++y) {
 #pragma unroll
@@ -639,26 +739,28 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
 #pragma unroll
                     for (int x = 4; x < 32; x <<= 1) l[y][e] += __shfl_xor_sync(0xffffffffu, l[y][e], x);
                     const float sum = l[y][e];
+                    const float2 unit = unit_of(d[y][e]);
+                    const float small = unit.y * ex2(-UP);
                     const int rr = y * 8 + tq * 2 + e;
                     if (rr < live) {
                         if (!whole) {
-                            float* const d = part + RM * 2 + rr * D;
+                            float* const to = part + RM * 2 + rr * D;
 #pragma unroll
                             for (int w = 0; w < NW; ++w)
-                                *reinterpret_cast<float4*>(d + L::value_channel(w, gq)) =
-                                    make_float4(o[2 * w][y][e] * unit, o[2 * w][y][e + 2] * unit,
-                                                o[2 * w + 1][y][e] * unit, o[2 * w + 1][y][e + 2] * unit);
-                            if (gq == 0) *reinterpret_cast<float2*>(part + rr * 2) = make_float2(m[y][e], sum);
+                                *reinterpret_cast<float4*>(to + L::value_channel(w, gq)) =
+                                    make_float4(o[2 * w][y][e] * small * unit.x, o[2 * w][y][e + 2] * small * unit.x,
+                                                o[2 * w + 1][y][e] * small * unit.x, o[2 * w + 1][y][e + 2] * small * unit.x);
+                            if (gq == 0) *reinterpret_cast<float2*>(part + rr * 2) = make_float2(M[y][e] - d[y][e], sum);
                         } else {
                             const int rho = C.rt * RM + rr, t = rho / G, head = C.h * G + rho - t * G;
-                            const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
-                            char* const d = a.out + ((C.lo + t) * a.out_stride + (long long)head * D) * 2;
+                            const float inv = (sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f) * small;
+                            char* const to = a.out + ((C.lo + t) * a.out_stride + (long long)head * D) * 2;
 #pragma unroll
                             for (int w = 0; w < NW; ++w)
-                                *reinterpret_cast<uint2*>(d + L::value_channel(w, gq) * 2) =
-                                    make_uint2(Num<T>::pack(o[2 * w][y][e] * unit * inv, o[2 * w][y][e + 2] * unit * inv),
-                                               Num<T>::pack(o[2 * w + 1][y][e] * unit * inv, o[2 * w + 1][y][e + 2] * unit * inv));
-                            if (gq == 0 && a.lse) a.lse[(long long)(C.lo + t) * (H * G) + head] = (m[y][e] + log2f(sum)) * LN2;
+                                *reinterpret_cast<uint2*>(to + L::value_channel(w, gq) * 2) =
+                                    make_uint2(Num<T>::pack(o[2 * w][y][e] * inv * unit.x, o[2 * w][y][e + 2] * inv * unit.x),
+                                               Num<T>::pack(o[2 * w + 1][y][e] * inv * unit.x, o[2 * w + 1][y][e + 2] * inv * unit.x));
+                            if (gq == 0 && a.lse) a.lse[(long long)(C.lo + t) * (H * G) + head] = (M[y][e] - d[y][e] + log2f(sum)) * LN2;
                         }
                     }
                 }

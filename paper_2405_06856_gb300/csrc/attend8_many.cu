@@ -12,7 +12,7 @@
 // A row tile's scores have two places: the next ones are formed while the softmax works on those before. A unit with one row
 // tile has its even and odd tiles done by the two sets of softmax warps, with an accumulator each, joined at its end. The
 // accumulators stay in tensor memory; they are rescaled only when a row's maximum has grown by more than 2^8 over the
-// one that its weights refer to, or a scale by more than 2^4.
+// one that its weights refer to.
 //
 // What bounds it: latency of a few warps a role. 16 warps share four schedulers, an instruction takes a warp 4 to 6 cycles,
 // and each role has some 200 of them for a tile, so code is kept small as well: with products, tiles and units
@@ -57,7 +57,7 @@ struct Many8 {
     static constexpr int factors = late + 8;             // of the rows' scores, for two units in turn
     static constexpr int other = (factors + 2 * 128 * 4 + 15) / 16 * 16;  // what the second half of the tiles gave a row
     static constexpr int info = other + 128 * 16;        // 8 tiles' Info
-    static constexpr int scratch = info + 8 * (64 * 8 + 32);
+    static constexpr int scratch = info + 8 * (64 * 8 + 16);
     static constexpr int pre = scratch + 96 * 8;
     static constexpr int bytes(int n_req) { return pre + Axis8::ints(n_req) * 4; }
     static constexpr int WARPS = 4 * MT + 1 + CONV;      // softmax, products, conversions
@@ -71,12 +71,14 @@ struct Many8 {
 struct Info {
     float k[64];    // factors of scores
     float lv[64];   // logarithms of the values' scales
-    float top[4];   // the largest are among these
     int valid[4];   // blocks of 16 keys on pages of the pool
 };
 
 // What a unit costs beside its tiles, in keys.
 constexpr int UNIT_KEYS = 512;
+
+// Room of the weights in half precision (attend8.cuh): a row's maxima may be 2^LAG behind.
+constexpr float UP = 7.0f, LAG = 8.0f;
 
 __device__ __forceinline__ uint64_t pair2(uint32_t lo, uint32_t hi) { return (uint64_t)hi << 32 | lo; }
 __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
@@ -252,11 +254,9 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                 if (part == 0 && lane == 0) {
                     const float k = *reinterpret_cast<const float*>(src + L::CPL * 512), v = *reinterpret_cast<const float*>(src + L::CPL * 512 + 4);
                     const int valid = *reinterpret_cast<const int*>(src + L::CPL * 512 + 8);
-                    const float lv = valid && u.tile * KT + g * 16 < u.len ? log_scale(v) : -INFINITY;
                     // (0 too as it is: the products that it meets are finite, and -inf only where it is not used)
                     info.k[g] = finite_scale(k);
-                    info.lv[g] = lv;
-                    info.top[g] = lv;
+                    info.lv[g] = valid && u.tile * KT + g * 16 < u.len ? log_scale(v) : LOG_ZERO;
                     info.valid[g] = valid;
                 }
 #pragma unroll
@@ -274,38 +274,31 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                 const char* const base = part ? a.tok.v : a.tok.k;
                 const long long stride = (part ? a.tok.v_stride : a.tok.k_stride) * 2;
                 int mine = 0;  // the largest exponent of this lane's row of the part
-                if constexpr (BF16) {
-                    // of two halves of a row a lane, of keys (if they are this job's) and values, not of infinities and NaN
+                {
+                    // of two halves of a row a lane, of keys (bfloat16, if they are this job's) and values, not of infinities and NaN
                     const int row = g * 16 + (lane >> 1);
                     int most = 0;
 #pragma unroll 1
                     for (int e = part; e < 2; ++e) {
-                        const char* const q = (e ? a.tok.v + (u.lo + row) * a.tok.v_stride * 2 : a.tok.k + (u.lo + row) * a.tok.k_stride * 2) +
-                                              (u.h * D + (lane & 1) * (D / 2)) * 2;
+                        if (!BF16 && e == 0) continue;
+                        const uint4* const q = reinterpret_cast<const uint4*>(
+                            (e ? a.tok.v + (u.lo + row) * a.tok.v_stride * 2 : a.tok.k + (u.lo + row) * a.tok.k_stride * 2) +
+                            (u.h * D + (lane & 1) * (D / 2)) * 2);
                         most = 0;
                         if (row < u.T) {
 #pragma unroll 4
                             for (int c = 0; c < D / 16; ++c) {
-                                const uint4 v = *reinterpret_cast<const uint4*>(q + c * 16);
-                                most = exponent(Num<T>::tame(v.x), exponent(Num<T>::tame(v.y), exponent(Num<T>::tame(v.z), exponent(Num<T>::tame(v.w), most))));
+                                const uint4 v = q[c];
+                                most = finite_exponent<T>(v.x, finite_exponent<T>(v.y, finite_exponent<T>(v.z, finite_exponent<T>(v.w, most))));
                             }
                         }
                         most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
                         if (e == part) mine = most;
                     }
-                    if (part == 0) {  // (the softmax has the values' scales with the keys)
-                        float lv = row < u.T ? (float)(min(max(most, 15), 254) - 141) : -INFINITY;
-                        if ((lane & 1) == 0) {
-                            info.k[row] = half_back(mine);
-                            info.lv[row] = lv;
-                        }
-#pragma unroll
-                        for (int x = 16; x; x >>= 1) lv = fmaxf(lv, __shfl_xor_sync(0xffffffffu, lv, x));
-                        if (lane == 0) info.top[g] = lv;
+                    if (part == 0 && (lane & 1) == 0) {  // (the softmax has the values' scales with the keys)
+                        info.k[row] = BF16 ? half_back(mine) : 1.0f;
+                        info.lv[row] = (float)(min(max(most, 15), 254) - 141);
                     }
-                } else if (part == 0) {
-                    if (lane < 16) info.k[g * 16 + lane] = 1.0f, info.lv[g * 16 + lane] = 0.0f;
-                    if (lane == 0) info.top[g] = 0.0f;
                 }
                 bool w = false;
 #pragma unroll 1
@@ -317,11 +310,9 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                         w = true;
                         v.x = Num<T>::tame(v.x), v.y = Num<T>::tame(v.y), v.z = Num<T>::tame(v.z), v.w = Num<T>::tame(v.w);
                     }
-                    if constexpr (BF16) {
-                        static_assert(16 * CH % 32 == 0, "all lanes take part");
-                        const float f = half_factor(__shfl_sync(0xffffffffu, mine, row * 2));
-                        v = make_uint4(to_half(v.x, f), to_half(v.y, f), to_half(v.z, f), to_half(v.w, f));
-                    }
+                    static_assert(16 * CH % 32 == 0, "all lanes take part");
+                    const float f = half_factor(__shfl_sync(0xffffffffu, mine, row * 2));
+                    if (BF16 || part) v = make_uint4(to_half<T>(v.x, f), to_half<T>(v.y, f), to_half<T>(v.z, f), to_half<T>(v.w, f));
                     *reinterpret_cast<uint4*>(d + (c >> 3) * (KT * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = v;
                 }
                 if (w) wilds[units & 7] = units + 1;
@@ -422,11 +413,13 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
             const uint4 none = make_uint4(0, 0, 0, 0);
             int top = 0;
             if constexpr (BF16) {
+                uint32_t most = 0;
 #pragma unroll 8
                 for (int c = 0; c < D / 8; ++c) {
                     const uint4 v = live ? __ldg(src + c) : none;
-                    top = exponent(v.x, exponent(v.y, exponent(v.z, exponent(v.w, top))));
+                    most = largest2(largest2(largest2(largest2(most, v.x), v.y), v.z), v.w);
                 }
+                top = exponent<T>(most);
             }
             const float f = half_factor(top);
             factor = (BF16 ? half_back(top) : 1.0f) * a.scale_log2;
@@ -441,7 +434,7 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                 }
                 if constexpr (BF16) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) x[i] = to_half(x[i], f);
+                    for (int i = 0; i < 16; ++i) x[i] = to_half<T>(x[i], f);
                 }
                 if constexpr (L::QS) {
 #pragma unroll
@@ -481,7 +474,7 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                 }
             } else {
                 const unsigned long long see = all_ancestors(a, u, row < rows ? (u.rt * RM + row0 + row) / G : 0, lane);
-                float m = -INFINITY, l = 0.0f, ref = -1000.0f;
+                float M = -INFINITY, l = 0.0f, d = 0.0f;  // (attend8.cuh)
 #pragma unroll 1
                 for (int y = 0; y < mine; ++y) {
                     const int t = split ? 2 * y + w : y, s = MT == 2 ? (y & 1) * 2 + w : y & 1;
@@ -501,82 +494,41 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                     tmem_start(v[1], st + 32);
                     const Info& info = infos[(done + t) & 7];
                     const int own = u.len - (u.tile + t) * KT;  // cached keys from the tile's start
-                    const float4 kf = *reinterpret_cast<const float4*>(info.k), lf = *reinterpret_cast<const float4*>(info.lv),
-                                 tops = *reinterpret_cast<const float4*>(info.top);
+                    const float4 kf = *reinterpret_cast<const float4*>(info.k), lf = *reinterpret_cast<const float4*>(info.lv);
                     const int4 valid = *reinterpret_cast<const int4*>(info.valid);
-                    const float scale_top = fmaxf(fmaxf(tops.x, tops.y), fmaxf(tops.z, tops.w));
-                    float f[4] = {kf.x * factor, kf.y * factor, kf.z * factor, kf.w * factor};
+                    const float lv[4] = {lf.x, lf.y, lf.z, lf.w}, hi = fmaxf(fmaxf(lf.x, lf.y), fmaxf(lf.z, lf.w)),
+                                lo = fminf(fminf(lf.x, lf.y), fminf(lf.z, lf.w));
+                    const bool all = own >= KT && (valid.x & valid.y & valid.z & valid.w);
+                    if (y == 0 && all) d = hi;
+                    const bool near = __all_sync(0xffffffffu, all && !(hi > d + FAR) && !(lo < d - FAR));
                     tmem_loaded(v[0]);
                     tmem_loaded(v[1]);
-                    if (own < KT || !(valid.x & valid.y & valid.z & valid.w)) {
-                        // keys that are not seen or have scales of their own: scores are scaled in their place
-                        const float* ks = info.k;
-                        const int step = own > 0 ? 0 : 1;
-#pragma unroll 1
-                        for (int c = 0; c < 4; ++c) {
-                            uint32_t z[16];
-                            tmem_load16(z, st + c * 16);
-                            const int left = own - c * 16;
-                            const uint32_t vis = own <= 0 ? (uint32_t)(see >> (c * 16))
-                                                 : !info.valid[c] ? 0u : left >= 16 ? 0xffffu : left > 0 ? (1u << left) - 1 : 0u;
-#pragma unroll
-                            for (int i = 0; i < 16; ++i)
-                                z[i] = vis >> i & 1 ? __float_as_uint(__uint_as_float(z[i]) * (ks[i * step] * factor)) : 0xff800000u;
-                            tmem_store16(st + c * 16, z);
-                            ks += step ? 16 : 1;
-                        }
-                        tmem_stored();
-                        f[0] = f[1] = f[2] = f[3] = 1.0f;
-                        tmem_load(v[0], st);
-                        tmem_load(v[1], st + 32);
-                    }
-                    float top = -INFINITY;
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        float t0 = -INFINITY, t1 = -INFINITY;
-#pragma unroll
-                        for (int i = 0; i < 16; i += 4) {
-                            const uint32_t* const e = &v[x / 2][x % 2 * 16 + i];
-                            t0 = fmaxf(fmaxf(t0, __uint_as_float(e[0])), __uint_as_float(e[1]));
-                            t1 = fmaxf(fmaxf(t1, __uint_as_float(e[2])), __uint_as_float(e[3]));
-                        }
-                        top = fmaxf(top, fmaxf(t0, t1) * f[x]);
-                    }
-                    if (y == 0) {
-                        m = top;
-                        ref = fmaxf(scale_top, -1000.0f);
-                    } else {
-                        const bool grown = top > m + 8.0f;  // (always where m is -inf and top is not)
-                        const bool larger = scale_top > ref + 4.0f;
-                        if (larger || __any_sync(0xffffffffu, grown)) {
-                            // the weights of the tile before are in the accumulator (those of the one before it were when
-                            // these scores were formed)
-                            ok = __all_sync(0xffffffffu, wait(sm0 + L::odone + (w * 2 + (y + 1 & 1)) * 8, (y & 1 ? weighed[0] : weighed[1]) - 1));
-                            if (!ok) break;
-                            tc_after();
-                            float g = grown ? ex2(m - top) : 1.0f;
-                            if (grown) m = top;
-                            l *= g;
-                            if (larger) {
-                                g *= ex2(ref - scale_top);
-                                ref = scale_top;
-                            }
-#pragma unroll 1
-                            for (int c = 0; c < D / 16; ++c) {
-                                uint32_t o[16];
-                                tmem_load16(o, om + c * 16);
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * g);
-                                tmem_store16(om + c * 16, o);
-                            }
-                        }
-                    }
-                    const float base = m == -INFINITY ? 0.0f : m;
-                    if (own > 0) {
-                        const float lv[4] = {lf.x, lf.y, lf.z, lf.w};
+                    float grow = 1.0f;  // what the accumulator is multiplied by: the row's maximum grew by more than LAG
+                    bool grown;
+                    if (near) {
+                        const float f[4] = {kf.x * factor, kf.y * factor, kf.z * factor, kf.w * factor};
+                        float top = -INFINITY;
 #pragma unroll
                         for (int x = 0; x < 4; ++x) {
-                            const float at = relative(lv[x], ref), shift = at - base;
+                            float t0 = -INFINITY, t1 = -INFINITY;
+#pragma unroll
+                            for (int i = 0; i < 16; i += 4) {
+                                const uint32_t* const e = &v[x / 2][x % 2 * 16 + i];
+                                t0 = fmaxf(fmaxf(t0, __uint_as_float(e[0])), __uint_as_float(e[1]));
+                                t1 = fmaxf(fmaxf(t1, __uint_as_float(e[2])), __uint_as_float(e[3]));
+                            }
+                            top = fmaxf(top, __fmaf_ru(fmaxf(t0, t1), f[x], lv[x]));
+                        }
+                        grown = y == 0 || top - M > LAG;
+                        if (grown) {
+                            grow = ex2(M - top);
+                            M = top;
+                        }
+                        const float base = M == -INFINITY ? 0.0f : M;
+                        float sums = 0.0f;
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            const float shift = __fadd_rd(lv[x] + UP, -base);
                             const uint64_t ff = pair2(__float_as_uint(f[x]), __float_as_uint(f[x])),
                                            bb = pair2(__float_as_uint(shift), __float_as_uint(shift));
                             uint64_t sum = 0;
@@ -588,29 +540,93 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                                 sum = add2(sum, pair2(__float_as_uint(e0), __float_as_uint(e1)));
                                 v[x / 2][x % 2 * 8 + i / 2] = Num<__half>::pack(e0, e1);
                             }
-                            l += (low2(sum) + high2(sum)) * ex2(-at);
+                            sums += (low2(sum) + high2(sum)) * ex2(d - UP - lv[x]);
                         }
+                        l = l * grow + sums;
                         // (the scores of all 64 keys have been read)
                         tmem_store16(st, *reinterpret_cast<const uint32_t(*)[16]>(&v[0][0]));
                         tmem_store16(st + 16, *reinterpret_cast<const uint32_t(*)[16]>(&v[1][0]));
                     } else {
-                        // new tokens: a scale each; weights lie where scores were that have been read
+                        // keys that are not seen or have scales of their own, or scales of very different size: scores are scaled in
+                        // their place, those of a block whose scale is none NaN
+                        const int step = own > 0 ? 0 : 1;
+                        float m = M - d, most = -INFINITY, with = -INFINITY;
+                        const float m0 = m == -INFINITY ? 0.0f : m;
+#pragma unroll 1
+                        for (int c = 0; c < 4; ++c) {
+                            uint32_t z[16];
+                            tmem_load16(z, st + c * 16);
+                            const int left = own - c * 16, at = step ? c * 16 : c;
+                            const uint32_t vis = own <= 0 ? (uint32_t)(see >> (c * 16))
+                                                 : !info.valid[c] ? 0u : left >= 16 ? 0xffffu : left > 0 ? (1u << left) - 1 : 0u;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const float k = info.k[at + i * step] * factor, b = info.lv[at + i * step];
+                                const float t = vis >> i & 1 ? fmaf(__uint_as_float(z[i]), k, b - b) : -INFINITY;
+                                most = fmaxf(most, t);
+                                with = fmaxf(with, (t - m0) + b);
+                                z[i] = __float_as_uint(t);
+                            }
+                            tmem_store16(st + c * 16, z);
+                        }
+                        tmem_stored();
+                        const float to = fmaxf(m, most), from = to == -INFINITY ? 0.0f : to;
+                        with -= from - m0;
+                        if (__any_sync(0xffffffffu, fabsf(from - m0) > 16384.0f)) {
+                            // (next to such differences logarithms are lost: from the new maximum on)
+                            with = -INFINITY;
+#pragma unroll 1
+                            for (int c = 0; c < 4; ++c) {
+                                uint32_t z[16];
+                                tmem_load16(z, st + c * 16);
+                                const int at = step ? c * 16 : c;
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) with = fmaxf(with, (__uint_as_float(z[i]) - from) + info.lv[at + i * step]);
+                            }
+                        }
+                        grown = y == 0 || most - m > LAG || with - (M - from) > LAG;  // (always where M is -inf and top is not)
+                        if (grown) {
+                            const float by = m - from, next = fmaxf(fmaxf(d + by, with), 2 * LOG_ZERO);
+                            grow = ex2(by + (d - next));
+                            l *= ex2(by);
+                            M = to == -INFINITY ? to : __fadd_ru(to, next);
+                            d = next;
+                            m = to;
+                        }
+                        const float base = m == -INFINITY ? 0.0f : m;
+                        // weights lie where scores were that have been read
 #pragma unroll 1
                         for (int c = 0; c < 4; ++c) {
                             uint32_t z[16], p[8];
                             tmem_load16(z, st + c * 16);
+                            const int at = step ? c * 16 : c;
 #pragma unroll
                             for (int i = 0; i < 16; i += 2) {
                                 float e[2];
 #pragma unroll
                                 for (int k = 0; k < 2; ++k) {
-                                    const float at = relative(info.lv[c * 16 + i + k], ref);
-                                    e[k] = ex2(__uint_as_float(z[i + k]) - base + at);
-                                    l += e[k] * ex2(-at);
+                                    const float t = __uint_as_float(z[i + k]) - base;
+                                    l += ex2(t);
+                                    e[k] = ex2(t + (info.lv[at + (i + k) * step] - d + UP));
                                 }
                                 p[i / 2] = Num<__half>::pack(e[0], e[1]);
                             }
                             tmem_store8(st + c * 8, p);
+                        }
+                    }
+                    if (y > 0 && __any_sync(0xffffffffu, grown)) {
+                        // the weights of the tile before are in the accumulator (those of the one before it were when
+                        // these scores were formed)
+                        ok = __all_sync(0xffffffffu, wait(sm0 + L::odone + (w * 2 + (y + 1 & 1)) * 8, (y & 1 ? weighed[0] : weighed[1]) - 1));
+                        if (!ok) break;
+                        tc_after();
+#pragma unroll 1
+                        for (int c = 0; c < D / 16; ++c) {
+                            uint32_t o[16];
+                            tmem_load16(o, om + c * 16);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * grow);
+                            tmem_store16(om + c * 16, o);
                         }
                     }
                     tmem_stored();
@@ -625,7 +641,7 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                     // the odd tiles: their accumulator stays where it is, the other warps take it from there
                     ok = __all_sync(0xffffffffu, wait(sm0 + last_done, last_phase));
                     if (!ok) break;
-                    if (!idle) other[row] = make_float4(m, l, ref, 0.0f);
+                    if (!idle) other[row] = make_float4(M - d, l, d, 0.0f);
                     __syncwarp();
                     if (lane == 0) mbar_arrive(sm0 + L::merged);
                     if (more) {
@@ -657,32 +673,36 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                     continue;
                 }
                 tc_after();
-                float unit = ex2(ref), unit1 = 0.0f;
+                float m = M - d;
+                float2 unit = unit_of(d), unit1 = make_float2(0.0f, 0.0f);
                 if (joins) {
                     const float4 x = other[row];
                     const float top = fmaxf(m, x.x), base = top == -INFINITY ? 0.0f : top, g0 = ex2(m - base), g1 = ex2(x.x - base);
                     l = l * g0 + x.y * g1;
-                    unit *= g0;
-                    unit1 = ex2(x.z) * g1;
+                    unit.x *= g0;
+                    unit1 = unit_of(x.z);
+                    unit1.x *= g1;
                     m = top;
                 }
                 const bool whole = u.tile == 0 && count == u.c;
                 const int rr = row0 + row, rho = u.rt * RM + rr, t = rho / G, hd = u.h * G + rho - t * G;
                 float* const part = part_of<D, RM>(a, me, u.tile == 0 ? 1 : 0);
-                const float scale = whole ? (l > 0.0f || l != l ? 1.0f / l : 0.0f) : 1.0f;
+                const float scale = (whole ? (l > 0.0f || l != l ? 1.0f / l : 0.0f) : 1.0f) * ex2(-UP);
+                unit.y *= scale;
+                unit1.y *= scale;
                 const bool wild = wilds[units & 7] == units + 1;
 #pragma unroll 1
                 for (int c = 0; c < D / 32; ++c) {
                     uint32_t o[32];
                     tmem_load(o, om + c * 32);
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * unit * scale);
+                    for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * unit.y * unit.x);
                     if (joins) {
                         uint32_t o1[32];
                         tmem_load(o1, om + L::HALVES * 64 + c * 32);
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            o[i] = __float_as_uint(fmaf(__uint_as_float(o1[i]) * unit1, scale, __uint_as_float(o[i])));
+                            o[i] = __float_as_uint(fmaf(__uint_as_float(o1[i]) * unit1.y, unit1.x, __uint_as_float(o[i])));
                     }
                     if (row < rows) {
                         if (wild) {
