@@ -268,6 +268,17 @@ __device__ __forceinline__ void join_rows(const AttendArgs& a, const Cursor& u, 
     }
 }
 
+// The smallest normal number: what multiplies results that are not finite and would be lost with 0.
+constexpr float NORMAL = 1.17549435e-38f;
+
+// What a worker's partial results of a row, (maximum, sum), are multiplied by. A negative sum: of results that are not finite
+// for their values, which count whatever their weight.
+__device__ __forceinline__ float part_factor(float2 ml, float ref)
+{
+    const float f = ex2(ml.x - ref);
+    return __float_as_int(ml.y) < 0 ? fmaxf(f, NORMAL) : f;
+}
+
 // Row rr (of token t, query head hd) of the unit under u, whose partial results the workers first .. last left with four
 // columns of all rows together; one thread.
 template <typename T, int D, int RM>
@@ -282,9 +293,10 @@ __device__ __forceinline__ void join_row(const AttendArgs& a, const Cursor& u, i
     for (int i = first; i <= last; ++i) {
         const float2 v = __ldcg(
             reinterpret_cast<const float2*>(part_of<D, RM>(a, i, i == first) + rr * 2));
-        sum += v.y * ex2(v.x - ref);
+        sum += fabsf(v.y) * part_factor(v, ref);
     }
-    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+    const float inv = 1.0f / sum;
+    const auto of = [&](float x) { return sum == 0.0f ? 0.0f : x * inv; };
     uint4* const d = reinterpret_cast<uint4*>(
         a.out + ((u.lo + t) * a.out_stride + (long long)hd * D) * 2);
 #pragma unroll 2
@@ -295,7 +307,7 @@ __device__ __forceinline__ void join_row(const AttendArgs& a, const Cursor& u, i
 #pragma unroll 2
         for (int i = first; i <= last; ++i) {
             const float* const p = part_of<D, RM>(a, i, i == first);
-            const float f = ex2(__ldcg(p + rr * 2) - ref);
+            const float f = part_factor(__ldcg(reinterpret_cast<const float2*>(p + rr * 2)), ref);
             const float4* const q = reinterpret_cast<const float4*>(p + RM * 2) + c * 8 * RM + rr;
 #pragma unroll
             for (int x = 0; x < 8; ++x) {
@@ -309,8 +321,8 @@ __device__ __forceinline__ void join_row(const AttendArgs& a, const Cursor& u, i
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
             const float4 y = acc[x * 2], z = acc[x * 2 + 1];
-            d[c * 4 + x] = make_uint4(Num<T>::pack(y.x * inv, y.y * inv), Num<T>::pack(y.z * inv, y.w * inv),
-                                      Num<T>::pack(z.x * inv, z.y * inv), Num<T>::pack(z.z * inv, z.w * inv));
+            d[c * 4 + x] = make_uint4(Num<T>::pack(of(y.x), of(y.y)), Num<T>::pack(of(y.z), of(y.w)),
+                                      Num<T>::pack(of(z.x), of(z.y)), Num<T>::pack(of(z.z), of(z.w)));
         }
     }
     if (a.lse) a.lse[(long long)(u.lo + t) * (a.kv.kv_heads * a.kv.group) + hd] = (ref + log2f(sum)) * LN2;

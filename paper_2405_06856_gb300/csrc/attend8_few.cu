@@ -41,7 +41,8 @@ struct Few8 {
     typedef typename std::conditional<TK == 64, unsigned long long, unsigned>::type Mask;  // a bit for each key
     static constexpr Mask FULL = TK == 16 ? (Mask)0xffff : ~(Mask)0;
     static constexpr int oks = WARPS * S * SLOT;                      // masks of tiles
-    static constexpr int scratch = oks + WARPS * S * 8;
+    static constexpr int ds = oks + WARPS * S * 8;                    // the rows' d, where they differ
+    static constexpr int scratch = ds + WARPS * NB * 8 * 4;
     static constexpr int pre = scratch + 96 * 8;
     static constexpr int bytes(int n_req) { return pre + Axis8::ints(n_req) * 4; }
 
@@ -151,8 +152,8 @@ __device__ __forceinline__ void join_rows8(const AttendArgs& a, const Cursor& u,
 #pragma unroll
                         for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
                         const float base = top == -INFINITY ? 0.0f : top, g = ex2(ref[y] - base);
-                        f[y] = lane < count ? ex2(ml[y].x - base) : 0.0f;
-                        sum[y] = sum[y] * g + (lane < count ? ml[y].y * f[y] : 0.0f);
+                        f[y] = lane < count ? part_factor(ml[y], base) : 0.0f;
+                        sum[y] = sum[y] * g + (lane < count ? fabsf(ml[y].y) * f[y] : 0.0f);
 #pragma unroll
                         for (int x = 0; x < N; ++x) acc[y][x] *= g;
                         ref[y] = top;
@@ -177,16 +178,17 @@ __device__ __forceinline__ void join_rows8(const AttendArgs& a, const Cursor& u,
             const int rr = r0 + y;
             if (rr >= live) break;
             const int rho = u.rt * RM + rr, t = rho / G, head = u.h * G + rho - t * G;
-            const float inv = sum[y] > 0.0f || sum[y] != sum[y] ? 1.0f / sum[y] : 0.0f;
+            const float inv = 1.0f / sum[y];
+            const auto of = [&](float x) { return sum[y] == 0.0f ? 0.0f : x * inv; };
             char* const d = a.out + ((u.lo + t) * a.out_stride + (long long)head * D + lane * N) * 2;
             if constexpr (N % 2 == 0) {
 #pragma unroll
                 for (int x = 0; x < N; x += 2)
-                    *reinterpret_cast<uint32_t*>(d + x * 2) = Num<T>::pack(acc[y][x] * inv, acc[y][x + 1] * inv);
+                    *reinterpret_cast<uint32_t*>(d + x * 2) = Num<T>::pack(of(acc[y][x]), of(acc[y][x + 1]));
             } else {
 #pragma unroll
                 for (int x = 0; x < N; ++x)
-                    *reinterpret_cast<unsigned short*>(d + x * 2) = (unsigned short)Num<T>::pack(acc[y][x] * inv, 0.0f);
+                    *reinterpret_cast<unsigned short*>(d + x * 2) = (unsigned short)Num<T>::pack(of(acc[y][x]), 0.0f);
             }
             if (lane == 0 && a.lse)
                 a.lse[(long long)(u.lo + t) * (a.kv.kv_heads * G) + head] =
@@ -210,6 +212,7 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
     char* const tiles = sm + warp * S * L::SLOT;
     const uint32_t tiles0 = smem_addr(tiles);
     Mask* const oks = reinterpret_cast<Mask*>(sm + L::oks) + warp * S;
+    float* const row_d = reinterpret_cast<float*>(sm + L::ds) + warp * NB * 8;
 
     Axis8 ax;
     if (!plan8<NT, TK, TN, RM>(a, ax, reinterpret_cast<int*>(sm + L::pre), reinterpret_cast<long long*>(sm + L::scratch),
@@ -351,11 +354,12 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
         cp_commit();
     }
 
-    float o[MO][NB][4], M[NB][2], l[NB][2], d[NB][2];  // channels of rows 2 tq, 2 tq + 1, and what attend8.cuh says
-    float d_least = 0.0f, d_most = 0.0f;     // of all rows
+    float o[MO][NB][4], M[NB][2], l[NB][2];  // channels of rows 2 tq, 2 tq + 1, and what attend8.cuh says
+    float d = 0.0f;
+    bool single = false;                     // whether the rows have a d each
     float unscale[NB];                       // of row gq of every block
     unsigned long long see[NB][2];
-    bool fresh = true;
+    bool fresh = true, wild = false;         // whether the unit's results hold values that are not finite
     int b = 0, tile0 = 0;  // a tile's place; the first tile of the unit that this warp has
     // A unit that warps share and whose part this one has written: a tile later it says so, and at the end of its next
     // unit it looks whether it was the last one to, which joins the parts; neither is waited for while there are tiles.
@@ -368,15 +372,15 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
         cp_commit();
         const int rows = C.T * G - C.rt * RM;
         if (fresh) {
-            fresh = false;
+            fresh = wild = single = false;
             tile0 = C.tile;
+            d = 0.0f;
 #pragma unroll
             for (int y = 0; y < NB; ++y) {
 #pragma unroll
                 for (int x = 0; x < MO; ++x) o[x][y][0] = o[x][y][1] = o[x][y][2] = o[x][y][3] = 0.0f;
                 M[y][0] = M[y][1] = -INFINITY;
                 l[y][0] = l[y][1] = 0.0f;
-                d[y][0] = d[y][1] = 0.0f;
                 see[y][0] = see[y][1] = 1;
                 uint2 q[MO];
 #pragma unroll
@@ -434,16 +438,12 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                 for (int x = 0; x < KB; ++x) {
                     if (okm >> (x * 16) & 1) hi = fmaxf(hi, lv[x]), lo = fminf(lo, lv[x]);
                 }
-                if (hi == -INFINITY) hi = C.tile == tile0 ? 0.0f : d_least;
+                if (hi == -INFINITY) hi = d;
 #pragma unroll
                 for (int x = 0; x < KB; ++x) lv[x] = okm >> (x * 16) & 1 ? lv[x] : hi;
             }
-            if (C.tile == tile0) {
-                d_least = d_most = hi;
-#pragma unroll
-                for (int y = 0; y < NB; ++y) d[y][0] = d[y][1] = hi;
-            }
-            odd = hi > d_least + FAR || lo < d_most - FAR;
+            if (C.tile == tile0) d = hi;
+            odd = single || hi > d + FAR || lo < d - FAR;
         }
         if (cached) {
             const Mask okm = oks[b];
@@ -506,6 +506,7 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                     for (int i = 0; i < D / 32; ++i)
                         most = largest2(largest2(largest2(largest2(most, v[i * 4].x), v[i * 4].y), v[i * 4].z), v[i * 4].w);
                     if (__any_sync(0xffffffffu, Num<T>::wild(most))) {
+                        wild = true;
                         most = 0;
 #pragma unroll 1
                         for (int i = 0; i < D / 8; ++i) most = largest2(most, Num<T>::tame(reinterpret_cast<const uint32_t*>(v + i / 4 * 4)[i % 4]));
@@ -570,43 +571,42 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
             const float up = hi + UP;
             float back[KB];
 #pragma unroll
-            for (int x = 0; x < KB; ++x) back[x] = ex2(hi - lv[x]);
+            for (int x = 0; x < KB; ++x) back[x] = ex2(d - UP - lv[x]);
 #pragma unroll
             for (int y = 0; y < NB; ++y) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const float at = __fadd_ru(M[y][e] == -INFINITY ? 0.0f : M[y][e], -up);
-                    float sum = 0.0f;
 #pragma unroll
                     for (int x = 0; x < KB; ++x) {
                         s[x][y][e] = ex2(s[x][y][e] - at);
                         s[x][y][e + 2] = ex2(s[x][y][e + 2] - at);
-                        sum = fmaf(s[x][y][e] + s[x][y][e + 2], back[x], sum);
+                        l[y][e] += (s[x][y][e] + s[x][y][e + 2]) * back[x];
                     }
-                    l[y][e] = fmaf(sum, ex2(d[y][e] - up), l[y][e]);
                 }
             }
         } else {
             // scores as they are. (Differences first: next to scores of any size logarithms would be lost)
-            float f[NB][2];
+            float f[NB][2], next[NB][2];
             bool moved = false;
 #pragma unroll
             for (int y = 0; y < NB; ++y) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float m = M[y][e] - d[y][e];
+                    const float before = single ? row_d[y * 8 + tq * 2 + e] : d, m = M[y][e] - before;
                     float top = -INFINITY, with = -INFINITY;
 #pragma unroll
                     for (int x = 0; x < KB; ++x) top = fmaxf(top, fmaxf(s[x][y][e], s[x][y][e + 2]));
                     const float to = fmaxf(m, row_max(top)), base = to == -INFINITY ? 0.0f : to;
 #pragma unroll
                     for (int x = 0; x < KB; ++x) with = fmaxf(with, (fmaxf(s[x][y][e], s[x][y][e + 2]) - base) + lv[x]);
-                    const float by = m - base, next = fmaxf(fmaxf(d[y][e] + by, row_max(with)), 2 * LOG_ZERO);
-                    f[y][e] = ex2(by + (d[y][e] - next));
+                    const float by = m - base;
+                    next[y][e] = fmaxf(fmaxf(before + by, row_max(with)), 2 * LOG_ZERO);
+                    f[y][e] = ex2(by + (before - next[y][e]));
+                    if (wild) f[y][e] = fmaxf(f[y][e], NORMAL);
                     moved = moved || f[y][e] != 1.0f;
                     l[y][e] *= ex2(by);
-                    M[y][e] = to == -INFINITY ? to : __fadd_ru(to, next);
-                    d[y][e] = next;
+                    M[y][e] = to == -INFINITY ? to : __fadd_ru(to, next[y][e]);
 #pragma unroll
                     for (int x = 0; x < KB; ++x) {
                         if (cached) {
@@ -614,13 +614,16 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                             for (int z = 0; z < 4; z += 2) {
                                 const float t = s[x][y][e + z] - base;
                                 l[y][e] += ex2(t);
-                                s[x][y][e + z] = ex2(t + (lv[x] - next + UP));
+                                s[x][y][e + z] = ex2(t + (lv[x] - next[y][e] + UP));
                             }
                         } else {
                             // (weights of new values stay in 32 bits, and have no scale)
                             const float t = s[x][y][e] - base;
                             l[y][e] += ex2(t);
-                            s[x][y][e] = ex2(t + (UP - next));
+                            s[x][y][e] = ex2(t + (UP - next[y][e]));
+                            // a value that is not finite counts for all rows that see it: no weight of theirs is 0
+                            const int key = first + x * 8 + gq;
+                            if (wild && key < C.T && (see[y][e] >> key & 1)) s[x][y][e] = fmaxf(s[x][y][e], 1.4e-45f);
                         }
                     }
                 }
@@ -636,18 +639,36 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                             o[x][y][e + 2] *= f[y][e];
                         }
             }
+            // one d for all rows again, where it does (behind new tokens nothing comes that would gain by it)
+            single = !cached;
             if (cached) {
-                d_least = d_most = d[0][0];
+                float least = next[0][0], most = next[0][0];
 #pragma unroll
                 for (int y = 0; y < NB; ++y) {
-                    d_least = fminf(d_least, fminf(d[y][0], d[y][1]));
-                    d_most = fmaxf(d_most, fmaxf(d[y][0], d[y][1]));
+                    least = fminf(least, fminf(next[y][0], next[y][1]));
+                    most = fmaxf(most, fmaxf(next[y][0], next[y][1]));
                 }
 #pragma unroll
                 for (int x = 1; x < 4; x <<= 1) {
-                    d_least = fminf(d_least, __shfl_xor_sync(0xffffffffu, d_least, x));
-                    d_most = fmaxf(d_most, __shfl_xor_sync(0xffffffffu, d_most, x));
+                    least = fminf(least, __shfl_xor_sync(0xffffffffu, least, x));
+                    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, x));
                 }
+                single = most - least > FAR;
+                if (!single) {
+                    d = least;
+#pragma unroll
+                    for (int y = 0; y < NB; ++y)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) l[y][e] *= ex2(d - next[y][e]);
+                }
+            }
+            if (single) {
+                __syncwarp();
+                if (gq == 0) {
+#pragma unroll
+                    for (int y = 0; y < NB; ++y) *reinterpret_cast<float2*>(row_d + y * 8 + tq * 2) = make_float2(next[y][0], next[y][1]);
+                }
+                __syncwarp();
             }
         }
         if (cached) {
@@ -739,7 +760,8 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
 #pragma unroll
                     for (int x = 4; x < 32; x <<= 1) l[y][e] += __shfl_xor_sync(0xffffffffu, l[y][e], x);
                     const float sum = l[y][e];
-                    const float2 unit = unit_of(d[y][e]);
+                    const float of_row = single ? row_d[y * 8 + tq * 2 + e] : d;
+                    const float2 unit = unit_of(of_row);
                     const float small = unit.y * ex2(-UP);
                     const int rr = y * 8 + tq * 2 + e;
                     if (rr < live) {
@@ -750,17 +772,18 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                                 *reinterpret_cast<float4*>(to + L::value_channel(w, gq)) =
                                     make_float4(o[2 * w][y][e] * small * unit.x, o[2 * w][y][e + 2] * small * unit.x,
                                                 o[2 * w + 1][y][e] * small * unit.x, o[2 * w + 1][y][e + 2] * small * unit.x);
-                            if (gq == 0) *reinterpret_cast<float2*>(part + rr * 2) = make_float2(M[y][e] - d[y][e], sum);
+                            if (gq == 0) *reinterpret_cast<float2*>(part + rr * 2) = make_float2(M[y][e] - of_row, wild ? -sum : sum);
                         } else {
                             const int rho = C.rt * RM + rr, t = rho / G, head = C.h * G + rho - t * G;
-                            const float inv = (sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f) * small;
+                            const float inv = 1.0f / sum * small;
+                            const auto of = [&](float x) { return sum == 0.0f ? 0.0f : x * inv * unit.x; };
                             char* const to = a.out + ((C.lo + t) * a.out_stride + (long long)head * D) * 2;
 #pragma unroll
                             for (int w = 0; w < NW; ++w)
                                 *reinterpret_cast<uint2*>(to + L::value_channel(w, gq) * 2) =
-                                    make_uint2(Num<T>::pack(o[2 * w][y][e] * inv * unit.x, o[2 * w][y][e + 2] * inv * unit.x),
-                                               Num<T>::pack(o[2 * w + 1][y][e] * inv * unit.x, o[2 * w + 1][y][e + 2] * inv * unit.x));
-                            if (gq == 0 && a.lse) a.lse[(long long)(C.lo + t) * (H * G) + head] = (M[y][e] - d[y][e] + log2f(sum)) * LN2;
+                                    make_uint2(Num<T>::pack(of(o[2 * w][y][e]), of(o[2 * w][y][e + 2])),
+                                               Num<T>::pack(of(o[2 * w + 1][y][e]), of(o[2 * w + 1][y][e + 2])));
+                            if (gq == 0 && a.lse) a.lse[(long long)(C.lo + t) * (H * G) + head] = (M[y][e] - of_row + log2f(sum)) * LN2;
                         }
                     }
                 }

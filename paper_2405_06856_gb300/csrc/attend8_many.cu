@@ -705,8 +705,8 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                             o[i] = __float_as_uint(fmaf(__uint_as_float(o1[i]) * unit1.y, unit1.x, __uint_as_float(o[i])));
                     }
                     if (row < rows) {
-                        if (wild) {
-                            // values that are not finite, of the tokens that this row sees
+                        if (wild && !(whole && l == 0.0f)) {
+                            // values that are not finite, of the tokens that this row sees, whatever their weight
                             for (int x = 0; x < u.T; ++x) {
                                 if (!(see >> x & 1)) continue;
                                 const unsigned short* p = reinterpret_cast<const unsigned short*>(
@@ -743,7 +743,7 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                 if (lane == 0) mbar_arrive(sm0 + L::ofree + w * 8);
                 if (joins && lane == 0) mbar_arrive(sm0 + L::ofree + 8);
                 if (row < rows) {
-                    if (!whole) *reinterpret_cast<float2*>(part + rr * 2) = make_float2(m, l);
+                    if (!whole) *reinterpret_cast<float2*>(part + rr * 2) = make_float2(m, wild ? -l : l);
                     else if (a.lse) a.lse[(long long)(u.lo + t) * (H * G) + hd] = (m + log2f(l)) * LN2;
                 }
                 if (!whole) {

@@ -242,3 +242,52 @@ def test_attend8_large_values_out_of_sight(A, kind, q_heads, toks):  # noqa: F81
     case["q"][1] = 0.0
     d = Dev8(A, case)
     check_ranges(case, *d.worker.attend(d.kv, d.tok, case["scale"]))
+
+
+# ---------------------------------------------------------------------------------------------------------
+# Values of new tokens that are not finite.
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("q_heads,dim,toks,held", [(4, 64, [3, 2], 20), (2, 128, [20, 3], 3), (2, 256, [14, 1], 0), (4, 96, [2, 3], 2000),
+                                                   (32, 64, [30, 20], 20), (16, 128, [40, 9], 0), (32, 96, [30, 9], 2000), (16, 256, [30, 4], 40)])
+@pytest.mark.parametrize("below", [0, 200])
+def test_attend8_values_that_are_not_finite(A, kind, q_heads, dim, toks, held, below):  # noqa: F811
+    """They make their channel what they are in the rows that see them, also where their weight is e^-200, and nothing in
+    other rows and channels."""
+    case = make8(kind, q_heads, 2, dim, 64, [held, 17], toks)
+    case["parent"][:] = np.concatenate([np.arange(t) - 1 for t in toks])  # chains: what comes later sees it
+    case["q"] = rounded(np.abs(case["q"]) + 0.5, kind)
+    at = toks[0] + 1 if len(toks) < 2 else 1
+    finite = case["v_new"].copy()
+    finite[at, 0, [3, 40]] = finite[at, 1, 7] = 0.0
+    case["v_new"] = finite
+    if below:
+        # a score at least 200 below any other: those of the rest are within 40
+        case["k_new"][at] = rounded(np.full(dim, -1600.0 / dim ** 0.5), kind)
+    d = Dev8(A, case)
+    want, want_lse = (f64(x) for x in d.worker.attend(d.kv, d.tok))
+    scores = np.einsum("thgd,hd->thg", case["q"].reshape(len(want), 2, -1, dim), case["k_new"][at]) * case["scale"]
+    assert not below or (scores[at:toks[0]].reshape(toks[0] - at, -1) - want_lse[at:toks[0]]).max() < -150
+    bad = case["v_new"].copy()
+    bad[at, 0, 3], bad[at, 0, 40], bad[at, 1, 7] = math.inf, math.nan, -math.inf
+    d = Dev8(A, dict(case, v_new=bad))
+    got, lse = (f64(x) for x in d.worker.attend(d.kv, d.tok))
+    g = q_heads // 2
+    seen = slice(at, toks[0])
+    want[seen, :g, 3], want[seen, :g, 40], want[seen, g:, 7] = math.inf, math.nan, -math.inf
+    np.testing.assert_array_equal(got, want)
+    np.testing.assert_array_equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("q_heads,toks", [(4, [2, 1]), (32, [30, 2])])
+def test_attend8_no_score_and_no_value(A, q_heads, toks):  # noqa: F811
+    """A row whose scores are all -inf has no result, whatever the values."""
+    case = make8("f16", q_heads, 2, 64, 16, [0, 20], toks)
+    case["q"] = rounded(np.abs(case["q"]) + 0.1, "f16")
+    case["k_new"][0] = -math.inf
+    case["v_new"][0, :, 3] = math.inf
+    case["parent"][:toks[0]] = -1
+    d = Dev8(A, case)
+    out, lse = d.worker.attend(d.kv, d.tok)
+    assert (out[0] == 0).all() and (lse[0] == -math.inf).all()
+    assert out[1:].isfinite().all()
