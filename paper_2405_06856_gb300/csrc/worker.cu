@@ -356,6 +356,12 @@ try {
     aladdin_tokens t = *tok;  // (values are not read: the keys stand for them)
     t.v = t.k;
     t.v_stride = t.k_stride;
+    if (pos) {  // (nor are the requests: the positions stand for them, all tokens for one)
+        if (t.n_req < 0 || t.n_req > ALADDIN_WORKER_MAX_REQUESTS) return ALADDIN_ERR_ARG;
+        t.n_req = 1;
+        t.off = pos;
+        t.parent = nullptr;
+    }
     int rc = check_tokens(wk, &t, q_out != nullptr, &a.tok);
     if (rc) return rc;
     if ((rc = check_rope(wk, rope, &a.rope))) return rc;

@@ -281,7 +281,7 @@ class Worker:
     def rotate(self, rope, tok, next_pos=None, pos=None, q_out=None, k_out=None):
         """(q, k) of the tokens rotated to their positions: ``pos`` (int32 [tokens]), or ``next_pos`` (int32 [requests];
         None: 0) plus a token's depth in its tree. q_out, k_out: None for a new tensor, the tokens' own tensor (in place),
-        another one, or False to leave them out."""
+        another one, or False to leave them out. Without ``pos`` tokens that no request has (padding) are not written."""
         if tok._shape != self._tok_shape and not (q_out is False and tok._shape == self._tok_bare):
             raise ValueError("the tokens do not have the worker's type or heads: %s, not %s"
                              % (tok._shape, self._tok_shape))
