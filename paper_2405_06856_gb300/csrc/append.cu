@@ -322,6 +322,8 @@ __global__ void __launch_bounds__(NT, PER_SM) k_append8(AppendArgs a, int wpu, i
                 // be a round behind)
                 asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(wpu * 32) : "memory");
                 for (int w = 0; w < wpu; ++w) most = fmaxf(most, tops[round & 1][group * wpu + w]);
+            } else {
+                __syncwarp();  // (all lanes have read the scale when the first writes it)
             }
             if (!live) continue;
             float scale = scale_of(most);

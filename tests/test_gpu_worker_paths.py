@@ -7,6 +7,7 @@ import pytest
 
 import worker8_ref as ref8
 from test_gpu_worker import A, Dev, f64, make, rounded  # noqa: F401
+from test_gpu_worker_cache8 import Dev8, make8
 from test_gpu_worker_rope import check_rotated, rope_of
 
 pytestmark = pytest.mark.gpu
@@ -54,3 +55,32 @@ def test_rotate_padding(A):  # noqa: F811
     q.fill_(9.0)
     d.worker.rotate(rope_of(A, freq, "half"), none, q_out=q, k_out=False)
     assert (q == 9.0).all() and d.worker.status() == 0
+
+
+# ---------------------------------------------------------------------------------------------------------
+# append8, a token at a time
+
+@pytest.mark.parametrize("kind,heads,dim,block", [("bf16", 8, 128, 16), ("f16", 3, 64, 64), ("bf16", 2, 96, 32), ("f16", 2, 256, 16)])
+def test_append8_scales_that_grow(A, kind, heads, dim, block):  # noqa: F811
+    """A token a call to each of many requests, each twice as large as the one before it: every call rounds what the
+    block holds again, under the scale that it had."""
+    import torch
+    n, steps = 60, 9
+    case = make8(kind, heads, heads, dim, 64, [(7 * r) % 50 for r in range(n)], [steps] * n, block, trees=False)
+    grow = np.tile(2.0 ** np.arange(steps), n)[:, None, None]
+    for name in ("k_new", "v_new"):
+        case[name] = rounded(np.sign(case[name]) * np.clip(np.abs(case[name]), 0.1, 1.0) * grow, kind)
+    d = Dev8(A, case)
+    off = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    for i in range(steps):
+        x = torch.arange(n, device="cuda") * steps + i
+        d.worker.append(d.kv, A.make_tokens(off, None, d.k_new[x], d.v_new[x]))
+    assert d.worker.status() == 0 and d.len.tolist() == [l + steps for l in case["len"]]
+    now = dict(case)
+    for i in range(steps):  # (one request after the other, a token at a time)
+        step = dict(now, len=[l + i for l in case["len"]], off=np.arange(n + 1), k_new=case["k_new"][i::steps], v_new=case["v_new"][i::steps])
+        now.update(ref8.append8(step, step["k_new"]))
+    nan = lambda c: np.where(c & 127 == 127, 127, c)
+    for name in ("k", "v"):
+        np.testing.assert_array_equal(getattr(d, name + "_scale").cpu().numpy(), now[name + "_scale"].astype(np.float32))
+        np.testing.assert_array_equal(nan(d.codes[name].cpu().numpy()), nan(now[name]))
