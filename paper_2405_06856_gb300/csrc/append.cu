@@ -210,6 +210,24 @@ __device__ __forceinline__ float2 values2(uint32_t u)
     return __half22float2(*reinterpret_cast<__half2*>(&h));
 }
 
+// What 32 bits hold of an exact result, the last bit set where that is not all of it: a rounding to fewer bits then comes out
+// as one of the exact result. The product with a scale's ratio, and the quotient by a scale that is no power of two.
+__device__ __forceinline__ float sticky(float cut, float rest)
+{
+    return rest != 0.0f ? __uint_as_float(__float_as_uint(cut) | 1u) : cut;
+}
+__device__ __forceinline__ float product_of(float z, float f)
+{
+    const float p = __fmul_rz(z, f);
+    return sticky(p, fmaf(z, f, -p));
+}
+__device__ __forceinline__ float quotient_of(float x, float s)
+{
+    if (s < 8.6736174e-19f) x *= 1.8446744e19f, s *= 1.8446744e19f;  // 2^-60, 2^64: so that 32 bits hold the rest
+    const float q = __fdiv_rz(x, s);
+    return sticky(q, fmaf(-q, s, x));
+}
+
 // The least power of two, 2^-126 at least, of which m (finite, >= 0) is 448 = 1.75 2^8 times at most.
 __device__ __forceinline__ float scale_of(float m)
 {
@@ -339,7 +357,7 @@ __global__ void __launch_bounds__(NT, PER_SM) k_append8(AppendArgs a, int wpu, i
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             const float2 z = values2((j < 2 ? c.x : c.y) >> (j & 1) * 16);
-                            w[j] = codes2(z.x * f, z.y * f);
+                            w[j] = codes2(product_of(z.x, f), product_of(z.y, f));
                         }
                         *d = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
                     }
@@ -347,7 +365,8 @@ __global__ void __launch_bounds__(NT, PER_SM) k_append8(AppendArgs a, int wpu, i
                     scale = old;
                 }
             }
-            const float inv = 1.0f / scale;
+            const bool power = !(__float_as_uint(scale) & 0x7fffff);
+            const float inv = power ? 1.0f / scale : 1.0f;
 #pragma unroll 1
             for (int s0 = lo; s0 < end; s0 += span) {
                 if (end - lo > span) load(s0);
@@ -356,6 +375,12 @@ __global__ void __launch_bounds__(NT, PER_SM) k_append8(AppendArgs a, int wpu, i
                     for (int i = 0; i < N; ++i)
 #pragma unroll
                         for (int j = 0; j < 8; ++j) x[i][j] += x[i][j] - x[i][j];
+                }
+                if (!power) {  // (a held scale of another origin)
+#pragma unroll
+                    for (int i = 0; i < N; ++i)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) x[i][j] = quotient_of(x[i][j], scale);
                 }
 #pragma unroll
                 for (int i = 0; i < N; ++i) {

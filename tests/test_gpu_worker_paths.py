@@ -84,3 +84,33 @@ def test_append8_scales_that_grow(A, kind, heads, dim, block):  # noqa: F811
     for name in ("k", "v"):
         np.testing.assert_array_equal(getattr(d, name + "_scale").cpu().numpy(), now[name + "_scale"].astype(np.float32))
         np.testing.assert_array_equal(nan(d.codes[name].cpu().numpy()), nan(now[name]))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("grow", [False, True])
+def test_append8_under_scales_of_another_origin(A, kind, grow):  # noqa: F811
+    """Held scales that are no powers of two: new values, many of them in the middle between two codes, are rounded once, and
+    so are the held codes under a scale that grows."""
+    odd = [3.0, 5.0, 7.0] + [float(np.float32(t / z)) for t in (9, 11, 13, 15, 17, 19, 21, 23, 25, 27, 29, 31) for z in (9, 10, 11, 13, 14, 15)]
+    scales = np.array([s for s in odd if math.frexp(s)[0] != 0.5], np.float32) * np.float32(2.0 ** -9)
+    n = len(scales)
+    case = make8(kind, 2, 2, 64, 16, [5] * n, [6] * n, 16, trees=False)
+    rng = np.random.default_rng(n)
+    ties = np.concatenate([(ref8.VALUES[40:120] + ref8.VALUES[41:121]) / 2, ref8.VALUES[30:126]])
+    for name in ("k", "v"):
+        for r, s in enumerate(scales):
+            p = case["table"][r][0]
+            case[name + "_scale"][p] = s
+            case[name][p, :, :5] = rng.integers(0, 127, (2, 5, 64)) + 128 * rng.integers(0, 2, (2, 5, 64))
+            x = rng.choice(ties, (6, 2, 64)) * rng.choice([-1.0, 1.0], (6, 2, 64)) * float(s)
+            if grow:
+                x[0, :, 0] = 448.0 * 4 * 2.0 ** math.ceil(math.log2(float(s)))
+            case[name + "_new"][r * 6:(r + 1) * 6] = rounded(x, kind)
+    d = Dev8(A, case)
+    d.worker.append(d.kv, d.tok)
+    assert d.worker.status() == 0
+    want = ref8.append8(case, case["k_new"])
+    nan = lambda c: np.where(c & 127 == 127, 127, c)
+    for name in ("k", "v"):
+        np.testing.assert_array_equal(getattr(d, name + "_scale").cpu().numpy(), want[name + "_scale"].astype(np.float32))
+        np.testing.assert_array_equal(nan(d.codes[name].cpu().numpy()), nan(want[name]))
