@@ -688,14 +688,15 @@ typedef struct aladdin_rope {
 int aladdin_rope_frequencies(int32_t dim, double base, int32_t scaling, double factor, double original,
                              double slow, double fast, double* freq, float* scale);
 
-/* turn[c] of n finite frequencies, on the host. */
+/* turn[c] of n finite frequencies, on the host; they have the 53 bits of a double: at position p the angle is off by
+ * |p freq[c]| 2^-52 radians and |p| 2^-64 turns at most. */
 int aladdin_rope_turns(int32_t n, const double* freq, uint64_t* turn);
 
 /* Rotate the new tokens' queries and keys to their positions: pos[t] for token t where pos is given, else next[r]
  * (0 where next is NULL) plus the token's depth in its request's tree (its index, for chains, which may have any
  * number of tokens). q_out, k_out [n_tok]: rows of q_out_stride and k_out_stride elements (multiples of 8), heads and
  * channels as in tok; each is NULL (not rotated), or tok's own array with its stride (in place), or memory apart from it.
- * 32-bit products, rounded once; sines and cosines are good to 2^-23. tok->v is not read, nor are n_req, off
+ * 32-bit products, rounded once; sines and cosines of the angles p turn[c] are good to 2^-23. tok->v is not read, nor are n_req, off
  * and parent with pos, where all tokens are rotated; without it outputs of tokens that no request has are not written. */
 int aladdin_worker_rotate(aladdin_worker* wk, const aladdin_rope* rope, const aladdin_tokens* tok,
                           const int32_t* next, const int32_t* pos, void* q_out, int64_t q_out_stride,

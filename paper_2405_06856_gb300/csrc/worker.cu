@@ -459,8 +459,10 @@ int aladdin_rope_turns(int32_t n, const double* freq, uint64_t* turn)
     for (int i = 0; i < n; ++i)
         if (!std::isfinite(freq[i])) return ALADDIN_ERR_ARG;
     for (int i = 0; i < n; ++i) {
-        const double t = freq[i] / (2.0 * M_PI), part = t - std::floor(t);  // (1 where t is barely below 0)
-        turn[i] = part < 1.0 ? (uint64_t)std::ldexp(part, 64) : 0;
+        // (of the magnitude: next to 1 the bits of a small negative one would be lost)
+        const double t = std::fabs(freq[i]) / (2.0 * M_PI);
+        const uint64_t u = (uint64_t)std::ldexp(t - std::floor(t), 64);
+        turn[i] = freq[i] < 0.0 ? 0 - u : u;
     }
     return ALADDIN_OK;
 }

@@ -1,0 +1,28 @@
+"""Frequencies in turns against exact arithmetic, and refusals of make_rope, on the host."""
+import math
+from fractions import Fraction
+
+import numpy as np
+import pytest
+
+PI = Fraction(314159265358979323846264338327950288419716939937510582097494459, 10 ** 62)
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2405_06856_gb300 import build
+    build.build()
+    from paper_2405_06856_gb300 import aladdin as A
+    return A
+
+
+@pytest.mark.parametrize("base", [10000.0, 500000.0, 1e8])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_turns_of_far_positions(lib, base, sign):
+    """|p freq| 2^-52 radians (the division's rounding 2^-53, that of 2 pi 2^-54) and, by the last of 64 bits, |p| 2^-64 turns."""
+    freq = np.concatenate([base ** (-np.arange(64) / 64), [0.3, 6.0, 7.0, 1e-9, 12345.678]]) * sign
+    for f, t in zip(freq, lib.aladdin_rope_turns(freq).tolist()):
+        for p in (1, -1, 131071, 2 ** 24 + 1, 2 ** 31 - 1, -2 ** 31):
+            off = Fraction(p * t % (1 << 64), 1 << 64) - p * Fraction(f) / (2 * PI)
+            off = abs(off - round(off))
+            assert off <= abs(p) * (Fraction(abs(f)) / (2 * PI) / (1 << 52) + Fraction(1, 1 << 64)), (f, p)
