@@ -122,7 +122,8 @@ def make_rope(dim, base=10000.0, layout="half", scaling=None, factor=1.0, origin
 
     layout: "half" (channels c, c + dim / 2 form a pair) or "interleaved" (2 c, 2 c + 1). Frequencies are base^(-2 c / dim),
     scaled for long contexts by ``factor``: "linear", "base", or "parts" (of a model made for ``original`` positions: pairs
-    that turn fewer than ``slow`` times in them are slowed down, those of more than ``fast`` times are left);
+    that turn fewer than ``slow`` times in them are slowed down, those of more than ``fast`` times are left, and in
+    between in proportion to the turns; a model with a ramp over the pairs' index gives ``freq``);
     or ``freq``, dim / 2 numbers in radians a position. ``scale`` multiplies rotated channels (default: 1, for "parts"
     0.1 ln(factor) + 1)."""
     if layout not in _LAYOUTS:
@@ -131,6 +132,8 @@ def make_rope(dim, base=10000.0, layout="half", scaling=None, factor=1.0, origin
         raise ValueError("scaling must be None or one of %s" % sorted(s for s in _SCALINGS if s))
     if dim < 2 or dim % 2:
         raise ValueError("dim must be even and at least 2")
+    if scaling is None and factor != 1.0:
+        raise ValueError("factor needs a scaling that it belongs to")
     if freq is None:
         if scaling == "parts" and original is None:
             raise ValueError("scaling by parts needs the positions that the model was made for (original)")

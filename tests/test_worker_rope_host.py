@@ -26,3 +26,14 @@ def test_turns_of_far_positions(lib, base, sign):
             off = Fraction(p * t % (1 << 64), 1 << 64) - p * Fraction(f) / (2 * PI)
             off = abs(off - round(off))
             assert off <= abs(p) * (Fraction(abs(f)) / (2 * PI) / (1 << 52) + Fraction(1, 1 << 64)), (f, p)
+
+
+def test_factor_without_scaling(lib):
+    """A factor that nothing would use is refused, not left out in silence."""
+    from paper_2405_06856_gb300 import worker as W
+    for more in (dict(), dict(freq=[1.0, 0.5])):
+        with pytest.raises(ValueError, match="factor"):
+            W.make_rope(4, factor=8.0, device="cpu", **more)
+        rope = W.make_rope(4, factor=1.0, device="cpu", **more)
+        assert rope.dim == 4 and rope.scale == 1.0
+    assert W.make_rope(4, scaling="linear", factor=8.0, device="cpu").dim == 4
