@@ -7,8 +7,8 @@ import pytest
 
 import worker8_ref as ref8
 from test_gpu_worker import A, Dev, f64, make, rounded  # noqa: F401
-from test_gpu_worker_cache8 import Dev8, make8
-from test_gpu_worker_rope import check_rotated, rope_of
+from test_gpu_worker_cache8 import Dev8, check_append8, keys8, make8
+from test_gpu_worker_rope import check_append, check_rotated, keys_at, rope_of
 
 pytestmark = pytest.mark.gpu
 
@@ -114,3 +114,70 @@ def test_append8_under_scales_of_another_origin(A, kind, grow):  # noqa: F811
     for name in ("k", "v"):
         np.testing.assert_array_equal(getattr(d, name + "_scale").cpu().numpy(), want[name + "_scale"].astype(np.float32))
         np.testing.assert_array_equal(nan(d.codes[name].cpu().numpy()), nan(want[name]))
+
+
+# ---------------------------------------------------------------------------------------------------------
+# Prompts: more units than the GPU has warps, several turns of every loop.
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("kind,q_heads,kv_heads,dim,turn", [("bf16", 40, 8, 64, 64), ("f16", 12, 4, 256, 256), ("bf16", 28, 4, 96, 64), ("f16", 64, 8, 128, 20)])
+@pytest.mark.parametrize("place", [False, True])
+def test_rotate_prompts(A, kind, q_heads, kv_heads, dim, turn, layout, place):  # noqa: F811
+    """A warp has a token's rows in several turns."""
+    import torch
+    toks = [1250, 0, 1, 77]
+    case = make(kind, q_heads, kv_heads, dim, 16, [0] * 4, toks, trees=False)
+    d = Dev(A, case)
+    freq = 10000.0 ** (-np.arange(turn // 2) / (turn // 2))
+    start = np.array([5000, 3, 0, 100000])
+    pos = np.repeat(start, toks) + ref8.depths(case["off"], None)
+    outs = dict(q_out=d.q, k_out=d.k_new) if place else {}
+    q, k = d.worker.rotate(rope_of(A, freq, layout), d.tok, torch.from_numpy(start.astype(np.int32)).cuda(), **outs)
+    assert d.worker.status() == 0
+    check_rotated(f64(q), case["q"], pos, freq, layout, 1.0, kind)
+    check_rotated(f64(k), case["k_new"], pos, freq, layout, 1.0, kind)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("kind,heads,dim,turn,page", [("bf16", 1, 64, 64, 16), ("f16", 8, 256, 256, 64), ("bf16", 12, 128, 96, 32), ("f16", 5, 96, 58, 128)])
+@pytest.mark.parametrize("rotated", [True, False])
+def test_append_prompts(A, kind, heads, dim, turn, page, layout, rotated):  # noqa: F811
+    """A warp has several units, turned on from one to the next across pages and requests, and a unit's heads in several turns;
+    a page outside the pool among them."""
+    toks = [3001, 0, 1, 2500, 64, 3200]
+    case = make(kind, heads, heads, dim, page, [5, 100, 16, 0, 31, 900], toks, trees=False)
+    case["next"] = [l + 70000 * r for r, l in enumerate(case["len"])]
+    case["table"][3, 700 // page] = -1
+    d = Dev(A, case)
+    freq = 10000.0 ** (-np.arange(turn // 2) / (turn // 2))
+    d.worker.append(d.kv, d.tok, rope_of(A, freq, layout) if rotated else None)
+    assert d.worker.status() == A.ERR_STATE and d.worker.status() == 0
+    if rotated:
+        check_append(case, d, *keys_at(case, freq, layout, kind))
+    else:
+        check_append(case, d, case["k_new"], np.zeros_like(case["k_new"]))
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("kind,heads,dim,turn,page,block,tokens", [
+    ("bf16", 4, 64, 64, 16, 16, 40000),    # a warp a block, several rows of heads a unit
+    ("f16", 2, 256, 40, 64, 16, 20500),    # four warps a block
+    ("bf16", 3, 128, 128, 128, 64, 27000)])  # eight
+def test_append8_prompts(A, kind, heads, dim, turn, page, block, tokens, layout):  # noqa: F811
+    """Several rows of heads a unit, several units a group of warps one after the other; infinities and NaN among them, which
+    one warp of several meets, and a page outside the pool."""
+    toks = [tokens // 2, 1, 0, tokens - tokens // 2]
+    case = make8(kind, heads, heads, dim, page, [block + 3, 7, 20, 0], toks, block, trees=False)
+    case["next"] = [l + 70000 * r for r, l in enumerate(case["len"])]
+    rng = np.random.default_rng(dim)
+    for name in ("k_new", "v_new"):
+        case[name] *= 2.0 ** rng.integers(-2, 3, (len(case[name]), 1, 1))
+        t, h, c = rng.integers(0, tokens, 40), rng.integers(0, heads, 40), rng.integers(0, dim, 40)
+        case[name][t, h, c] = rng.choice([math.inf, -math.inf, math.nan], 40)
+    case["table"][3, 700 // page] = len(case["k"])
+    d = Dev8(A, case)
+    freq = 10000.0 ** (-np.arange(turn // 2) / (turn // 2))
+    d.worker.append(d.kv, d.tok, rope_of(A, freq, layout))
+    assert d.worker.status() == A.ERR_STATE and d.worker.status() == 0
+    with np.errstate(invalid="ignore"):
+        check_append8(case, d, *keys8(case, freq, layout))
