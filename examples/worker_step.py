@@ -56,7 +56,8 @@ class ServingWorker:
         width = -(-(max(lengths) + room) // page)
         pages = n * width
         self.table = torch.from_numpy(self.rng.permutation(pages).astype(np.int32)).view(n, width).to(dev)
-        self.k, self.v = normal(pages, kv_heads, page, dim).to(dt), normal(pages, kv_heads, page, dim).to(dt)
+        if cache != 8:
+            self.k, self.v = normal(pages, kv_heads, page, dim).to(dt), normal(pages, kv_heads, page, dim).to(dt)
         self.rope = A.make_rope(dim, scaling="parts", factor=4.0, original=8192) if rotary else None
         self.eight, self.budget = cache == 8, None
         self.root = torch.randint(0, vocab, (n,), generator=self.gen, device=dev)  # each request's last token
