@@ -9,10 +9,10 @@
 //   seven warps convert, 16 keys or values at a time in turn: codes come by asynchronous copies a few of those ahead, each
 //   lane's own, and go as half precision into a ring of shared memory, K0 V0 K1 V1 ..., in the 128-byte-swizzled layout of
 //   the matrix descriptors. New tokens have a tile of their own; those of bfloat16 are scaled by a power of two for each.
-// A row tile's scores have two places: the next ones are formed while the softmax works on those before. A unit with one row
-// tile has its even and odd tiles done by the two sets of softmax warps, with an accumulator each, joined at its end. The
-// accumulators stay in tensor memory; they are rescaled only when a row's maximum has grown by more than 2^8 over the
-// one that its weights refer to.
+// A row tile's scores have two places: the next ones are formed while the softmax works on those before. (Even and odd tiles of a
+// single row tile by the two sets of softmax warps, with an accumulator each, took 5 to 10% longer: 64 requests of 1,500 tokens,
+// 64 rows of 128 channels, 137 us for 124.) The accumulators stay in tensor memory; they are rescaled only when a row's
+// maximum has grown by more than 2^8 over the one that its weights refer to.
 //
 // What bounds it: latency of a few warps a role. 16 warps share four schedulers, an instruction takes a warp 4 to 6 cycles,
 // and each role has some 200 of them for a tile, so code is kept small as well: with products, tiles and units
@@ -50,13 +50,11 @@ struct Many8 {
     static constexpr int raw = q + MT * QT;
     static constexpr int bars = (raw + CONV * NF * RAW + 15) / 16 * 16;
     static constexpr int full = bars, empty = full + NB * 8, qready = empty + NB * 8, sready = qready + 16,
-                         pready = sready + 32, odone = pready + 32, ofree = odone + 32, merged = ofree + 16, over = merged + 8,
+                         pready = sready + 32, odone = pready + 32, ofree = odone + 32, over = ofree + 16,
                          tmem = over + 8;
     static constexpr int wild = tmem + 8;                // 8 flags of units
     static constexpr int late = wild + 8 * 4;            // whether a wait ran out
-    static constexpr int factors = late + 8;             // of the rows' scores, for two units in turn
-    static constexpr int other = (factors + 2 * 128 * 4 + 15) / 16 * 16;  // what the second half of the tiles gave a row
-    static constexpr int info = other + 128 * 16;        // 8 tiles' Info
+    static constexpr int info = (late + 8 + 15) / 16 * 16;  // 8 tiles' Info
     static constexpr int scratch = info + 8 * (64 * 8 + 16);
     static constexpr int pre = scratch + 96 * 8;
     static constexpr int bytes(int n_req) { return pre + Axis8::ints(n_req) * 4; }
@@ -141,7 +139,6 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
             mbar_init(sm0 + L::ofree + w * 8, 4);
         }
         for (int w = 0; w < 4; ++w) mbar_init(sm0 + L::sready + w * 8, 1);
-        mbar_init(sm0 + L::merged, 4);
         mbar_init(sm0 + L::over, 1);
         for (int u = 0; u < 8; ++u) wilds[u] = 0;
         *late = 0;
@@ -165,6 +162,8 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
     auto active = [&](const Cursor& u) { return MT == 2 && u.T * G - u.rt * RM > 128 ? 2 : 1; };
     // to the next unit
     auto next_unit = [&](Cursor& u) { next_unit8<KT, KT, RM>(a, ax, u); };
+    // where the scores of row tile w and a unit's tile y lie
+    auto place = [&](int w, int y) { return MT == 2 ? (y & 1) * 2 + w : y & 1; };
     bool ok = true;  // no wait of this warp ran out
 
     // Every role goes over the units of the range, and in each over its tiles; tile `done` + t of the range has places
@@ -325,36 +324,33 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
         cp_wait<0>();
     } else if (warp == 4 * MT) {
         // ------------------------------------------------------------ products
-        // Steps of a tile and a row tile each; of a unit with one row tile the even and the odd tiles have an accumulator and
-        // softmax warps each, as two row tiles would. The scores of step k go to place k % 4 (256 channels: 2), and are
-        // formed when the products with values of the step `ahead` before have been started: a step's scores are formed
-        // while the softmax works on those before.
+        // Steps of a tile and a row tile each. A row tile's scores have two places in turn (place 2 (y % 2) + w of tile y and row
+        // tile w; 256 channels: y % 2), and are formed when the products with values of the step two tiles before have been
+        // started: a step's scores are formed while the softmax works on those before.
         constexpr uint32_t qk = product<__half>(KT, false), pv = product<__half>(D, true);
-        constexpr int PL = L::PLACES;
         if (elected()) {  // (one thread waits and issues)
             Cursor u = C;
             int asked[2] = {0, 0}, run[4] = {0, 0, 0, 0}, started[2] = {0, 0};
 #pragma unroll 1
             for (int done = 0; done < n && ok;) {
                 const int count = min(u.c - u.tile, n - done), two = active(u) == 2;
-                // (of single tiles as many ahead as the ring holds)
-                const int steps = two ? 2 * count : count, ahead = two || NB >= 2 * PL ? PL : MT == 2 ? NB / 2 : 2;
+                const int steps = two ? 2 * count : count, ahead = two ? 4 : 2;
                 if (two) ok = wait(sm0 + L::qready + 8, asked[1]++);
                 ok = ok && wait(sm0 + L::qready, asked[0]++);
 #pragma unroll 1
                 for (int k = -ahead; k < steps; ++k) {
                     if (k >= 0) {
                         // out += P V of step k
-                        const int w = MT == 2 ? k & 1 : 0, y = MT == 2 ? k >> 1 : k, v = 2 * (done + (two ? y : k)) + 1, x2 = w * 2 + (y & 1);
+                        const int w = two ? k & 1 : 0, y = two ? k >> 1 : k, v = 2 * (done + y) + 1, x2 = w * 2 + (y & 1);
                         ok = ok && wait(sm0 + L::pready + x2 * 8, x2 == 0 ? run[0]++ : x2 == 1 ? run[1]++ : x2 == 2 ? run[2]++ : run[3]++);
-                        if (w == 0 || !two) ok = ok && wait(sm0 + L::full + v % NB * 8, v / NB);
+                        if (w == 0) ok = ok && wait(sm0 + L::full + v % NB * 8, v / NB);
                         if (y == 0) {
                             const int before = w ? started[1]++ : started[0]++;
                             if (before > 0) ok = ok && wait(sm0 + L::ofree + w * 8, before - 1);
                         }
                         if (!ok) break;
                         tc_after();
-                        const uint32_t v0 = operand_lo(sm0 + v % NB * L::TILE, KT * 128), at = tm + L::s0 + (k & (PL - 1)) * KT,
+                        const uint32_t v0 = operand_lo(sm0 + v % NB * L::TILE, KT * 128), at = tm + L::s0 + place(w, y) * KT,
                                        o = tm + L::o0 + w * (L::HALVES * 64);
 #pragma unroll
                         for (int x = 0; x < KT / 16; ++x)
@@ -365,13 +361,13 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                     const int z = k + ahead;
                     if (z < steps) {
                         // S = Q K' of step z
-                        const int w = MT == 2 ? z & 1 : 0, i = 2 * (done + (two ? z >> 1 : z));
-                        if (w == 0 || !two) ok = ok && wait(sm0 + L::full + i % NB * 8, i / NB);
+                        const int w = two ? z & 1 : 0, y = two ? z >> 1 : z, i = 2 * (done + y);
+                        if (w == 0) ok = ok && wait(sm0 + L::full + i % NB * 8, i / NB);
                         if (!ok) break;
                         tc_after();
-                        const uint32_t k0 = operand_lo(sm0 + i % NB * L::TILE, 0), at = tm + L::s0 + (z & (PL - 1)) * KT;
+                        const uint32_t k0 = operand_lo(sm0 + i % NB * L::TILE, 0), at = tm + L::s0 + place(w, y) * KT;
                         if constexpr (L::QS) {
-                            const uint32_t q0 = operand_lo(sm0 + L::q + (two ? w : 0) * L::QT, 0);
+                            const uint32_t q0 = operand_lo(sm0 + L::q + w * L::QT, 0);
 #pragma unroll
                             for (int x = 0; x < D / 16; ++x)
                                 tc_mma_ss(at, whole(q0 + ((x >> 2) * 128 * 128 + (x & 3) * 32) / 16, OPERAND_HI),
@@ -382,7 +378,7 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                             for (int x = 0; x < D / 16; ++x)
                                 tc_mma_ts(at, q0 + x * 8, whole(k0 + ((x >> 2) * KT * 128 + (x & 3) * 32) / 16, OPERAND_HI), qk, x > 0);
                         }
-                        tc_commit(sm0 + L::sready + (z & (PL - 1)) * 8);
+                        tc_commit(sm0 + L::sready + place(w, y) * 8);
                         if (w == 1 || !two) tc_commit(sm0 + L::empty + i % NB * 8);
                     }
                 }
@@ -396,11 +392,9 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
         const int w = warp >> 2, row = tid & 127, first_row = warp * 32;
         const uint32_t lanes = (uint32_t)(warp & 3) * 32u << 16, om = tm + lanes + L::o0 + w * (L::HALVES * 64);
         float factor = 0.0f;  // of this row's scores
-        int weighed[2] = {0, 0}, merges = 0;  // this row tile's steps so far, even and odd ones; units whose halves were joined
-        float* const factors = reinterpret_cast<float*>(sm + L::factors);
-        float4* const other = reinterpret_cast<float4*>(sm + L::other);
+        int weighed[2] = {0, 0};  // this row tile's steps so far, of even and odd tiles
         // this row's queries of the unit under u, 32 channels a time, into shared (tensor) memory
-        auto queries = [&](const Cursor& u, int number) {
+        auto queries = [&](const Cursor& u) {
             if (u.T * G - u.rt * RM <= w * 128) return;
             if (u.T * G - u.rt * RM <= first_row) {  // (none of this warp's rows: whatever lies there meets no other row)
                 if (lane == 0) mbar_arrive(sm0 + L::qready + w * 8);
@@ -423,7 +417,6 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
             }
             const float f = half_factor(top);
             factor = (BF16 ? half_back(top) : 1.0f) * a.scale_log2;
-            if (MT == 2 && w == 0) factors[(number & 1) * 128 + row] = factor;
 #pragma unroll 1
             for (int c = 0; c < D / 32; ++c) {
                 uint32_t x[16];
@@ -457,27 +450,26 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
             if (lane == 0) mbar_arrive(sm0 + L::qready + w * 8);
         };
         Cursor u = C;
-        queries(u, 0);
+        queries(u);
         int units = 0;
 #pragma unroll 1
         for (int done = 0; done < n && ok;) {
             const int count = min(u.c - u.tile, n - done);
-            const bool more = done + count < n, two = active(u) == 2, split = MT == 2 && !two;
-            // this warp's rows of the unit, from row0 on, and how many of the tiles are its own: all, or every other one
-            const int row0 = two ? w * 128 : 0, rows = u.T * G - u.rt * RM - row0, mine = split ? (count + 1 - w) / 2 : count;
+            const bool more = done + count < n;
+            const int rows = u.T * G - u.rt * RM - w * 128;  // of the row tile
             const bool idle = rows <= (warp & 3) * 32;
             Cursor next = u;
-            if (mine == 0) {
+            if (rows <= 0) {
                 if (more) {
                     next_unit(next);
-                    queries(next, units + 1);
+                    queries(next);
                 }
             } else {
-                const unsigned long long see = all_ancestors(a, u, row < rows ? (u.rt * RM + row0 + row) / G : 0, lane);
+                const unsigned long long see = all_ancestors(a, u, row < rows ? (u.rt * RM + w * 128 + row) / G : 0, lane);
                 float M = -INFINITY, l = 0.0f, d = 0.0f;  // (attend8.cuh)
 #pragma unroll 1
-                for (int y = 0; y < mine; ++y) {
-                    const int t = split ? 2 * y + w : y, s = MT == 2 ? (y & 1) * 2 + w : y & 1;
+                for (int y = 0; y < count; ++y) {
+                    const int s = place(w, y);
                     ok = __all_sync(0xffffffffu, wait(sm0 + L::sready + s * 8, y & 1 ? weighed[1] : weighed[0]));
                     if (!ok) break;
                     if (y & 1) ++weighed[1];
@@ -486,14 +478,13 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                         if (lane == 0) mbar_arrive(sm0 + L::pready + (w * 2 + (y & 1)) * 8);
                         continue;
                     }
-                    if (split && w && y == 0) factor = factors[(units & 1) * 128 + row];
                     tc_after();
                     const uint32_t st = tm + lanes + L::s0 + s * KT;
                     uint32_t v[2][32];
                     tmem_start(v[0], st);
                     tmem_start(v[1], st + 32);
-                    const Info& info = infos[(done + t) & 7];
-                    const int own = u.len - (u.tile + t) * KT;  // cached keys from the tile's start
+                    const Info& info = infos[(done + y) & 7];
+                    const int own = u.len - (u.tile + y) * KT;  // cached keys from the tile's start
                     const float4 kf = *reinterpret_cast<const float4*>(info.k), lf = *reinterpret_cast<const float4*>(info.lv);
                     const int4 valid = *reinterpret_cast<const int4*>(info.valid);
                     const float lv[4] = {lf.x, lf.y, lf.z, lf.w}, hi = fmaxf(fmaxf(lf.x, lf.y), fmaxf(lf.z, lf.w)),
@@ -635,61 +626,27 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                     if (lane == 0) mbar_arrive(sm0 + L::pready + (w * 2 + (y & 1)) * 8);
                 }
                 if (!ok) break;
-                const int last_done = L::odone + (w * 2 + (mine - 1 & 1)) * 8, last_phase = (mine & 1 ? weighed[0] : weighed[1]) - 1;
-                const bool joins = split && count > 1;
-                if (joins && w) {
-                    // the odd tiles: their accumulator stays where it is, the other warps take it from there
-                    ok = __all_sync(0xffffffffu, wait(sm0 + last_done, last_phase));
-                    if (!ok) break;
-                    if (!idle) other[row] = make_float4(M - d, l, d, 0.0f);
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(sm0 + L::merged);
-                    if (more) {
-                        next_unit(next);
-                        queries(next, units + 1);
-                    }
-                    done += count;
-                    ++units;
-                    u = next;
-                    continue;
-                }
                 // the next unit's queries, while the last products run: this unit's scores are done
-                if (joins) {
-                    ok = __all_sync(0xffffffffu, wait(sm0 + L::merged, merges++));
-                    if (!ok) break;
-                }
                 if (more) {
                     next_unit(next);
-                    queries(next, units + 1);
+                    queries(next);
                 }
-                ok = __all_sync(0xffffffffu, wait(sm0 + last_done, last_phase));
+                ok = __all_sync(0xffffffffu, wait(sm0 + L::odone + (w * 2 + (count - 1 & 1)) * 8, (count & 1 ? weighed[0] : weighed[1]) - 1));
                 if (!ok) break;
                 if (idle) {
                     if (lane == 0) mbar_arrive(sm0 + L::ofree + w * 8);
-                    if (joins && lane == 0) mbar_arrive(sm0 + L::ofree + 8);
                     done += count;
                     ++units;
                     u = next;
                     continue;
                 }
                 tc_after();
-                float m = M - d;
-                float2 unit = unit_of(d), unit1 = make_float2(0.0f, 0.0f);
-                if (joins) {
-                    const float4 x = other[row];
-                    const float top = fmaxf(m, x.x), base = top == -INFINITY ? 0.0f : top, g0 = ex2(m - base), g1 = ex2(x.x - base);
-                    l = l * g0 + x.y * g1;
-                    unit.x *= g0;
-                    unit1 = unit_of(x.z);
-                    unit1.x *= g1;
-                    m = top;
-                }
+                const float m = M - d;
                 const bool whole = u.tile == 0 && count == u.c;
-                const int rr = row0 + row, rho = u.rt * RM + rr, t = rho / G, hd = u.h * G + rho - t * G;
+                const int rr = w * 128 + row, rho = u.rt * RM + rr, t = rho / G, hd = u.h * G + rho - t * G;
                 float* const part = part_of<D, RM>(a, me, u.tile == 0 ? 1 : 0);
-                const float scale = (whole ? (l > 0.0f || l != l ? 1.0f / l : 0.0f) : 1.0f) * ex2(-UP);
-                unit.y *= scale;
-                unit1.y *= scale;
+                float2 unit = unit_of(d);
+                unit.y *= (whole ? (l > 0.0f || l != l ? 1.0f / l : 0.0f) : 1.0f) * ex2(-UP);
                 const bool wild = wilds[units & 7] == units + 1;
 #pragma unroll 1
                 for (int c = 0; c < D / 32; ++c) {
@@ -697,13 +654,6 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                     tmem_load(o, om + c * 32);
 #pragma unroll
                     for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * unit.y * unit.x);
-                    if (joins) {
-                        uint32_t o1[32];
-                        tmem_load(o1, om + L::HALVES * 64 + c * 32);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            o[i] = __float_as_uint(fmaf(__uint_as_float(o1[i]) * unit1.y, unit1.x, __uint_as_float(o[i])));
-                    }
                     if (row < rows) {
                         if (wild && !(whole && l == 0.0f)) {
                             // values that are not finite, of the tokens that this row sees, whatever their weight
@@ -741,7 +691,6 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                 tc_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(sm0 + L::ofree + w * 8);
-                if (joins && lane == 0) mbar_arrive(sm0 + L::ofree + 8);
                 if (row < rows) {
                     if (!whole) *reinterpret_cast<float2*>(part + rr * 2) = make_float2(m, wild ? -l : l);
                     else if (a.lse) a.lse[(long long)(u.lo + t) * (H * G) + hd] = (m + log2f(l)) * LN2;
