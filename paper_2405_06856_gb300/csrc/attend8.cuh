@@ -318,41 +318,45 @@ __device__ __forceinline__ int arrive_at(int* counter)
     return before;
 }
 
-// The tokens that token t of the request under u sees, itself among them; all lanes together, each its own t. A
-// parent that is not an earlier token counts as none and is recorded. (A lane holds two tokens; every round joins what a
-// token sees with what the one at the end of it sees: the walk up by loads, one after the other, took 10 times as long.)
-__device__ __forceinline__ unsigned long long all_ancestors(const AttendArgs& a, const Cursor& u, int t, int lane)
-{
-    int up[2];
+// What the tokens of the request under u see, themselves among them; all lanes together. A parent that is not an earlier
+// token counts as none and is recorded. (A lane holds two tokens; every round joins what a token sees with what the one at
+// the end of it sees: the walk up by loads, one after the other, took 10 times as long.)
+struct Ancestors {
     unsigned long long see[2];
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        const int i = e * 32 + lane;
-        up[e] = i >= u.T ? -1 : a.tok.parent ? a.tok.parent[u.lo + i] : i - 1;
-        if (up[e] < -1 || up[e] >= i) {
-            atomicOr(a.err, WORKER_BAD_INPUT);
-            up[e] = -1;
-        }
-        see[e] = 1ull << i;
-    }
-    const auto of = [&](int i) {
+
+    // of token t, each lane its own
+    __device__ __forceinline__ unsigned long long of(int i) const
+    {
         const unsigned long long x = __shfl_sync(0xffffffffu, see[0], i & 31), y = __shfl_sync(0xffffffffu, see[1], i & 31);
         return i < 0 ? 0ull : i < 32 ? x : y;
-    };
-#pragma unroll 1
-    for (int span = 1; span < u.T; span *= 2) {
-        const unsigned long long s0 = of(up[0]), s1 = of(up[1]);
-        int next[2];
+    }
+    __device__ __forceinline__ Ancestors(const AttendArgs& a, const Cursor& u, int lane)
+    {
+        int up[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const int x = __shfl_sync(0xffffffffu, up[0], up[e] & 31), y = __shfl_sync(0xffffffffu, up[1], up[e] & 31);
-            next[e] = up[e] < 0 ? -1 : up[e] < 32 ? x : y;
+            const int i = e * 32 + lane;
+            up[e] = i >= u.T ? -1 : a.tok.parent ? a.tok.parent[u.lo + i] : i - 1;
+            if (up[e] < -1 || up[e] >= i) {
+                atomicOr(a.err, WORKER_BAD_INPUT);
+                up[e] = -1;
+            }
+            see[e] = 1ull << i;
         }
-        see[0] |= s0, see[1] |= s1;
-        up[0] = next[0], up[1] = next[1];
+#pragma unroll 1
+        for (int span = 1; span < u.T; span *= 2) {
+            const unsigned long long s0 = of(up[0]), s1 = of(up[1]);
+            int next[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int x = __shfl_sync(0xffffffffu, up[0], up[e] & 31), y = __shfl_sync(0xffffffffu, up[1], up[e] & 31);
+                next[e] = up[e] < 0 ? -1 : up[e] < 32 ? x : y;
+            }
+            see[0] |= s0, see[1] |= s1;
+            up[0] = next[0], up[1] = next[1];
+        }
     }
-    return of(t);
-}
+};
 
 }  // namespace wk
 }  // namespace aladdin

@@ -42,8 +42,11 @@ struct Few8 {
     static constexpr Mask FULL = TK == 16 ? (Mask)0xffff : ~(Mask)0;
     static constexpr int oks = WARPS * S * SLOT;                      // masks of tiles
     static constexpr int ds = oks + WARPS * S * 8;                    // the rows' d, where they differ
-    static constexpr int scratch = ds + WARPS * NB * 8 * 4;
-    static constexpr int pre = scratch + 96 * 8;
+    static constexpr int pending = ds + WARPS * NB * 8 * 4;           // a warp's Pending
+    static constexpr int pre = pending + WARPS * 24;
+    static constexpr int scratch = 0;                                 // of the plan, in front of all tiles
+    // (up to 196 KB, 66 requests, leave the cache of the SM twice as much as more would, which registers in local memory
+    // need: 64 requests of 1,000 tokens, 256 channels, 99 us for 61)
     static constexpr int bytes(int n_req) { return pre + Axis8::ints(n_req) * 4; }
 
     // byte of chunk c (16 bytes) of a tile's row, keys and values
@@ -85,6 +88,74 @@ __device__ __forceinline__ float row_max(float v)
     return v;
 }
 
+// What a tile of cached keys whose logarithms are not all near d works on: a lane's scores as they are, their logarithms, its
+// rows' state, what their results are multiplied by, and the d of all rows.
+template <int KB, int NB>
+struct Far {
+    float s[KB][NB][4], lv[KB], M[NB][2], l[NB][2], d[NB][2], f[NB][2], all;
+};
+
+// Weights in the place of scores; whether the rows have a d each from here on, in row_d.
+template <int KB, int NB>
+__device__ __noinline__ bool far_tile(Far<KB, NB>& t, float* row_d)
+{
+    const int lane = threadIdx.x & 31, gq = lane >> 2, tq = lane & 3;
+    float least = INFINITY, most = -INFINITY;
+#pragma unroll 1
+    for (int r = 0; r < NB * 2; ++r) {
+        const int y = r >> 1, e = r & 1;
+        const float before = t.d[y][e], m = t.M[y][e] - before;
+        float top = -INFINITY, with = -INFINITY;
+#pragma unroll
+        for (int x = 0; x < KB; ++x) top = fmaxf(top, fmaxf(t.s[x][y][e], t.s[x][y][e + 2]));
+        const float to = fmaxf(m, row_max(top)), base = to == -INFINITY ? 0.0f : to;
+        // (differences first: next to scores of any size logarithms would be lost)
+#pragma unroll
+        for (int x = 0; x < KB; ++x) with = fmaxf(with, (fmaxf(t.s[x][y][e], t.s[x][y][e + 2]) - base) + t.lv[x]);
+        const float by = m - base, next = fmaxf(fmaxf(before + by, row_max(with)), 2 * LOG_ZERO);
+        float l = t.l[y][e] * ex2(by);
+#pragma unroll
+        for (int x = 0; x < KB; ++x) {
+#pragma unroll
+            for (int z = 0; z < 4; z += 2) {
+                const float w = t.s[x][y][e + z] - base;
+                l += ex2(w);
+                t.s[x][y][e + z] = ex2(w + (t.lv[x] - next + UP));
+            }
+        }
+        t.f[y][e] = ex2(by + (before - next));
+        t.l[y][e] = l;
+        t.M[y][e] = to == -INFINITY ? to : __fadd_ru(to, next);
+        t.d[y][e] = next;
+        least = fminf(least, next);
+        most = fmaxf(most, next);
+    }
+#pragma unroll
+    for (int x = 1; x < 4; x <<= 1) {
+        least = fminf(least, __shfl_xor_sync(0xffffffffu, least, x));
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, x));
+    }
+    // one d for all rows again, where it does
+    const bool single = most - least > FAR;
+    __syncwarp();
+#pragma unroll 1
+    for (int r = 0; r < NB * 2; ++r) {
+        const int y = r >> 1, e = r & 1;
+        if (!single) t.l[y][e] *= ex2(least - t.d[y][e]);
+        else if (gq == 0) row_d[y * 8 + tq * 2 + e] = t.d[y][e];
+    }
+    __syncwarp();
+    t.all = least;
+    return single;
+}
+
+// A unit whose partial results the workers first .. last left.
+struct Pending {
+    int h, rt, lo, T;  // of its Cursor
+    int first, last;
+};
+static_assert(sizeof(Pending) == 24, "the room for it");
+
 // N consecutive floats that other warps wrote
 template <int N>
 __device__ __forceinline__ void load_row(float (&v)[N], const float* p)
@@ -104,12 +175,12 @@ __device__ __forceinline__ void load_row(float (&v)[N], const float* p)
     }
 }
 
-// The rows below live of the unit under u, whose partial results the workers first .. last left; one warp, D / 32 columns
-// a lane. What another SM wrote is 1,500 cycles away: the maxima and sums of up to 32 partial results, one a lane, and
+// The rows below live of a unit; one warp, D / 32 columns a lane. What another SM wrote is 1,500 cycles away: the maxima and sums of up to 32 partial results, one a lane, and
 // the columns of up to four of them are on their way together.
 template <typename T, int D, int RM>
-__device__ __forceinline__ void join_rows8(const AttendArgs& a, const Cursor& u, int first, int last, int live, int lane)
+__device__ __forceinline__ void join_rows8(const AttendArgs& a, const Pending& u, int live, int lane)
 {
+    const int first = u.first, last = u.last;
     // (fewer together where accumulators and queries take most registers anyway: the kernel around this does not spill)
     constexpr int N = D / 32, U = D == 256 ? 1 : D * RM > 8 * 128 ? 2 : 4, ROWS = 4;
     const int G = a.kv.group;
@@ -358,13 +429,12 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
     float d = 0.0f;
     bool single = false;                     // whether the rows have a d each
     float unscale[NB];                       // of row gq of every block
-    unsigned long long see[NB][2];
     bool fresh = true, wild = false;         // whether the unit's results hold values that are not finite
     int b = 0, tile0 = 0;  // a tile's place; the first tile of the unit that this warp has
     // A unit that warps share and whose part this one has written: a tile later it says so, and at the end of its next
     // unit it looks whether it was the last one to, which joins the parts; neither is waited for while there are tiles.
-    Cursor P = C;
-    int pend = 0, p_first = 0, p_last = 0, p_before = 0;  // 1: written, 2: said
+    Pending& P = *reinterpret_cast<Pending*>(sm + L::pending + warp * 24);
+    int pend = 0, p_before = 0;  // 1: written, 2: said
 
     for (int j = 0; j < n; ++j) {
         __syncwarp();
@@ -381,7 +451,6 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                 for (int x = 0; x < MO; ++x) o[x][y][0] = o[x][y][1] = o[x][y][2] = o[x][y][3] = 0.0f;
                 M[y][0] = M[y][1] = -INFINITY;
                 l[y][0] = l[y][1] = 0.0f;
-                see[y][0] = see[y][1] = 1;
                 uint2 q[MO];
 #pragma unroll
                 for (int x = 0; x < MO; ++x) q[x] = AHEAD ? qn[AHEAD ? x : 0][y] : query(C, y, x);
@@ -401,15 +470,6 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                 next_unit8<TK, TN, RM>(a, ax, u);
                 queries_of(u);
             }
-            if (C.T > 1) {
-#pragma unroll
-                for (int y = 0; y < NB; ++y)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int rr = y * 8 + tq * 2 + e;
-                        see[y][e] = all_ancestors(a, C, rr < rows ? (C.rt * RM + rr) / G : 0, lane);
-                    }
-            }
         }
         cp_wait<S - 1>();
         __syncwarp();
@@ -420,6 +480,7 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
         float s[KB][NB][4];  // keys gq, gq + 8 of a block by rows 2 tq, 2 tq + 1
         float lv[KB];          // logarithms of the scales of the blocks' values, or of what key gq of a block has for one
         float hi = -INFINITY;  // the largest
+        unsigned seen = 0;     // by the rows, of this lane's new keys
         bool odd = true;       // whether a row's d is not within reach of all of them (attend8.cuh)
         if (cached) {
             // (a block without keys has no part, and one whose scale is none makes its scores NaN)
@@ -494,6 +555,21 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                             if (!(okm >> (x * 16 + (e >> 1) * 8 + gq) & 1)) s[x][y][e] = -INFINITY;
             }
         } else {
+            // what the rows see (looked for here: between the tiles it would cost registers)
+            unsigned long long see[NB][2];
+            if (C.T > 1) {
+                const Ancestors tree(a, C, lane);
+#pragma unroll
+                for (int y = 0; y < NB; ++y)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int rr = y * 8 + tq * 2 + e;
+                        see[y][e] = tree.of(rr < rows ? (C.rt * RM + rr) / G : 0);
+                    }
+            } else {
+#pragma unroll
+                for (int y = 0; y < NB; ++y) see[y][0] = see[y][1] = 1;
+            }
             // 8 new keys in the place of 16
 #pragma unroll
             for (int x = 0; x < KB; ++x) {
@@ -531,7 +607,9 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                 for (int y = 0; y < NB; ++y) {
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        s[x][y][e] = key < C.T && (see[y][e] >> key & 1) ? s[x][y][e] * a.scale_log2 : -INFINITY;
+                        const bool is = key < C.T && (see[y][e] >> key & 1);
+                        s[x][y][e] = is ? s[x][y][e] * a.scale_log2 : -INFINITY;
+                        seen |= (unsigned)is << (x * NB + y) * 2 + e;
                         s[x][y][e + 2] = -INFINITY;
                     }
                 }
@@ -585,8 +663,48 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                     }
                 }
             }
+        } else if (cached) {
+            // (a function of its own, by way of local memory: its code between the tiles' would cost every one of them, 20 rows of 64
+            // channels 10%)
+            Far<KB, NB> far;
+#pragma unroll
+            for (int y = 0; y < NB; ++y) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    far.M[y][e] = M[y][e], far.l[y][e] = l[y][e];
+                    far.d[y][e] = single ? row_d[y * 8 + tq * 2 + e] : d;
+                }
+#pragma unroll
+                for (int x = 0; x < KB; ++x) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) far.s[x][y][e] = s[x][y][e];
+                }
+            }
+#pragma unroll
+            for (int x = 0; x < KB; ++x) far.lv[x] = lv[x];
+            far.all = d;
+            single = far_tile<KB, NB>(far, row_d);
+            d = far.all;
+#pragma unroll
+            for (int y = 0; y < NB; ++y) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    M[y][e] = far.M[y][e], l[y][e] = far.l[y][e];
+                    const float f = far.f[y][e];
+#pragma unroll
+                    for (int x = 0; x < MO; ++x) {
+                        o[x][y][e] *= f;
+                        o[x][y][e + 2] *= f;
+                    }
+                }
+#pragma unroll
+                for (int x = 0; x < KB; ++x) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[x][y][e] = far.s[x][y][e];
+                }
+            }
         } else {
-            // scores as they are. (Differences first: next to scores of any size logarithms would be lost)
+            // new tokens have a logarithm each. (Differences first: next to scores of any size logarithms would be lost)
             float f[NB][2], next[NB][2];
             bool moved = false;
 #pragma unroll
@@ -596,10 +714,10 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                     const float before = single ? row_d[y * 8 + tq * 2 + e] : d, m = M[y][e] - before;
                     float top = -INFINITY, with = -INFINITY;
 #pragma unroll
-                    for (int x = 0; x < KB; ++x) top = fmaxf(top, fmaxf(s[x][y][e], s[x][y][e + 2]));
+                    for (int x = 0; x < KB; ++x) top = fmaxf(top, s[x][y][e]);
                     const float to = fmaxf(m, row_max(top)), base = to == -INFINITY ? 0.0f : to;
 #pragma unroll
-                    for (int x = 0; x < KB; ++x) with = fmaxf(with, (fmaxf(s[x][y][e], s[x][y][e + 2]) - base) + lv[x]);
+                    for (int x = 0; x < KB; ++x) with = fmaxf(with, (s[x][y][e] - base) + lv[x]);
                     const float by = m - base;
                     next[y][e] = fmaxf(fmaxf(before + by, row_max(with)), 2 * LOG_ZERO);
                     f[y][e] = ex2(by + (before - next[y][e]));
@@ -609,22 +727,12 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                     M[y][e] = to == -INFINITY ? to : __fadd_ru(to, next[y][e]);
 #pragma unroll
                     for (int x = 0; x < KB; ++x) {
-                        if (cached) {
-#pragma unroll
-                            for (int z = 0; z < 4; z += 2) {
-                                const float t = s[x][y][e + z] - base;
-                                l[y][e] += ex2(t);
-                                s[x][y][e + z] = ex2(t + (lv[x] - next[y][e] + UP));
-                            }
-                        } else {
-                            // (weights of new values stay in 32 bits, and have no scale)
-                            const float t = s[x][y][e] - base;
-                            l[y][e] += ex2(t);
-                            s[x][y][e] = ex2(t + (UP - next[y][e]));
-                            // a value that is not finite counts for all rows that see it: no weight of theirs is 0
-                            const int key = first + x * 8 + gq;
-                            if (wild && key < C.T && (see[y][e] >> key & 1)) s[x][y][e] = fmaxf(s[x][y][e], 1.4e-45f);
-                        }
+                        // (their weights stay in 32 bits, and have no scale)
+                        const float t = s[x][y][e] - base;
+                        l[y][e] += ex2(t);
+                        s[x][y][e] = ex2(t + (UP - next[y][e]));
+                        // a value that is not finite counts for all rows that see it: no weight of theirs is 0
+                        if (wild && (seen >> (x * NB + y) * 2 + e & 1)) s[x][y][e] = fmaxf(s[x][y][e], 1.4e-45f);
                     }
                 }
             }
@@ -639,37 +747,13 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
                             o[x][y][e + 2] *= f[y][e];
                         }
             }
-            // one d for all rows again, where it does (behind new tokens nothing comes that would gain by it)
-            single = !cached;
-            if (cached) {
-                float least = next[0][0], most = next[0][0];
+            single = true;
+            __syncwarp();
+            if (gq == 0) {
 #pragma unroll
-                for (int y = 0; y < NB; ++y) {
-                    least = fminf(least, fminf(next[y][0], next[y][1]));
-                    most = fmaxf(most, fmaxf(next[y][0], next[y][1]));
-                }
-#pragma unroll
-                for (int x = 1; x < 4; x <<= 1) {
-                    least = fminf(least, __shfl_xor_sync(0xffffffffu, least, x));
-                    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, x));
-                }
-                single = most - least > FAR;
-                if (!single) {
-                    d = least;
-#pragma unroll
-                    for (int y = 0; y < NB; ++y)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) l[y][e] *= ex2(d - next[y][e]);
-                }
+                for (int y = 0; y < NB; ++y) *reinterpret_cast<float2*>(row_d + y * 8 + tq * 2) = make_float2(next[y][0], next[y][1]);
             }
-            if (single) {
-                __syncwarp();
-                if (gq == 0) {
-#pragma unroll
-                    for (int y = 0; y < NB; ++y) *reinterpret_cast<float2*>(row_d + y * 8 + tq * 2) = make_float2(next[y][0], next[y][1]);
-                }
-                __syncwarp();
-            }
+            __syncwarp();
         }
         if (cached) {
 #pragma unroll
@@ -746,7 +830,7 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
         }
 
         if (pend == 1) {
-            if (lane == 0) p_before = arrive_at(a.arrived + p_first);
+            if (lane == 0) p_before = arrive_at(a.arrived + P.first);
             pend = 2;
         }
         if (C.tile + 1 == C.c || j + 1 == n) {
@@ -792,21 +876,24 @@ __global__ void __launch_bounds__(Few8<D, NB>::WARPS * 32, 1) k_attend8_few(Atte
 #pragma unroll 1
             while (pend || add) {
                 if (pend) {
-                    if (__shfl_sync(0xffffffffu, p_before, 0) == p_last - p_first) {
-                        if (lane == 0) a.arrived[p_first] = 0;
+                    const Pending p = P;
+                    if (__shfl_sync(0xffffffffu, p_before, 0) == p.last - p.first) {
+                        if (lane == 0) a.arrived[p.first] = 0;
                         asm volatile("fence.acq_rel.gpu;" ::: "memory");
-                        join_rows8<T, D, RM>(a, P, p_first, p_last, min(P.T * G - P.rt * RM, RM), lane);
+                        join_rows8<T, D, RM>(a, p, min(p.T * G - p.rt * RM, RM), lane);
                     }
                     pend = 0;
                 }
                 if (!add) break;
                 add = false;
-                P = C;
-                ax.sharers(P, p_first, p_last);
+                Pending p = {C.h, C.rt, C.lo, C.T, 0, 0};
+                ax.sharers(C, p.first, p.last);
+                __syncwarp();
+                if (lane == 0) P = p;
                 __syncwarp();
                 pend = 1;
                 if (j + 1 < n) break;
-                if (lane == 0) p_before = arrive_at(a.arrived + p_first);
+                if (lane == 0) p_before = arrive_at(a.arrived + P.first);
                 pend = 2;
             }
             fresh = true;

@@ -465,7 +465,7 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                     queries(next);
                 }
             } else {
-                const unsigned long long see = all_ancestors(a, u, row < rows ? (u.rt * RM + w * 128 + row) / G : 0, lane);
+                const unsigned long long see = Ancestors(a, u, lane).of(row < rows ? (u.rt * RM + w * 128 + row) / G : 0);
                 float M = -INFINITY, l = 0.0f, d = 0.0f;  // (attend8.cuh)
 #pragma unroll 1
                 for (int y = 0; y < count; ++y) {
