@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(Many8<D, MT>::WARPS * 32, 1) k_attend8_many(At
                         if (i % L::HALVES == L::HALVES - 1) p += eight;
                     }
                 } else {
-#pragma unroll 1
+#pragma unroll(D == 96 ? 3 : 1)  // (96 channels have no other way: rolled, 37 requests of trees up to 5 take 54 us for 48)
                     for (int i = 0; i < L::CPL; ++i) {
                         const bool in = valid && row_of(i) < own;
                         cp16(d + i * 512 + lane * 16, src + (in ? row_of(i) * a.kv.token_stride + channel_of(i) : 0), in);
