@@ -739,7 +739,9 @@ int aladdin_worker_append8(aladdin_worker* wk, const aladdin_kv8* kv, const alad
 
 /* aladdin_worker_attend over a cache of 8 bits; the new tokens, of 16 bits, are not in it. Scores are 32-bit sums
  * of exact products with the codes, times their scales; the weights meet the values' codes in 16 bits, half precision: good to
- * 2^-11 of themselves down to 2^-21 of the largest product of a weight and its value's scale in the row, and 0 below 2^-32 of it.
+ * 2^-11 of themselves down to 2^-21 of the largest product of a weight and its value's scale in the row, and 0 below 2^-32 of it
+ * (under scales that are 2^90 apart and more also where the weight itself is below 2^-46 of the row's largest). Queries of
+ * bfloat16, and new keys where rows are many, lose what is below 2^-28 of the largest channel of their row.
  * Scales are >= 0; one that is not finite makes the rows of its request not finite, and a new token's value that is
  * not finite its channel of the rows that see it, whatever its weight (but of rows whose scores are all -inf). Reads k, v,
  * table, len and the scales of kv. */

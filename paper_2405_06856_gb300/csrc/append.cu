@@ -18,7 +18,7 @@
 // token, a search and new angles each: 49); 36,000 tokens, 4 heads of 96, into 8 bits in blocks of 64: 51 us, 1.6 TB/s, half of the
 // instruction slots and the rest latency of rounds that end in a barrier (one warp a block that reads its rows twice:
 // 66). In blocks of 16 with 8 heads of 128 in the half layout, 222 MB: 129 us (all warps of a CTA waiting for one another: 45
-// more). One token each of 128 requests: 6 and 9 us with the launch, a chain of look-ups.
+// more; in this layout 100 to 150 bytes a thread do not fit into registers). One token each of 128 requests: 6 and 9 us with the launch, a chain of look-ups.
 //
 // The kernels lay the requests' units on one axis (a prefix sum by each CTA, which keeps what the units need of them) and
 // go over it with all warps of the GPU. The last CTA to finish advances the lengths.

@@ -18,9 +18,10 @@
 // not finite.
 //
 // Measured: two requests of 110,108 cached tokens, 32 heads of 64 channels in f16, scales for 64 tokens: 86 us, 5.2 TB/s of
-// 6.75 that a copy reaches; 128 requests of 83,336 tokens, 32 query and 8 key heads of 128 channels in bf16: 46 us, 3.7
+// 6.75 that a copy reaches; 128 requests of 83,336 tokens, 32 query and 8 key heads of 128 channels in bf16: 48 us, 3.6
 // TB/s. There 6 us go by until the first codes are there and 10 to 15 in the ends of units, where what another SM wrote is
-// 1,500 cycles away; in between two warps a scheduler wait for their own results.
+// 1,500 cycles away; in between two warps a scheduler wait for their own results, and for instructions: code that few tiles need
+// costs all of them where it lies between theirs.
 #include "attend8.cuh"
 
 namespace aladdin {
@@ -181,7 +182,8 @@ template <typename T, int D, int RM>
 __device__ __forceinline__ void join_rows8(const AttendArgs& a, const Pending& u, int live, int lane)
 {
     const int first = u.first, last = u.last;
-    // (fewer together where accumulators and queries take most registers anyway: the kernel around this does not spill)
+    // (fewer together where accumulators and queries take most registers anyway: the kernel around this keeps to registers but
+    // with 64 channels and 12 warps, 60 bytes a thread, and with 256 of bfloat16, 350)
     constexpr int N = D / 32, U = D == 256 ? 1 : D * RM > 8 * 128 ? 2 : 4, ROWS = 4;
     const int G = a.kv.group;
 #pragma unroll 1

@@ -8,7 +8,8 @@
 //   one thread issues the products: scores S = Q K' and out += P V, P from tensor memory;
 //   seven warps convert, 16 keys or values at a time in turn: codes come by asynchronous copies a few of those ahead, each
 //   lane's own, and go as half precision into a ring of shared memory, K0 V0 K1 V1 ..., in the 128-byte-swizzled layout of
-//   the matrix descriptors. New tokens have a tile of their own; those of bfloat16 are scaled by a power of two for each.
+//   the matrix descriptors. New tokens have a tile of their own; their values, and keys of bfloat16, are scaled by a power of
+//   two for each.
 // A row tile's scores have two places: the next ones are formed while the softmax works on those before. (Even and odd tiles of a
 // single row tile by the two sets of softmax warps, with an accumulator each, took 5 to 10% longer: 64 requests of 1,500 tokens,
 // 64 rows of 128 channels, 137 us for 124.) The accumulators stay in tensor memory; they are rescaled only when a row's
@@ -19,8 +20,8 @@
 // unrolled into the roles' loops (145 KB of code) a quarter of the warps' time went into fetching instructions. Measured,
 // 24 requests of 60,854 cached tokens with trees of up to 64 tokens, 64 query and 8 key heads of 128 channels: 324 us so,
 // 219 with a loop over units and one over tiles in each role, 205 with queries in shared memory and two places of
-// scores, 500 TFLOP/s of 1,888 that a large product reaches; 37 requests of 57,837 tokens with trees of up to 5, 28 and
-// 4 heads of 96: 63 us, and 50 since seven warps convert in turn.
+// scores, 195 with weights that refer to one maximum for each row, 521 TFLOP/s of 1,888 that a large product reaches; 37
+// requests of 57,837 tokens with trees of up to 5, 28 and 4 heads of 96: 63 us, and 48 since seven warps convert in turn.
 //
 // New tokens' values that are not finite would reach rows that do not see them (0 times infinity): they are replaced by
 // 0 in shared memory, and rows that do see them get them added at the end.

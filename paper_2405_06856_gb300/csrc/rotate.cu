@@ -6,8 +6,9 @@
 // row's other half, which the same warp has just brought in. All loads of a row come
 // before the first store to it, so that the outputs may be the inputs.
 //
-// Measured: pieces of prompts of 18,274 tokens, 32 heads of 96 channels: 41 us, 5.4 TB/s of 6.75 that a copy reaches; trees of
-// 1,185 tokens, 72 heads of 128: 11 us, 3.9 TB/s, of it 3 until positions are known (a token's rows in four times as many parts: 16, as each forms its
+// Measured: pieces of prompts of 18,275 tokens, 32 heads of 96 channels: 41 us, 5.4 TB/s of 6.75 that a copy reaches; trees of
+// 1,185 tokens, 72 heads of 128: 11 us, 3.9 TB/s, of it 3 until positions are known, which the rows' loads wait for although they
+// need not (a token's rows in four times as many parts: 16, as each forms its
 // angles).
 #include "rope.cuh"
 
