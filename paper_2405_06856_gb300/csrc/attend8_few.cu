@@ -46,7 +46,7 @@ struct Few8 {
     static constexpr int pending = ds + WARPS * NB * 8 * 4;           // a warp's Pending
     static constexpr int pre = pending + WARPS * 24;
     static constexpr int scratch = 0;                                 // of the plan, in front of all tiles
-    // (up to 196 KB, 66 requests, leave the cache of the SM twice as much as more would, which registers in local memory
+    // (up to 196 KB, some 70 requests, leave the cache of the SM twice as much as more would, which registers in local memory
     // need: 64 requests of 1,000 tokens, 256 channels, 99 us for 61)
     static constexpr int bytes(int n_req) { return pre + Axis8::ints(n_req) * 4; }
 
